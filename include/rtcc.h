@@ -416,6 +416,147 @@ rtcc_status rtcc_pillarise_noalloc(const rtcc_model_config* cfg, const float* d_
                                    int32_t* d_stats, void* d_image, void* stream);
 
 /* ------------------------------------------------------------------------ */
+/* Token memory: keys and values of tokens, and attention over them         */
+/* (no counterpart in the paper)                                            */
+/* ------------------------------------------------------------------------ */
+
+/*
+ * A token memory holds the key and value vectors of tokens -- the BEV cells of
+ * the agents' maps, objects, the steps of a sequence -- as rows of caller-owned
+ * device arrays.  A sequence owns a slot of consecutive rows (an agent's map, a
+ * request's history); several sequences may also share rows.  Three calls:
+ * rtcc_memory_append finds the rows of new tokens, rtcc_qkv_prepare norms,
+ * rotates and writes them, rtcc_memory_attention attends to them.  All work is
+ * enqueued on `stream` (a cudaStream_t; NULL = the default stream) of the
+ * current device, nothing is allocated or synchronised, and every call may be
+ * captured into a CUDA graph.  Device pointers must stay valid until the work
+ * is done; outputs must not overlap inputs except where stated.  RTCC_E_ARG
+ * for sizes, strides, pointers or alignment outside what is stated, before any
+ * work is enqueued; RTCC_E_CUDA when a launch fails.
+ */
+
+/*
+ * Rows for new tokens.  Sequence s holds d_held[s] rows of its slot d_slot[s]
+ * (d_slot NULL: slot s), the rows [slot * capacity, (slot + 1) * capacity), and
+ * receives d_new[s] more.  Tokens are numbered sequence after sequence:
+ *   d_offsets int32 [n_seqs + 1]  first token of each sequence; last = total
+ *   d_rows    int32 [n_tokens]    memory row of each token, -1 = none
+ *   d_seq, d_pos int32 [n_tokens] its sequence and its place in it (may be NULL)
+ *   d_begin, d_end int32 [n_seqs] the sequence's rows once its tokens are in
+ *   d_length  int32 [n_seqs]      their number, at most capacity
+ * A token past its slot's capacity gets row -1; entries past the total get -1
+ * in all three token arrays.  Tokens that do not fit into n_tokens are dropped:
+ * offsets are cut there, and they do not count towards the length.  Negative
+ * counts read as 0, held counts are cut to the capacity, and a negative slot
+ * or one whose rows pass 2^31 gets no rows and an empty span.
+ * 0 <= n_seqs <= 16384, capacity >= 1, n_tokens >= 0; d_length may be neither
+ * d_held nor d_new.
+ */
+rtcc_status rtcc_memory_append(int32_t n_seqs, int32_t capacity, int32_t n_tokens,
+                               const int32_t* d_new, const int32_t* d_held, const int32_t* d_slot,
+                               int32_t* d_offsets, int32_t* d_rows, int32_t* d_seq,
+                               int32_t* d_pos, int32_t* d_begin, int32_t* d_end,
+                               int32_t* d_length, void* stream);
+
+/* Shapes of rtcc_qkv_prepare.  Strides count elements, are multiples of 8 and
+ * not negative; the channels of a head are contiguous. */
+typedef struct {
+  int32_t heads, kv_heads;          /* of q; of k and v                      */
+  int32_t head_dim;                 /* a multiple of 8 in 8..128             */
+  int32_t dtype;                    /* rtcc_dtype of all vectors             */
+  int32_t n_tokens;
+  int32_t n_rows;                   /* rows of the memory                    */
+  int64_t q_row, q_head, k_row, k_head, v_row, v_head;        /* inputs      */
+  int64_t qo_row, qo_head, km_row, km_head, vm_row, vm_head;  /* outputs     */
+  int32_t axis_pairs[3];            /* channel pairs turned by t, y, x; their
+                                       sum is at most head_dim / 2, channels
+                                       beyond 2 x sum are not turned         */
+  int32_t interleaved;              /* 1: pair m = channels (2m, 2m + 1);
+                                       0: channels (m, m + sum)              */
+  int32_t norm;                     /* 1: RMS norm of each head first        */
+  float theta;                      /* frequency base, >= 1                  */
+  float eps;                        /* of the norm, >= 0                     */
+} rtcc_prepare_config;
+
+/*
+ * Queries and keys of n_tokens tokens made ready: per token and head of q and k
+ *   x^ = x * rsqrt(mean(x^2) + eps) * gain      (without norm: x * gain)
+ * in float32, then pair m of axis a, of n_a pairs, turned by the angle
+ * pos_a * theta^(-m / n_a):  (u, v) -> (u cos - v sin, u sin + v cos), and one
+ * rounding to the storage type.  Axis t's pairs come first, then y's, then x's.
+ * Queries go to d_q_out; keys, values (copied) and, if d_coord is given, the
+ * coordinates (y, x) go to the memory row d_rows[i] of token i (d_rows NULL:
+ * row i); a token whose row is outside [0, n_rows) writes its query only.  Rows
+ * of one call must differ.
+ * d_q, d_k, d_v: each may be NULL together with its output.  d_q_gain,
+ * d_k_gain float32 [head_dim], NULL = 1.  d_pos float32 [n_tokens][3] = (t, y,
+ * x).  d_coord float32 [n_rows][2].  Vectors are 16-byte aligned, d_coord
+ * 8-byte, the rest 4-byte.  d_q_out may be d_q with the same strides.
+ */
+rtcc_status rtcc_qkv_prepare(const rtcc_prepare_config* cfg, const void* d_q, const void* d_k,
+                             const void* d_v, const float* d_q_gain, const float* d_k_gain,
+                             const float* d_pos, const int32_t* d_rows, void* d_q_out,
+                             void* d_k_mem, void* d_v_mem, float* d_coord, void* stream);
+
+/* Shapes of rtcc_memory_attention; strides as in rtcc_prepare_config. */
+typedef struct {
+  int32_t heads, kv_heads;          /* heads is a multiple of kv_heads: query
+                                       head h reads key head
+                                       h / (heads / kv_heads)                */
+  int32_t head_dim;                 /* a multiple of 8 in 8..128             */
+  int32_t dtype;                    /* rtcc_dtype of q, k, v and out         */
+  int32_t n_q;                      /* tokens of all sequences               */
+  int32_t n_rows;                   /* rows of the memory                    */
+  int64_t q_row, q_head, k_row, k_head, v_row, v_head, out_row, out_head;
+  int32_t n_seqs;
+  int32_t max_q, max_k;             /* the longest sequence's tokens and keys;
+                                       they size the launch only: results hold
+                                       for longer ones too                   */
+  int32_t causal;                   /* 1: the causal mask below              */
+  int32_t n_slots, slot_rows;       /* agents' slots of slot_rows rows each,
+                                       n_slots <= 64, covering all rows;
+                                       0 without d_present                   */
+  int32_t q_pos_row;                /* floats from one token's q_pos to the
+                                       next, >= 2                            */
+  float scale;                      /* of q.k, usually 1 / sqrt(head_dim)    */
+  float cap;                        /* scores are capped at +-cap; 0: no cap */
+} rtcc_attn_config;
+
+/*
+ * Attention of every sequence's tokens over its span of the memory.  Sequence s
+ * has the tokens [d_q_offsets[s], d_q_offsets[s + 1]) and the keys in rows
+ * [d_k_begin[s], d_k_end[s]); n and m are their numbers.  For token i of the
+ * sequence, key j (both from 0) and query head h:
+ *   x = scale * q.k;   x = cap * tanh(x / cap) if cap > 0;
+ *   x = x - slopes[h] * (|dy| + |dx|) if d_slopes is given, with the difference
+ *       of the token's d_q_pos and the row's d_k_pos;
+ *   key j is visible unless its row lies in a slot whose d_present is 0, or
+ *   causal is set and j > i + m - n (the tokens are the span's last rows) and
+ *   j >= d_prefix[s] (a prefix that every token sees; NULL = 0);
+ *   out = sum of softmax(x) v over the visible keys, lse = ln sum exp(x).
+ * A token that sees no key gets out = 0 and lse = -inf.  Sums and the softmax
+ * are float32; the probabilities are rounded to the storage type for their
+ * product with v, as out is.  Rows that no token of a sequence sees (outside
+ * the span, in an absent slot) are not used: they may hold anything, infinities
+ * and NaN included.  Tokens of no sequence are left untouched.  Offsets and
+ * spans are cut to [0, n_q] and [0, n_rows].
+ * d_lse float32 [n_q][heads] (may be NULL); d_present int32 [n_slots];
+ * d_slopes float32 [heads], d_q_pos [n_q][q_pos_row], d_k_pos [n_rows][2], all
+ * three or none; d_out may be d_q with the same strides.  d_workspace: scratch
+ * for splitting long spans over the GPU, used until the work is done, any
+ * content; more than chunks * n_q * heads * (head_dim + 2) * 4 bytes is of no
+ * use, without it (NULL, or too small) spans are not split.  q, k, v, out and
+ * the workspace are 16-byte aligned, d_k_pos 8-byte, the rest 4-byte.
+ */
+rtcc_status rtcc_memory_attention(const rtcc_attn_config* cfg, const void* d_q, const void* d_k,
+                                  const void* d_v, const int32_t* d_q_offsets,
+                                  const int32_t* d_k_begin, const int32_t* d_k_end,
+                                  const int32_t* d_prefix, const int32_t* d_present,
+                                  const float* d_slopes, const float* d_q_pos,
+                                  const float* d_k_pos, void* d_out, float* d_lse,
+                                  void* d_workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------ */
 /* Release controller alone (host only; no GPU needed)                      */
 /* ------------------------------------------------------------------------ */
 

@@ -1,0 +1,96 @@
+// Host side of the attention over the token memory: argument checks, the
+// choice of kernel and of the split of long spans.
+#include <math.h>
+
+#include "attn.cuh"
+#include "kernels.h"
+#include "rtcc.h"
+
+namespace rtcc {
+namespace {
+
+bool misaligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
+bool bad_stride(int64_t s) { return s < 0 || s % 8 != 0; }
+
+}  // namespace
+}  // namespace rtcc
+
+using namespace rtcc;
+
+extern "C" rtcc_status rtcc_memory_attention(const rtcc_attn_config* c, const void* d_q, const void* d_k,
+                                             const void* d_v, const int32_t* d_q_offsets,
+                                             const int32_t* d_k_begin, const int32_t* d_k_end,
+                                             const int32_t* d_prefix, const int32_t* d_present,
+                                             const float* d_slopes, const float* d_q_pos,
+                                             const float* d_k_pos, void* d_out, float* d_lse,
+                                             void* d_workspace, size_t workspace_bytes, void* stream) {
+  if (!c) return RTCC_E_ARG;
+  if (c->dtype != RTCC_FP16 && c->dtype != RTCC_BF16) return RTCC_E_ARG;
+  if (c->heads < 1 || c->heads > 4096 || c->kv_heads < 1 || c->heads % c->kv_heads) return RTCC_E_ARG;
+  if (c->head_dim < 8 || c->head_dim > 128 || c->head_dim % 8) return RTCC_E_ARG;
+  if (c->n_q < 0 || c->n_rows < 0 || c->n_seqs < 0 || c->max_q < 0 || c->max_k < 0) return RTCC_E_ARG;
+  if ((long long)c->n_q * c->heads > 0x7FFFFFFFLL) return RTCC_E_ARG;
+  const int64_t strides[] = {c->q_row, c->q_head, c->k_row, c->k_head, c->v_row, c->v_head, c->out_row, c->out_head};
+  for (int64_t s : strides)
+    if (bad_stride(s)) return RTCC_E_ARG;
+  if (!isfinite(c->scale) || !isfinite(c->cap) || c->cap < 0.f) return RTCC_E_ARG;
+  if (c->n_slots < 0 || c->n_slots > kMaxSlots || (c->n_slots > 0) != (d_present != nullptr)) return RTCC_E_ARG;
+  if (c->n_slots > 0 && (c->slot_rows < 1 || (long long)c->n_slots * c->slot_rows < c->n_rows)) return RTCC_E_ARG;
+  if ((d_slopes != nullptr) != (d_q_pos != nullptr) || (d_slopes != nullptr) != (d_k_pos != nullptr)) return RTCC_E_ARG;
+  if (d_slopes && c->q_pos_row < 2) return RTCC_E_ARG;
+  if (c->n_seqs > 0 && (!d_q_offsets || !d_k_begin || !d_k_end)) return RTCC_E_ARG;
+  if (c->n_q > 0 && (!d_q || !d_out)) return RTCC_E_ARG;
+  if (c->n_rows > 0 && (!d_k || !d_v)) return RTCC_E_ARG;
+  const void* by16[] = {d_q, d_k, d_v, d_out, d_workspace};
+  for (const void* p : by16)
+    if (misaligned(p, 16)) return RTCC_E_ARG;
+  const void* by4[] = {d_q_offsets, d_k_begin, d_k_end, d_prefix, d_present, d_slopes, d_q_pos, d_lse};
+  for (const void* p : by4)
+    if (misaligned(p, 4)) return RTCC_E_ARG;
+  if (misaligned(d_k_pos, 8)) return RTCC_E_ARG;
+  if (c->n_q == 0 || c->n_seqs == 0) return RTCC_OK;
+
+  int dev = 0, sms = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess ||
+      cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
+    return RTCC_E_CUDA;
+  AttnArgs a{};
+  a.q = d_q; a.k = d_k; a.v = d_v; a.out = d_out; a.lse = d_lse;
+  a.q_offsets = d_q_offsets; a.k_begin = d_k_begin; a.k_end = d_k_end;
+  a.prefix = d_prefix; a.present = d_present;
+  a.slopes = d_slopes; a.q_pos = d_q_pos; a.k_pos = d_k_pos;
+  a.q_row = c->q_row; a.q_head = c->q_head; a.k_row = c->k_row; a.k_head = c->k_head;
+  a.v_row = c->v_row; a.v_head = c->v_head; a.out_row = c->out_row; a.out_head = c->out_head;
+  a.n_q = c->n_q; a.n_rows = c->n_rows; a.heads = c->heads; a.kv_heads = c->kv_heads;
+  a.group = c->heads / c->kv_heads; a.dim = c->head_dim; a.n_seqs = c->n_seqs; a.causal = c->causal != 0;
+  a.n_slots = c->n_slots; a.slot_rows = c->n_slots ? c->slot_rows : 1; a.q_pos_row = c->q_pos_row;
+  a.cap_log2 = c->cap * kLog2e;
+  a.scale_log2 = c->cap > 0.f ? c->scale / c->cap : c->scale * kLog2e;
+
+  const int max_q = c->max_q < 1 ? 1 : c->max_q > c->n_q ? c->n_q : c->max_q;
+  const int max_k = c->max_k < 1 ? 1 : c->max_k > c->n_rows ? (c->n_rows < 1 ? 1 : c->n_rows) : c->max_k;
+  const int unit = attn_rows_unit(c->head_dim), rows = attn_rows_per_block();
+  long long groups = ((long long)max_q * a.group + rows - 1) / rows;
+  long long units = (long long)c->n_seqs * a.kv_heads;
+  while (units * groups > 0x3FFFFFFF && groups > 1) groups = (groups + 1) / 2;   // blocks then loop
+  if (units > 0x3FFFFFFF) return RTCC_E_ARG;
+  units *= groups;
+  a.row_groups = (int)groups;
+  // chunks of the span: enough blocks for a few rounds over the SMs (two blocks
+  // fit on one), each at least four tiles a warp, within the workspace
+  const long long want = (4LL * 2 * sms + units - 1) / units;
+  long long chunks = (max_k + 4LL * unit - 1) / (4LL * unit);
+  if (chunks > want) chunks = want;
+  const size_t part = (size_t)c->n_q * c->heads * (c->head_dim * sizeof(float) + sizeof(float2));
+  if (!d_workspace || workspace_bytes / part < (size_t)chunks) chunks = d_workspace ? (long long)(workspace_bytes / part) : 1;
+  if (chunks < 1) chunks = 1;
+  a.n_chunks = (int)chunks;
+  a.chunk = (int)((max_k + chunks - 1) / chunks);
+  a.part_o = static_cast<float*>(d_workspace);
+  a.part_ml = reinterpret_cast<float2*>(a.part_o + (size_t)chunks * c->n_q * c->heads * c->head_dim);
+  const bool bf16 = c->dtype == RTCC_BF16;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (launch_attn_rows(a, bf16, st) != cudaSuccess) return RTCC_E_CUDA;
+  if (chunks > 1 && launch_attn_join(a, unit, max_q, bf16, st) != cudaSuccess) return RTCC_E_CUDA;
+  return RTCC_OK;
+}

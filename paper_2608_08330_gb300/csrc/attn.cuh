@@ -1,0 +1,73 @@
+// Shared by the attention kernels over the token memory: arguments, spans of
+// the sequences, the absent slots' mask and the score's arithmetic.
+#pragma once
+
+#include "common.cuh"
+
+namespace rtcc {
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+constexpr int kMaxSlots = 64;
+
+struct AttnArgs {
+  const void *q, *k, *v;
+  void* out;
+  float* lse;                    // [n_q][heads], may be null
+  const int *q_offsets, *k_begin, *k_end;
+  const int* prefix;             // may be null
+  const int* present;            // [n_slots], may be null
+  const float *slopes, *q_pos, *k_pos;
+  float* part_o;                 // [n_chunks][n_q * heads][dim] when n_chunks > 1
+  float2* part_ml;               // [n_chunks][n_q * heads]: running maximum (log2) and sum
+  long long q_row, q_head, k_row, k_head, v_row, v_head, out_row, out_head;
+  int n_q, n_rows, heads, kv_heads, group, dim, n_seqs, causal;
+  int n_slots, slot_rows, q_pos_row;
+  int n_chunks, chunk;           // key chunks per sequence at most, keys per chunk at least
+  int row_groups;                // blocks along the rows of one sequence and key head
+  float scale_log2;              // scale * log2(e); with a cap: scale / cap
+  float cap_log2;                // cap * log2(e), 0 = no cap
+};
+
+// One sequence: its tokens [q0, q0 + nq) and memory rows [kb, kb + nk).  Offsets
+// come from device memory, so they are cut to the arrays' extents.
+struct AttnSpan {
+  int q0, nq, kb, nk, prefix;
+};
+
+__device__ __forceinline__ AttnSpan attn_span(const AttnArgs& A, int seq) {
+  AttnSpan s;
+  const int q0 = A.q_offsets[seq], q1 = A.q_offsets[seq + 1];
+  const int kb = A.k_begin[seq], ke = A.k_end[seq];
+  s.q0 = min(max(q0, 0), A.n_q);
+  s.nq = min(max(q1, s.q0), A.n_q) - s.q0;
+  s.kb = min(max(kb, 0), A.n_rows);
+  s.nk = min(max(ke, s.kb), A.n_rows) - s.kb;
+  s.prefix = A.prefix ? min(max(A.prefix[seq], 0), s.nk) : 0;
+  return s;
+}
+
+// Keys [0, n) of the span that token i of the sequence sees (slots aside).
+__device__ __forceinline__ int attn_visible(const AttnArgs& A, const AttnSpan& s, int i) {
+  if (!A.causal) return s.nk;
+  return max(0, min(s.nk, max(s.prefix, i + 1 + s.nk - s.nq)));
+}
+
+// Bit s set: slot s is present (all ones without slots).  Whole warp.
+__device__ __forceinline__ unsigned long long attn_slot_mask(const AttnArgs& A, int lane) {
+  if (!A.present) return ~0ull;
+  const unsigned lo = __ballot_sync(0xFFFFFFFFu, lane < A.n_slots && A.present[min(lane, A.n_slots - 1)] != 0);
+  const unsigned hi =
+      __ballot_sync(0xFFFFFFFFu, lane + 32 < A.n_slots && A.present[min(lane + 32, A.n_slots - 1)] != 0);
+  return (unsigned long long)hi << 32 | lo;
+}
+
+// Keys per chunk of a sequence: the launch's, or more where the sequence is
+// longer than the launch was told; the chunks in use follow.
+__device__ __forceinline__ int attn_chunk(const AttnArgs& A, int nk, int unit) {
+  const int need = (int)(((long long)nk + A.n_chunks - 1) / A.n_chunks);
+  const int c = max(A.chunk, need);
+  return (c + unit - 1) / unit * unit;
+}
+
+}  // namespace rtcc

@@ -1,0 +1,424 @@
+// Attention of a few rows over long spans of the token memory, and the join of
+// partial results.
+//
+//   s_ij = cap tanh(scale q_i.k_j / cap) - slope_h |r_i - r_j|_1   (cap 0: no tanh)
+//   out_i = sum_j softmax_j(s_ij) v_j,  lse_i = ln sum_j exp(s_ij)
+//   j over the visible keys; no visible key: out_i = 0, lse_i = -inf
+//
+// A row is a (token, head) pair; the heads that share a key head are rows of
+// the same block, so every key and value is read once per 16 rows.  A block has
+// 16 rows (the M of mma.m16n8k16), one key head and one chunk of the span; its
+// four warps take key tiles in turn, each with a running maximum, sum and
+// 16 x dim accumulator in registers and a ring of three tiles of its own in
+// shared memory filled by 16-byte asynchronous copies (no block barrier in the
+// loop).  Rows of the memory that no query may see are never read: their place
+// in the tile is zero-filled, so stale or non-finite contents do not matter.
+// With few rows the memory's bytes bound it, and splitting the span into chunks
+// fills the GPU; k_attn_join merges the chunks in index order.
+#include "attn.cuh"
+#include "kernels.h"
+
+namespace rtcc {
+namespace {
+
+constexpr int kWarps = 4;
+constexpr int kStages = 3;
+constexpr int kRows = 16;
+
+template <int DP> struct RowsCfg {               // DP: head size padded to 64 or 128
+  static constexpr int KT = DP == 64 ? 32 : 16;  // keys per tile: 4 KB of keys, 4 KB of values
+  static constexpr int kTileBytes = KT * DP * 2;
+  static constexpr int kPosBytes = KT * 8;
+  static constexpr int kStageBytes = 2 * kTileBytes + kPosBytes;
+  static constexpr int kRing = kWarps * kStages * kStageBytes;
+  static constexpr int kMerge = kWarps * kRows * (DP + 4) * 4;   // the warps' accumulators at the end
+  static constexpr int kSmem = kRing > kMerge ? kRing : kMerge;
+};
+
+__device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool live) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(live ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void cp8(uint32_t dst, const void* src, bool live) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst), "l"(src), "r"(live ? 8 : 0) : "memory");
+}
+__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+__device__ __forceinline__ void ldm4(uint32_t a, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(a)
+               : "memory");
+}
+__device__ __forceinline__ void ldm4t(uint32_t a, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(a)
+               : "memory");
+}
+
+template <typename T>
+__device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1);
+template <>
+__device__ __forceinline__ void mma16816<__half>(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+template <>
+__device__ __forceinline__ void mma16816<__nv_bfloat16>(float (&d)[4], const uint32_t (&a)[4], uint32_t b0,
+                                                        uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+// tanh(u) = 1 - 2 / (1 + e^2u): its absolute error (about 2e-7) is what counts
+// here, since the cap multiplies it into a score.
+__device__ __forceinline__ float tanh_abs(float u) {
+  return 1.0f - __fdividef(2.0f, 1.0f + exp2f(fminf(2.0f * kLog2e * u, 64.0f)));
+}
+
+// Byte offset of 16-byte unit c of row r in a tile of DP-channel rows; units
+// are permuted within 128-byte lines so that ldmatrix reads 8 rows without
+// bank conflicts.
+template <int DP>
+__device__ __forceinline__ uint32_t tile_off(int r, int c) {
+  return (uint32_t)(r * DP * 2 + (c & ~7) * 16 + (((c ^ r) & 7) * 16));
+}
+
+template <typename T, int DP>
+__global__ void __launch_bounds__(kWarps * 32, 2) k_attn_rows(const __grid_constant__ AttnArgs A) {
+  using C = RowsCfg<DP>;
+  constexpr int KT = C::KT;
+  extern __shared__ __align__(128) unsigned char smem[];
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+  // block -> (sequence, key head, first row group, chunk), chunks fastest
+  int b = blockIdx.x;
+  const int chunk = b % A.n_chunks;
+  b /= A.n_chunks;
+  const int rg0 = b % A.row_groups;
+  b /= A.row_groups;
+  const int kvh = b % A.kv_heads;
+  const int seq = b / A.kv_heads;
+  const AttnSpan S = attn_span(A, seq);
+  const int rows_all = S.nq * A.group;
+  const int per = attn_chunk(A, S.nk, KT * kWarps);
+  const int c0 = (int)min((long long)per * chunk, (long long)S.nk), c1 = min(S.nk - c0, per) + c0;
+  if (chunk > 0 && c0 >= S.nk) return;           // not in use; chunk 0 always answers
+  const unsigned long long slots = attn_slot_mask(A, lane);
+  const uint32_t ring = smem_u32(smem) + w * kStages * C::kStageBytes;
+  const unsigned char* ring_g = smem + w * kStages * C::kStageBytes;
+  const bool dist = A.slopes != nullptr;
+  const T* kbase = static_cast<const T*>(A.k) + (long long)kvh * A.k_head;
+  const T* vbase = static_cast<const T*>(A.v) + (long long)kvh * A.v_head;
+
+  for (int rg = rg0; rg * kRows < rows_all; rg += A.row_groups) {
+    const int r0 = rg * kRows;
+    // this lane's two rows: lane / 4 and 8 further
+    int hi[2], head[2];
+    bool row_ok[2];
+    long long tok[2];
+    float slope[2], qy[2], qx[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int r = r0 + lane / 4 + 8 * i;
+      row_ok[i] = r < rows_all;
+      const int ql = row_ok[i] ? r / A.group : 0;
+      head[i] = kvh * A.group + (row_ok[i] ? r % A.group : 0);
+      tok[i] = S.q0 + ql;
+      hi[i] = row_ok[i] ? attn_visible(A, S, ql) : 0;
+      slope[i] = dist ? A.slopes[head[i]] * kLog2e : 0.f;
+      qy[i] = dist && row_ok[i] ? A.q_pos[tok[i] * A.q_pos_row] : 0.f;
+      qx[i] = dist && row_ok[i] ? A.q_pos[tok[i] * A.q_pos_row + 1] : 0.f;
+    }
+    // the rows' reach: keys past it are not read
+    int reach = max(hi[0], hi[1]), least = min(row_ok[0] ? hi[0] : S.nk, row_ok[1] ? hi[1] : S.nk);
+#pragma unroll
+    for (int d = 4; d < 32; d <<= 1) {
+      reach = max(reach, __shfl_xor_sync(0xFFFFFFFFu, reach, d));
+      least = min(least, __shfl_xor_sync(0xFFFFFFFFu, least, d));
+    }
+    const int end = min(c1, reach);
+    // A fragments of Q
+    uint32_t qa[DP / 16][4];
+#pragma unroll
+    for (int s = 0; s < DP / 16; ++s)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int col = s * 16 + (lane % 4) * 2 + (i >> 1) * 8;
+        const int rr = i & 1;
+        qa[s][i] = row_ok[rr] && col < A.dim
+                       ? *reinterpret_cast<const uint32_t*>(static_cast<const T*>(A.q) + tok[rr] * A.q_row +
+                                                            (long long)head[rr] * A.q_head + col)
+                       : 0u;
+      }
+    float o[DP / 8][4];
+#pragma unroll
+    for (int n = 0; n < DP / 8; ++n) o[n][0] = o[n][1] = o[n][2] = o[n][3] = 0.f;
+    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+
+    const int n_tiles = end > c0 ? (end - c0 + KT - 1) / KT : 0;
+    // bits of the tile's keys that may be read: in the span's reach, slot present
+    auto key_bits = [&](int t) -> unsigned {
+      const int j = c0 + t * KT + lane;
+      bool ok = t < n_tiles && lane < KT && j < end;
+      if (ok && A.present) ok = (slots >> min((S.kb + j) / A.slot_rows, 63)) & 1;
+      return __ballot_sync(0xFFFFFFFFu, ok);
+    };
+    auto load = [&](int t, int stage) {
+      const unsigned bits = key_bits(t);
+      if (bits) {
+        const uint32_t ks = ring + stage * C::kStageBytes, vs = ks + C::kTileBytes, ps = vs + C::kTileBytes;
+        constexpr int U = DP / 8;                // 16-byte units of a row
+#pragma unroll
+        for (int i = 0; i < KT * U / 32; ++i) {
+          const int idx = i * 32 + lane, r = idx / U, c = idx % U;
+          const bool live = (bits >> r) & 1 && c * 8 < A.dim;
+          const long long row = live ? (long long)S.kb + c0 + t * KT + r : 0;
+          const int col = live ? c * 8 : 0;
+          const uint32_t at = tile_off<DP>(r, c);
+          cp16(ks + at, kbase + row * A.k_row + col, live);
+          cp16(vs + at, vbase + row * A.v_row + col, live);
+        }
+        if (dist && lane < KT) {
+          const bool live = (bits >> lane) & 1;
+          const long long row = live ? (long long)S.kb + c0 + t * KT + lane : 0;
+          cp8(ps + lane * 8, A.k_pos + 2 * row, live);
+        }
+      }
+      cp_commit();
+    };
+#pragma unroll
+    for (int s = 0; s < kStages - 1; ++s) load(w + s * kWarps, s);
+    int stage = 0;
+    for (int t = w; t < n_tiles; t += kWarps) {
+      cp_wait<kStages - 2>();
+      __syncwarp();
+      load(t + (kStages - 1) * kWarps, (stage + kStages - 1) % kStages);
+      const unsigned bits = key_bits(t);
+      if (bits) {
+        const uint32_t ks = ring + stage * C::kStageBytes, vs = ks + C::kTileBytes;
+        const float2* ps = reinterpret_cast<const float2*>(ring_g + stage * C::kStageBytes + 2 * C::kTileBytes);
+        float s[KT / 8][4];
+#pragma unroll
+        for (int n = 0; n < KT / 8; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f;
+#pragma unroll
+        for (int d = 0; d < DP / 32; ++d)        // 32 channels: two k16 steps, one ldmatrix.x4 per 8 keys
+#pragma unroll
+          for (int n = 0; n < KT / 8; ++n) {
+            uint32_t kb4[4];
+            ldm4(ks + tile_off<DP>(n * 8 + (lane & 7), d * 4 + (lane >> 3)), kb4);
+            mma16816<T>(s[n], qa[2 * d], kb4[0], kb4[1]);
+            mma16816<T>(s[n], qa[2 * d + 1], kb4[2], kb4[3]);
+          }
+        const int j0 = c0 + t * KT;
+        const unsigned full = KT == 32 ? 0xFFFFFFFFu : (1u << KT) - 1u;
+        const bool edge = bits != full || j0 + KT > least;
+        float top[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+        for (int n = 0; n < KT / 8; ++n)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int key = n * 8 + (lane & 3) * 2 + (i & 1), rr = i >> 1;
+            float x = s[n][i] * A.scale_log2;
+            if (A.cap_log2 > 0.f) x = A.cap_log2 * tanh_abs(x);
+            if (dist) {
+              const float2 p = ps[key];
+              x = fmaf(-slope[rr], fabsf(qy[rr] - p.x) + fabsf(qx[rr] - p.y), x);
+            }
+            if (edge && !(((bits >> key) & 1) && j0 + key < hi[rr])) x = -INFINITY;
+            s[n][i] = x;
+            top[rr] = fmaxf(top[rr], x);
+          }
+#pragma unroll
+        for (int rr = 0; rr < 2; ++rr) {
+          top[rr] = fmaxf(top[rr], __shfl_xor_sync(0xFFFFFFFFu, top[rr], 1));
+          top[rr] = fmaxf(top[rr], __shfl_xor_sync(0xFFFFFFFFu, top[rr], 2));
+          const float mn = fmaxf(m[rr], top[rr]);
+          const float base = mn == -INFINITY ? 0.f : mn;
+          const float f = exp2f(m[rr] - base);   // m = -inf: 0
+          m[rr] = mn;
+          l[rr] *= f;
+          top[rr] = base;
+          if (__any_sync(0xFFFFFFFFu, f != 1.0f)) {
+#pragma unroll
+            for (int n = 0; n < DP / 8; ++n) {
+              o[n][2 * rr] *= f;
+              o[n][2 * rr + 1] *= f;
+            }
+          }
+        }
+#pragma unroll
+        for (int n = 0; n < KT / 8; ++n)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            s[n][i] = exp2f(s[n][i] - top[i >> 1]);
+            l[i >> 1] += s[n][i];
+          }
+#pragma unroll
+        for (int kk = 0; kk < KT / 16; ++kk) {
+          uint32_t pa[4];                        // probabilities rounded to the storage type for the product
+          pa[0] = Store<T>::pack2(s[2 * kk][0], s[2 * kk][1]);
+          pa[1] = Store<T>::pack2(s[2 * kk][2], s[2 * kk][3]);
+          pa[2] = Store<T>::pack2(s[2 * kk + 1][0], s[2 * kk + 1][1]);
+          pa[3] = Store<T>::pack2(s[2 * kk + 1][2], s[2 * kk + 1][3]);
+#pragma unroll
+          for (int n = 0; n < DP / 16; ++n) {
+            uint32_t vb[4];
+            ldm4t(vs + tile_off<DP>(kk * 16 + (lane & 15), n * 2 + (lane >> 4)), vb);
+            mma16816<T>(o[2 * n], pa, vb[0], vb[1]);
+            mma16816<T>(o[2 * n + 1], pa, vb[2], vb[3]);
+          }
+        }
+      }
+      stage = (stage + 1) % kStages;
+    }
+    cp_wait<0>();
+#pragma unroll
+    for (int rr = 0; rr < 2; ++rr) {
+      l[rr] += __shfl_xor_sync(0xFFFFFFFFu, l[rr], 1);
+      l[rr] += __shfl_xor_sync(0xFFFFFFFFu, l[rr], 2);
+    }
+    // merge the four warps' states through shared memory (the ring is done with)
+    __syncthreads();
+    float* mo = reinterpret_cast<float*>(smem);  // [warp][row][DP + 4]: accumulator, maximum, sum
+    constexpr int P = DP + 4;
+#pragma unroll
+    for (int rr = 0; rr < 2; ++rr) {
+      float* dst = mo + (w * kRows + lane / 4 + 8 * rr) * P;
+#pragma unroll
+      for (int n = 0; n < DP / 8; ++n)
+        *reinterpret_cast<float2*>(dst + n * 8 + (lane & 3) * 2) = make_float2(o[n][2 * rr], o[n][2 * rr + 1]);
+      if ((lane & 3) == 0) {
+        dst[DP] = m[rr];
+        dst[DP + 1] = l[rr];
+      }
+    }
+    __syncthreads();
+    for (int idx = threadIdx.x; idx < kRows * (DP / 4); idx += kWarps * 32) {
+      const int r = idx / (DP / 4), c = (idx % (DP / 4)) * 4;
+      if (r0 + r >= rows_all) continue;
+      float mm = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < kWarps; ++i) mm = fmaxf(mm, mo[(i * kRows + r) * P + DP]);
+      const float base = mm == -INFINITY ? 0.f : mm;
+      float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+      float ll = 0.f;
+#pragma unroll
+      for (int i = 0; i < kWarps; ++i) {
+        const float* src = mo + (i * kRows + r) * P;
+        const float f = exp2f(src[DP] - base);
+        const float4 x = *reinterpret_cast<const float4*>(src + c);
+        acc.x = fmaf(f, x.x, acc.x);
+        acc.y = fmaf(f, x.y, acc.y);
+        acc.z = fmaf(f, x.z, acc.z);
+        acc.w = fmaf(f, x.w, acc.w);
+        ll = fmaf(f, src[DP + 1], ll);
+      }
+      if (c >= A.dim) continue;
+      const long long t = S.q0 + (r0 + r) / A.group;
+      const int h = kvh * A.group + (r0 + r) % A.group;
+      const long long R = t * A.heads + h;
+      if (A.n_chunks > 1) {
+        const long long at = (long long)chunk * A.n_q * A.heads + R;
+        *reinterpret_cast<float4*>(A.part_o + at * A.dim + c) = acc;
+        if (c == 0) A.part_ml[at] = make_float2(mm, ll);
+      } else {
+        const float inv = ll > 0.f ? 1.0f / ll : (ll == 0.f ? 0.f : ll);
+        uint2 u;
+        u.x = Store<T>::pack2(acc.x * inv, acc.y * inv);
+        u.y = Store<T>::pack2(acc.z * inv, acc.w * inv);
+        *reinterpret_cast<uint2*>(static_cast<T*>(A.out) + t * A.out_row + (long long)h * A.out_head + c) = u;
+        if (c == 0 && A.lse) A.lse[R] = ll == 0.f ? -INFINITY : (mm + log2f(ll)) * kLn2;
+      }
+    }
+    __syncthreads();
+  }
+}
+
+// out_i = sum_c 2^(m_c - M) O_c / sum_c 2^(m_c - M) l_c over the chunks in use,
+// in index order: one warp per row, 4 channels per lane.
+constexpr int kJoinWarps = 4;
+template <typename T>
+__global__ void __launch_bounds__(kJoinWarps * 32) k_attn_join(const __grid_constant__ AttnArgs A, int unit,
+                                                               int blocks_per_seq) {
+  pdl_wait();
+  const int seq = blockIdx.x / blocks_per_seq, b = blockIdx.x % blocks_per_seq;
+  const int lane = threadIdx.x & 31;
+  const AttnSpan S = attn_span(A, seq);
+  const int per = attn_chunk(A, S.nk, unit);
+  const int used = max(1, (int)(((long long)S.nk + per - 1) / per));
+  const long long rows = (long long)S.nq * A.heads, stride = (long long)A.n_q * A.heads;
+  for (long long i = (long long)b * kJoinWarps + (threadIdx.x >> 5); i < rows; i += (long long)blocks_per_seq * kJoinWarps) {
+    const long long R = (long long)S.q0 * A.heads + i;
+    float mm = -INFINITY;
+    for (int c = lane; c < used; c += 32) mm = fmaxf(mm, A.part_ml[c * stride + R].x);
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) mm = fmaxf(mm, __shfl_xor_sync(0xFFFFFFFFu, mm, d));
+    const float base = mm == -INFINITY ? 0.f : mm;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    float ll = 0.f;
+    const int c4 = lane * 4;
+    for (int c = 0; c < used; ++c) {
+      const float2 ml = A.part_ml[c * stride + R];
+      const float f = exp2f(ml.x - base);
+      ll = fmaf(f, ml.y, ll);
+      if (c4 < A.dim) {
+        const float4 x = *reinterpret_cast<const float4*>(A.part_o + (c * stride + R) * A.dim + c4);
+        acc.x = fmaf(f, x.x, acc.x);
+        acc.y = fmaf(f, x.y, acc.y);
+        acc.z = fmaf(f, x.z, acc.z);
+        acc.w = fmaf(f, x.w, acc.w);
+      }
+    }
+    const long long t = R / A.heads;
+    const int h = (int)(R % A.heads);
+    const float inv = ll > 0.f ? 1.0f / ll : (ll == 0.f ? 0.f : ll);
+    if (c4 < A.dim) {
+      uint2 u;
+      u.x = Store<T>::pack2(acc.x * inv, acc.y * inv);
+      u.y = Store<T>::pack2(acc.z * inv, acc.w * inv);
+      *reinterpret_cast<uint2*>(static_cast<T*>(A.out) + t * A.out_row + (long long)h * A.out_head + c4) = u;
+    }
+    if (lane == 0 && A.lse) A.lse[R] = ll == 0.f ? -INFINITY : (mm + log2f(ll)) * kLn2;
+  }
+}
+
+template <typename T, int DP>
+cudaError_t launch_rows_t(const AttnArgs& a, cudaStream_t st) {
+  using C = RowsCfg<DP>;
+  cudaError_t e = cudaFuncSetAttribute(k_attn_rows<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem);
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t lc = {};
+  lc.gridDim = dim3((unsigned)((long long)a.n_seqs * a.kv_heads * a.row_groups * a.n_chunks));
+  lc.blockDim = dim3(kWarps * 32);
+  lc.dynamicSmemBytes = C::kSmem;
+  lc.stream = st;
+  return cudaLaunchKernelEx(&lc, k_attn_rows<T, DP>, a);
+}
+
+}  // namespace
+
+int attn_rows_unit(int dim) { return kWarps * (dim <= 64 ? RowsCfg<64>::KT : RowsCfg<128>::KT); }
+int attn_rows_per_block() { return kRows; }
+
+cudaError_t launch_attn_rows(const AttnArgs& a, bool bf16, cudaStream_t st) {
+  if (a.dim <= 64) return bf16 ? launch_rows_t<__nv_bfloat16, 64>(a, st) : launch_rows_t<__half, 64>(a, st);
+  return bf16 ? launch_rows_t<__nv_bfloat16, 128>(a, st) : launch_rows_t<__half, 128>(a, st);
+}
+
+cudaError_t launch_attn_join(const AttnArgs& a, int unit, int max_q, bool bf16, cudaStream_t st) {
+  long long per = ((long long)max_q * a.heads + kJoinWarps - 1) / kJoinWarps;
+  if (per < 1) per = 1;
+  if (per > 4096) per = 4096;
+  while ((long long)a.n_seqs * per > 0x7FFFFFFF && per > 1) per /= 2;
+  const dim3 grid((unsigned)((long long)a.n_seqs * per));
+  return bf16 ? launch_pdl(k_attn_join<__nv_bfloat16>, grid, dim3(kJoinWarps * 32), 0, st, a, unit, (int)per)
+              : launch_pdl(k_attn_join<__half>, grid, dim3(kJoinWarps * 32), 0, st, a, unit, (int)per);
+}
+
+}  // namespace rtcc

@@ -356,4 +356,12 @@ struct NmsArgs {
 size_t nms_mask_words(int max_boxes);
 cudaError_t launch_nms(const NmsArgs& a, cudaStream_t st);
 
+// Attention over the token memory (attn.cuh, attn_rows.cu).
+struct AttnArgs;
+int attn_rows_unit(int dim);       // chunks of the span are multiples of this many keys
+int attn_rows_per_block();         // (token, head) rows per block
+cudaError_t launch_attn_rows(const AttnArgs& a, bool bf16, cudaStream_t st);
+// Merge of the chunks' partial results into out and lse.
+cudaError_t launch_attn_join(const AttnArgs& a, int unit, int max_q, bool bf16, cudaStream_t st);
+
 }  // namespace rtcc

@@ -74,6 +74,30 @@ class rtcc_conv_plan(C.Structure):
                 ("items", C.c_int32)]
 
 
+class rtcc_prepare_config(C.Structure):
+    _fields_ = [
+        ("heads", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32), ("dtype", C.c_int32),
+        ("n_tokens", C.c_int32), ("n_rows", C.c_int32),
+        ("q_row", C.c_int64), ("q_head", C.c_int64), ("k_row", C.c_int64), ("k_head", C.c_int64),
+        ("v_row", C.c_int64), ("v_head", C.c_int64), ("qo_row", C.c_int64), ("qo_head", C.c_int64),
+        ("km_row", C.c_int64), ("km_head", C.c_int64), ("vm_row", C.c_int64), ("vm_head", C.c_int64),
+        ("axis_pairs", C.c_int32 * 3), ("interleaved", C.c_int32), ("norm", C.c_int32),
+        ("theta", C.c_float), ("eps", C.c_float),
+    ]
+
+
+class rtcc_attn_config(C.Structure):
+    _fields_ = [
+        ("heads", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32), ("dtype", C.c_int32),
+        ("n_q", C.c_int32), ("n_rows", C.c_int32),
+        ("q_row", C.c_int64), ("q_head", C.c_int64), ("k_row", C.c_int64), ("k_head", C.c_int64),
+        ("v_row", C.c_int64), ("v_head", C.c_int64), ("out_row", C.c_int64), ("out_head", C.c_int64),
+        ("n_seqs", C.c_int32), ("max_q", C.c_int32), ("max_k", C.c_int32), ("causal", C.c_int32),
+        ("n_slots", C.c_int32), ("slot_rows", C.c_int32), ("q_pos_row", C.c_int32),
+        ("scale", C.c_float), ("cap", C.c_float),
+    ]
+
+
 BOX_DTYPE = np.dtype([("x", "<f4"), ("y", "<f4"), ("z", "<f4"), ("l", "<f4"), ("w", "<f4"),
                       ("h", "<f4"), ("yaw", "<f4"), ("score", "<f4"), ("anchor", "<i4")])
 
@@ -153,6 +177,10 @@ def load(path: Optional[str] = None) -> C.CDLL:
         "rtcc_pillarise_noalloc": (S, [C.POINTER(rtcc_model_config), C.c_void_p, C.c_int32,
                                        C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
                                        C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]),
+        "rtcc_memory_append": (S, [C.c_int32] * 3 + [C.c_void_p] * 11),
+        "rtcc_qkv_prepare": (S, [C.POINTER(rtcc_prepare_config)] + [C.c_void_p] * 12),
+        "rtcc_memory_attention": (S, [C.POINTER(rtcc_attn_config)] + [C.c_void_p] * 14 +
+                                  [C.c_size_t, C.c_void_p]),
     }
     for name, (res, args) in sig.items():
         f = getattr(lib, name)
@@ -166,6 +194,11 @@ def _chk(status: int, where: str) -> int:
     if status != OK:
         raise RTCCError(status, where)
     return status
+
+
+def check(status: int, where: str = "rtcc") -> int:
+    """Raise RTCCError unless `status` is OK; returns it."""
+    return _chk(status, where)
 
 
 def _ptr(a: Optional[np.ndarray]):
@@ -408,6 +441,53 @@ def rtcc_pillarise_noalloc(cfg: rtcc_model_config, d_points: int, n_points: int,
     return load().rtcc_pillarise_noalloc(C.byref(cfg), d_points, n_points, d_pfn_w, d_pfn_b,
                                          d_cell2pillar, d_pillar_cell, d_count, d_stats,
                                          d_image, stream or None)
+
+
+# --------------------------------------------------------------------------
+# token memory; every d_* is a device address (0 or None: NULL)
+# --------------------------------------------------------------------------
+
+def rtcc_memory_append(n_seqs: int, capacity: int, n_tokens: int, d_new, d_held, d_slot, d_offsets,
+                       d_rows, d_seq, d_pos, d_begin, d_end, d_length, stream: int = 0) -> int:
+    """Memory rows, offsets, spans and lengths for new tokens (see rtcc.h)."""
+    return load().rtcc_memory_append(n_seqs, capacity, n_tokens, d_new, d_held, d_slot, d_offsets,
+                                     d_rows, d_seq, d_pos, d_begin, d_end, d_length, stream or None)
+
+
+def prepare_config(heads: int, kv_heads: int, head_dim: int, dtype: int, n_tokens: int, n_rows: int,
+                   q, k, v, q_out, k_mem, v_mem, axis_pairs, interleaved: bool = False,
+                   norm: bool = True, theta: float = 10000.0, eps: float = 1e-6) -> rtcc_prepare_config:
+    """Shapes of rtcc_qkv_prepare; q .. v_mem are the arrays' (row, head)
+    strides in elements, axis_pairs the pairs of (t, y, x)."""
+    return rtcc_prepare_config(heads, kv_heads, head_dim, dtype, n_tokens, n_rows, *q, *k, *v, *q_out,
+                               *k_mem, *v_mem, tuple(axis_pairs), interleaved, norm, theta, eps)
+
+
+def rtcc_qkv_prepare(cfg: rtcc_prepare_config, d_q, d_k, d_v, d_q_gain, d_k_gain, d_pos, d_rows,
+                     d_q_out, d_k_mem, d_v_mem, d_coord, stream: int = 0) -> int:
+    """Norm, rotation and memory write of new tokens (see rtcc.h)."""
+    return load().rtcc_qkv_prepare(cfg, d_q, d_k, d_v, d_q_gain, d_k_gain, d_pos, d_rows, d_q_out,
+                                   d_k_mem, d_v_mem, d_coord, stream or None)
+
+
+def attn_config(heads: int, kv_heads: int, head_dim: int, dtype: int, n_q: int, n_rows: int, q, k, v,
+                out, n_seqs: int, max_q: int, max_k: int, causal: bool = False, n_slots: int = 0,
+                slot_rows: int = 0, q_pos_row: int = 2, scale: Optional[float] = None,
+                cap: float = 0.0) -> rtcc_attn_config:
+    """Shapes of rtcc_memory_attention; q .. out are the arrays' (row, head)
+    strides in elements; scale None = 1 / sqrt(head_dim)."""
+    return rtcc_attn_config(heads, kv_heads, head_dim, dtype, n_q, n_rows, *q, *k, *v, *out, n_seqs, max_q,
+                            max_k, causal, n_slots, slot_rows, q_pos_row,
+                            head_dim ** -0.5 if scale is None else scale, cap)
+
+
+def rtcc_memory_attention(cfg: rtcc_attn_config, d_q, d_k, d_v, d_q_offsets, d_k_begin, d_k_end, d_prefix,
+                          d_present, d_slopes, d_q_pos, d_k_pos, d_out, d_lse, d_workspace,
+                          workspace_bytes: int, stream: int = 0) -> int:
+    """Attention over spans of the token memory (see rtcc.h)."""
+    return load().rtcc_memory_attention(cfg, d_q, d_k, d_v, d_q_offsets, d_k_begin, d_k_end, d_prefix,
+                                        d_present, d_slopes, d_q_pos, d_k_pos, d_out, d_lse, d_workspace,
+                                        workspace_bytes, stream or None)
 
 
 # --------------------------------------------------------------------------
