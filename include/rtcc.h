@@ -556,6 +556,13 @@ rtcc_status rtcc_memory_attention(const rtcc_attn_config* cfg, const void* d_q, 
                                   const float* d_k_pos, void* d_out, float* d_lse,
                                   void* d_workspace, size_t workspace_bytes, void* stream);
 
+/*
+ * Wait for `stream` and report on the attention calls of this device since the
+ * last report: RTCC_E_DEVICE if a kernel gave up one of its bounded waits (its
+ * outputs are then not valid), else RTCC_OK.  Not during a stream capture.
+ */
+rtcc_status rtcc_memory_attention_status(void* stream);
+
 /* ------------------------------------------------------------------------ */
 /* Release controller alone (host only; no GPU needed)                      */
 /* ------------------------------------------------------------------------ */

@@ -9,6 +9,8 @@
 namespace rtcc {
 namespace {
 
+constexpr int kTcRows = 64;
+
 bool misaligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
 bool bad_stride(int64_t s) { return s < 0 || s % 8 != 0; }
 
@@ -34,6 +36,7 @@ extern "C" rtcc_status rtcc_memory_attention(const rtcc_attn_config* c, const vo
   for (int64_t s : strides)
     if (bad_stride(s)) return RTCC_E_ARG;
   if (!isfinite(c->scale) || !isfinite(c->cap) || c->cap < 0.f) return RTCC_E_ARG;
+  if (c->cap > 0.f && !isfinite(c->scale / c->cap)) return RTCC_E_ARG;
   if (c->n_slots < 0 || c->n_slots > kMaxSlots || (c->n_slots > 0) != (d_present != nullptr)) return RTCC_E_ARG;
   if (c->n_slots > 0 && (c->slot_rows < 1 || (long long)c->n_slots * c->slot_rows < c->n_rows)) return RTCC_E_ARG;
   if ((d_slopes != nullptr) != (d_q_pos != nullptr) || (d_slopes != nullptr) != (d_k_pos != nullptr)) return RTCC_E_ARG;
@@ -69,28 +72,49 @@ extern "C" rtcc_status rtcc_memory_attention(const rtcc_attn_config* c, const vo
 
   const int max_q = c->max_q < 1 ? 1 : c->max_q > c->n_q ? c->n_q : c->max_q;
   const int max_k = c->max_k < 1 ? 1 : c->max_k > c->n_rows ? (c->n_rows < 1 ? 1 : c->n_rows) : c->max_k;
-  const int unit = attn_rows_unit(c->head_dim), rows = attn_rows_per_block();
-  long long groups = ((long long)max_q * a.group + rows - 1) / rows;
-  long long units = (long long)c->n_seqs * a.kv_heads;
-  while (units * groups > 0x3FFFFFFF && groups > 1) groups = (groups + 1) / 2;   // blocks then loop
-  if (units > 0x3FFFFFFF) return RTCC_E_ARG;
-  units *= groups;
-  a.row_groups = (int)groups;
-  // chunks of the span: enough blocks for a few rounds over the SMs (two blocks
-  // fit on one), each at least four tiles a warp, within the workspace
-  const long long want = (4LL * 2 * sms + units - 1) / units;
-  long long chunks = (max_k + 4LL * unit - 1) / (4LL * unit);
-  if (chunks > want) chunks = want;
-  const size_t part = (size_t)c->n_q * c->heads * (c->head_dim * sizeof(float) + sizeof(float2));
-  if (!d_workspace || workspace_bytes / part < (size_t)chunks) chunks = d_workspace ? (long long)(workspace_bytes / part) : 1;
-  if (chunks < 1) chunks = 1;
-  a.n_chunks = (int)chunks;
-  a.chunk = (int)((max_k + chunks - 1) / chunks);
-  a.part_o = static_cast<float*>(d_workspace);
-  a.part_ml = reinterpret_cast<float2*>(a.part_o + (size_t)chunks * c->n_q * c->heads * c->head_dim);
   const bool bf16 = c->dtype == RTCC_BF16;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  if (launch_attn_rows(a, bf16, st) != cudaSuccess) return RTCC_E_CUDA;
-  if (chunks > 1 && launch_attn_join(a, unit, max_q, bf16, st) != cudaSuccess) return RTCC_E_CUDA;
-  return RTCC_OK;
+  // The tensor-core kernel from kTcRows (token, head) rows per key head on.  It
+  // needs a positive scale (its maximum is taken over unscaled scores) and a cap
+  // its polynomial's coefficients can express.
+  bool tc = (long long)max_q * a.group > kTcRows && a.group <= 128 && c->scale > 0.f && a.scale_log2 < 1e4f &&
+            c->n_rows > 0;
+  for (;; tc = false) {
+    const int unit = tc ? attn_tc_unit() : attn_rows_unit(c->head_dim);
+    const long long step = tc ? attn_tc_tokens_per_block(a.group) : 1;
+    long long groups = tc ? (max_q + step - 1) / step
+                          : ((long long)max_q * a.group + attn_rows_per_block() - 1) / attn_rows_per_block();
+    long long units = (long long)c->n_seqs * a.kv_heads;
+    if (units > 0x3FFFFFFF) return RTCC_E_ARG;
+    while (units * groups > 0x3FFFFFFF && groups > 1) groups = (groups + 1) / 2;   // blocks then loop
+    units *= groups;
+    a.row_groups = (int)groups;
+    // Chunks of the span: enough blocks for a few rounds over the SMs (the
+    // few-rows kernel has two blocks on one), each at least four tiles (a warp),
+    // within the workspace.
+    const long long want = ((tc ? 2LL : 8LL) * sms + units - 1) / units;
+    long long chunks = (max_k + 4LL * unit - 1) / (4LL * unit);
+    if (chunks > want) chunks = want;
+    if (tc && units >= sms) chunks = 1;
+    while (chunks > 1 && units * chunks > 0x7FFFFFFF) chunks /= 2;
+    const size_t part = (size_t)c->n_q * c->heads * (c->head_dim * sizeof(float) + sizeof(float2));
+    const long long room = d_workspace ? (long long)(workspace_bytes / part) : 0;
+    if (chunks > room) chunks = room;
+    if (chunks < 1) chunks = 1;
+    a.n_chunks = (int)chunks;
+    a.chunk = (int)((max_k + chunks - 1) / chunks);
+    a.part_o = static_cast<float*>(d_workspace);
+    a.part_ml = reinterpret_cast<float2*>(a.part_o + (size_t)chunks * c->n_q * c->heads * c->head_dim);
+    const cudaError_t e = tc ? launch_attn_tc(a, bf16, st) : launch_attn_rows(a, bf16, st);
+    if (tc && e == cudaErrorNotSupported) continue;
+    if (e != cudaSuccess) return RTCC_E_CUDA;
+    if (chunks > 1 && launch_attn_join(a, unit, max_q, bf16, st) != cudaSuccess) return RTCC_E_CUDA;
+    return RTCC_OK;
+  }
+}
+
+extern "C" rtcc_status rtcc_memory_attention_status(void* stream) {
+  int err = 0;
+  if (attn_tc_error(&err, static_cast<cudaStream_t>(stream)) != cudaSuccess) return RTCC_E_CUDA;
+  return err ? RTCC_E_DEVICE : RTCC_OK;
 }

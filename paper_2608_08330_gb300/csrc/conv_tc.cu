@@ -1082,6 +1082,27 @@ cudaError_t tmap_3d(CUtensorMap* m, const void* base, bool bf16, uint64_t inner,
   return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
 
+cudaError_t tmap_rows(CUtensorMap* m, const void* base, bool bf16, uint64_t dim, uint64_t heads, uint64_t rows,
+                      uint64_t head_stride, uint64_t row_stride, uint32_t box_heads, uint32_t box_rows) {
+  EncodeFn enc = encode_fn();
+  if (!enc) return cudaErrorNotSupported;
+  // a dimension of one element has no stride of its own
+  if (heads == 1) head_stride = dim;
+  if (rows == 1) row_stride = head_stride * heads;
+  if (head_stride == 0 || row_stride == 0 || head_stride >= 1ull << 39 || row_stride >= 1ull << 39)
+    return cudaErrorNotSupported;
+  const CUtensorMapDataType dt =
+      bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+  cuuint64_t dims[3] = {dim, heads, rows};
+  cuuint64_t strides[2] = {head_stride * 2, row_stride * 2};
+  cuuint32_t box[3] = {64, box_heads, box_rows};
+  cuuint32_t es[3] = {1, 1, 1};
+  const CUresult r = enc(m, dt, 3, const_cast<void*>(base), dims, strides, box, es,
+                         CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                         CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorNotSupported;
+}
+
 int conv_tile_w() { return TW; }
 int conv_tile_h() { return TH; }
 int conv_tile_m() { return BM; }

@@ -304,6 +304,11 @@ cudaError_t tmap_2d(CUtensorMap* m, const void* base, bool bf16, uint64_t inner,
 cudaError_t tmap_3d(CUtensorMap* m, const void* base, bool bf16, uint64_t inner, uint64_t mid,
                     uint64_t outer, uint32_t box_inner, uint32_t box_mid, uint32_t box_outer,
                     int swizzle_bytes);
+// Vectors of `dim` channels at strides in elements, [rows][heads][dim], in boxes
+// of 64 channels of box_heads heads of box_rows rows, 128-byte swizzle;
+// cudaErrorNotSupported where a tensor map cannot describe them.
+cudaError_t tmap_rows(CUtensorMap* m, const void* base, bool bf16, uint64_t dim, uint64_t heads, uint64_t rows,
+                      uint64_t head_stride, uint64_t row_stride, uint32_t box_heads, uint32_t box_rows);
 // Head weight permutation expected by the fusion kernel (host side).
 void permute_head_weights(const float* w /*[16][C]*/, int C, float* out /*[16*C]*/);
 
@@ -356,11 +361,18 @@ struct NmsArgs {
 size_t nms_mask_words(int max_boxes);
 cudaError_t launch_nms(const NmsArgs& a, cudaStream_t st);
 
-// Attention over the token memory (attn.cuh, attn_rows.cu).
+// Attention over the token memory: few rows (attn_rows.cu), many (attn_tc.cu).
 struct AttnArgs;
 int attn_rows_unit(int dim);       // chunks of the span are multiples of this many keys
 int attn_rows_per_block();         // (token, head) rows per block
 cudaError_t launch_attn_rows(const AttnArgs& a, bool bf16, cudaStream_t st);
+// The tensor-core kernel for many rows (attn_tc.cu): its chunks' unit, tokens
+// per block, launch (cudaErrorNotSupported: the arrays do not fit a tensor map),
+// and the error word of its bounded waits, read and cleared.
+int attn_tc_unit();
+int attn_tc_tokens_per_block(int group);
+cudaError_t launch_attn_tc(const AttnArgs& a, bool bf16, cudaStream_t st);
+cudaError_t attn_tc_error(int* err, cudaStream_t st);
 // Merge of the chunks' partial results into out and lse.
 cudaError_t launch_attn_join(const AttnArgs& a, int unit, int max_q, bool bf16, cudaStream_t st);
 

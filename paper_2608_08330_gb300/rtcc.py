@@ -181,6 +181,7 @@ def load(path: Optional[str] = None) -> C.CDLL:
         "rtcc_qkv_prepare": (S, [C.POINTER(rtcc_prepare_config)] + [C.c_void_p] * 12),
         "rtcc_memory_attention": (S, [C.POINTER(rtcc_attn_config)] + [C.c_void_p] * 14 +
                                   [C.c_size_t, C.c_void_p]),
+        "rtcc_memory_attention_status": (S, [C.c_void_p]),
     }
     for name, (res, args) in sig.items():
         f = getattr(lib, name)
@@ -488,6 +489,11 @@ def rtcc_memory_attention(cfg: rtcc_attn_config, d_q, d_k, d_v, d_q_offsets, d_k
     return load().rtcc_memory_attention(cfg, d_q, d_k, d_v, d_q_offsets, d_k_begin, d_k_end, d_prefix,
                                         d_present, d_slopes, d_q_pos, d_k_pos, d_out, d_lse, d_workspace,
                                         workspace_bytes, stream or None)
+
+
+def rtcc_memory_attention_status(stream: int = 0) -> int:
+    """Wait for `stream`; E_DEVICE if an attention kernel gave up a wait."""
+    return load().rtcc_memory_attention_status(stream or None)
 
 
 # --------------------------------------------------------------------------
