@@ -67,6 +67,12 @@ extern "C" rtcc_status rtcc_memory_attention(const rtcc_attn_config* c, const vo
   a.n_q = c->n_q; a.n_rows = c->n_rows; a.heads = c->heads; a.kv_heads = c->kv_heads;
   a.group = c->heads / c->kv_heads; a.dim = c->head_dim; a.n_seqs = c->n_seqs; a.causal = c->causal != 0;
   a.n_slots = c->n_slots; a.slot_rows = c->n_slots ? c->slot_rows : 1; a.q_pos_row = c->q_pos_row;
+  // with l = ceil(log2(d)), ceil(2^(31 + l) / d) is a 32-bit multiplier that divides
+  // every row number (below 2^31) exactly
+  int l = 0;
+  while ((1LL << l) < a.slot_rows) ++l;
+  a.slot_mul = (uint32_t)(((1ull << (31 + l)) + a.slot_rows - 1) / a.slot_rows);
+  a.slot_shift = 31 + l;
   a.cap_log2 = c->cap * kLog2e;
   a.scale_log2 = c->cap > 0.f ? c->scale / c->cap : c->scale * kLog2e;
 

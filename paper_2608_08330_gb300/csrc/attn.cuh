@@ -23,6 +23,7 @@ struct AttnArgs {
   long long q_row, q_head, k_row, k_head, v_row, v_head, out_row, out_head;
   int n_q, n_rows, heads, kv_heads, group, dim, n_seqs, causal;
   int n_slots, slot_rows, q_pos_row;
+  uint32_t slot_mul, slot_shift; // row / slot_rows = row * slot_mul >> slot_shift
   int n_chunks, chunk;           // key chunks per sequence at most, keys per chunk at least
   int row_groups;                // blocks along the rows of one sequence and key head
   float scale_log2;              // scale * log2(e); with a cap: scale / cap
@@ -51,6 +52,11 @@ __device__ __forceinline__ AttnSpan attn_span(const AttnArgs& A, int seq) {
 __device__ __forceinline__ int attn_visible(const AttnArgs& A, const AttnSpan& s, int i) {
   if (!A.causal) return s.nk;
   return max(0, min(s.nk, max(s.prefix, i + 1 + s.nk - s.nq)));
+}
+
+// Slot of a memory row (there are at most 64).
+__device__ __forceinline__ int slot_of(const AttnArgs& A, int row) {
+  return (int)min((uint32_t)(((unsigned long long)(uint32_t)row * A.slot_mul) >> A.slot_shift), 63u);
 }
 
 // Bit s set: slot s is present (all ones without slots).  Whole warp.

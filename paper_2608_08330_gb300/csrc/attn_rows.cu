@@ -166,7 +166,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) k_attn_rows(const __grid_const
     auto key_bits = [&](int t) -> unsigned {
       const int j = c0 + t * KT + lane;
       bool ok = t < n_tiles && lane < KT && j < end;
-      if (ok && A.present) ok = (slots >> min((S.kb + j) / A.slot_rows, 63)) & 1;
+      if (ok && A.present) ok = (slots >> slot_of(A, S.kb + j)) & 1;
       return __ballot_sync(0xFFFFFFFFu, ok);
     };
     auto load = [&](int t, int stage) {
