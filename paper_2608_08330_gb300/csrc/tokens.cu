@@ -17,9 +17,11 @@
 //   x^ = x * rsqrt(mean(x^2) + eps) * gain,
 //   and pair m of axis a of x^ turned by pos_a * theta^(-m / pairs_a);
 //   q goes to a dense output, k, v and the (y, x) coordinates to the token's
-//   memory row.  It reads and writes every vector once, so HBM bounds it: a
-//   lane holds 8 channels (one 16-byte load and store), 2 to 16 lanes share a
-//   head, and a token's angles are computed once per warp, not once per head.
+//   memory row.  It reads and writes every vector once, so HBM bounds it.  A
+//   thread keeps one place (a head's 8 channels: one 16-byte load and store) for
+//   all the tokens it sees, so pointers, gains and the place's kind are set up
+//   once; it has up to four tokens' vectors in flight, and a block computes the
+//   angles of its batch of tokens once for all heads in the meantime.
 #include <math.h>
 
 #include "common.cuh"
@@ -121,7 +123,8 @@ __global__ void __launch_bounds__(kAppendThreads) k_memory_append(const AppendAr
 // prepare
 // ---------------------------------------------------------------------------
 
-constexpr int kPrepWarps = 8;
+constexpr int kPrepThreads = 256;                // at most, per block
+constexpr int kPrepBatch = 4;                    // tokens in flight per thread
 constexpr int kMaxPairs = 64;
 
 struct PrepArgs {
@@ -132,16 +135,21 @@ struct PrepArgs {
   float* coord;
   long long q_row, q_head, k_row, k_head, v_row, v_head;
   long long qo_row, qo_head, km_row, km_head, vm_row, vm_head;
-  int n_tokens, n_rows, heads, kv_heads, dim;
+  int n_tokens, n_rows, n_qh, n_kh, n_vh, dim;
   int n_rot;                   // pairs of all axes together
   int end_t, end_y;            // pairs [0, end_t) turn by t, [end_t, end_y) by y, the rest by x
-  int interleaved, norm, split;
+  int norm;
+  int places, side, batch;     // threads per token in a block, tokens side by side, tokens per thread
   float eps;
   // turns per unit of position, theta^(-m / n) / 2 pi, as the sum of two floats:
   // the product with a position stays exact to a small fraction of a turn at
   // positions where one float's rounding would be most of a turn
   float turn_hi[kMaxPairs], turn_lo[kMaxPairs];
 };
+
+// How pairs lie: none, (2m, 2m + 1), or (m, m + n_rot) with n_rot a multiple of
+// 8 (the partner is another lane's whole vector) or not (read again, an L1 hit).
+enum { kTurnNone, kTurnInterleaved, kTurnLanes, kTurnAny };
 
 template <typename T>
 __device__ __forceinline__ void unpack8(uint4 u, float (&x)[8]) {
@@ -155,107 +163,162 @@ __device__ __forceinline__ uint4 pack8(const float (&x)[8]) {
                     Store<T>::pack2(x[6], x[7]));
 }
 
-// LP lanes hold one head (8 channels each, LP * 8 >= dim); a warp takes 32 / LP
-// heads of one token at a time, over the token's q, k and v heads in a row.
-template <typename T, int LP>
-__global__ void __launch_bounds__(kPrepWarps * 32) k_qkv_prepare(const __grid_constant__ PrepArgs A) {
+// LP lanes hold one head (8 channels each, LP * 8 >= dim).  blockIdx.y picks the
+// block's heads, threads are [side][places].
+template <typename T, int LP, int TURN>
+__global__ void __launch_bounds__(kPrepThreads) k_qkv_prepare(const __grid_constant__ PrepArgs A) {
+  extern __shared__ __align__(16) float2 cs[];   // [2][side * batch][n_rot]: cos, sin
   __shared__ float2 turn[kMaxPairs];
-  __shared__ float2 cs[kPrepWarps][kMaxPairs];
-  const int tid = threadIdx.x, lane = tid & 31, wib = tid >> 5;
+  const int tid = threadIdx.x;
   for (int i = tid; i < A.n_rot; i += blockDim.x) turn[i] = make_float2(A.turn_hi[i], A.turn_lo[i]);
-  __syncthreads();
-  constexpr int HPW = 32 / LP;
-  const int e0 = (lane % LP) * 8;                // first channel of this lane
-  const bool in_dim = e0 < A.dim;
-  const int n_q = A.q ? A.heads : 0, n_k = A.k ? A.kv_heads : 0, n_v = A.v ? A.kv_heads : 0;
-  const int all = n_q + n_k + n_v;
-  const int passes = (all + HPW - 1) / HPW;
-  const float inv_dim = 1.0f / A.dim;
-  const long long items = (long long)A.n_tokens * A.split;
-  for (long long it = (long long)blockIdx.x * kPrepWarps + wib; it < items; it += (long long)gridDim.x * kPrepWarps) {
-    const int tok = (int)(it / A.split), part = (int)(it % A.split);
-    const int p0 = (int)((long long)passes * part / A.split), p1 = (int)((long long)passes * (part + 1) / A.split);
-    const int row_in = A.rows ? A.rows[tok] : tok;
-    const bool stored = row_in >= 0 && row_in < A.n_rows;
-    const long long row = stored ? row_in : 0;
-    const float pt = A.pos[3LL * tok], py = A.pos[3LL * tok + 1], px = A.pos[3LL * tok + 2];
-    if (part == 0 && lane == 0 && stored && A.coord)
-      *reinterpret_cast<float2*>(A.coord + 2 * row) = make_float2(py, px);
-    __syncwarp();
-    for (int i = lane; i < A.n_rot; i += 32) {
-      const float p = i < A.end_t ? pt : i < A.end_y ? py : px;
-      const float2 f = turn[i];
-      const float t = p * f.x;
-      const float frac = (t - rintf(t)) + fmaf(p, f.y, fmaf(p, f.x, -t));
-      float2 c;
-      sincospif(2.0f * frac, &c.y, &c.x);
-      cs[wib][i] = c;
+  const int per_block = A.places * A.side;       // threads with a place; the rest help with the angles
+  const int sub = tid / A.places, place = tid - sub * A.places;
+  const int e0 = (place % LP) * 8;               // first channel
+  const int h = blockIdx.y * (A.places / LP) + place / LP;
+  const bool is_q = h < A.n_qh, is_k = !is_q && h < A.n_qh + A.n_kh;
+  const bool turned = is_q || is_k;
+  const bool live = tid < per_block && h < A.n_qh + A.n_kh + A.n_vh && e0 < A.dim;
+  const T* src = nullptr;
+  T* dst = nullptr;
+  long long src_row = 0, dst_row = 0;
+  if (live) {
+    if (is_q) {
+      src = static_cast<const T*>(A.q) + h * A.q_head;
+      dst = static_cast<T*>(A.q_out) + h * A.qo_head;
+      src_row = A.q_row;
+      dst_row = A.qo_row;
+    } else if (is_k) {
+      src = static_cast<const T*>(A.k) + (h - A.n_qh) * A.k_head;
+      dst = static_cast<T*>(A.k_mem) + (h - A.n_qh) * A.km_head;
+      src_row = A.k_row;
+      dst_row = A.km_row;
+    } else {
+      src = static_cast<const T*>(A.v) + (h - A.n_qh - A.n_kh) * A.v_head;
+      dst = static_cast<T*>(A.v_mem) + (h - A.n_qh - A.n_kh) * A.vm_head;
+      src_row = A.v_row;
+      dst_row = A.vm_row;
     }
-    __syncwarp();
-    for (int p = p0; p < p1; ++p) {
-      const int h = p * HPW + lane / LP;
-      const bool is_q = h < n_q, is_k = !is_q && h < n_q + n_k;
-      const bool live = h < all && in_dim;
-      const T* src = nullptr;
-      T* dst = nullptr;
-      if (is_q) {
-        src = static_cast<const T*>(A.q) + (long long)tok * A.q_row + (long long)h * A.q_head;
-        dst = static_cast<T*>(A.q_out) + (long long)tok * A.qo_row + (long long)h * A.qo_head;
-      } else if (is_k) {
-        src = static_cast<const T*>(A.k) + (long long)tok * A.k_row + (long long)(h - n_q) * A.k_head;
-        dst = static_cast<T*>(A.k_mem) + row * A.km_row + (long long)(h - n_q) * A.km_head;
-      } else {
-        src = static_cast<const T*>(A.v) + (long long)tok * A.v_row + (long long)(h - n_q - n_k) * A.v_head;
-        dst = static_cast<T*>(A.v_mem) + row * A.vm_row + (long long)(h - n_q - n_k) * A.vm_head;
+  }
+  const float* gain = is_q ? A.q_gain : A.k_gain;
+  float gn[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) gn[i] = live && turned && gain ? gain[e0 + i] : 1.0f;
+  // the partner's place, for pairs that lie n_rot channels apart
+  const int apart = A.n_rot / 8;
+  const bool low = e0 < A.n_rot, in_rot = e0 < 2 * A.n_rot;
+  float go[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    go[i] = TURN == kTurnLanes && live && turned && gain && in_rot ? gain[e0 + i + (low ? A.n_rot : -A.n_rot)] : 1.0f;
+  const float inv_dim = 1.0f / A.dim;
+  const int per_batch = A.side * A.batch;
+  int buf = 0;
+  __syncthreads();
+  for (long long t0 = (long long)blockIdx.x * per_batch; t0 < A.n_tokens; t0 += (long long)gridDim.x * per_batch) {
+    uint4 raw[kPrepBatch];
+    long long to[kPrepBatch];                    // the output row, -1 = none
+#pragma unroll
+    for (int u = 0; u < kPrepBatch; ++u) {
+      const long long tok = t0 + u * A.side + sub;
+      const bool on = live && u < A.batch && tok < A.n_tokens;
+      raw[u] = on ? *reinterpret_cast<const uint4*>(src + tok * src_row + e0) : make_uint4(0u, 0u, 0u, 0u);
+      long long row = on ? tok : -1;
+      if (on && !is_q) {
+        row = A.rows ? A.rows[tok] : tok;
+        if (row >= A.n_rows) row = -1;
       }
-      const bool write = live && (is_q || stored);
-      uint4 raw = make_uint4(0u, 0u, 0u, 0u);
-      if (live) raw = *reinterpret_cast<const uint4*>(src + e0);
-      float x[8];
-      unpack8<T>(raw, x);
+      to[u] = row;
+    }
+    float2* c = cs + buf * per_batch * A.n_rot;
+    if (TURN != kTurnNone || A.coord) {
+      // the batch's angles, one (token, pair) a thread at a time
+      const int n = (int)min((long long)per_batch, A.n_tokens - t0);
+      if (TURN != kTurnNone)
+        for (int i = tid; i < n * A.n_rot; i += blockDim.x) {
+          const int tk = i / A.n_rot, m = i - tk * A.n_rot;
+          const float p = A.pos[3 * (t0 + tk) + (m < A.end_t ? 0 : m < A.end_y ? 1 : 2)];
+          const float2 f = turn[m];
+          const float t = p * f.x;
+          const float frac = (t - rintf(t)) + fmaf(p, f.y, fmaf(p, f.x, -t));
+          float2 v;
+          sincospif(2.0f * frac, &v.y, &v.x);
+          c[i] = v;
+        }
+      if (A.coord && blockIdx.y == 0)
+        for (int i = tid; i < n; i += blockDim.x) {
+          const long long row = A.rows ? A.rows[t0 + i] : t0 + i;
+          if (row >= 0 && row < A.n_rows)
+            *reinterpret_cast<float2*>(A.coord + 2 * row) =
+                make_float2(A.pos[3 * (t0 + i) + 1], A.pos[3 * (t0 + i) + 2]);
+        }
+      if (TURN != kTurnNone) __syncthreads();    // the other buffer's readers are past it
+    }
+    buf ^= 1;
+#pragma unroll
+    for (int u = 0; u < kPrepBatch; ++u) {
+      if (u >= A.batch) break;
+      float x[8], y[8];
+      unpack8<T>(raw[u], x);
       float sum = 0.f;
 #pragma unroll
       for (int i = 0; i < 8; ++i) sum = fmaf(x[i], x[i], sum);
 #pragma unroll
       for (int d = 1; d < LP; d <<= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, d);
       const float r = A.norm ? rsqrtf(fmaf(sum, inv_dim, A.eps)) : 1.0f;
-      const float* gain = is_q ? A.q_gain : A.k_gain;
-      const bool turned = live && (is_q || is_k);
-      float y[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) y[i] = turned ? x[i] * r * (gain ? gain[e0 + i] : 1.0f) : x[i];
-      if (A.n_rot > 0) {
-        if (A.interleaved) {
-          if (turned) {
+      for (int i = 0; i < 8; ++i) y[i] = x[i] * (r * gn[i]);
+      const float2* ct = c + (u * A.side + sub) * A.n_rot;
+      if (TURN == kTurnInterleaved) {
+        const int m0 = e0 >> 1;
+        if (live && turned) {
 #pragma unroll
-            for (int i = 0; i < 8; i += 2) {
-              const int m = (e0 + i) >> 1;
-              if (m < A.n_rot) {
-                const float2 c = cs[wib][m];
-                const float a = y[i], b = y[i + 1];
-                y[i] = a * c.x - b * c.y;
-                y[i + 1] = a * c.y + b * c.x;
-              }
+          for (int i = 0; i < 4; ++i) {
+            if (m0 + i < A.n_rot) {
+              const float2 v = ct[m0 + i];
+              const float a = y[2 * i], b = y[2 * i + 1];
+              y[2 * i] = a * v.x - b * v.y;
+              y[2 * i + 1] = a * v.y + b * v.x;
             }
           }
-        } else if (turned) {
-          // the partner channel lies n_rot further on (or back), in general in
-          // another lane's vector at another place: read again (an L1 hit)
+        }
+      } else if (TURN == kTurnLanes) {
+        const int from = low ? (place % LP) + apart : (place % LP) - apart;
+        uint4 o;
+        o.x = __shfl_sync(0xFFFFFFFFu, raw[u].x, from, LP);
+        o.y = __shfl_sync(0xFFFFFFFFu, raw[u].y, from, LP);
+        o.z = __shfl_sync(0xFFFFFFFFu, raw[u].z, from, LP);
+        o.w = __shfl_sync(0xFFFFFFFFu, raw[u].w, from, LP);
+        if (live && turned && in_rot) {
+          float z[8];
+          unpack8<T>(o, z);
+          const float4* cv = reinterpret_cast<const float4*>(ct + (low ? e0 : e0 - A.n_rot));
+#pragma unroll
+          for (int i = 0; i < 8; i += 2) {
+            const float4 v = cv[i / 2];          // cos, sin of two pairs
+            const float o0 = z[i] * (r * go[i]), o1 = z[i + 1] * (r * go[i + 1]);
+            y[i] = y[i] * v.x + (low ? -o0 : o0) * v.y;
+            y[i + 1] = y[i + 1] * v.z + (low ? -o1 : o1) * v.w;
+          }
+        }
+      } else if (TURN == kTurnAny) {
+        const long long tok = t0 + u * A.side + sub;
+        if (live && turned && tok < A.n_tokens) {
+          const T* head = src + tok * src_row;
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
             const int e = e0 + i;
             if (e < 2 * A.n_rot) {
-              const bool low = e < A.n_rot;
-              const int o = low ? e + A.n_rot : e - A.n_rot;
-              const float other = Store<T>::to_f(src[o]) * r * (gain ? gain[o] : 1.0f);
-              const float2 c = cs[wib][low ? e : o];
-              y[i] = low ? y[i] * c.x - other * c.y : other * c.y + y[i] * c.x;
+              const bool lo = e < A.n_rot;
+              const int o = lo ? e + A.n_rot : e - A.n_rot;
+              const float other = Store<T>::to_f(head[o]) * (r * (gain ? gain[o] : 1.0f));
+              const float2 v = ct[lo ? e : o];
+              y[i] = y[i] * v.x + (lo ? -other : other) * v.y;
             }
           }
         }
+        __syncwarp();                            // every lane has read: q_out may be q
       }
-      __syncwarp();                              // every lane has read: q_out may be q
-      if (write) *reinterpret_cast<uint4*>(dst + e0) = turned ? pack8<T>(y) : raw;
+      if (to[u] >= 0) *reinterpret_cast<uint4*>(dst + to[u] * dst_row + e0) = turned ? pack8<T>(y) : raw[u];
     }
   }
 }
@@ -271,16 +334,22 @@ int sm_count() {
   return sms;
 }
 
+template <typename T, int LP>
+cudaError_t launch_prepare_t(const PrepArgs& a, int turn, const cudaLaunchConfig_t& lc) {
+  switch (turn) {
+    case kTurnNone: return cudaLaunchKernelEx(&lc, k_qkv_prepare<T, LP, kTurnNone>, a);
+    case kTurnInterleaved: return cudaLaunchKernelEx(&lc, k_qkv_prepare<T, LP, kTurnInterleaved>, a);
+    case kTurnLanes: return cudaLaunchKernelEx(&lc, k_qkv_prepare<T, LP, kTurnLanes>, a);
+    default: return cudaLaunchKernelEx(&lc, k_qkv_prepare<T, LP, kTurnAny>, a);
+  }
+}
+
 template <typename T>
-cudaError_t launch_prepare(const PrepArgs& a, int blocks, cudaStream_t st) {
-  cudaLaunchConfig_t lc = {};
-  lc.gridDim = dim3(blocks);
-  lc.blockDim = dim3(kPrepWarps * 32);
-  lc.stream = st;
-  if (a.dim <= 16) return cudaLaunchKernelEx(&lc, k_qkv_prepare<T, 2>, a);
-  if (a.dim <= 32) return cudaLaunchKernelEx(&lc, k_qkv_prepare<T, 4>, a);
-  if (a.dim <= 64) return cudaLaunchKernelEx(&lc, k_qkv_prepare<T, 8>, a);
-  return cudaLaunchKernelEx(&lc, k_qkv_prepare<T, 16>, a);
+cudaError_t launch_prepare(const PrepArgs& a, int lp, int turn, const cudaLaunchConfig_t& lc) {
+  if (lp == 2) return launch_prepare_t<T, 2>(a, turn, lc);
+  if (lp == 4) return launch_prepare_t<T, 4>(a, turn, lc);
+  if (lp == 8) return launch_prepare_t<T, 8>(a, turn, lc);
+  return launch_prepare_t<T, 16>(a, turn, lc);
 }
 
 }  // namespace
@@ -368,10 +437,11 @@ extern "C" rtcc_status rtcc_qkv_prepare(const rtcc_prepare_config* c, const void
   a.q_row = c->q_row; a.q_head = c->q_head; a.k_row = c->k_row; a.k_head = c->k_head;
   a.v_row = c->v_row; a.v_head = c->v_head; a.qo_row = c->qo_row; a.qo_head = c->qo_head;
   a.km_row = c->km_row; a.km_head = c->km_head; a.vm_row = c->vm_row; a.vm_head = c->vm_head;
-  a.n_tokens = c->n_tokens; a.n_rows = c->n_rows; a.heads = c->heads; a.kv_heads = c->kv_heads;
+  a.n_tokens = c->n_tokens; a.n_rows = c->n_rows;
+  a.n_qh = d_q ? c->heads : 0; a.n_kh = d_k ? c->kv_heads : 0; a.n_vh = d_v ? c->kv_heads : 0;
   a.dim = c->head_dim; a.n_rot = (int)pairs;
   a.end_t = c->axis_pairs[0]; a.end_y = c->axis_pairs[0] + c->axis_pairs[1];
-  a.interleaved = c->interleaved != 0; a.norm = c->norm != 0; a.eps = c->eps;
+  a.norm = c->norm != 0; a.eps = c->eps;
   int at = 0;
   for (int ax = 0; ax < 3; ++ax) {
     const int n = c->axis_pairs[ax];
@@ -383,18 +453,31 @@ extern "C" rtcc_status rtcc_qkv_prepare(const rtcc_prepare_config* c, const void
       a.turn_lo[at] = (float)(f - (double)a.turn_hi[at]);
     }
   }
+  // Threads: a place per head and 8 channels, heads over blockIdx.y where they do
+  // not fit a block, several tokens side by side where they are few.
   const int lp = a.dim <= 16 ? 2 : a.dim <= 32 ? 4 : a.dim <= 64 ? 8 : 16;
-  const int all = (d_q ? a.heads : 0) + (d_k ? a.kv_heads : 0) + (d_v ? a.kv_heads : 0);
-  const int passes = (all + 32 / lp - 1) / (32 / lp);
-  const long long want = (long long)sms * 32;     // warps that fill the GPU
-  long long split = (want + a.n_tokens - 1) / a.n_tokens;
-  if (split > passes) split = passes;
-  a.split = (int)split;
-  long long blocks = ((long long)a.n_tokens * split + kPrepWarps - 1) / kPrepWarps;
-  const long long most = (long long)sms * 16;
+  const int turn = pairs == 0 ? kTurnNone : c->interleaved ? kTurnInterleaved
+                   : pairs % 8 == 0 ? kTurnLanes : kTurnAny;
+  const int heads = a.n_qh + a.n_kh + a.n_vh;
+  const int fit = kPrepThreads / lp;              // heads in a block at most
+  const int ys = (heads + fit - 1) / fit, per = (heads + ys - 1) / ys;
+  a.places = per * lp;
+  a.side = kPrepThreads / a.places;
+  while (a.side > 1 && sizeof(float2) * 2 * a.side * kPrepBatch * a.n_rot > 48 * 1024) a.side /= 2;
+  // four tokens a thread, fewer while that leaves SMs without a block
+  const long long columns = (a.n_tokens + a.side - 1LL) / a.side;
+  a.batch = kPrepBatch;
+  while (a.batch > 1 && (columns + a.batch - 1) / a.batch * ys < 2LL * sms) a.batch /= 2;
+  while (a.side > 1 && (a.n_tokens + a.side * a.batch - 1LL) / (a.side * a.batch) * ys < sms) a.side /= 2;
+  long long blocks = (a.n_tokens + (long long)a.side * a.batch - 1) / ((long long)a.side * a.batch);
+  const long long most = (8LL * sms + ys - 1) / ys;
   if (blocks > most) blocks = most;
-  cudaStream_t st = static_cast<cudaStream_t>(stream);
-  const cudaError_t e = c->dtype == RTCC_BF16 ? launch_prepare<__nv_bfloat16>(a, (int)blocks, st)
-                                              : launch_prepare<__half>(a, (int)blocks, st);
+  cudaLaunchConfig_t lc = {};
+  lc.gridDim = dim3((unsigned)blocks, (unsigned)ys);
+  lc.blockDim = dim3((a.places * a.side + 31) / 32 * 32);
+  lc.dynamicSmemBytes = sizeof(float2) * 2 * a.side * a.batch * a.n_rot;
+  lc.stream = static_cast<cudaStream_t>(stream);
+  const cudaError_t e = c->dtype == RTCC_BF16 ? launch_prepare<__nv_bfloat16>(a, lp, turn, lc)
+                                              : launch_prepare<__half>(a, lp, turn, lc);
   return e == cudaSuccess ? RTCC_OK : RTCC_E_CUDA;
 }
