@@ -41,10 +41,6 @@ __device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool live) {
 __device__ __forceinline__ void cp8(uint32_t dst, const void* src, bool live) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst), "l"(src), "r"(live ? 8 : 0) : "memory");
 }
-__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-
 __device__ __forceinline__ void ldm4(uint32_t a, uint32_t (&r)[4]) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
@@ -190,13 +186,13 @@ __global__ void __launch_bounds__(kWarps * 32, 2) k_attn_rows(const __grid_const
           cp8(ps + lane * 8, A.k_pos + 2 * row, live);
         }
       }
-      cp_commit();
+      cp_async_commit();
     };
 #pragma unroll
     for (int s = 0; s < kStages - 1; ++s) load(w + s * kWarps, s);
     int stage = 0;
     for (int t = w; t < n_tiles; t += kWarps) {
-      cp_wait<kStages - 2>();
+      cp_async_wait<kStages - 2>();
       __syncwarp();
       load(t + (kStages - 1) * kWarps, (stage + kStages - 1) % kStages);
       const unsigned bits = key_bits(t);
@@ -277,7 +273,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) k_attn_rows(const __grid_const
       }
       stage = (stage + 1) % kStages;
     }
-    cp_wait<0>();
+    cp_async_wait<0>();
 #pragma unroll
     for (int rr = 0; rr < 2; ++rr) {
       l[rr] += __shfl_xor_sync(0xFFFFFFFFu, l[rr], 1);

@@ -17,11 +17,13 @@
 //   x^ = x * rsqrt(mean(x^2) + eps) * gain,
 //   and pair m of axis a of x^ turned by pos_a * theta^(-m / pairs_a);
 //   q goes to a dense output, k, v and the (y, x) coordinates to the token's
-//   memory row.  It reads and writes every vector once, so HBM bounds it.  A
-//   thread keeps one place (a head's 8 channels: one 16-byte load and store) for
-//   all the tokens it sees, so pointers, gains and the place's kind are set up
-//   once; it has up to four tokens' vectors in flight, and a block computes the
-//   angles of its batch of tokens once for all heads in the meantime.
+//   memory row.  It reads and writes every vector once, so HBM bounds it.  2 to 16
+//   lanes hold one token (8 channels, one 16-byte copy in and one store out each)
+//   and go through its heads: a lane's angles are computed once and stay in
+//   registers for all heads.  Eight heads' vectors are on their way to a ring in
+//   shared memory, every thread's own places, so nothing is waited for but the
+//   copy itself.  With few tokens a token's heads are divided among several groups
+//   of lanes.
 #include <math.h>
 
 #include "common.cuh"
@@ -123,8 +125,8 @@ __global__ void __launch_bounds__(kAppendThreads) k_memory_append(const AppendAr
 // prepare
 // ---------------------------------------------------------------------------
 
-constexpr int kPrepThreads = 256;                // at most, per block
-constexpr int kPrepBatch = 4;                    // tokens in flight per thread
+constexpr int kPrepThreads = 128;
+constexpr int kPrepPairs = 4;                    // pairs of heads on their way per lane
 constexpr int kMaxPairs = 64;
 
 struct PrepArgs {
@@ -139,7 +141,6 @@ struct PrepArgs {
   int n_rot;                   // pairs of all axes together
   int end_t, end_y;            // pairs [0, end_t) turn by t, [end_t, end_y) by y, the rest by x
   int norm;
-  int places, side, batch;     // threads per token in a block, tokens side by side, tokens per thread
   float eps;
   // turns per unit of position, theta^(-m / n) / 2 pi, as the sum of two floats:
   // the product with a position stays exact to a small fraction of a turn at
@@ -151,176 +152,190 @@ struct PrepArgs {
 // 8 (the partner is another lane's whole vector) or not (read again, an L1 hit).
 enum { kTurnNone, kTurnInterleaved, kTurnLanes, kTurnAny };
 
-template <typename T>
-__device__ __forceinline__ void unpack8(uint4 u, float (&x)[8]) {
-  const float2 a = Store<T>::unpack2(u.x), b = Store<T>::unpack2(u.y), c = Store<T>::unpack2(u.z),
-               d = Store<T>::unpack2(u.w);
-  x[0] = a.x; x[1] = a.y; x[2] = b.x; x[3] = b.y; x[4] = c.x; x[5] = c.y; x[6] = d.x; x[7] = d.y;
-}
-template <typename T>
-__device__ __forceinline__ uint4 pack8(const float (&x)[8]) {
-  return make_uint4(Store<T>::pack2(x[0], x[1]), Store<T>::pack2(x[2], x[3]), Store<T>::pack2(x[4], x[5]),
-                    Store<T>::pack2(x[6], x[7]));
+// cos and sin of p * 2 pi * (hi + lo).  The turns are reduced to [-1/2, 1/2]
+// exactly enough before the hardware's sine and cosine (absolute error below 2^-21,
+// against 2^-11 or 2^-8 of the result's rounding).
+__device__ __forceinline__ float2 cos_sin(float p, float2 f) {
+  const float t = p * f.x;
+  const float frac = (t - rintf(t)) + fmaf(p, f.y, fmaf(p, f.x, -t));
+  float2 c;
+  __sincosf(6.283185307f * frac, &c.y, &c.x);
+  return c;
 }
 
-// LP lanes hold one head (8 channels each, LP * 8 >= dim).  blockIdx.y picks the
-// block's heads, threads are [side][places].
+// LP lanes hold one token's channels (8 each, LP * 8 >= dim); blockIdx.y of
+// gridDim.y takes its share of the q, k and v heads.
 template <typename T, int LP, int TURN>
-__global__ void __launch_bounds__(kPrepThreads) k_qkv_prepare(const __grid_constant__ PrepArgs A) {
-  extern __shared__ __align__(16) float2 cs[];   // [2][side * batch][n_rot]: cos, sin
+__global__ void __launch_bounds__(kPrepThreads, 6) k_qkv_prepare(const __grid_constant__ PrepArgs A) {
   __shared__ float2 turn[kMaxPairs];
+  __shared__ uint4 ring[kPrepPairs][2][kPrepThreads];
   const int tid = threadIdx.x;
-  for (int i = tid; i < A.n_rot; i += blockDim.x) turn[i] = make_float2(A.turn_hi[i], A.turn_lo[i]);
-  const int per_block = A.places * A.side;       // threads with a place; the rest help with the angles
-  const int sub = tid / A.places, place = tid - sub * A.places;
-  const int e0 = (place % LP) * 8;               // first channel
-  const int h = blockIdx.y * (A.places / LP) + place / LP;
-  const bool is_q = h < A.n_qh, is_k = !is_q && h < A.n_qh + A.n_kh;
-  const bool turned = is_q || is_k;
-  const bool live = tid < per_block && h < A.n_qh + A.n_kh + A.n_vh && e0 < A.dim;
-  const T* src = nullptr;
-  T* dst = nullptr;
-  long long src_row = 0, dst_row = 0;
-  if (live) {
-    if (is_q) {
-      src = static_cast<const T*>(A.q) + h * A.q_head;
-      dst = static_cast<T*>(A.q_out) + h * A.qo_head;
-      src_row = A.q_row;
-      dst_row = A.qo_row;
-    } else if (is_k) {
-      src = static_cast<const T*>(A.k) + (h - A.n_qh) * A.k_head;
-      dst = static_cast<T*>(A.k_mem) + (h - A.n_qh) * A.km_head;
-      src_row = A.k_row;
-      dst_row = A.km_row;
-    } else {
-      src = static_cast<const T*>(A.v) + (h - A.n_qh - A.n_kh) * A.v_head;
-      dst = static_cast<T*>(A.v_mem) + (h - A.n_qh - A.n_kh) * A.vm_head;
-      src_row = A.v_row;
-      dst_row = A.vm_row;
+  for (int i = tid; i < A.n_rot; i += kPrepThreads) turn[i] = make_float2(A.turn_hi[i], A.turn_lo[i]);
+  const long long id = (long long)blockIdx.x * kPrepThreads + tid;
+  const int lane = (int)(id % LP), e0 = lane * 8;
+  const bool live = id / LP < A.n_tokens && e0 < A.dim;
+  const long long tok = min(id / LP, (long long)A.n_tokens - 1);
+  // this block's heads of q, k and v, in pairs
+  const int all = A.n_qh + A.n_kh + A.n_vh;
+  const int h0 = (int)((long long)all * blockIdx.y / gridDim.y), h1 = (int)((long long)all * (blockIdx.y + 1) / gridDim.y);
+  const int q0 = min(h0, A.n_qh), q1 = min(h1, A.n_qh);
+  const int k0 = min(max(h0 - A.n_qh, 0), A.n_kh), k1 = min(max(h1 - A.n_qh, 0), A.n_kh);
+  const int v0 = max(h0 - A.n_qh - A.n_kh, 0), v1 = max(h1 - A.n_qh - A.n_kh, 0);
+  const int qp = (q1 - q0 + 1) / 2, kp = qp + (k1 - k0 + 1) / 2, vp = kp + (v1 - v0 + 1) / 2;
+  const T* qs = static_cast<const T*>(A.q) + tok * A.q_row + e0;
+  const T* ks = static_cast<const T*>(A.k) + tok * A.k_row + e0;
+  const T* vs = static_cast<const T*>(A.v) + tok * A.v_row + e0;
+  auto issue = [&](int j) {                      // pair j on its way
+    if (live && j < vp) {
+      const T* src;
+      long long step;
+      int n;
+      if (j < qp) {
+        src = qs + (q0 + 2 * j) * A.q_head, step = A.q_head, n = q1 - q0 - 2 * j;
+      } else if (j < kp) {
+        src = ks + (k0 + 2 * (j - qp)) * A.k_head, step = A.k_head, n = k1 - k0 - 2 * (j - qp);
+      } else {
+        src = vs + (v0 + 2 * (j - kp)) * A.v_head, step = A.v_head, n = v1 - v0 - 2 * (j - kp);
+      }
+      uint4(*slot)[kPrepThreads] = ring[j % kPrepPairs];
+      cp_async16(&slot[0][tid], src);
+      if (n > 1) cp_async16(&slot[1][tid], src + step);
+    }
+    cp_async_commit();
+  };
+#pragma unroll
+  for (int j = 0; j < kPrepPairs; ++j) issue(j);
+  const long long row = A.rows ? A.rows[tok] : tok;
+  const bool stored = live && row >= 0 && row < A.n_rows;
+  const float pos[3] = {A.pos[3 * tok], A.pos[3 * tok + 1], A.pos[3 * tok + 2]};
+  if (A.coord && blockIdx.y == 0 && stored && lane == 0)
+    *reinterpret_cast<float2*>(A.coord + 2 * row) = make_float2(pos[1], pos[2]);
+  __syncthreads();                               // the table of turns
+
+  // This lane's cosines and sines: channel e of a pair becomes x_e cs + x_other sn,
+  // the sine's sign with it (1 and 0 where nothing turns).  The two channels of
+  // an interleaved pair share theirs.
+  constexpr int P = TURN == kTurnInterleaved ? 2 : 4;
+  float2 cs[P], sn[P];
+  const bool low = e0 < A.n_rot, in_rot = e0 < 2 * A.n_rot;
+  if (TURN != kTurnNone && kp > 0) {
+#pragma unroll
+    for (int i = 0; i < 2 * P; ++i) {
+      const int e = e0 + i;
+      const int m = TURN == kTurnInterleaved ? e0 / 2 + i : e < A.n_rot ? e : e - A.n_rot;
+      float2 c = make_float2(1.0f, 0.0f);
+      if (m < A.n_rot) c = cos_sin(m < A.end_t ? pos[0] : m < A.end_y ? pos[1] : pos[2], turn[m]);
+      if (TURN != kTurnInterleaved && e < A.n_rot) c.y = -c.y;
+      (i & 1 ? cs[i / 2].y : cs[i / 2].x) = c.x;
+      (i & 1 ? sn[i / 2].y : sn[i / 2].x) = c.y;
     }
   }
-  const float* gain = is_q ? A.q_gain : A.k_gain;
-  float gn[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) gn[i] = live && turned && gain ? gain[e0 + i] : 1.0f;
-  // the partner's place, for pairs that lie n_rot channels apart
-  const int apart = A.n_rot / 8;
-  const bool low = e0 < A.n_rot, in_rot = e0 < 2 * A.n_rot;
-  float go[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i)
-    go[i] = TURN == kTurnLanes && live && turned && gain && in_rot ? gain[e0 + i + (low ? A.n_rot : -A.n_rot)] : 1.0f;
   const float inv_dim = 1.0f / A.dim;
-  const int per_batch = A.side * A.batch;
-  int buf = 0;
-  __syncthreads();
-  for (long long t0 = (long long)blockIdx.x * per_batch; t0 < A.n_tokens; t0 += (long long)gridDim.x * per_batch) {
-    uint4 raw[kPrepBatch];
-    long long to[kPrepBatch];                    // the output row, -1 = none
+
+  // pairs [j0, j1) are heads [0, n) of q or k, at src and dst
+  auto heads = [&](int j0, int j1, int n, const T* src, long long src_step, T* dst, long long dst_step, bool write,
+                   const float* gain) {
+    float2 gn[4], go[4];                         // gains: own, and the partner's
 #pragma unroll
-    for (int u = 0; u < kPrepBatch; ++u) {
-      const long long tok = t0 + u * A.side + sub;
-      const bool on = live && u < A.batch && tok < A.n_tokens;
-      raw[u] = on ? *reinterpret_cast<const uint4*>(src + tok * src_row + e0) : make_uint4(0u, 0u, 0u, 0u);
-      long long row = on ? tok : -1;
-      if (on && !is_q) {
-        row = A.rows ? A.rows[tok] : tok;
-        if (row >= A.n_rows) row = -1;
+    for (int i = 0; i < 4; ++i) {
+      gn[i] = gain && live ? make_float2(gain[e0 + 2 * i], gain[e0 + 2 * i + 1]) : make_float2(1.f, 1.f);
+      go[i] = make_float2(1.f, 1.f);
+      if (TURN == kTurnLanes && gain && live && in_rot) {
+        const int o = e0 + 2 * i + (low ? A.n_rot : -A.n_rot);
+        go[i] = make_float2(gain[o], gain[o + 1]);
       }
-      to[u] = row;
     }
-    float2* c = cs + buf * per_batch * A.n_rot;
-    if (TURN != kTurnNone || A.coord) {
-      // the batch's angles, one (token, pair) a thread at a time
-      const int n = (int)min((long long)per_batch, A.n_tokens - t0);
-      if (TURN != kTurnNone)
-        for (int i = tid; i < n * A.n_rot; i += blockDim.x) {
-          const int tk = i / A.n_rot, m = i - tk * A.n_rot;
-          const float p = A.pos[3 * (t0 + tk) + (m < A.end_t ? 0 : m < A.end_y ? 1 : 2)];
-          const float2 f = turn[m];
-          const float t = p * f.x;
-          const float frac = (t - rintf(t)) + fmaf(p, f.y, fmaf(p, f.x, -t));
-          float2 v;
-          sincospif(2.0f * frac, &v.y, &v.x);
-          c[i] = v;
+    for (int j = j0; j < j1; ++j, n -= 2, src += 2 * src_step, dst += 2 * dst_step) {
+      cp_async_wait<kPrepPairs - 1>();
+      uint4 raw[2];
+      raw[0] = live ? ring[j % kPrepPairs][0][tid] : make_uint4(0u, 0u, 0u, 0u);
+      raw[1] = live && n > 1 ? ring[j % kPrepPairs][1][tid] : make_uint4(0u, 0u, 0u, 0u);
+      issue(j + kPrepPairs);
+      float rs[2] = {1.f, 1.f};
+      if (A.norm) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          float2 x = Store<T>::unpack2(raw[u].x);
+          float2 q = mul2(x, x);
+          x = Store<T>::unpack2(raw[u].y);
+          q = fma2(x, x, q);
+          x = Store<T>::unpack2(raw[u].z);
+          q = fma2(x, x, q);
+          x = Store<T>::unpack2(raw[u].w);
+          q = fma2(x, x, q);
+          rs[u] = q.x + q.y;
         }
-      if (A.coord && blockIdx.y == 0)
-        for (int i = tid; i < n; i += blockDim.x) {
-          const long long row = A.rows ? A.rows[t0 + i] : t0 + i;
-          if (row >= 0 && row < A.n_rows)
-            *reinterpret_cast<float2*>(A.coord + 2 * row) =
-                make_float2(A.pos[3 * (t0 + i) + 1], A.pos[3 * (t0 + i) + 2]);
-        }
-      if (TURN != kTurnNone) __syncthreads();    // the other buffer's readers are past it
-    }
-    buf ^= 1;
 #pragma unroll
-    for (int u = 0; u < kPrepBatch; ++u) {
-      if (u >= A.batch) break;
-      float x[8], y[8];
-      unpack8<T>(raw[u], x);
-      float sum = 0.f;
+        for (int d = 1; d < LP; d <<= 1)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) sum = fmaf(x[i], x[i], sum);
+          for (int u = 0; u < 2; ++u) rs[u] += __shfl_xor_sync(0xFFFFFFFFu, rs[u], d);
 #pragma unroll
-      for (int d = 1; d < LP; d <<= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, d);
-      const float r = A.norm ? rsqrtf(fmaf(sum, inv_dim, A.eps)) : 1.0f;
+        for (int u = 0; u < 2; ++u) rs[u] = rsqrtf(fmaf(rs[u], inv_dim, A.eps));
+      }
 #pragma unroll
-      for (int i = 0; i < 8; ++i) y[i] = x[i] * (r * gn[i]);
-      const float2* ct = c + (u * A.side + sub) * A.n_rot;
-      if (TURN == kTurnInterleaved) {
-        const int m0 = e0 >> 1;
-        if (live && turned) {
+      for (int u = 0; u < 2; ++u) {
+        if (u >= n) continue;                    // the same for the whole block
+        const float2 rr = make_float2(rs[u], rs[u]);
+        float2 y[4];
+        y[0] = mul2(mul2(Store<T>::unpack2(raw[u].x), rr), gn[0]);
+        y[1] = mul2(mul2(Store<T>::unpack2(raw[u].y), rr), gn[1]);
+        y[2] = mul2(mul2(Store<T>::unpack2(raw[u].z), rr), gn[2]);
+        y[3] = mul2(mul2(Store<T>::unpack2(raw[u].w), rr), gn[3]);
+        if (TURN == kTurnInterleaved) {
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            if (m0 + i < A.n_rot) {
-              const float2 v = ct[m0 + i];
-              const float a = y[2 * i], b = y[2 * i + 1];
-              y[2 * i] = a * v.x - b * v.y;
-              y[2 * i + 1] = a * v.y + b * v.x;
-            }
+            const float c = i & 1 ? cs[i / 2].y : cs[i / 2].x, s = i & 1 ? sn[i / 2].y : sn[i / 2].x;
+            y[i] = make_float2(y[i].x * c - y[i].y * s, y[i].x * s + y[i].y * c);
           }
-        }
-      } else if (TURN == kTurnLanes) {
-        const int from = low ? (place % LP) + apart : (place % LP) - apart;
-        uint4 o;
-        o.x = __shfl_sync(0xFFFFFFFFu, raw[u].x, from, LP);
-        o.y = __shfl_sync(0xFFFFFFFFu, raw[u].y, from, LP);
-        o.z = __shfl_sync(0xFFFFFFFFu, raw[u].z, from, LP);
-        o.w = __shfl_sync(0xFFFFFFFFu, raw[u].w, from, LP);
-        if (live && turned && in_rot) {
-          float z[8];
-          unpack8<T>(o, z);
-          const float4* cv = reinterpret_cast<const float4*>(ct + (low ? e0 : e0 - A.n_rot));
+        } else if (TURN == kTurnLanes) {
+          const int from = lane + (low ? A.n_rot / 8 : -(A.n_rot / 8));
+          float2 z[4];
+          z[0] = Store<T>::unpack2(__shfl_sync(0xFFFFFFFFu, raw[u].x, from, LP));
+          z[1] = Store<T>::unpack2(__shfl_sync(0xFFFFFFFFu, raw[u].y, from, LP));
+          z[2] = Store<T>::unpack2(__shfl_sync(0xFFFFFFFFu, raw[u].z, from, LP));
+          z[3] = Store<T>::unpack2(__shfl_sync(0xFFFFFFFFu, raw[u].w, from, LP));
+          if (in_rot) {
 #pragma unroll
-          for (int i = 0; i < 8; i += 2) {
-            const float4 v = cv[i / 2];          // cos, sin of two pairs
-            const float o0 = z[i] * (r * go[i]), o1 = z[i + 1] * (r * go[i + 1]);
-            y[i] = y[i] * v.x + (low ? -o0 : o0) * v.y;
-            y[i + 1] = y[i + 1] * v.z + (low ? -o1 : o1) * v.w;
+            for (int i = 0; i < 4; ++i) y[i] = fma2(y[i], cs[i], mul2(mul2(mul2(z[i], rr), go[i]), sn[i]));
           }
-        }
-      } else if (TURN == kTurnAny) {
-        const long long tok = t0 + u * A.side + sub;
-        if (live && turned && tok < A.n_tokens) {
-          const T* head = src + tok * src_row;
+        } else if (TURN == kTurnAny) {
+          if (live) {
+            const T* head = src + u * src_step - e0;
+            auto other = [&](int e) {
+              if (e >= 2 * A.n_rot) return 0.f;
+              const int o = e < A.n_rot ? e + A.n_rot : e - A.n_rot;
+              return Store<T>::to_f(head[o]) * rs[u] * (gain ? gain[o] : 1.0f);
+            };
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const int e = e0 + i;
-            if (e < 2 * A.n_rot) {
-              const bool lo = e < A.n_rot;
-              const int o = lo ? e + A.n_rot : e - A.n_rot;
-              const float other = Store<T>::to_f(head[o]) * (r * (gain ? gain[o] : 1.0f));
-              const float2 v = ct[lo ? e : o];
-              y[i] = y[i] * v.x + (lo ? -other : other) * v.y;
-            }
+            for (int i = 0; i < 4; ++i)
+              y[i] = fma2(y[i], cs[i], mul2(make_float2(other(e0 + 2 * i), other(e0 + 2 * i + 1)), sn[i]));
           }
+          __syncwarp();                          // every lane has read: q_out may be q
         }
-        __syncwarp();                            // every lane has read: q_out may be q
+        if (write)
+          *reinterpret_cast<uint4*>(dst + u * dst_step) =
+              make_uint4(Store<T>::pack2(y[0].x, y[0].y), Store<T>::pack2(y[1].x, y[1].y),
+                         Store<T>::pack2(y[2].x, y[2].y), Store<T>::pack2(y[3].x, y[3].y));
       }
-      if (to[u] >= 0) *reinterpret_cast<uint4*>(dst + to[u] * dst_row + e0) = turned ? pack8<T>(y) : raw[u];
     }
+  };
+  if (qp > 0)
+    heads(0, qp, q1 - q0, qs + q0 * A.q_head, A.q_head,
+          static_cast<T*>(A.q_out) + tok * A.qo_row + q0 * A.qo_head + e0, A.qo_head, live, A.q_gain);
+  const long long to = stored ? row : 0;
+  if (kp > qp)
+    heads(qp, kp, k1 - k0, ks + k0 * A.k_head, A.k_head, static_cast<T*>(A.k_mem) + to * A.km_row + k0 * A.km_head + e0,
+          A.km_head, stored, A.k_gain);
+  T* vd = static_cast<T*>(A.v_mem) + to * A.vm_row + v0 * A.vm_head + e0;
+  for (int j = kp, n = v1 - v0; j < vp; ++j, n -= 2, vd += 2 * A.vm_head) {
+    cp_async_wait<kPrepPairs - 1>();
+    if (stored) {
+      *reinterpret_cast<uint4*>(vd) = ring[j % kPrepPairs][0][tid];
+      if (n > 1) *reinterpret_cast<uint4*>(vd + A.vm_head) = ring[j % kPrepPairs][1][tid];
+    }
+    issue(j + kPrepPairs);
   }
+  cp_async_wait<0>();
 }
 
 bool misaligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
@@ -453,29 +468,18 @@ extern "C" rtcc_status rtcc_qkv_prepare(const rtcc_prepare_config* c, const void
       a.turn_lo[at] = (float)(f - (double)a.turn_hi[at]);
     }
   }
-  // Threads: a place per head and 8 channels, heads over blockIdx.y where they do
-  // not fit a block, several tokens side by side where they are few.
   const int lp = a.dim <= 16 ? 2 : a.dim <= 32 ? 4 : a.dim <= 64 ? 8 : 16;
   const int turn = pairs == 0 ? kTurnNone : c->interleaved ? kTurnInterleaved
                    : pairs % 8 == 0 ? kTurnLanes : kTurnAny;
+  // a token's heads stay together unless that leaves threads for less than half
+  // of what the GPU holds (1024 a SM)
   const int heads = a.n_qh + a.n_kh + a.n_vh;
-  const int fit = kPrepThreads / lp;              // heads in a block at most
-  const int ys = (heads + fit - 1) / fit, per = (heads + ys - 1) / ys;
-  a.places = per * lp;
-  a.side = kPrepThreads / a.places;
-  while (a.side > 1 && sizeof(float2) * 2 * a.side * kPrepBatch * a.n_rot > 48 * 1024) a.side /= 2;
-  // four tokens a thread, fewer while that leaves SMs without a block
-  const long long columns = (a.n_tokens + a.side - 1LL) / a.side;
-  a.batch = kPrepBatch;
-  while (a.batch > 1 && (columns + a.batch - 1) / a.batch * ys < 2LL * sms) a.batch /= 2;
-  while (a.side > 1 && (a.n_tokens + a.side * a.batch - 1LL) / (a.side * a.batch) * ys < sms) a.side /= 2;
-  long long blocks = (a.n_tokens + (long long)a.side * a.batch - 1) / ((long long)a.side * a.batch);
-  const long long most = (8LL * sms + ys - 1) / ys;
-  if (blocks > most) blocks = most;
+  const long long threads = (long long)a.n_tokens * lp;
+  long long parts = (512LL * sms + threads - 1) / threads;
+  if (parts > heads) parts = heads;
   cudaLaunchConfig_t lc = {};
-  lc.gridDim = dim3((unsigned)blocks, (unsigned)ys);
-  lc.blockDim = dim3((a.places * a.side + 31) / 32 * 32);
-  lc.dynamicSmemBytes = sizeof(float2) * 2 * a.side * a.batch * a.n_rot;
+  lc.gridDim = dim3((unsigned)((threads + kPrepThreads - 1) / kPrepThreads), (unsigned)parts);
+  lc.blockDim = dim3(kPrepThreads);
   lc.stream = static_cast<cudaStream_t>(stream);
   const cudaError_t e = c->dtype == RTCC_BF16 ? launch_prepare<__nv_bfloat16>(a, lp, turn, lc)
                                               : launch_prepare<__half>(a, lp, turn, lc);
