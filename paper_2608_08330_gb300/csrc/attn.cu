@@ -2,6 +2,8 @@
 // choice of kernel and of the split of long spans.
 #include <math.h>
 
+#include <algorithm>
+
 #include "attn.cuh"
 #include "kernels.h"
 #include "rtcc.h"
@@ -10,6 +12,56 @@ namespace rtcc {
 namespace {
 
 constexpr int kTcRows = 64;
+
+// Chunks of the span for the few-rows kernel, two blocks of which run on an SM.  A
+// block costs about kBegin to begin and end, and a step of its four warps (32 KB of
+// keys and values) about kStep, the memory's share of it when all blocks run.
+// One sequence: whole rounds of blocks; 110,537 keys of 2 heads take 34 us in one
+// round, 53 in four.  Several sequences are taken to be ragged: blocks of unlike
+// lengths run into one another, so the number weighs what they cost to begin
+// against the last one's length; 61 sequences of up to 16,384 keys and 8 heads take
+// 310 us in 3 chunks, 287 in 5.
+long long rows_chunks(long long units, int n_seqs, long long steps, long long most, int sms) {
+  constexpr double kBegin = 7.0, kStep = 1.5;
+  const long long slots = 2LL * sms;
+  long long best = 1;
+  if (n_seqs > 1) {
+    best = (long long)(sqrt((double)steps * kStep * slots / (units * kBegin)) + 0.5);
+  } else {
+    double least = 0;
+    for (long long k = 1; k <= 8; ++k) {
+      const long long c = std::max(1LL, std::min(most, slots * k / units));
+      const double cost = (double)((units * c + slots - 1) / slots) * (kBegin + kStep * ((steps + c - 1) / c)) + 0.02 * c;
+      if (k == 1 || cost < least) {
+        least = cost;
+        best = c;
+      }
+    }
+  }
+  return std::max(1LL, std::min(best, most));
+}
+
+// Chunks of the span for the tensor-core kernel, which has one block on an SM: the
+// number of least cost, in steps of 64 keys.  Rounds of blocks over the SMs, each
+// with its share of the steps and about four steps' time to begin and end, and for
+// the merge two steps' time and the traffic of the partial results (a step takes
+// about 1.2 us).  With 384 units of 768 steps, one chunk leaves the third round
+// half empty, five fill 13 rounds.
+long long tc_chunks(long long units, long long steps, long long most, int sms, int streams, long long n_q, int heads,
+                    int dim) {
+  long long best = 1;
+  double least = 0;
+  for (long long c = 1; c <= std::max(1LL, std::min(most, 64LL)); ++c) {
+    const double rounds = (double)((units * c + sms - 1) / sms);
+    double cost = rounds * ((double)((steps + c - 1) / c) + 4);
+    if (c * streams > 1) cost += 2 + 8e-6 * (double)(c * streams * n_q * heads) * dim / (6.8 * 1.2);
+    if (c == 1 || cost < least) {
+      least = cost;
+      best = c;
+    }
+  }
+  return best;
+}
 
 bool misaligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
 bool bad_stride(int64_t s) { return s < 0 || s % 8 != 0; }
@@ -85,9 +137,13 @@ extern "C" rtcc_status rtcc_memory_attention(const rtcc_attn_config* c, const vo
   // its polynomial's coefficients can express.
   bool tc = (long long)max_q * a.group > kTcRows && a.group <= 128 && c->scale > 0.f && a.scale_log2 < 1e4f &&
             c->n_rows > 0;
+  const size_t part = (size_t)c->n_q * c->heads * (c->head_dim * sizeof(float) + sizeof(float2));
+  const long long room = d_workspace ? (long long)(workspace_bytes / part) : 0;
   for (;; tc = false) {
-    const int unit = tc ? attn_tc_unit() : attn_rows_unit(c->head_dim);
-    const long long step = tc ? attn_tc_tokens_per_block(a.group) : 1;
+    a.streams = tc ? attn_tc_streams(c->head_dim, a.group, max_q) : 1;
+    if (a.streams > room) a.streams = 1;
+    a.unit = tc ? attn_tc_unit(a.streams) : attn_rows_unit(c->head_dim);
+    const long long step = tc ? attn_tc_tokens_per_block(c->head_dim, a.group, a.streams) : 1;
     long long groups = tc ? (max_q + step - 1) / step
                           : ((long long)max_q * a.group + attn_rows_per_block() - 1) / attn_rows_per_block();
     long long units = (long long)c->n_seqs * a.kv_heads;
@@ -95,26 +151,20 @@ extern "C" rtcc_status rtcc_memory_attention(const rtcc_attn_config* c, const vo
     while (units * groups > 0x3FFFFFFF && groups > 1) groups = (groups + 1) / 2;   // blocks then loop
     units *= groups;
     a.row_groups = (int)groups;
-    // Chunks of the span: enough blocks for a few rounds over the SMs (the
-    // few-rows kernel has two blocks on one), each at least four tiles (a warp),
-    // within the workspace.
-    const long long want = ((tc ? 2LL : 8LL) * sms + units - 1) / units;
-    long long chunks = (max_k + 4LL * unit - 1) / (4LL * unit);
-    if (chunks > want) chunks = want;
-    if (tc && units >= sms) chunks = 1;
-    while (chunks > 1 && units * chunks > 0x7FFFFFFF) chunks /= 2;
-    const size_t part = (size_t)c->n_q * c->heads * (c->head_dim * sizeof(float) + sizeof(float2));
-    const long long room = d_workspace ? (long long)(workspace_bytes / part) : 0;
-    if (chunks > room) chunks = room;
-    if (chunks < 1) chunks = 1;
+    const long long steps = (max_k + a.unit - 1LL) / a.unit;
+    long long most = tc ? (steps + 3) / 4 : steps;
+    if (most > room / a.streams) most = room / a.streams;
+    if (most > 0x7FFFFFFF / units) most = 0x7FFFFFFF / units;
+    const long long chunks = tc ? tc_chunks(units, steps, most, sms, a.streams, a.n_q, a.heads, a.dim)
+                                : rows_chunks(units, c->n_seqs, steps, most, sms);
     a.n_chunks = (int)chunks;
     a.chunk = (int)((max_k + chunks - 1) / chunks);
     a.part_o = static_cast<float*>(d_workspace);
-    a.part_ml = reinterpret_cast<float2*>(a.part_o + (size_t)chunks * c->n_q * c->heads * c->head_dim);
+    a.part_ml = reinterpret_cast<float2*>(a.part_o + (size_t)chunks * a.streams * c->n_q * c->heads * c->head_dim);
     const cudaError_t e = tc ? launch_attn_tc(a, bf16, st) : launch_attn_rows(a, bf16, st);
     if (tc && e == cudaErrorNotSupported) continue;
     if (e != cudaSuccess) return RTCC_E_CUDA;
-    if (chunks > 1 && launch_attn_join(a, unit, max_q, bf16, st) != cudaSuccess) return RTCC_E_CUDA;
+    if (chunks * a.streams > 1 && launch_attn_join(a, max_q, bf16, st) != cudaSuccess) return RTCC_E_CUDA;
     return RTCC_OK;
   }
 }

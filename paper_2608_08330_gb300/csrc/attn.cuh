@@ -18,13 +18,14 @@ struct AttnArgs {
   const int* prefix;             // may be null
   const int* present;            // [n_slots], may be null
   const float *slopes, *q_pos, *k_pos;
-  float* part_o;                 // [n_chunks][n_q * heads][dim] when n_chunks > 1
-  float2* part_ml;               // [n_chunks][n_q * heads]: running maximum (log2) and sum
+  float* part_o;                 // [n_chunks * streams][n_q * heads][dim] when there are several
+  float2* part_ml;               // [n_chunks * streams][n_q * heads]: running maximum (log2) and sum
   long long q_row, q_head, k_row, k_head, v_row, v_head, out_row, out_head;
   int n_q, n_rows, heads, kv_heads, group, dim, n_seqs, causal;
   int n_slots, slot_rows, q_pos_row;
   uint32_t slot_mul, slot_shift; // row / slot_rows = row * slot_mul >> slot_shift
-  int n_chunks, chunk;           // key chunks per sequence at most, keys per chunk at least
+  int n_chunks, chunk, unit;     // key chunks per sequence at most, keys per chunk at least, a multiple of unit
+  int streams;                   // partial results per chunk
   int row_groups;                // blocks along the rows of one sequence and key head
   float scale_log2;              // scale * log2(e); with a cap: scale / cap
   float cap_log2;                // cap * log2(e), 0 = no cap

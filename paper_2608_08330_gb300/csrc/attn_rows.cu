@@ -102,7 +102,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) k_attn_rows(const __grid_const
   const int seq = b / A.kv_heads;
   const AttnSpan S = attn_span(A, seq);
   const int rows_all = S.nq * A.group;
-  const int per = attn_chunk(A, S.nk, KT * kWarps);
+  const int per = attn_chunk(A, S.nk, A.unit);
   const int c0 = (int)min((long long)per * chunk, (long long)S.nk), c1 = min(S.nk - c0, per) + c0;
   if (chunk > 0 && c0 >= S.nk) return;           // not in use; chunk 0 always answers
   const unsigned long long slots = attn_slot_mask(A, lane);
@@ -336,22 +336,27 @@ __global__ void __launch_bounds__(kWarps * 32, 2) k_attn_rows(const __grid_const
   }
 }
 
-// out_i = sum_c 2^(m_c - M) O_c / sum_c 2^(m_c - M) l_c over the chunks in use,
-// in index order: one warp per row, 4 channels per lane.
+// out_i = sum_c 2^(m_c - M) O_c / sum_c 2^(m_c - M) l_c over the partial results
+// in use: W warps per row (4 where there are many partial results, which one warp
+// would read one after another: 5 rows of 600 took 120 us), 4 channels per lane.
+// Every warp sums its share in index order, then the shares are summed in order.
 constexpr int kJoinWarps = 4;
-template <typename T>
-__global__ void __launch_bounds__(kJoinWarps * 32) k_attn_join(const __grid_constant__ AttnArgs A, int unit,
-                                                               int blocks_per_seq) {
+template <typename T, int W>
+__global__ void __launch_bounds__(kJoinWarps * 32) k_attn_join(const __grid_constant__ AttnArgs A, int blocks_per_seq) {
+  __shared__ float4 sum_o[kJoinWarps][32];
+  __shared__ float2 sum_ml[kJoinWarps];
   pdl_wait();
   const int seq = blockIdx.x / blocks_per_seq, b = blockIdx.x % blocks_per_seq;
-  const int lane = threadIdx.x & 31;
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
   const AttnSpan S = attn_span(A, seq);
-  const int per = attn_chunk(A, S.nk, unit);
-  const int used = max(1, (int)(((long long)S.nk + per - 1) / per));
+  const int per = attn_chunk(A, S.nk, A.unit);
+  const int used = max(1, (int)(((long long)S.nk + per - 1) / per)) * A.streams;
   const long long rows = (long long)S.nq * A.heads, stride = (long long)A.n_q * A.heads;
-  for (long long i = (long long)b * kJoinWarps + (threadIdx.x >> 5); i < rows; i += (long long)blocks_per_seq * kJoinWarps) {
+  constexpr int kRowsAtOnce = kJoinWarps / W;
+  const int first = W == 1 ? 0 : w;              // this warp's partial results: first, first + W, ...
+  for (long long i = (long long)b * kRowsAtOnce + (W == 1 ? w : 0); i < rows; i += (long long)blocks_per_seq * kRowsAtOnce) {
     const long long R = (long long)S.q0 * A.heads + i;
-    float mm = -INFINITY;
+    float mm = -INFINITY;                        // the row's maximum
     for (int c = lane; c < used; c += 32) mm = fmaxf(mm, A.part_ml[c * stride + R].x);
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) mm = fmaxf(mm, __shfl_xor_sync(0xFFFFFFFFu, mm, d));
@@ -359,28 +364,58 @@ __global__ void __launch_bounds__(kJoinWarps * 32) k_attn_join(const __grid_cons
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
     float ll = 0.f;
     const int c4 = lane * 4;
-    for (int c = 0; c < used; ++c) {
-      const float2 ml = A.part_ml[c * stride + R];
-      const float f = exp2f(ml.x - base);
-      ll = fmaf(f, ml.y, ll);
-      if (c4 < A.dim) {
-        const float4 x = *reinterpret_cast<const float4*>(A.part_o + (c * stride + R) * A.dim + c4);
-        acc.x = fmaf(f, x.x, acc.x);
-        acc.y = fmaf(f, x.y, acc.y);
-        acc.z = fmaf(f, x.z, acc.z);
-        acc.w = fmaf(f, x.w, acc.w);
+    const bool on = c4 < A.dim;
+    constexpr int U = 8;                         // loads in flight
+    for (int c0 = first; c0 < used; c0 += U * W) {
+      float2 ml[U];
+      float4 x[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int c = c0 + u * W;
+        const bool in = c < used;
+        ml[u] = in ? A.part_ml[c * stride + R] : make_float2(-INFINITY, 0.f);
+        x[u] = in && on ? *reinterpret_cast<const float4*>(A.part_o + (c * stride + R) * A.dim + c4)
+                        : make_float4(0.f, 0.f, 0.f, 0.f);
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const float f = exp2f(ml[u].x - base);
+        ll = fmaf(f, ml[u].y, ll);
+        acc.x = fmaf(f, x[u].x, acc.x);
+        acc.y = fmaf(f, x[u].y, acc.y);
+        acc.z = fmaf(f, x[u].z, acc.z);
+        acc.w = fmaf(f, x[u].w, acc.w);
       }
     }
-    const long long t = R / A.heads;
-    const int h = (int)(R % A.heads);
-    const float inv = ll > 0.f ? 1.0f / ll : (ll == 0.f ? 0.f : ll);
-    if (c4 < A.dim) {
-      uint2 u;
-      u.x = Store<T>::pack2(acc.x * inv, acc.y * inv);
-      u.y = Store<T>::pack2(acc.z * inv, acc.w * inv);
-      *reinterpret_cast<uint2*>(static_cast<T*>(A.out) + t * A.out_row + (long long)h * A.out_head + c4) = u;
+    if (W > 1) {
+      sum_o[w][lane] = acc;
+      if (lane == 0) sum_ml[w] = make_float2(0.f, ll);
+      __syncthreads();
+      if (w == 0) {
+#pragma unroll
+        for (int v = 1; v < W; ++v) {
+          const float4 y = sum_o[v][lane];
+          acc.x += y.x;
+          acc.y += y.y;
+          acc.z += y.z;
+          acc.w += y.w;
+          ll += sum_ml[v].y;
+        }
+      }
     }
-    if (lane == 0 && A.lse) A.lse[R] = ll == 0.f ? -INFINITY : (mm + log2f(ll)) * kLn2;
+    if (W == 1 || w == 0) {
+      const long long t = R / A.heads;
+      const int h = (int)(R % A.heads);
+      const float inv = ll > 0.f ? 1.0f / ll : (ll == 0.f ? 0.f : ll);
+      if (on) {
+        uint2 u;
+        u.x = Store<T>::pack2(acc.x * inv, acc.y * inv);
+        u.y = Store<T>::pack2(acc.z * inv, acc.w * inv);
+        *reinterpret_cast<uint2*>(static_cast<T*>(A.out) + t * A.out_row + (long long)h * A.out_head + c4) = u;
+      }
+      if (lane == 0 && A.lse) A.lse[R] = ll == 0.f ? -INFINITY : (mm + log2f(ll)) * kLn2;
+    }
+    if (W > 1) __syncthreads();                  // before the next row's sums
   }
 }
 
@@ -407,14 +442,19 @@ cudaError_t launch_attn_rows(const AttnArgs& a, bool bf16, cudaStream_t st) {
   return bf16 ? launch_rows_t<__nv_bfloat16, 128>(a, st) : launch_rows_t<__half, 128>(a, st);
 }
 
-cudaError_t launch_attn_join(const AttnArgs& a, int unit, int max_q, bool bf16, cudaStream_t st) {
-  long long per = ((long long)max_q * a.heads + kJoinWarps - 1) / kJoinWarps;
+cudaError_t launch_attn_join(const AttnArgs& a, int max_q, bool bf16, cudaStream_t st) {
+  const bool wide = (long long)a.n_chunks * a.streams > 8;
+  const int at_once = wide ? 1 : kJoinWarps;     // rows of a block
+  long long per = ((long long)max_q * a.heads + at_once - 1) / at_once;
   if (per < 1) per = 1;
   if (per > 4096) per = 4096;
   while ((long long)a.n_seqs * per > 0x7FFFFFFF && per > 1) per /= 2;
-  const dim3 grid((unsigned)((long long)a.n_seqs * per));
-  return bf16 ? launch_pdl(k_attn_join<__nv_bfloat16>, grid, dim3(kJoinWarps * 32), 0, st, a, unit, (int)per)
-              : launch_pdl(k_attn_join<__half>, grid, dim3(kJoinWarps * 32), 0, st, a, unit, (int)per);
+  const dim3 grid((unsigned)((long long)a.n_seqs * per)), block(kJoinWarps * 32);
+  if (wide)
+    return bf16 ? launch_pdl(k_attn_join<__nv_bfloat16, kJoinWarps>, grid, block, 0, st, a, (int)per)
+                : launch_pdl(k_attn_join<__half, kJoinWarps>, grid, block, 0, st, a, (int)per);
+  return bf16 ? launch_pdl(k_attn_join<__nv_bfloat16, 1>, grid, block, 0, st, a, (int)per)
+              : launch_pdl(k_attn_join<__half, 1>, grid, block, 0, st, a, (int)per);
 }
 
 }  // namespace rtcc

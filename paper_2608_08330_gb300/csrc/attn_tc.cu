@@ -1,32 +1,35 @@
 // Attention of many rows over the token memory on the 5th-generation tensor
 // cores (the formula is in attn_rows.cu).
 //
-// A block has two tiles of up to 128 rows and one key head; the query heads
-// that share it are rows of the same tile (row r: token r / group, head
-// r % group), so keys and values are read once for all of them.  Per 128 keys
-// and tile:  S = Q K^T (128 x 128 floats in tensor memory), the softmax warps
-// turn S into P = exp2(x - m), rounded to the storage type and written over S in
-// tensor memory, and O += P V takes P from there.  The softmax goes by halves of
-// 64 keys, which keeps a row's scores in registers, and the product of the first
-// half starts while the second is still at work.  While one tile's softmax
-// runs, the tensor pipe works for the other tile.  S and O of both tiles fill
-// tensor memory: 2 x 128 + 2 x head size columns of 512.
+// A block has up to four tiles of 128 rows and one key head; the query heads that
+// share it are rows of the same tile (row r: token r / group, head r % group), so
+// keys and values are read once for all of them.  Keys come in steps of 64.  A
+// "chain" is one tile's way through its steps:  S = Q K^T (128 x 64 floats in
+// tensor memory), four softmax warps turn S into P = exp2(x - m), rounded to the
+// storage type and written over S, and O += P V takes P from there.  Chains run
+// beside each other, so that one's softmax covers another's products: four for
+// heads of up to 64 channels (S and O of each: 4 x (64 + 64) = 512 columns of
+// tensor memory), two for heads of up to 128, each with two S, so that the next
+// scores are there when a softmax ends (2 x (2 x 64 + 128)).
 //
-// Roles: warps 0-3 softmax and epilogue of tile 0, warps 4-7 of tile 1 (a thread
-// owns a row: no shuffles), warp 8 loads (TMA, one thread), warps 9 and 10 issue
-// the products of tile 0 and 1 (one thread issues an MMA in about 100 clocks, so
-// two issue for one tensor pipe), warp 11 zeroes value rows at edges.  Keys and
-// values share one ring of 128-row slots in the order they are used: K0 V0 K1 V1
-// ..., so even slots hold keys and odd ones values.
+// With few rows the chains share a tile and take its steps in turn ("streams"):
+// a stream writes a partial result as a chunk of the span does, and k_attn_join
+// merges them.
 //
-// The running maximum m moves only when a row's new maximum exceeds it by more
-// than 2^8 in P (kSlack): P stays below 2^8, far inside either storage type's
-// range, O is rescaled rarely, by the softmax threads themselves, and x - m is
-// formed with the m of the step before inside the score's last multiply-add.
+// Roles: four softmax warps per chain (a thread owns a row: no shuffles), then a
+// warp that loads keys (TMA, one lane) and stages their coordinates, one that
+// loads values and zeroes those of keys nobody sees, and two that issue the
+// products of half of the chains each.
+//
+// The running maximum m of a row moves late: P = exp2(x - m) is formed in one
+// pass with the m of the step before, and where a row's maximum has passed m by
+// more than 2^8 in P (kSlack) O and the sum are scaled down before the next step.
+// Up to 2^15 (kHard), inside fp16's range, nothing is done again; beyond, and at
+// masked steps and a row's first, a slower form of the step handles everything.
 //
 // Key rows nobody may see (past the span, in an absent slot) are skipped as
-// whole tiles; in a tile at the edge their scores are replaced, not added to,
-// and their value rows are zeroed in shared memory before the product, so their
+// whole steps; in a step at the edge their scores are replaced, not added to, and
+// their value rows are zeroed in shared memory before the product, so their
 // contents never reach a result.
 #include <type_traits>
 
@@ -36,25 +39,31 @@
 namespace rtcc {
 namespace {
 
-constexpr int kThreads = 384;
-constexpr int kKeys = 128;                       // keys per tile
-constexpr int kHalf = 64;                        // keys per softmax step
-constexpr int kChunkBytes = 128 * 128;           // 128 rows x 64 channels
-constexpr float kSlack = 8.0f;
+constexpr int kKeys = 64;                        // keys per step
+constexpr int kBox = 64 * 128;                   // 64 keys x 64 channels
+constexpr int kQBox = 128 * 128;                 // 128 rows x 64 channels
+constexpr float kSlack = 8.0f, kHard = 15.0f;
 
-__device__ int g_attn_err;                       // bit b: a wait on barrier b ran out
+__device__ int g_attn_err;                       // bit b: a wait on barrier b (mod 32) ran out
 
 template <int DP> struct TcCfg {
   static constexpr int NC = DP / 64;             // 64-channel chunks (one 128-byte swizzle line each)
-  static constexpr int kTile = NC * kChunkBytes;
-  static constexpr int kSlots = DP == 64 ? 8 : 4;
-  static constexpr int kQ = 2 * kTile;
-  static constexpr int kPos = kSlots / 2 * 2 * kKeys * 4;   // [tile in the ring][y | x][128]
-  // Tensor memory.  With 64-channel heads P has columns of its own, and the next
-  // S may be made as soon as this one is in registers; with 128 it covers S.
-  static constexpr bool kOwnP = DP == 64;
-  static constexpr int kO = 256, kOStep = DP, kP = kOwnP ? 384 : 0, kPStep = kOwnP ? 64 : 128;
-  static constexpr int kSmem = kQ + kSlots * kTile + kPos + 1024;
+  static constexpr int kChains = 2;
+  static constexpr int kS = 2;    // S per chain
+  static constexpr int kRing = DP == 64 ? 8 : 4; // steps of keys and of values in shared memory
+  static constexpr int kPart = 64;           // scores a thread takes at a time
+  static constexpr int kStep = NC * kBox;
+  static constexpr int kQ = kChains * NC * kQBox;
+  static constexpr int kPos = kRing * 2 * kKeys * 4;         // [step in the ring][y | x][64]
+  static constexpr int kSmem = kQ + 2 * kRing * kStep + kPos + 1024;
+  static constexpr int kWarps = 4 * kChains + 4;
+  // tensor memory: S of every chain, then O of every chain
+  static constexpr int kO = kChains * kS * kKeys;
+  static_assert(kO + kChains * DP <= 512, "tensor memory");
+  // barriers
+  static constexpr int FULL = 0, FREE = kRing, VOK = 2 * kRing, SFULL = 3 * kRing,
+                       PREADY = SFULL + kChains * kS, DONE = PREADY + kChains * kS,
+                       QFULL = DONE + kChains * kS, QFREE = QFULL + 1, DRAIN = QFREE + 1, kBars = DRAIN + 2;
 };
 
 struct TcMaps {
@@ -65,22 +74,6 @@ struct TcMaps {
 struct TanhPoly {
   float c[4];
 };
-
-// Each half of P has a barrier of its own (BAR_PREADY + 2 w + h): a softmax warp
-// may finish both halves before the first is waited for, and one barrier's
-// parity would then have come round.  For the same reason every role that waits
-// on a slot's barrier does so once for every use of the slot.
-enum : int { BAR_QFULL, BAR_QFREE, BAR_SFULL, BAR_PREADY = BAR_SFULL + 2, BAR_ODONE = BAR_PREADY + 4,
-             BAR_HALF = BAR_ODONE + 2, BAR_DONE = BAR_HALF + 2, BAR_SFREE = BAR_DONE + 2, BAR_DRAIN = BAR_SFREE + 2,
-             BAR_FULL = BAR_DRAIN + 2, BAR_EMPTY = BAR_FULL + 8,
-             BAR_VOK = BAR_EMPTY + 8, BAR_N = BAR_VOK + 8 };
-__host__ __device__ constexpr int bar_count(int i, bool dist) {
-  return (i >= BAR_PREADY && i < BAR_PREADY + 4) || i == BAR_SFREE || i == BAR_SFREE + 1 ? 4   // a tile's softmax warps
-         : i == BAR_QFREE                      ? 2           // both product warps
-         : dist && i >= BAR_FULL && i < BAR_FULL + 8 ? 2 - (i - BAR_FULL) % 2  // keys: and the coordinates
-         : i >= BAR_EMPTY && i < BAR_EMPTY + 8 ? 2 + (i - BAR_EMPTY) % 2   // and, for values, warp 11
-                                               : 1;
-}
 
 __device__ __forceinline__ void tmem_ld32_issue(uint32_t a, float* x) {
   uint32_t* r = reinterpret_cast<uint32_t*>(x);
@@ -162,11 +155,11 @@ __device__ __forceinline__ void umma_commit_elected(uint64_t* bar) {
 }
 // Descriptor of V as the B operand [head size][keys], head size contiguous
 // (MN-major): 64-channel lines of 128 bytes, 8 keys per 1024 bytes, the next 64
-// channels a chunk further.
+// channels a box further.
 __device__ __forceinline__ uint64_t desc_v(uint32_t saddr) {
   uint64_t d = 0;
   d |= static_cast<uint64_t>((saddr >> 4) & 0x3FFFu);
-  d |= static_cast<uint64_t>(kChunkBytes >> 4) << 16;
+  d |= static_cast<uint64_t>(kBox >> 4) << 16;
   d |= static_cast<uint64_t>(1024 >> 4) << 32;
   d |= static_cast<uint64_t>(1u) << 46;
   d |= static_cast<uint64_t>(2u) << 61;
@@ -183,12 +176,14 @@ __device__ __forceinline__ float tanh_abs(float u) {
 }
 __device__ __forceinline__ float2 both(float a) { return make_float2(a, a); }
 
-// A walk over the key tiles of a chunk that have a key in a present slot.  Every
-// role walks; which tiles are skipped, and which are `partial` (some key in an
-// absent slot), depends on the chunk's end c1 alone, so all roles agree.
+// A walk over the steps of a chunk that have a key in a present slot, and their
+// number.  Every role walks; which steps are skipped, and which are `partial` (some
+// key in an absent slot), depends on the chunk's end c1 alone, so all roles agree.
 struct Walk {
-  int t, end_key, c1;                            // current tile; tiles that begin before end_key count
+  int t, end_key, c1;                            // current step; steps that begin before end_key count
+  int g;                                         // steps since the block began
   bool partial;
+  __device__ __forceinline__ bool live() const { return t * kKeys < end_key; }
   __device__ __forceinline__ void settle(const AttnArgs& A, const AttnSpan& S, unsigned long long slots, bool all) {
     partial = false;
     if (all) return;
@@ -200,7 +195,26 @@ struct Walk {
       if (have) return;
     }
   }
-  __device__ __forceinline__ bool live() const { return t * kKeys < end_key; }
+  __device__ __forceinline__ void next(const AttnArgs& A, const AttnSpan& S, unsigned long long slots, bool all) {
+    ++t;
+    ++g;
+    settle(A, S, slots, all);
+  }
+  // to the next step of a stream: one whose number is `stream` in every `streams`
+  __device__ __forceinline__ void seek(const AttnArgs& A, const AttnSpan& S, unsigned long long slots, bool all,
+                                       int streams, int stream) {
+    while (live() && (g & (streams - 1)) != stream) next(A, S, slots, all);
+  }
+  __device__ __forceinline__ void next_own(const AttnArgs& A, const AttnSpan& S, unsigned long long slots, bool all,
+                                           int streams, int stream) {
+    if (all) {                                   // nothing to skip
+      t += streams;
+      g += streams;
+      return;
+    }
+    next(A, S, slots, all);
+    seek(A, S, slots, all, streams, stream);
+  }
 };
 
 // Bit c: key j0 + c, c < 64, lies before `lim` and in a present slot.
@@ -220,23 +234,33 @@ __device__ __forceinline__ unsigned long long key_mask(const AttnArgs& A, const 
   return bits;
 }
 
+// A block that gave up stays for about 2 ms, so that no copy of its own (a few
+// microseconds at most) is in flight when it ends.
+__device__ __forceinline__ void outlast_copies() {
+  const long long t0 = clock64();
+  while (clock64() - t0 < kWaitBudgetCycles / 500) {
+  }
+}
+
 template <typename T, int DP, bool CAP, bool DIST>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(TcCfg<DP>::kWarps * 32, 1)
     k_attn_tc(const __grid_constant__ AttnArgs A, const __grid_constant__ TcMaps M, const TanhPoly poly) {
   using C = TcCfg<DP>;
   extern __shared__ unsigned char smem_raw[];
-  __shared__ uint64_t bar[BAR_N];
+  __shared__ uint64_t bar[C::kBars];
   __shared__ uint32_t tmem_base;
   __shared__ int gave_up;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   unsigned char* smem =
       reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
   unsigned char* sq = smem;
-  unsigned char* ring = smem + C::kQ;
-  float* spos = reinterpret_cast<float*>(ring + C::kSlots * C::kTile);
+  unsigned char* sk = smem + C::kQ;
+  unsigned char* sv = sk + C::kRing * C::kStep;
+  float* spos = reinterpret_cast<float*>(sv + C::kRing * C::kStep);
 
   // block -> (row group, chunk, key head, sequence); the last rows of a causal
   // sequence have the longest reach and go first
+  const int streams = A.streams, tiles = C::kChains / streams;
   int b = blockIdx.x;
   int rg0 = b % A.row_groups;
   b /= A.row_groups;
@@ -246,15 +270,22 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int seq = b / A.kv_heads;
   const AttnSpan S = attn_span(A, seq);
   const int qpt = 128 / A.group;                 // tokens per tile
-  const int groups = (S.nq + 2 * qpt - 1) / (2 * qpt);
+  const int groups = (S.nq + tiles * qpt - 1) / (tiles * qpt);
   if (A.causal) rg0 = A.row_groups - 1 - rg0;
-  const int per = attn_chunk(A, S.nk, kKeys);
+  const int per = attn_chunk(A, S.nk, A.unit);
   const int c0 = (int)min((long long)per * chunk, (long long)S.nk), c1 = min(S.nk - c0, per) + c0;
   if (rg0 >= groups || (chunk > 0 && c0 >= S.nk)) return;   // not in use; chunk 0 always answers
 
   if (warp == 0) {
     if (lane == 0) {
-      for (int i = 0; i < BAR_N; ++i) mbar_init(&bar[i], bar_count(i, DIST));
+      for (int i = 0; i < C::kBars; ++i) {
+        int n = 1;
+        if (i < C::FREE) n = 2;                                                              // keys and values
+        if (i >= C::FREE && i < C::VOK) n = tiles;                                           // the chains of a stream
+        if (i >= C::PREADY && i < C::DONE) n = 4;                                            // a chain's softmax warps
+        if (i == C::QFREE) n = 2;                                                            // the product warps
+        mbar_init(&bar[i], n);
+      }
       fence_barrier_init();
       gave_up = 0;
       tma_prefetch_desc(&M.q);
@@ -263,7 +294,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     __syncwarp();
   }
-  if (warp == 9) {
+  if (warp == 4 * C::kChains + 2) {
     tmem_alloc(&tmem_base, 512);
     tmem_relinquish();
   }
@@ -278,489 +309,495 @@ __global__ void __launch_bounds__(kThreads, 1)
     all = ((slots >> s0) & want) == want;
   }
   volatile int* stop = &gave_up;
-  // a wait that runs out marks the block; every role then leaves its loops
-  auto wait_one = [&](int i, uint32_t parity) -> bool {
-    if (mbar_wait(&bar[i], parity)) return *stop == 0;
-    *stop = 1;
-    atomicOr(&g_attn_err, 1 << (i & 31));
-    return false;
-  };
-  // the same by a whole warp, which goes on or leaves together
+  // A wait by a whole warp; one that runs out marks the block, and every role then
+  // leaves its loops.  A slot's barrier is waited for at every use by each role
+  // that waits on it at all (a slot belongs to one stream), so parities suffice.
+  const uint32_t bar0 = smem_u32(bar);
   auto wait = [&](int i, uint32_t parity) -> bool {
-    if (__all_sync(0xFFFFFFFFu, mbar_try_wait(&bar[i], parity))) return true;
-    return __all_sync(0xFFFFFFFFu, wait_one(i, parity));
+    uint32_t in;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(in)
+        : "r"(bar0 + i * 8), "r"(parity)
+        : "memory");
+    if (__all_sync(0xFFFFFFFFu, in)) return true;
+    bool ok = mbar_wait(&bar[i], parity);
+    if (!ok) {
+      *stop = 1;
+      atomicOr(&g_attn_err, 1 << (i & 31));
+    }
+    return __all_sync(0xFFFFFFFFu, ok && *stop == 0);
   };
   // keys that tile w of row group rg reaches within this chunk
   auto reach = [&](int rg, int w) -> int {
-    const int i0 = (rg * 2 + w) * qpt;
+    const int i0 = (rg * tiles + w) * qpt;
     if (i0 >= S.nq) return c0;
     return max(c0, min(c1, attn_visible(A, S, min(i0 + qpt, S.nq) - 1)));
   };
-  // whether the tile has value rows to zero
+  auto reach_all = [&](int rg) -> int {
+    int e = reach(rg, 0);
+    for (int w = 1; w < tiles; ++w) e = max(e, reach(rg, w));
+    return e;
+  };
+  // whether the step has value rows to zero
   auto patched = [&](const Walk& k) -> bool { return k.partial || k.t * kKeys + kKeys > S.nk; };
+  auto place = [](int g) { return g & (C::kRing - 1); };
+  auto phase = [](int g) { return (uint32_t)(g / C::kRing) & 1u; };
 
-  if (warp == 8) {
-    // ---------------------------------------------------------------- loads
-    if (lane == 0) {
-      int slot = 0;
-      uint32_t ph = 1, item = 0;                 // a fresh slot counts as empty
-      long long issued = 0;
-      bool ok = true;
-      auto put = [&](const CUtensorMap* m, int row) {
-        ok = wait_one(BAR_EMPTY + slot, ph);
-        if (!ok) return;
-        mbar_arrive_expect_tx(&bar[BAR_FULL + slot], C::kTile);
-#pragma unroll
-        for (int c = 0; c < C::NC; ++c)
-          tma_load_3d(ring + slot * C::kTile + c * kChunkBytes, m, &bar[BAR_FULL + slot], c * 64, kvh, row);
-        ++issued;
-        if (++slot == C::kSlots) {
-          slot = 0;
-          ph ^= 1;
-        }
-      };
-      for (int rg = rg0; rg < groups && ok; rg += A.row_groups, ++item) {
-        if (item > 0 && !(ok = wait_one(BAR_QFREE, (item - 1) & 1))) break;
-        mbar_arrive_expect_tx(&bar[BAR_QFULL], 2 * C::NC * qpt * A.group * 128);
-        for (int w = 0; w < 2; ++w)
+  if (warp == 4 * C::kChains) {
+    // ------------------------------------------ queries, keys, coordinates
+    bool ok = true;
+    uint32_t item = 0;
+    int g = 0;
+    for (int rg = rg0; rg < groups && ok; rg += A.row_groups, ++item) {
+      if (item > 0 && !(ok = wait(C::QFREE, (item - 1) & 1))) break;
+      if (lane == 0) {
+        mbar_arrive_expect_tx(&bar[C::QFULL], tiles * C::NC * qpt * A.group * 128);
+        for (int w = 0; w < tiles; ++w)
 #pragma unroll
           for (int c = 0; c < C::NC; ++c)
-            tma_load_3d(sq + w * C::kTile + c * kChunkBytes, &M.q, &bar[BAR_QFULL], c * 64, kvh * A.group,
-                        S.q0 + (rg * 2 + w) * qpt);
-        Walk k{c0 / kKeys, max(reach(rg, 0), reach(rg, 1)), c1, false};
-        for (k.settle(A, S, slots, all); k.live() && ok; ++k.t, k.settle(A, S, slots, all)) {
-          put(&M.k, S.kb + k.t * kKeys);
-          if (ok) put(&M.v, S.kb + k.t * kKeys);
-        }
+            tma_load_3d(sq + (w * C::NC + c) * kQBox, &M.q, &bar[C::QFULL], c * 64, kvh * A.group,
+                        S.q0 + (rg * tiles + w) * qpt);
       }
-      // leave no copy in flight behind (only a block that gave up has any)
-      if (!ok) {
-        mbar_wait(&bar[BAR_QFULL], item & 1);
-        for (long long i = max(0LL, issued - C::kSlots); i < issued; ++i)
-          mbar_wait(&bar[BAR_FULL + (int)(i % C::kSlots)], (uint32_t)((i / C::kSlots) & 1));
-      }
-    }
-    __syncwarp();
-  } else if (warp == 9 || warp == 10) {
-    // ------------------------------------------------------ products of tile w
-    const int w = __shfl_sync(0xFFFFFFFFu, warp - 9, 0);
-    constexpr uint32_t fmt = std::is_same<T, __nv_bfloat16>::value;
-    constexpr uint32_t id_s = idesc_f16(128, kKeys, fmt);
-    constexpr uint32_t id_o = idesc_f16(128, DP, fmt) | (1u << 16);      // B is MN-major
-    const uint32_t t_s = tmem + w * 128, t_o = tmem + C::kO + w * C::kOStep,
-                   t_p = tmem + C::kP + w * C::kPStep;
-    const uint64_t dq = smem_desc(smem_u32(sq + w * C::kTile), 1024, 2);
-    const uint64_t dk = smem_desc(smem_u32(ring), 1024, 2), dv = desc_v(smem_u32(ring));
-    constexpr uint64_t kSlotStep = C::kTile >> 4, kChunkStep = kChunkBytes >> 4, kHalfStep = (kHalf * 128) >> 4;
-    int slot = 0;
-    uint32_t ph = 0, item = 0, p_ph = 0, vok = 0;                        // bit s of vok: slot s's patch phase
-    bool ok = true;
-    auto advance = [&]() {
-      if (++slot == C::kSlots) {
-        slot = 0;
-        ph ^= 1;
-      }
-    };
-    auto score = [&](int ks) {                   // S = Q K^T; the slot is free when it is done
-#pragma unroll
-      for (int c = 0; c < C::NC; ++c)
-        umma4_ss(t_s, dq + c * kChunkStep, dk + ks * kSlotStep + c * kChunkStep, id_s, c > 0);
-      umma_commit_elected(&bar[BAR_SFULL + w]);
-      umma_commit_elected(&bar[BAR_EMPTY + ks]);
-    };
-    auto skip = [&](int s) {                     // this tile does not use the slot
-      if (lane == 0) mbar_arrive(&bar[BAR_EMPTY + s]);
-    };
-    for (int rg = rg0; rg < groups && ok; rg += A.row_groups, ++item) {
-      const int e = reach(rg, w);
-      Walk k{c0 / kKeys, max(e, reach(rg, w ^ 1)), c1, false};
-      k.settle(A, S, slots, all);
-      ok = wait(BAR_QFULL, item & 1);
-      if (ok && k.live()) {
-        ok = wait(BAR_FULL + slot, ph);
-        if (ok) {
-          tc_fence_after();
-          if (k.t * kKeys < e) score(slot); else skip(slot);
-        }
-        advance();
-      }
-      uint32_t begun = 0;
-      while (ok && k.live()) {
-        const int vs = slot;
-        if (!(ok = wait(BAR_FULL + vs, ph))) break;
-        advance();
-        const bool mine = k.t * kKeys < e, zeroed = patched(k);
-        Walk nk = k;
-        ++nk.t;
-        nk.settle(A, S, slots, all);
-        const int ks = slot;
-        const uint32_t kph = ph;
-        if (nk.live()) advance();
-        const bool more = nk.live() && nk.t * kKeys < e;
-        if (mine) {
-          if (zeroed && !(ok = wait(BAR_VOK + vs, (vok >> vs) & 1))) break;
-          const uint64_t d = dv + vs * kSlotStep;
-          if (!(ok = wait(BAR_PREADY + 2 * w, p_ph))) break;
-          tc_fence_after();
-          umma4_ts(t_o, t_p, d, id_o, begun);
-          umma_commit_elected(&bar[BAR_HALF + w]);
-          if (C::kOwnP && more) {
-            if (!(ok = wait(BAR_FULL + ks, kph))) break;
-            if (!(ok = wait(BAR_SFREE + w, p_ph))) break;
-            tc_fence_after();
-            score(ks);
-          }
-          if (!(ok = wait(BAR_PREADY + 2 * w + 1, p_ph))) break;
-          tc_fence_after();
-          umma4_ts(t_o, t_p + 32, d + kHalfStep, id_o, 1);
-          umma_commit_elected(&bar[BAR_EMPTY + vs]);
-          if (C::kOwnP) umma_commit_elected(&bar[BAR_DONE + w]);
-          p_ph ^= 1;
-          begun = 1;
-        } else {
-          skip(vs);
-        }
-        if (zeroed) vok ^= 1u << vs;
-        if (mine && !more) umma_commit_elected(&bar[BAR_ODONE + w]);
-        if (nk.live() && !(C::kOwnP && mine && more)) {
-          if (!(ok = wait(BAR_FULL + ks, kph))) break;
-          tc_fence_after();
-          if (more) score(ks); else skip(ks);
-        }
-        k = nk;
-      }
-      if (ok) umma_commit_elected(&bar[BAR_QFREE]);
       __syncwarp();
-    }
-    // no product may still run when tensor memory is freed
-    umma_commit_elected(&bar[BAR_DRAIN + w]);
-    if (!mbar_wait(&bar[BAR_DRAIN + w], 0)) atomicOr(&g_attn_err, 1 << (BAR_DRAIN + w));
-    __syncwarp();
-  } else if (warp == 11) {
-    // ------------ the keys' coordinates; value rows nobody sees: zero
-    int tile = 0, last_tile = 0;                 // place in the ring: slots 2 tile and 2 tile + 1
-    uint32_t ph = 0, last_ph = 0;
-    bool ok = true, pending = false;
-    Walk last{};
-    // the values of the tile before, one step behind the coordinates
-    auto patch = [&]() {
-      const int slot = 2 * last_tile + 1;
-      if (!(ok = wait(BAR_FULL + slot, last_ph))) return;
-      if (patched(last)) {
-        unsigned char* rows = ring + slot * C::kTile;
-        for (int h = 0; h < kKeys; h += 64) {
-          const unsigned long long keep = key_mask(A, S, slots, last.t * kKeys + h, S.nk);
-          for (int i = lane; i < 64; i += 32)
-            if (!((keep >> i) & 1))
-              for (int c = 0; c < C::NC; ++c)
-                for (int u = 0; u < 8; ++u)
-                  *reinterpret_cast<uint4*>(rows + c * kChunkBytes + (h + i) * 128 + u * 16) =
-                      make_uint4(0u, 0u, 0u, 0u);
-        }
-        fence_async_smem();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&bar[BAR_VOK + slot]);
-      }
-      if (lane == 0) mbar_arrive(&bar[BAR_EMPTY + slot]);
-    };
-    for (int rg = rg0; rg < groups && ok; rg += A.row_groups) {
-      Walk k{c0 / kKeys, max(reach(rg, 0), reach(rg, 1)), c1, false};
-      for (k.settle(A, S, slots, all); k.live(); ++k.t, k.settle(A, S, slots, all)) {
+      Walk k{c0 / kKeys, reach_all(rg), c1, g, false};
+      for (k.settle(A, S, slots, all); k.live(); k.next(A, S, slots, all)) {
+        const int p = place(k.g);
+        float2 at[2];
         if (DIST) {
-          float2 at[4];
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
+          for (int i = 0; i < 2; ++i)
             at[i] = *reinterpret_cast<const float2*>(
                 A.k_pos + 2 * (long long)min(S.kb + k.t * kKeys + i * 32 + lane, A.n_rows - 1));
-          // the ring's tile has been read when its values are released
-          if (!(ok = wait(BAR_EMPTY + 2 * tile + 1, ph ^ 1))) break;
-          float* d = spos + tile * 2 * kKeys + lane;
+        }
+        if (!(ok = wait(C::FREE + p, phase(k.g) ^ 1))) break;
+        if (DIST) {
+          float* d = spos + p * 2 * kKeys + lane;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
+          for (int i = 0; i < 2; ++i) {
             d[i * 32] = at[i].x;
             d[kKeys + i * 32] = at[i].y;
           }
           __syncwarp();
-          if (lane == 0) mbar_arrive(&bar[BAR_FULL + 2 * tile]);
         }
-        if (pending) {
-          patch();
-          if (!ok) break;
+        if (lane == 0) {
+          mbar_arrive_expect_tx(&bar[C::FULL + p], C::kStep);
+#pragma unroll
+          for (int c = 0; c < C::NC; ++c)
+            tma_load_3d(sk + p * C::kStep + c * kBox, &M.k, &bar[C::FULL + p], c * 64, kvh, S.kb + k.t * kKeys);
         }
+        __syncwarp();
+      }
+      g = k.g;
+    }
+    if (!ok) outlast_copies();
+  } else if (warp == 4 * C::kChains + 1) {
+    // ------------------------------------------ values, and zeroes at edges
+    bool ok = true;
+    int g = 0;
+    Walk last{};
+    bool pending = false;
+    auto patch = [&]() -> bool {                 // the step before, one behind the loads
+      if (!pending || !patched(last)) return true;
+      const int p = place(last.g);
+      if (!wait(C::FULL + p, phase(last.g))) return false;
+      const unsigned long long keep = key_mask(A, S, slots, last.t * kKeys, S.nk);
+      for (int i = lane; i < kKeys; i += 32)
+        if (!((keep >> i) & 1))
+          for (int c = 0; c < C::NC; ++c)
+            for (int u = 0; u < 8; ++u)
+              *reinterpret_cast<uint4*>(sv + p * C::kStep + c * kBox + i * 128 + u * 16) = make_uint4(0u, 0u, 0u, 0u);
+      fence_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&bar[C::VOK + p]);
+      return true;
+    };
+    for (int rg = rg0; rg < groups && ok; rg += A.row_groups) {
+      Walk k{c0 / kKeys, reach_all(rg), c1, g, false};
+      for (k.settle(A, S, slots, all); k.live(); k.next(A, S, slots, all)) {
+        // with a ring of one stream's steps the patch of the step before must not
+        // wait behind this step's slot
+        if (!(ok = patch())) break;
+        const int p = place(k.g);
+        if (!(ok = wait(C::FREE + p, phase(k.g) ^ 1))) break;
+        if (lane == 0) {
+          mbar_arrive_expect_tx(&bar[C::FULL + p], C::kStep);
+#pragma unroll
+          for (int c = 0; c < C::NC; ++c)
+            tma_load_3d(sv + p * C::kStep + c * kBox, &M.v, &bar[C::FULL + p], c * 64, kvh, S.kb + k.t * kKeys);
+        }
+        __syncwarp();
         pending = true;
         last = k;
-        last_tile = tile;
-        last_ph = ph;
-        if (++tile == C::kSlots / 2) {
-          tile = 0;
-          ph ^= 1;
-        }
       }
+      g = k.g;
     }
-    if (ok && pending) patch();
+    if (ok) ok = patch();
+    if (!ok) outlast_copies();
+  } else if (warp > 4 * C::kChains) {
+    // ------------------------------------------------------------- products
+    constexpr int kOwn = C::kChains / 2;         // chains of this warp
+    const int first = __shfl_sync(0xFFFFFFFFu, (warp - 4 * C::kChains - 2) * kOwn, 0);
+    constexpr uint32_t fmt = std::is_same<T, __nv_bfloat16>::value;
+    constexpr uint32_t id_s = idesc_f16(128, kKeys, fmt);
+    constexpr uint32_t id_o = idesc_f16(128, DP, fmt) | (1u << 16);      // B is MN-major
+    constexpr uint64_t kStepUnits = C::kStep >> 4, kBoxUnits = kBox >> 4, kQBoxUnits = kQBox >> 4;
+    const uint64_t dk = smem_desc(smem_u32(sk), 1024, 2), dv = desc_v(smem_u32(sv));
+    const uint64_t dq = smem_desc(smem_u32(sq), 1024, 2);
+    bool ok = true;
+    uint32_t item = 0, vok = 0;                  // bit p of vok: the patch phase of place p
+    int g = 0;
+    uint32_t n_qk[kOwn] = {}, n_pv[kOwn] = {};   // products issued per chain
+    for (int rg = rg0; rg < groups && ok; rg += A.row_groups, ++item) {
+      const int end = reach_all(rg);
+      Walk qk[kOwn], pv[kOwn];
+      int e[kOwn];
+      uint32_t begun = 0;
+#pragma unroll
+      for (int c = 0; c < kOwn; ++c) {
+        const int stream = (first + c) & (streams - 1);
+        e[c] = reach(rg, (first + c) / streams);
+        qk[c] = Walk{c0 / kKeys, end, c1, g, false};
+        qk[c].settle(A, S, slots, all);
+        qk[c].seek(A, S, slots, all, streams, stream);
+        pv[c] = qk[c];
+      }
+      // S = Q K^T of chain c's next step (its values are there as well)
+      auto score = [&](int c) -> bool {
+        if (!qk[c].live()) return true;
+        const int chain = first + c, p = place(qk[c].g);
+        if (!wait(C::FULL + p, phase(qk[c].g))) return false;
+        if (qk[c].t * kKeys < e[c]) {
+          tc_fence_after();
+          const uint32_t s = chain * C::kS + (n_qk[c] & (C::kS - 1));
+          const uint64_t q = dq + (chain / streams) * C::NC * kQBoxUnits, kd = dk + p * kStepUnits;
+#pragma unroll
+          for (int i = 0; i < C::NC; ++i)
+            umma4_ss(tmem + s * kKeys, q + i * kQBoxUnits, kd + i * kBoxUnits, id_s, i > 0);
+          umma_commit_elected(&bar[C::SFULL + s]);
+          ++n_qk[c];
+        }
+        qk[c].next_own(A, S, slots, all, streams, chain & (streams - 1));
+        return true;
+      };
+      // O += P V of chain c's next step; keys and values are released when it is done
+      auto value = [&](int c) -> bool {
+        if (!pv[c].live()) return true;
+        const int chain = first + c, p = place(pv[c].g);
+        const bool zeroed = patched(pv[c]);
+        if (pv[c].t * kKeys < e[c]) {
+          if (zeroed && !wait(C::VOK + p, (vok >> (p + 8 * c)) & 1)) return false;
+          const uint32_t s = chain * C::kS + (n_pv[c] & (C::kS - 1));
+          if (!wait(C::PREADY + s, (n_pv[c] / C::kS) & 1)) return false;
+          tc_fence_after();
+          umma4_ts(tmem + C::kO + chain * DP, tmem + s * kKeys, dv + p * kStepUnits, id_o, (begun >> c) & 1);
+          umma_commit_elected(&bar[C::FREE + p]);
+          if (C::kS > 1) umma_commit_elected(&bar[C::DONE + s]);
+          ++n_pv[c];
+          begun |= 1u << c;
+        } else if (lane == 0) {
+          mbar_arrive(&bar[C::FREE + p]);
+        }
+        if (zeroed) vok ^= 1u << (p + 8 * c);
+        pv[c].next_own(A, S, slots, all, streams, chain & (streams - 1));
+        return true;
+      };
+      ok = wait(C::QFULL, item & 1);
+#pragma unroll
+      for (int i = 0; i < C::kS; ++i)
+#pragma unroll
+        for (int c = 0; c < kOwn; ++c) ok = ok && score(c);
+      while (ok) {
+        bool more = false;
+#pragma unroll
+        for (int c = 0; c < kOwn; ++c) {
+          ok = ok && value(c) && score(c);
+          more = more || pv[c].live();
+        }
+        if (!more) break;
+      }
+      // the steps of the whole group, for the next group's places
+      Walk k{c0 / kKeys, end, c1, g, false};
+      if (rg + A.row_groups < groups)
+        for (k.settle(A, S, slots, all); k.live(); k.next(A, S, slots, all)) {
+        }
+      g = k.g;
+      if (C::kS == 1)
+#pragma unroll
+        for (int c = 0; c < kOwn; ++c)
+          if (ok && ((begun >> c) & 1)) umma_commit_elected(&bar[C::DONE + first + c]);
+      if (ok) umma_commit_elected(&bar[C::QFREE]);
+      __syncwarp();
+    }
+    // no product may still run when tensor memory is freed
+    const int drain = C::DRAIN + first / kOwn;
+    umma_commit_elected(&bar[drain]);
+    if (!mbar_wait(&bar[drain], 0)) atomicOr(&g_attn_err, 1 << (drain & 31));
+    __syncwarp();
   } else {
     // -------------------------------------------------------------- softmax
-    const int w = warp >> 2, r = tid & 127;
+    const int chain = warp >> 2, r = tid & 127, w = chain / streams, stream = chain & (streams - 1);
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-    const uint32_t ts = tmem + w * 128 + lanes, to = tmem + C::kO + w * C::kOStep + lanes,
-                   tp = tmem + C::kP + w * C::kPStep + lanes;
-    uint32_t s_ph = 0, o_ph = 0, k_ph = 0, d_ph = 0;
-    int tile = 0;                                // place in the ring, for the coordinates
+    const uint32_t ts0 = tmem + chain * C::kS * kKeys + lanes, to = tmem + C::kO + chain * DP + lanes;
+    uint32_t n = 0;                              // steps of this chain since the block began
+    int g = 0;
     bool ok = true;
+    // With one S, this step's S is complete only after the product of the step
+    // before, and DONE marks the end of a row group.  With two S a product may lag:
+    // DONE marks every step's, by turns on two barriers, since it may lag two steps.
+    auto done = [&](uint32_t i) -> int { return C::DONE + chain * C::kS + (i & (C::kS - 1)); };
+    uint32_t ends = 0;                           // row groups of this chain that had a step
+    auto phase_s = [](uint32_t i) -> uint32_t { return (i / C::kS) & 1; };
     for (int rg = rg0; rg < groups && ok; rg += A.row_groups) {
-      const int i0 = (rg * 2 + w) * qpt;
-      const int e_all = max(reach(rg, w), reach(rg, w ^ 1));
+      const int i0 = (rg * tiles + w) * qpt;
       const int ql = i0 + r / A.group;
       const bool valid = r < qpt * A.group && ql < S.nq;
       const int head = kvh * A.group + r % A.group;
       const long long tok = S.q0 + min(ql, S.nq - 1);        // a row without a token computes nothing
       const int hi = valid ? min(c1, attn_visible(A, S, ql)) : 0;
       const int all_see = i0 < S.nq ? min(c1, attn_visible(A, S, i0)) : 0;   // every row sees the keys before this
-      const int e = reach(rg, w);
       float qy = 0.f, qx = 0.f, slope = 0.f;
       if (DIST) {
         qy = -A.q_pos[tok * A.q_pos_row];
         qx = -A.q_pos[tok * A.q_pos_row + 1];
         slope = -A.slopes[head] * kLog2e;
       }
-      float m = -INFINITY, l = 0.f;
-      bool later = false;                      // a tile of this group came before
-      Walk k{c0 / kKeys, e, c1, false};
+      float m = -INFINITY, l = 0.f, late = 0.f;  // late: how far the maximum has passed m, if beyond the slack
+      bool begun = false, lagging = false;       // for the warp: all its rows have an m; some row's `late` is not 0
+      Walk k{c0 / kKeys, reach(rg, w), c1, g, false};
       k.settle(A, S, slots, all);
-      const bool any = k.live();
-      while (ok && k.live()) {
-        const int j0 = k.t * kKeys;
-        const bool edge = k.partial || j0 + kKeys > all_see;
-        const float* py = spos + tile * 2 * kKeys;
-        ++k.t;
-        k.settle(A, S, slots, all);
-        ok = wait(BAR_SFULL + w, s_ph);
-        if (DIST && ok) ok = wait(BAR_FULL + 2 * tile, k_ph);            // complete since before S
-        if (!ok) break;
-        tc_fence_after();
-        if (++tile == C::kSlots / 2) {
-          tile = 0;
-          k_ph ^= 1;
-        }
+      k.seek(A, S, slots, all, streams, stream);
+      const uint32_t n0 = n;
+      // Rows' maxima go up by `up`: O and the sum so far are scaled down, once the
+      // product before is done with O.
+      auto rise = [&](float up) -> bool {
+        if (n > n0) {
+          if (C::kS > 1 && !wait(done(n - 1), phase_s(n - 1))) return false;
+          tc_fence_after();
+          const float f = ex2(-up);
 #pragma unroll 1
-        for (int h = 0; h < 2; ++h) {
-          const float* pyh = py + h * kHalf;
-          bool slow = edge || __any_sync(0xFFFFFFFFu, valid && m == -INFINITY);
-          bool waited = !C::kOwnP || h == 1 || !later;
-          // The previous tile's products are done with P and O before either changes
-          // (with P over S they ended before this S was complete).
-          auto settled = [&]() -> bool {
-            if (waited) return true;
-            waited = true;
-            if (!wait(BAR_DONE + w, d_ph)) return false;
-            d_ph ^= 1;
-            tc_fence_after();
-            return true;
-          };
-          // Rows' maxima go up by `up`: what they have summed so far is scaled down.
-          auto rise = [&](float up) -> bool {
-            if (__any_sync(0xFFFFFFFFu, up > 0.f && l > 0.f)) {
-              if (h == 1) {                      // the first half's product into O
-                if (!wait(BAR_HALF + w, s_ph)) return false;
-                tc_fence_after();
-              }
-              const float f = l > 0.f ? ex2(-up) : 1.0f;
-#pragma unroll 1
-              for (int c = 0; c < DP; c += 32) {
-                float o[32];
-                tmem_ld32_issue(to + c, o);
-                tmem_ld_wait();
-                reg_fence32(o);
-#pragma unroll
-                for (int i = 0; i < 32; ++i) o[i] *= f;
-                tmem_st32(to + c, reinterpret_cast<const uint32_t*>(o));
-              }
-              l *= f;
-            }
-            return true;
-          };
-          bool again = !slow;
-          while (again) {
-            // One pass, with the maximum so far: z = score (log2 units) - m, p = exp2(z).
-            // Only afterwards is it seen whether a maximum had to move, and then the pass
-            // is repeated, or a score was too large for the polynomial (below).
-            const float m0 = m;
-            float2 x2[kHalf / 2];
-            float* x = reinterpret_cast<float*>(x2);
-            tmem_ld32_issue(ts + h * kHalf, x);
-            tmem_ld32_issue(ts + h * kHalf + 32, x + 32);
+          for (int c = 0; c < DP; c += 32) {
+            float o[32];
+            tmem_ld32_issue(to + c, o);
             tmem_ld_wait();
-            reg_fence32(x);
-            reg_fence32(x + 32);
-            float b0 = 0.f, b1 = 0.f, t0 = -INFINITY, t1 = -INFINITY;
+            reg_fence32(o);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) o[i] *= f;
+            tmem_st32(to + c, reinterpret_cast<const uint32_t*>(o));
+          }
+        }
+        return true;
+      };
+      while (k.live()) {
+        const int j0 = k.t * kKeys;
+        const bool edge = k.partial || j0 + kKeys > all_see, plain = begun && !edge;
+        const uint32_t s = chain * C::kS + (n & (C::kS - 1)), ts = ts0 + (n & (C::kS - 1)) * kKeys;
+        const float* py = spos + place(k.g) * 2 * kKeys;
+        if (!(ok = wait(C::SFULL + s, phase_s(n)))) break;
+        if (DIST && !(ok = wait(C::FULL + place(k.g), phase(k.g)))) break;     // complete since before S
+        tc_fence_after();
+        if (lagging) {
+          if (!(ok = rise(late))) break;
+          l *= ex2(-late);
+          m += late;
+          late = 0.f;
+          lagging = false;
+        }
+        k.next_own(A, S, slots, all, streams, stream);
+#pragma unroll 1
+        for (int h = 0; h < kKeys; h += C::kPart) {
+          constexpr int N = C::kPart;
+          const float* pyh = py + h;
+          bool slow = !plain;
+          if (plain) {
+            // one pass with the maximum as it is: z = score (log2 units) - m, p = exp2(z)
+            float2 x2[N / 2];
+            float* x = reinterpret_cast<float*>(x2);
+#pragma unroll
+            for (int c = 0; c < N; c += 32) tmem_ld32_issue(ts + h + c, x + c);
+            tmem_ld_wait();
+#pragma unroll
+            for (int c = 0; c < N; c += 32) reg_fence32(x + c);
+            float b0 = 0.f, t0 = -INFINITY, t1 = -INFINITY;
             float2 s0 = both(0.f), s1 = both(0.f);
-            uint32_t pk[kHalf / 2];
-            constexpr int G = DIST ? 4 : 8;      // pairs abreast: a multiply-add's latency is several issue slots
+            uint32_t pk[N / 2];
+            constexpr int G = DIST ? 4 : 8;      // pairs abreast
 #pragma unroll
-            for (int i = 0; i < kHalf / 2; i += G) {
-              float2 a[G];                       // what is added to the capped score
+            for (int ii = 0; ii < N / 2 + 2 * G; ii += G) {
+              // group ii's scores, the exponentials of the group before, and the sums
+              // and packing of the one before that: each waits on nothing recent
+              if (ii < N / 2) {
+                const int i = ii;
+                float2 a[G];                       // what is added to the capped score
 #pragma unroll
-              for (int g = 0; g < G; ++g) a[g] = both(-m0);
-              if (DIST) {
-                float2 y[G], d[G];
+                for (int u = 0; u < G; ++u) a[u] = both(-m);
+                if (DIST) {
+                  float2 y[G], d[G];
 #pragma unroll
-                for (int g = 0; g < G; g += 2) {
-                  const float4 ky = *reinterpret_cast<const float4*>(pyh + 2 * (i + g));
-                  const float4 kx = *reinterpret_cast<const float4*>(pyh + kKeys + 2 * (i + g));
-                  y[g] = make_float2(ky.x, ky.y);
-                  y[g + 1] = make_float2(ky.z, ky.w);
-                  d[g] = make_float2(kx.x, kx.y);
-                  d[g + 1] = make_float2(kx.z, kx.w);
+                  for (int u = 0; u < G; u += 2) {
+                    const float4 ky = *reinterpret_cast<const float4*>(pyh + 2 * (i + u));
+                    const float4 kx = *reinterpret_cast<const float4*>(pyh + kKeys + 2 * (i + u));
+                    y[u] = make_float2(ky.x, ky.y);
+                    y[u + 1] = make_float2(ky.z, ky.w);
+                    d[u] = make_float2(kx.x, kx.y);
+                    d[u + 1] = make_float2(kx.z, kx.w);
+                  }
+#pragma unroll
+                  for (int u = 0; u < G; ++u) {
+                    y[u] = add2(y[u], both(qy));
+                    d[u] = add2(d[u], both(qx));
+                  }
+#pragma unroll
+                  for (int u = 0; u < G; ++u)
+                    y[u] = make_float2(fabsf(y[u].x) + fabsf(d[u].x), fabsf(y[u].y) + fabsf(d[u].y));
+#pragma unroll
+                  for (int u = 0; u < G; ++u) a[u] = fma2(y[u], both(slope), a[u]);
                 }
+                if (!CAP) {
 #pragma unroll
-                for (int g = 0; g < G; ++g) {
-                  y[g] = add2(y[g], both(qy));
-                  d[g] = add2(d[g], both(qx));
+                  for (int u = 0; u < G; ++u) x2[i + u] = fma2(x2[i + u], both(A.scale_log2), a[u]);
+                } else {
+                  // an odd polynomial: |error| <= 1.5e-7 cap for |x| <= cap / 2
+                  float2 w2[G], p[G];
+#pragma unroll
+                  for (int u = 0; u < G; ++u) {
+                    b0 = fmaxf(b0, fmaxf(fabsf(x2[i + u].x), fabsf(x2[i + u].y)));
+                    w2[u] = mul2(x2[i + u], x2[i + u]);
+                  }
+#pragma unroll
+                  for (int u = 0; u < G; ++u) p[u] = fma2(w2[u], both(poly.c[3]), both(poly.c[2]));
+#pragma unroll
+                  for (int u = 0; u < G; ++u) p[u] = fma2(w2[u], p[u], both(poly.c[1]));
+#pragma unroll
+                  for (int u = 0; u < G; ++u) p[u] = fma2(w2[u], p[u], both(poly.c[0]));
+#pragma unroll
+                  for (int u = 0; u < G; ++u) x2[i + u] = fma2(x2[i + u], p[u], a[u]);
                 }
-#pragma unroll
-                for (int g = 0; g < G; ++g)
-                  y[g] = make_float2(fabsf(y[g].x) + fabsf(d[g].x), fabsf(y[g].y) + fabsf(d[g].y));
-#pragma unroll
-                for (int g = 0; g < G; ++g) a[g] = fma2(y[g], both(slope), a[g]);
               }
-              if (!CAP) {
+              if (ii >= G && ii < N / 2 + G) {
 #pragma unroll
-                for (int g = 0; g < G; ++g) x2[i + g] = fma2(x2[i + g], both(A.scale_log2), a[g]);
-              } else {
-                // an odd polynomial: |error| <= 1.5e-7 cap for |x| <= cap / 2
-                float2 w2[G], p[G];
-#pragma unroll
-                for (int g = 0; g < G; ++g) {
-                  b0 = fmaxf(b0, fmaxf(fabsf(x2[i + g].x), fabsf(x2[i + g].y)));
-                  w2[g] = mul2(x2[i + g], x2[i + g]);
+                for (int u = 0; u < G; ++u) {
+                  float2& z = x2[ii - G + u];
+                  (u & 1 ? t1 : t0) = fmaxf(u & 1 ? t1 : t0, fmaxf(z.x, z.y));
+                  z = make_float2(ex2(z.x), ex2(z.y));
                 }
-#pragma unroll
-                for (int g = 0; g < G; ++g) p[g] = fma2(w2[g], both(poly.c[3]), both(poly.c[2]));
-#pragma unroll
-                for (int g = 0; g < G; ++g) p[g] = fma2(w2[g], p[g], both(poly.c[1]));
-#pragma unroll
-                for (int g = 0; g < G; ++g) p[g] = fma2(w2[g], p[g], both(poly.c[0]));
-#pragma unroll
-                for (int g = 0; g < G; ++g) x2[i + g] = fma2(x2[i + g], p[g], a[g]);
               }
+              if (ii >= 2 * G) {
 #pragma unroll
-              for (int g = 0; g < G; g += 2) {
-                t0 = fmaxf(t0, fmaxf(x2[i + g].x, x2[i + g].y));
-                t1 = fmaxf(t1, fmaxf(x2[i + g + 1].x, x2[i + g + 1].y));
-                const float2 u = make_float2(ex2(x2[i + g].x), ex2(x2[i + g].y));
-                const float2 v = make_float2(ex2(x2[i + g + 1].x), ex2(x2[i + g + 1].y));
-                s0 = add2(s0, u);
-                s1 = add2(s1, v);
-                pk[i + g] = Store<T>::pack2(u.x, u.y);     // the probabilities as the product takes them
-                pk[i + g + 1] = Store<T>::pack2(v.x, v.y);
+                for (int u = 0; u < G; ++u) {
+                  const float2 z = x2[ii - 2 * G + u];
+                  if (u & 1) s1 = add2(s1, z);
+                  else s0 = add2(s0, z);
+                  pk[ii - 2 * G + u] = Store<T>::pack2(z.x, z.y);      // the probabilities as the product takes them
+                }
               }
             }
             const float top = fmaxf(t0, t1);
-            // without a distance bias a maximum hardly ever moves after the first tiles
-            slow = __any_sync(0xFFFFFFFFu, valid && ((CAP && !(fmaxf(b0, b1) * A.scale_log2 <= 0.5f)) ||
-                                                     (!DIST && top > kSlack)));
-            if (slow || !(ok = settled())) break;
-            again = DIST && __any_sync(0xFFFFFFFFu, valid && top > kSlack);
-            if (again) {
-              // one row has to move: all of the warp that can do
-              const float up = valid ? fmaxf(top, 0.f) : 0.f;
-              if (!(ok = rise(up))) break;
-              m += up;
-            } else {
-              if (C::kOwnP && h == 1) {          // S is done with: the next one may come
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&bar[BAR_SFREE + w]);
+            if (__any_sync(0xFFFFFFFFu, valid && ((CAP && !(b0 * A.scale_log2 <= 0.5f)) || top > kSlack))) {
+              // too large for the polynomial, or for P; or m lags behind from here on
+              slow = __any_sync(0xFFFFFFFFu, valid && ((CAP && !(b0 * A.scale_log2 <= 0.5f)) || top > kHard));
+              if (!slow) {
+                if (valid && top > kSlack) late = fmaxf(late, top);
+                lagging = true;
               }
+            }
+            if (!slow) {
               l += (s0.x + s0.y) + (s1.x + s1.y);
-              tmem_st32(tp + h * 32, pk);
+              if constexpr (N == 32) tmem_st16(ts + h / 2, pk);
+              else tmem_st32(ts + h / 2, pk);
             }
           }
-          if (!ok) break;
           if (slow) {
-            // In two passes over S, 32 keys at a time: scores with tanh itself, masked,
-            // put back into S with their maximum; then the probabilities.
-            const unsigned long long keep =
-                edge ? key_mask(A, S, slots, j0 + h * kHalf, hi) : ~0ull;
-            const float m0 = m == -INFINITY ? 0.f : m;
-            float top = -INFINITY;
+            // 32 keys at a time, with tanh itself, masks, and maxima that move at once
+            const unsigned long long keep = edge ? key_mask(A, S, slots, j0, hi) : ~0ull;
+            tmem_st_wait();                      // the first half's probabilities, should they be scaled
 #pragma unroll 1
-            for (int c = 0; c < kHalf; c += 32) {
+            for (int c = h; c < h + N; c += 32) {
+              const float m0 = m == -INFINITY ? 0.f : m;
               float y[32];
-              tmem_ld32_issue(ts + h * kHalf + c, y);
+              tmem_ld32_issue(ts + c, y);
               tmem_ld_wait();
               reg_fence32(y);
               const uint32_t bits = (uint32_t)(keep >> c);
+              float top = -INFINITY;
 #pragma unroll
               for (int i = 0; i < 32; ++i) {
                 y[i] *= A.scale_log2;
                 if (CAP) y[i] = A.cap_log2 * tanh_abs(y[i]);
-                if (DIST) y[i] = fmaf(fabsf(pyh[c + i] + qy) + fabsf(pyh[kKeys + c + i] + qx), slope, y[i]);
+                if (DIST) y[i] = fmaf(fabsf(py[c + i] + qy) + fabsf(py[kKeys + c + i] + qx), slope, y[i]);
                 y[i] = (bits >> i) & 1 ? y[i] - m0 : -INFINITY;
                 top = fmaxf(top, y[i]);
               }
-              tmem_st32(ts + h * kHalf + c, reinterpret_cast<const uint32_t*>(y));
-            }
-            tmem_st_wait();
-            if (!(ok = settled())) break;
-            // the maximum moves at once from nothing, later only past the slack
-            const bool move = m == -INFINITY ? top > -INFINITY : top > kSlack;
-            const float up = move ? top : 0.f;
-            if (!(ok = rise(m == -INFINITY ? 0.f : up))) break;
-            if (move) m = m0 + up;
+              // from nothing at once, later past the slack
+              const float up = (m == -INFINITY ? top > -INFINITY : top > kSlack) ? top : 0.f;
+              if (__any_sync(0xFFFFFFFFu, up != 0.f && l > 0.f)) {
+                const float f = l > 0.f ? up : 0.f;
+                if (!(ok = rise(f))) break;
+                l *= ex2(-f);
+                if (c > 0) {                     // this step's probabilities so far
+                  uint32_t u[16];
 #pragma unroll 1
-            for (int c = 0; c < kHalf; c += 32) {
-              float y[32];
-              tmem_ld32_issue(ts + h * kHalf + c, y);
-              tmem_ld_wait();
-              reg_fence32(y);
+                  for (int i = 0; i < c / 2; i += 16) {
+                    tmem_ld16_issue(ts + i, u);
+                    tmem_ld_wait();
+                    tmem_reg_fence(u);
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) {
+                      const float2 v = Store<T>::unpack2(u[j]);
+                      u[j] = Store<T>::pack2(v.x * ex2(-f), v.y * ex2(-f));
+                    }
+                    tmem_st16(ts + i, u);
+                  }
+                }
+              }
+              if (m != -INFINITY) {
+                m += up;
+                late = fmaxf(late - up, 0.f);
+              } else if (top > -INFINITY) {
+                m = up;
+              }
               uint32_t pk[16];
 #pragma unroll
               for (int i = 0; i < 32; i += 2) {
-                const float u = ex2(y[i] - up), v = ex2(y[i + 1] - up);
-                l += u + v;
-                pk[i / 2] = Store<T>::pack2(u, v);
+                const float v0 = ex2(y[i] - up), v1 = ex2(y[i + 1] - up);
+                l += v0 + v1;
+                pk[i / 2] = Store<T>::pack2(v0, v1);
               }
-              tmem_st16(tp + h * 32 + c / 2, pk);
+              tmem_st16(ts + c / 2, pk);
+              tmem_st_wait();
+              if (l != l && m == -INFINITY) m = 0.f;         // a NaN row never gets a maximum: it is done with
             }
-            if (l != l && m == -INFINITY) m = 0.f;         // a NaN row never gets a maximum: it is done with
-            if (C::kOwnP && h == 1) {
-              tc_fence_before();
-              __syncwarp();
-              if (lane == 0) mbar_arrive(&bar[BAR_SFREE + w]);
-            }
+            if (!ok) break;
+            begun = !__any_sync(0xFFFFFFFFu, valid && m == -INFINITY);
+            lagging = __any_sync(0xFFFFFFFFu, late > 0.f);
           }
-          tmem_st_wait();
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(&bar[BAR_PREADY + 2 * w + h]);
         }
         if (!ok) break;
-        s_ph ^= 1;
-        later = true;
+        tmem_st_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&bar[C::PREADY + s]);
+        ++n;
       }
       if (!ok) break;
-      // the tiles that only the other rows reach pass through the ring as well
-      for (k.end_key = e_all; k.live(); ++k.t, k.settle(A, S, slots, all))
-        if (++tile == C::kSlots / 2) {
-          tile = 0;
-          k_ph ^= 1;
+      // the steps of the whole group, for the next group's places
+      if (rg + A.row_groups < groups) {
+        Walk a{c0 / kKeys, reach_all(rg), c1, g, false};
+        for (a.settle(A, S, slots, all); a.live(); a.next(A, S, slots, all)) {
         }
+        g = a.g;
+      }
       // ---- out = O / l
       const long long R = tok * A.heads + head;
+      const bool any = n > n0;
       if (any) {
-        ok = wait(BAR_ODONE + w, o_ph);
-        o_ph ^= 1;
-        if (C::kOwnP && ok) {                    // the last tile's, so that none is left over
-          ok = wait(BAR_DONE + w, d_ph);
-          d_ph ^= 1;
-        }
-        if (!ok) break;
+        if (!(ok = C::kS > 1 ? wait(done(n - 1), phase_s(n - 1)) : wait(C::DONE + chain, ends & 1))) break;
+        ++ends;
         tc_fence_after();
       }
       const float inv = l > 0.f ? 1.0f / l : (l == 0.f ? 0.f : l);
-      const bool split = A.n_chunks > 1;
-      const long long at = (long long)chunk * A.n_q * A.heads + R;
+      const bool split = A.n_chunks * streams > 1;
+      const long long at = (long long)(chunk * streams + stream) * A.n_q * A.heads + R;
 #pragma unroll 1
       for (int c = 0; c < DP; c += 32) {
         float o[32];
@@ -801,9 +838,10 @@ __global__ void __launch_bounds__(kThreads, 1)
       __syncwarp();
     }
   }
+  __syncwarp();
   tc_fence_before();
   __syncthreads();
-  if (warp == 9) {
+  if (warp == 4 * C::kChains + 2) {
     tc_fence_after();
     tmem_dealloc(tmem, 512);
   }
@@ -825,7 +863,7 @@ cudaError_t launch_tc_t(const AttnArgs& a, const TcMaps& m, cudaStream_t st) {
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t lc = {};
   lc.gridDim = dim3((unsigned)((long long)a.n_seqs * a.kv_heads * a.n_chunks * a.row_groups));
-  lc.blockDim = dim3(kThreads);
+  lc.blockDim = dim3(TcCfg<DP>::kWarps * 32);
   lc.dynamicSmemBytes = TcCfg<DP>::kSmem;
   lc.stream = st;
   return cudaLaunchKernelEx(&lc, kern, a, m, poly);
@@ -833,8 +871,17 @@ cudaError_t launch_tc_t(const AttnArgs& a, const TcMaps& m, cudaStream_t st) {
 
 }  // namespace
 
-int attn_tc_unit() { return kKeys; }
-int attn_tc_tokens_per_block(int group) { return 2 * (128 / group); }
+// Streams: two chains share a tile where that leaves fewer of them idle (tiles in
+// all over chains at work: 300 rows are 3 tiles, so 3 blocks of half the steps
+// each instead of 2 of all).
+int attn_tc_streams(int dim, int group, int max_q) {
+  const long long tiles = (max_q + 128 / group - 1) / (128 / group);
+  return tiles % 2 ? 2 : 1;
+}
+int attn_tc_tokens_per_block(int dim, int group, int streams) {
+  return (dim <= 64 ? TcCfg<64>::kChains : TcCfg<128>::kChains) / streams * (128 / group);
+}
+int attn_tc_unit(int streams) { return kKeys * streams; }
 
 // cudaErrorNotSupported where the arrays cannot be described to the TMA unit
 // (a zero stride over more than one head or row, or one of 2^40 bytes or more).
