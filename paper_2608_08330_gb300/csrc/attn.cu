@@ -11,7 +11,10 @@
 namespace rtcc {
 namespace {
 
-constexpr int kTcRows = 64;
+// The tensor-core kernel takes over from this many (token, head) rows of a key head
+// on: 33 rows over 9 ragged histories of 5001 keys, heads of 80, take 24 us there
+// and 27 in blocks of 16 rows, 30 rows over 50,000 keys, heads of 64, 25 and 23.
+constexpr int kTcRows = 32;
 
 // Chunks of the span for the few-rows kernel, two blocks of which run on an SM.  A
 // block costs about kBegin to begin and end, and a step of its four warps (32 KB of
@@ -22,7 +25,7 @@ constexpr int kTcRows = 64;
 // against the last one's length; 61 sequences of up to 16,384 keys and 8 heads take
 // 310 us in 3 chunks, 287 in 5.
 long long rows_chunks(long long units, int n_seqs, long long steps, long long most, int sms) {
-  constexpr double kBegin = 7.0, kStep = 1.5;
+  constexpr double kBegin = 10.0, kStep = 1.5;
   const long long slots = 2LL * sms;
   long long best = 1;
   if (n_seqs > 1) {
@@ -105,10 +108,8 @@ extern "C" rtcc_status rtcc_memory_attention(const rtcc_attn_config* c, const vo
   if (misaligned(d_k_pos, 8)) return RTCC_E_ARG;
   if (c->n_q == 0 || c->n_seqs == 0) return RTCC_OK;
 
-  int dev = 0, sms = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess ||
-      cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
-    return RTCC_E_CUDA;
+  const int sms = sm_count();
+  if (sms < 1) return RTCC_E_CUDA;
   AttnArgs a{};
   a.q = d_q; a.k = d_k; a.v = d_v; a.out = d_out; a.lse = d_lse;
   a.q_offsets = d_q_offsets; a.k_begin = d_k_begin; a.k_end = d_k_end;

@@ -422,7 +422,8 @@ __global__ void __launch_bounds__(kJoinWarps * 32) k_attn_join(const __grid_cons
 template <typename T, int DP>
 cudaError_t launch_rows_t(const AttnArgs& a, cudaStream_t st) {
   using C = RowsCfg<DP>;
-  cudaError_t e = cudaFuncSetAttribute(k_attn_rows<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem);
+  static std::atomic<uint64_t> allowed{0};
+  const cudaError_t e = allow_smem(reinterpret_cast<const void*>(k_attn_rows<T, DP>), C::kSmem, &allowed);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t lc = {};
   lc.gridDim = dim3((unsigned)((long long)a.n_seqs * a.kv_heads * a.row_groups * a.n_chunks));

@@ -177,17 +177,25 @@ __device__ __forceinline__ float tanh_abs(float u) {
 __device__ __forceinline__ float2 both(float a) { return make_float2(a, a); }
 
 // A walk over the steps of a chunk that have a key in a present slot, and their
-// number.  Every role walks; which steps are skipped, and which are `partial` (some
-// key in an absent slot), depends on the chunk's end c1 alone, so all roles agree.
+// number, from the last key a row group reaches to the chunk's first: with a
+// distance bias the nearest keys of a causal row come last, so going back the
+// maxima are met first and hardly move.  Every role walks; which steps are skipped,
+// and which are `partial` (some key in an absent slot), depends on the chunk's end
+// c1 alone, so all roles agree.
 struct Walk {
-  int t, end_key, c1;                            // current step; steps that begin before end_key count
+  int t, t0, c1;                                 // current step, the chunk's first
   int g;                                         // steps since the block began
   bool partial;
-  __device__ __forceinline__ bool live() const { return t * kKeys < end_key; }
+  __device__ __forceinline__ Walk() {}
+  __device__ __forceinline__ Walk(int c0, int end_key, int c1_, int g_)
+      : t((end_key + kKeys - 1) / kKeys - 1), t0(c0 / kKeys), c1(c1_), g(g_), partial(false) {
+    if (end_key <= c0) t = t0 - 1;
+  }
+  __device__ __forceinline__ bool live() const { return t >= t0; }
   __device__ __forceinline__ void settle(const AttnArgs& A, const AttnSpan& S, unsigned long long slots, bool all) {
     partial = false;
     if (all) return;
-    for (; live(); ++t) {
+    for (; live(); --t) {
       const int r0 = S.kb + t * kKeys, r1 = S.kb + min(t * kKeys + kKeys, c1) - 1;
       const int s0 = slot_of(A, r0), s1 = slot_of(A, r1);
       const unsigned long long want = ~0ull >> (63 - (s1 - s0)), have = (slots >> s0) & want;
@@ -196,7 +204,7 @@ struct Walk {
     }
   }
   __device__ __forceinline__ void next(const AttnArgs& A, const AttnSpan& S, unsigned long long slots, bool all) {
-    ++t;
+    --t;
     ++g;
     settle(A, S, slots, all);
   }
@@ -208,7 +216,7 @@ struct Walk {
   __device__ __forceinline__ void next_own(const AttnArgs& A, const AttnSpan& S, unsigned long long slots, bool all,
                                            int streams, int stream) {
     if (all) {                                   // nothing to skip
-      t += streams;
+      t -= streams;
       g += streams;
       return;
     }
@@ -360,7 +368,7 @@ __global__ void __launch_bounds__(TcCfg<DP>::kWarps * 32, 1)
                         S.q0 + (rg * tiles + w) * qpt);
       }
       __syncwarp();
-      Walk k{c0 / kKeys, reach_all(rg), c1, g, false};
+      Walk k(c0, reach_all(rg), c1, g);
       for (k.settle(A, S, slots, all); k.live(); k.next(A, S, slots, all)) {
         const int p = place(k.g);
         float2 at[2];
@@ -395,7 +403,7 @@ __global__ void __launch_bounds__(TcCfg<DP>::kWarps * 32, 1)
     // ------------------------------------------ values, and zeroes at edges
     bool ok = true;
     int g = 0;
-    Walk last{};
+    Walk last;
     bool pending = false;
     auto patch = [&]() -> bool {                 // the step before, one behind the loads
       if (!pending || !patched(last)) return true;
@@ -413,7 +421,7 @@ __global__ void __launch_bounds__(TcCfg<DP>::kWarps * 32, 1)
       return true;
     };
     for (int rg = rg0; rg < groups && ok; rg += A.row_groups) {
-      Walk k{c0 / kKeys, reach_all(rg), c1, g, false};
+      Walk k(c0, reach_all(rg), c1, g);
       for (k.settle(A, S, slots, all); k.live(); k.next(A, S, slots, all)) {
         // with a ring of one stream's steps the patch of the step before must not
         // wait behind this step's slot
@@ -457,7 +465,7 @@ __global__ void __launch_bounds__(TcCfg<DP>::kWarps * 32, 1)
       for (int c = 0; c < kOwn; ++c) {
         const int stream = (first + c) & (streams - 1);
         e[c] = reach(rg, (first + c) / streams);
-        qk[c] = Walk{c0 / kKeys, end, c1, g, false};
+        qk[c] = Walk(c0, end, c1, g);
         qk[c].settle(A, S, slots, all);
         qk[c].seek(A, S, slots, all, streams, stream);
         pv[c] = qk[c];
@@ -517,7 +525,7 @@ __global__ void __launch_bounds__(TcCfg<DP>::kWarps * 32, 1)
         if (!more) break;
       }
       // the steps of the whole group, for the next group's places
-      Walk k{c0 / kKeys, end, c1, g, false};
+      Walk k(c0, end, c1, g);
       if (rg + A.row_groups < groups)
         for (k.settle(A, S, slots, all); k.live(); k.next(A, S, slots, all)) {
         }
@@ -564,9 +572,11 @@ __global__ void __launch_bounds__(TcCfg<DP>::kWarps * 32, 1)
       }
       float m = -INFINITY, l = 0.f, late = 0.f;  // late: how far the maximum has passed m, if beyond the slack
       bool begun = false, lagging = false;       // for the warp: all its rows have an m; some row's `late` is not 0
-      Walk k{c0 / kKeys, reach(rg, w), c1, g, false};
+      const int e = reach(rg, w);
+      Walk k(c0, reach_all(rg), c1, g);
       k.settle(A, S, slots, all);
       k.seek(A, S, slots, all, streams, stream);
+      while (k.live() && k.t * kKeys >= e) k.next_own(A, S, slots, all, streams, stream);   // other tiles' steps
       const uint32_t n0 = n;
       // Rows' maxima go up by `up`: O and the sum so far are scaled down, once the
       // product before is done with O.
@@ -782,7 +792,7 @@ __global__ void __launch_bounds__(TcCfg<DP>::kWarps * 32, 1)
       if (!ok) break;
       // the steps of the whole group, for the next group's places
       if (rg + A.row_groups < groups) {
-        Walk a{c0 / kKeys, reach_all(rg), c1, g, false};
+        Walk a(c0, reach_all(rg), c1, g);
         for (a.settle(A, S, slots, all); a.live(); a.next(A, S, slots, all)) {
         }
         g = a.g;
@@ -857,9 +867,11 @@ cudaError_t launch_tc_t(const AttnArgs& a, const TcMaps& m, cudaStream_t st) {
     double f = (double)a.cap_log2 * a.scale_log2;
     for (int i = 0; i < 4; ++i, f *= (double)a.scale_log2 * a.scale_log2) poly.c[i] = (float)(f * kTanh[i]);
   }
-  auto kern = a.cap_log2 > 0.f ? (a.slopes ? k_attn_tc<T, DP, true, true> : k_attn_tc<T, DP, true, false>)
-                               : (a.slopes ? k_attn_tc<T, DP, false, true> : k_attn_tc<T, DP, false, false>);
-  const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, TcCfg<DP>::kSmem);
+  const bool cap = a.cap_log2 > 0.f, dist = a.slopes != nullptr;
+  auto kern = cap ? (dist ? k_attn_tc<T, DP, true, true> : k_attn_tc<T, DP, true, false>)
+                  : (dist ? k_attn_tc<T, DP, false, true> : k_attn_tc<T, DP, false, false>);
+  static std::atomic<uint64_t> allowed[4];
+  const cudaError_t e = allow_smem(reinterpret_cast<const void*>(kern), TcCfg<DP>::kSmem, &allowed[2 * cap + dist]);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t lc = {};
   lc.gridDim = dim3((unsigned)((long long)a.n_seqs * a.kv_heads * a.n_chunks * a.row_groups));

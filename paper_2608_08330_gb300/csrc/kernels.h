@@ -5,6 +5,7 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
 #include <vector>
 
 #include "rtcc.h"
@@ -361,6 +362,11 @@ struct NmsArgs {
 size_t nms_mask_words(int max_boxes);
 cudaError_t launch_nms(const NmsArgs& a, cudaStream_t st);
 
+// SMs of the current device, 0 on an error (tokens.cu).
+int sm_count();
+// Let `kernel` use `bytes` of dynamic shared memory on the current device;
+// `devices` remembers where that is done already.
+cudaError_t allow_smem(const void* kernel, int bytes, std::atomic<uint64_t>* devices);
 // Attention over the token memory: few rows (attn_rows.cu), many (attn_tc.cu).
 struct AttnArgs;
 int attn_rows_unit(int dim);       // chunks of the span are multiples of this many keys

@@ -26,6 +26,8 @@
 //   of lanes.
 #include <math.h>
 
+#include <atomic>
+
 #include "common.cuh"
 #include "kernels.h"
 #include "rtcc.h"
@@ -341,14 +343,6 @@ __global__ void __launch_bounds__(kPrepThreads, 6) k_qkv_prepare(const __grid_co
 bool misaligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
 bool bad_stride(int64_t s) { return s < 0 || s % 8 != 0; }
 
-int sm_count() {
-  int dev = 0, sms = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess ||
-      cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
-    return 0;
-  return sms;
-}
-
 template <typename T, int LP>
 cudaError_t launch_prepare_t(const PrepArgs& a, int turn, const cudaLaunchConfig_t& lc) {
   switch (turn) {
@@ -367,7 +361,31 @@ cudaError_t launch_prepare(const PrepArgs& a, int lp, int turn, const cudaLaunch
   return launch_prepare_t<T, 16>(a, turn, lc);
 }
 
+constexpr int kMaxDevices = 64;
+std::atomic<int> g_sms[kMaxDevices];             // 0: not asked yet
+
 }  // namespace
+
+int sm_count() {
+  int dev = 0, n = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return 0;
+  n = g_sms[dev].load(std::memory_order_relaxed);
+  if (n == 0 && cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess)
+    g_sms[dev].store(n, std::memory_order_relaxed);
+  return n;
+}
+
+cudaError_t allow_smem(const void* kernel, int bytes, std::atomic<uint64_t>* devices) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  const uint64_t bit = 1ull << (dev & 63);
+  if (dev < 64 && (devices->load(std::memory_order_relaxed) & bit)) return cudaSuccess;
+  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == cudaSuccess && dev < 64) devices->fetch_or(bit, std::memory_order_relaxed);
+  return e;
+}
+
 }  // namespace rtcc
 
 using namespace rtcc;
@@ -395,9 +413,9 @@ extern "C" rtcc_status rtcc_memory_append(int32_t n_seqs, int32_t capacity, int3
   if (blocks > sms) blocks = sms;
   if (blocks < 1) blocks = 1;
   const size_t smem = sizeof(int) * ((size_t)n_seqs + 1);
-  if (smem > 48 * 1024 &&
-      cudaFuncSetAttribute(k_memory_append, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                           (int)(sizeof(int) * (kMaxSeqs + 1))) != cudaSuccess)
+  static std::atomic<uint64_t> allowed{0};
+  if (smem > 48 * 1024 && allow_smem(reinterpret_cast<const void*>(k_memory_append), (int)(sizeof(int) * (kMaxSeqs + 1)),
+                                     &allowed) != cudaSuccess)
     return RTCC_E_CUDA;
   cudaLaunchConfig_t lc = {};
   lc.gridDim = dim3((unsigned)blocks);

@@ -10,6 +10,7 @@ from __future__ import annotations
 import ctypes as C
 import math
 import os
+import struct
 from typing import Optional
 
 import numpy as np
@@ -97,6 +98,11 @@ class rtcc_attn_config(C.Structure):
         ("scale", C.c_float), ("cap", C.c_float),
     ]
 
+
+# the two structs' fields in order, packed in one go (field by field takes twice as long)
+_PREPARE = struct.Struct("=6i12q3i2i2f4x")
+_ATTN = struct.Struct("=6i8q7i2f4x")
+assert _PREPARE.size == C.sizeof(rtcc_prepare_config) and _ATTN.size == C.sizeof(rtcc_attn_config)
 
 BOX_DTYPE = np.dtype([("x", "<f4"), ("y", "<f4"), ("z", "<f4"), ("l", "<f4"), ("w", "<f4"),
                       ("h", "<f4"), ("yaw", "<f4"), ("score", "<f4"), ("anchor", "<i4")])
@@ -460,8 +466,9 @@ def prepare_config(heads: int, kv_heads: int, head_dim: int, dtype: int, n_token
                    norm: bool = True, theta: float = 10000.0, eps: float = 1e-6) -> rtcc_prepare_config:
     """Shapes of rtcc_qkv_prepare; q .. v_mem are the arrays' (row, head)
     strides in elements, axis_pairs the pairs of (t, y, x)."""
-    return rtcc_prepare_config(heads, kv_heads, head_dim, dtype, n_tokens, n_rows, *q, *k, *v, *q_out,
-                               *k_mem, *v_mem, tuple(axis_pairs), interleaved, norm, theta, eps)
+    return rtcc_prepare_config.from_buffer_copy(_PREPARE.pack(
+        heads, kv_heads, head_dim, dtype, n_tokens, n_rows, *q, *k, *v, *q_out, *k_mem, *v_mem, *axis_pairs,
+        interleaved, norm, theta, eps))
 
 
 def rtcc_qkv_prepare(cfg: rtcc_prepare_config, d_q, d_k, d_v, d_q_gain, d_k_gain, d_pos, d_rows,
@@ -477,9 +484,9 @@ def attn_config(heads: int, kv_heads: int, head_dim: int, dtype: int, n_q: int, 
                 cap: float = 0.0) -> rtcc_attn_config:
     """Shapes of rtcc_memory_attention; q .. out are the arrays' (row, head)
     strides in elements; scale None = 1 / sqrt(head_dim)."""
-    return rtcc_attn_config(heads, kv_heads, head_dim, dtype, n_q, n_rows, *q, *k, *v, *out, n_seqs, max_q,
-                            max_k, causal, n_slots, slot_rows, q_pos_row,
-                            head_dim ** -0.5 if scale is None else scale, cap)
+    return rtcc_attn_config.from_buffer_copy(_ATTN.pack(
+        heads, kv_heads, head_dim, dtype, n_q, n_rows, *q, *k, *v, *out, n_seqs, max_q, max_k, causal, n_slots,
+        slot_rows, q_pos_row, head_dim ** -0.5 if scale is None else scale, cap))
 
 
 def rtcc_memory_attention(cfg: rtcc_attn_config, d_q, d_k, d_v, d_q_offsets, d_k_begin, d_k_end, d_prefix,
