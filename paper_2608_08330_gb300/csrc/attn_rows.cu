@@ -72,6 +72,14 @@ __device__ __forceinline__ void mma16816<__nv_bfloat16>(float (&d)[4], const uin
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
+// Two floats as hi + lo of the storage type.
+template <typename T>
+__device__ __forceinline__ void split2(float a, float b, uint32_t& hi, uint32_t& lo) {
+  hi = Store<T>::pack2(a, b);
+  const float2 h = Store<T>::unpack2(hi);
+  lo = Store<T>::pack2(a - h.x, b - h.y);
+}
+
 // tanh(u) = 1 - 2 / (1 + e^2u): its absolute error (about 2e-7) is what counts
 // here, since the cap multiplies it into a score.
 __device__ __forceinline__ float tanh_abs(float u) {
@@ -257,17 +265,21 @@ __global__ void __launch_bounds__(kWarps * 32, 2) k_attn_rows(const __grid_const
           }
 #pragma unroll
         for (int kk = 0; kk < KT / 16; ++kk) {
-          uint32_t pa[4];                        // probabilities rounded to the storage type for the product
-          pa[0] = Store<T>::pack2(s[2 * kk][0], s[2 * kk][1]);
-          pa[1] = Store<T>::pack2(s[2 * kk][2], s[2 * kk][3]);
-          pa[2] = Store<T>::pack2(s[2 * kk + 1][0], s[2 * kk + 1][1]);
-          pa[3] = Store<T>::pack2(s[2 * kk + 1][2], s[2 * kk + 1][3]);
+          // probabilities as two terms of the storage type, so that their rounding
+          // (2^-22 or 2^-16) adds nothing to the result's; the memory leaves time for it
+          uint32_t pa[4], pl[4];
+          split2<T>(s[2 * kk][0], s[2 * kk][1], pa[0], pl[0]);
+          split2<T>(s[2 * kk][2], s[2 * kk][3], pa[1], pl[1]);
+          split2<T>(s[2 * kk + 1][0], s[2 * kk + 1][1], pa[2], pl[2]);
+          split2<T>(s[2 * kk + 1][2], s[2 * kk + 1][3], pa[3], pl[3]);
 #pragma unroll
           for (int n = 0; n < DP / 16; ++n) {
             uint32_t vb[4];
             ldm4t(vs + tile_off<DP>(kk * 16 + (lane & 15), n * 2 + (lane >> 4)), vb);
             mma16816<T>(o[2 * n], pa, vb[0], vb[1]);
             mma16816<T>(o[2 * n + 1], pa, vb[2], vb[3]);
+            mma16816<T>(o[2 * n], pl, vb[0], vb[1]);
+            mma16816<T>(o[2 * n + 1], pl, vb[2], vb[3]);
           }
         }
       }

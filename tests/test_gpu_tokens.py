@@ -568,3 +568,37 @@ def test_append_prepare_attend_step_by_step(R):
             v = xs[:, heads + kv + h // 2]
             lim = (2 * 2.0 ** -11 + 2 * (2 * 2.0 ** -11 * 8)) * (p @ np.abs(v)) + 1e-6
             assert (np.abs(got[:, h] - p @ v) <= lim).all()
+
+
+def test_token_fusion_of_a_frame(R):
+    """The example's whole path on a small frame, against the formula in float64
+    on the frame's own feature maps.  q and k carry one rounding each (u relative
+    of every product: 2 u of a score's largest magnitude, sqrt(dim) after the
+    norm), besides the attention's own errors."""
+    from paper_2608_08330_gb300 import token_fusion as F
+    for absent in ((), (1,)):
+        cfg, maps = F.frame_maps("tiny", 3, absent)
+        cell = cfg.pillar * cfg.feat_stride
+        out, lse = F.fuse(maps, cfg.dtype, cfg.feat_h, cfg.feat_w, cell)
+        cells, (heads, dim) = cfg.feat_h * cfg.feat_w, F.head_layout(cfg.feat_ch)
+        kw = dict(axis_pairs=F.axis_pairs(dim), interleaved=False, norm=True, theta=F.THETA, eps=F.EPS)
+        x = [U.u16_to_f64(m, cfg.dtype).reshape(cells, heads, dim) for m in maps if m is not None]
+        pos = [F.positions(k, cfg.feat_h, cfg.feat_w, cell) for k, m in enumerate(maps) if m is not None]
+        q = turn_reference(x[0], None, pos[0], **kw)[0]
+        k = np.concatenate([turn_reference(a, None, p, **kw)[0] for a, p in zip(x, pos)])
+        v, yx = np.concatenate(x), np.concatenate(pos)[:, 1:].astype(np.float64)
+        u = ROUND[cfg.dtype]
+        for i in np.linspace(0, cells - 1, 40).astype(int):
+            for h in range(heads):
+                s = k[:, h] @ q[i, h] / math.sqrt(dim)
+                s = F.CAP * np.tanh(s / F.CAP) - float(F.slopes(heads)[h]) * np.abs(yx - yx[i]).sum(1)
+                p = np.exp(s - s.max())
+                want, A = p @ v[:, h] / p.sum(), p @ np.abs(v[:, h]) / p.sum()
+                d = 2 * u * math.sqrt(dim)
+                assert (np.abs(f64(out[i, h]) - want) <= (2 * u + 2 * d) * A + 1e-6).all()
+                assert abs(float(lse[i, h]) - (np.log(p.sum()) + s.max())) <= d + 1e-5
+
+
+def test_attention_status_is_clean(R):
+    Case([300], [500], heads=2, kv=2).run(R).check()
+    assert R.rtcc_memory_attention_status() == R.OK
