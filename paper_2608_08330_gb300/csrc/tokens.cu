@@ -220,16 +220,31 @@ __global__ void __launch_bounds__(kPrepThreads, 6) k_qkv_prepare(const __grid_co
   constexpr int P = TURN == kTurnInterleaved ? 2 : 4;
   float2 cs[P], sn[P];
   const bool low = e0 < A.n_rot, in_rot = e0 < 2 * A.n_rot;
-  if (TURN != kTurnNone && kp > 0) {
+  auto angle = [&](int m) -> float2 {            // pair m's cosine and sine
+    if (m >= A.n_rot) return make_float2(1.0f, 0.0f);
+    return cos_sin(m < A.end_t ? pos[0] : m < A.end_y ? pos[1] : pos[2], turn[m]);
+  };
+  if (TURN == kTurnLanes && kp > 0) {
+    // the partner's lane has the same eight pairs: four each, and an exchange
+    const int from = lane + (low ? A.n_rot / 8 : -(A.n_rot / 8)), base = low ? e0 : e0 - A.n_rot + 4;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 own = angle(in_rot ? base + i : A.n_rot);
+      const float ox = __shfl_sync(0xFFFFFFFFu, own.x, from, LP), oy = __shfl_sync(0xFFFFFFFFu, own.y, from, LP);
+      const float2 c0 = low ? own : make_float2(ox, oy), c1 = low ? make_float2(ox, oy) : own;   // pairs i, i + 4
+      const float sign = low ? -1.0f : 1.0f;
+      (i & 1 ? cs[i / 2].y : cs[i / 2].x) = in_rot ? c0.x : 1.0f;
+      (i & 1 ? cs[i / 2 + 2].y : cs[i / 2 + 2].x) = in_rot ? c1.x : 1.0f;
+      (i & 1 ? sn[i / 2].y : sn[i / 2].x) = in_rot ? sign * c0.y : 0.0f;
+      (i & 1 ? sn[i / 2 + 2].y : sn[i / 2 + 2].x) = in_rot ? sign * c1.y : 0.0f;
+    }
+  } else if (TURN != kTurnNone && kp > 0) {
 #pragma unroll
     for (int i = 0; i < 2 * P; ++i) {
       const int e = e0 + i;
-      const int m = TURN == kTurnInterleaved ? e0 / 2 + i : e < A.n_rot ? e : e - A.n_rot;
-      float2 c = make_float2(1.0f, 0.0f);
-      if (m < A.n_rot) c = cos_sin(m < A.end_t ? pos[0] : m < A.end_y ? pos[1] : pos[2], turn[m]);
-      if (TURN != kTurnInterleaved && e < A.n_rot) c.y = -c.y;
+      const float2 c = angle(TURN == kTurnInterleaved ? e0 / 2 + i : e < A.n_rot ? e : e - A.n_rot);
       (i & 1 ? cs[i / 2].y : cs[i / 2].x) = c.x;
-      (i & 1 ? sn[i / 2].y : sn[i / 2].x) = c.y;
+      (i & 1 ? sn[i / 2].y : sn[i / 2].x) = TURN != kTurnInterleaved && e < A.n_rot ? -c.y : c.y;
     }
   }
   const float inv_dim = 1.0f / A.dim;
@@ -490,7 +505,8 @@ extern "C" rtcc_status rtcc_qkv_prepare(const rtcc_prepare_config* c, const void
   const int turn = pairs == 0 ? kTurnNone : c->interleaved ? kTurnInterleaved
                    : pairs % 8 == 0 ? kTurnLanes : kTurnAny;
   // a token's heads stay together unless that leaves threads for less than half
-  // of what the GPU holds (1024 a SM)
+  // of what the GPU holds (1024 a SM; twice and four times that many took up to
+  // 13 and 40 % longer on 3000 to 20,000 tokens)
   const int heads = a.n_qh + a.n_kh + a.n_vh;
   const long long threads = (long long)a.n_tokens * lp;
   long long parts = (512LL * sms + threads - 1) / threads;
