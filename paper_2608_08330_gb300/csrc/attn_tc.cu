@@ -291,6 +291,7 @@ __global__ void __launch_bounds__(TcCfg<DP>::kWarps * 32, 1)
         if (i < C::FREE) n = 2;                                                              // keys and values
         if (i >= C::FREE && i < C::VOK) n = tiles;                                           // the chains of a stream
         if (i >= C::PREADY && i < C::DONE) n = 4;                                            // a chain's softmax warps
+        if (DIST && i >= C::SFULL && i < C::PREADY) n = 2;                                   // S, and its coordinates
         if (i == C::QFREE) n = 2;                                                            // the product warps
         mbar_init(&bar[i], n);
       }
@@ -483,6 +484,8 @@ __global__ void __launch_bounds__(TcCfg<DP>::kWarps * 32, 1)
           for (int i = 0; i < C::NC; ++i)
             umma4_ss(tmem + s * kKeys, q + i * kQBoxUnits, kd + i * kBoxUnits, id_s, i > 0);
           umma_commit_elected(&bar[C::SFULL + s]);
+          // this warp has seen the step's coordinates: its arrival passes them on
+          if (DIST && lane == 0) mbar_arrive(&bar[C::SFULL + s]);
           ++n_qk[c];
         }
         qk[c].next_own(A, S, slots, all, streams, chain & (streams - 1));
@@ -604,7 +607,6 @@ __global__ void __launch_bounds__(TcCfg<DP>::kWarps * 32, 1)
         const uint32_t s = chain * C::kS + (n & (C::kS - 1)), ts = ts0 + (n & (C::kS - 1)) * kKeys;
         const float* py = spos + place(k.g) * 2 * kKeys;
         if (!(ok = wait(C::SFULL + s, phase_s(n)))) break;
-        if (DIST && !(ok = wait(C::FULL + place(k.g), phase(k.g)))) break;     // complete since before S
         tc_fence_after();
         if (lagging) {
           if (!(ok = rise(late))) break;
