@@ -51,7 +51,6 @@ template <int DP> struct TcCfg {
   static constexpr int kChains = 2;
   static constexpr int kS = 2;    // S per chain
   static constexpr int kRing = DP == 64 ? 8 : 4; // steps of keys and of values in shared memory
-  static constexpr int kPart = 64;           // scores a thread takes at a time
   static constexpr int kStep = NC * kBox;
   static constexpr int kQ = kChains * NC * kQBox;
   static constexpr int kPos = kRing * 2 * kKeys * 4;         // [step in the ring][y | x][64]
@@ -601,44 +600,55 @@ __global__ void __launch_bounds__(TcCfg<DP>::kWarps * 32, 1)
         }
         return true;
       };
-      while (k.live()) {
-        const int j0 = k.t * kKeys;
-        const bool edge = k.partial || j0 + kKeys > all_see, plain = begun && !edge;
-        const uint32_t s = chain * C::kS + (n & (C::kS - 1)), ts = ts0 + (n & (C::kS - 1)) * kKeys;
-        const float* py = spos + place(k.g) * 2 * kKeys;
-        if (!(ok = wait(C::SFULL + s, phase_s(n)))) break;
+      // S of the next step is there; maxima that lag behind are raised first
+      auto begin = [&]() -> bool {
+        if (!wait(C::SFULL + chain * C::kS + (n & (C::kS - 1)), phase_s(n))) return false;
         tc_fence_after();
         if (lagging) {
-          if (!(ok = rise(late))) break;
+          if (!rise(late)) return false;
           l *= ex2(-late);
           m += late;
           late = 0.f;
           lagging = false;
         }
+        return true;
+      };
+      // P of the step is complete
+      auto publish = [&]() {
+        tmem_st_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&bar[C::PREADY + chain * C::kS + (n & (C::kS - 1))]);
+        ++n;
         k.next_own(A, S, slots, all, streams, stream);
-#pragma unroll 1
-        for (int h = 0; h < kKeys; h += C::kPart) {
-          constexpr int N = C::kPart;
-          const float* pyh = py + h;
-          bool slow = !plain;
-          if (plain) {
+      };
+      while (k.live()) {
+        const bool edge = k.partial || k.t * kKeys + kKeys > all_see;
+        if (begun && !edge) {
+          // going back, no further step is at the edge unless a slot is absent
+          int run = all ? (k.t - k.t0) / streams + 1 : 1;
+          bool slow = false;
+          do {
+            const uint32_t ts = ts0 + (n & (C::kS - 1)) * kKeys;
+            const float* py = spos + place(k.g) * 2 * kKeys;
+            if (!(ok = begin())) break;
             // one pass with the maximum as it is: z = score (log2 units) - m, p = exp2(z)
-            float2 x2[N / 2];
+            float2 x2[kKeys / 2];
             float* x = reinterpret_cast<float*>(x2);
 #pragma unroll
-            for (int c = 0; c < N; c += 32) tmem_ld32_issue(ts + h + c, x + c);
+            for (int c = 0; c < kKeys; c += 32) tmem_ld32_issue(ts + c, x + c);
             tmem_ld_wait();
 #pragma unroll
-            for (int c = 0; c < N; c += 32) reg_fence32(x + c);
+            for (int c = 0; c < kKeys; c += 32) reg_fence32(x + c);
             float b0 = 0.f, t0 = -INFINITY, t1 = -INFINITY;
             float2 s0 = both(0.f), s1 = both(0.f);
-            uint32_t pk[N / 2];
+            uint32_t pk[kKeys / 2];
             constexpr int G = DIST ? 4 : 8;      // pairs abreast
 #pragma unroll
-            for (int ii = 0; ii < N / 2 + 2 * G; ii += G) {
+            for (int ii = 0; ii < kKeys / 2 + 2 * G; ii += G) {
               // group ii's scores, the exponentials of the group before, and the sums
               // and packing of the one before that: each waits on nothing recent
-              if (ii < N / 2) {
+              if (ii < kKeys / 2) {
                 const int i = ii;
                 float2 a[G];                       // what is added to the capped score
 #pragma unroll
@@ -647,8 +657,8 @@ __global__ void __launch_bounds__(TcCfg<DP>::kWarps * 32, 1)
                   float2 y[G], d[G];
 #pragma unroll
                   for (int u = 0; u < G; u += 2) {
-                    const float4 ky = *reinterpret_cast<const float4*>(pyh + 2 * (i + u));
-                    const float4 kx = *reinterpret_cast<const float4*>(pyh + kKeys + 2 * (i + u));
+                    const float4 ky = *reinterpret_cast<const float4*>(py + 2 * (i + u));
+                    const float4 kx = *reinterpret_cast<const float4*>(py + kKeys + 2 * (i + u));
                     y[u] = make_float2(ky.x, ky.y);
                     y[u + 1] = make_float2(ky.z, ky.w);
                     d[u] = make_float2(kx.x, kx.y);
@@ -686,7 +696,7 @@ __global__ void __launch_bounds__(TcCfg<DP>::kWarps * 32, 1)
                   for (int u = 0; u < G; ++u) x2[i + u] = fma2(x2[i + u], p[u], a[u]);
                 }
               }
-              if (ii >= G && ii < N / 2 + G) {
+              if (ii >= G && ii < kKeys / 2 + G) {
 #pragma unroll
                 for (int u = 0; u < G; ++u) {
                   float2& z = x2[ii - G + u];
@@ -708,88 +718,83 @@ __global__ void __launch_bounds__(TcCfg<DP>::kWarps * 32, 1)
             if (__any_sync(0xFFFFFFFFu, valid && ((CAP && !(b0 * A.scale_log2 <= 0.5f)) || top > kSlack))) {
               // too large for the polynomial, or for P; or m lags behind from here on
               slow = __any_sync(0xFFFFFFFFu, valid && ((CAP && !(b0 * A.scale_log2 <= 0.5f)) || top > kHard));
-              if (!slow) {
-                if (valid && top > kSlack) late = fmaxf(late, top);
-                lagging = true;
-              }
+              if (slow) break;
+              if (valid && top > kSlack) late = fmaxf(late, top);
+              lagging = true;
             }
-            if (!slow) {
-              l += (s0.x + s0.y) + (s1.x + s1.y);
-              if constexpr (N == 32) tmem_st16(ts + h / 2, pk);
-              else tmem_st32(ts + h / 2, pk);
-            }
+            l += (s0.x + s0.y) + (s1.x + s1.y);
+            tmem_st32(ts, pk);
+            publish();
+          } while (--run > 0);
+          if (!ok) break;
+          if (!slow) continue;
+        } else if (!(ok = begin())) {
+          break;
+        }
+        const uint32_t ts = ts0 + (n & (C::kS - 1)) * kKeys;
+        const float* py = spos + place(k.g) * 2 * kKeys;
+        // 32 keys at a time, with tanh itself, masks, and maxima that move at once
+        const unsigned long long keep = edge ? key_mask(A, S, slots, k.t * kKeys, hi) : ~0ull;
+#pragma unroll 1
+        for (int c = 0; c < kKeys; c += 32) {
+          const float m0 = m == -INFINITY ? 0.f : m;
+          float y[32];
+          tmem_ld32_issue(ts + c, y);
+          tmem_ld_wait();
+          reg_fence32(y);
+          const uint32_t bits = (uint32_t)(keep >> c);
+          float top = -INFINITY;
+#pragma unroll
+          for (int i = 0; i < 32; ++i) {
+            y[i] *= A.scale_log2;
+            if (CAP) y[i] = A.cap_log2 * tanh_abs(y[i]);
+            if (DIST) y[i] = fmaf(fabsf(py[c + i] + qy) + fabsf(py[kKeys + c + i] + qx), slope, y[i]);
+            y[i] = (bits >> i) & 1 ? y[i] - m0 : -INFINITY;
+            top = fmaxf(top, y[i]);
           }
-          if (slow) {
-            // 32 keys at a time, with tanh itself, masks, and maxima that move at once
-            const unsigned long long keep = edge ? key_mask(A, S, slots, j0, hi) : ~0ull;
-            tmem_st_wait();                      // the first half's probabilities, should they be scaled
+          // from nothing at once, later past the slack
+          const float up = (m == -INFINITY ? top > -INFINITY : top > kSlack) ? top : 0.f;
+          if (__any_sync(0xFFFFFFFFu, up != 0.f && l > 0.f)) {
+            const float f = l > 0.f ? up : 0.f;
+            if (!(ok = rise(f))) break;
+            l *= ex2(-f);
+            if (c > 0) {                     // this step's probabilities so far
+              uint32_t u[16];
 #pragma unroll 1
-            for (int c = h; c < h + N; c += 32) {
-              const float m0 = m == -INFINITY ? 0.f : m;
-              float y[32];
-              tmem_ld32_issue(ts + c, y);
-              tmem_ld_wait();
-              reg_fence32(y);
-              const uint32_t bits = (uint32_t)(keep >> c);
-              float top = -INFINITY;
+              for (int i = 0; i < c / 2; i += 16) {
+                tmem_ld16_issue(ts + i, u);
+                tmem_ld_wait();
+                tmem_reg_fence(u);
 #pragma unroll
-              for (int i = 0; i < 32; ++i) {
-                y[i] *= A.scale_log2;
-                if (CAP) y[i] = A.cap_log2 * tanh_abs(y[i]);
-                if (DIST) y[i] = fmaf(fabsf(py[c + i] + qy) + fabsf(py[kKeys + c + i] + qx), slope, y[i]);
-                y[i] = (bits >> i) & 1 ? y[i] - m0 : -INFINITY;
-                top = fmaxf(top, y[i]);
-              }
-              // from nothing at once, later past the slack
-              const float up = (m == -INFINITY ? top > -INFINITY : top > kSlack) ? top : 0.f;
-              if (__any_sync(0xFFFFFFFFu, up != 0.f && l > 0.f)) {
-                const float f = l > 0.f ? up : 0.f;
-                if (!(ok = rise(f))) break;
-                l *= ex2(-f);
-                if (c > 0) {                     // this step's probabilities so far
-                  uint32_t u[16];
-#pragma unroll 1
-                  for (int i = 0; i < c / 2; i += 16) {
-                    tmem_ld16_issue(ts + i, u);
-                    tmem_ld_wait();
-                    tmem_reg_fence(u);
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) {
-                      const float2 v = Store<T>::unpack2(u[j]);
-                      u[j] = Store<T>::pack2(v.x * ex2(-f), v.y * ex2(-f));
-                    }
-                    tmem_st16(ts + i, u);
-                  }
+                for (int j = 0; j < 16; ++j) {
+                  const float2 v = Store<T>::unpack2(u[j]);
+                  u[j] = Store<T>::pack2(v.x * ex2(-f), v.y * ex2(-f));
                 }
+                tmem_st16(ts + i, u);
               }
-              if (m != -INFINITY) {
-                m += up;
-                late = fmaxf(late - up, 0.f);
-              } else if (top > -INFINITY) {
-                m = up;
-              }
-              uint32_t pk[16];
-#pragma unroll
-              for (int i = 0; i < 32; i += 2) {
-                const float v0 = ex2(y[i] - up), v1 = ex2(y[i + 1] - up);
-                l += v0 + v1;
-                pk[i / 2] = Store<T>::pack2(v0, v1);
-              }
-              tmem_st16(ts + c / 2, pk);
-              tmem_st_wait();
-              if (l != l && m == -INFINITY) m = 0.f;         // a NaN row never gets a maximum: it is done with
             }
-            if (!ok) break;
-            begun = !__any_sync(0xFFFFFFFFu, valid && m == -INFINITY);
-            lagging = __any_sync(0xFFFFFFFFu, late > 0.f);
           }
+          if (m != -INFINITY) {
+            m += up;
+            late = fmaxf(late - up, 0.f);
+          } else if (top > -INFINITY) {
+            m = up;
+          }
+          uint32_t pk[16];
+#pragma unroll
+          for (int i = 0; i < 32; i += 2) {
+            const float v0 = ex2(y[i] - up), v1 = ex2(y[i + 1] - up);
+            l += v0 + v1;
+            pk[i / 2] = Store<T>::pack2(v0, v1);
+          }
+          tmem_st16(ts + c / 2, pk);
+          tmem_st_wait();
+          if (l != l && m == -INFINITY) m = 0.f;         // a NaN row never gets a maximum: it is done with
         }
         if (!ok) break;
-        tmem_st_wait();
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&bar[C::PREADY + s]);
-        ++n;
+        begun = !__any_sync(0xFFFFFFFFu, valid && m == -INFINITY);
+        lagging = __any_sync(0xFFFFFFFFu, late > 0.f);
+        publish();
       }
       if (!ok) break;
       // the steps of the whole group, for the next group's places
