@@ -141,10 +141,10 @@ extern "C" rtcc_status rtcc_memory_attention(const rtcc_attn_config* c, const vo
   const size_t part = (size_t)c->n_q * c->heads * (c->head_dim * sizeof(float) + sizeof(float2));
   const long long room = d_workspace ? (long long)(workspace_bytes / part) : 0;
   for (;; tc = false) {
-    a.streams = tc ? attn_tc_streams(c->head_dim, a.group, max_q) : 1;
+    a.streams = tc ? attn_tc_streams(a.group, max_q) : 1;
     if (a.streams > room) a.streams = 1;
     a.unit = tc ? attn_tc_unit(a.streams) : attn_rows_unit(c->head_dim);
-    const long long step = tc ? attn_tc_tokens_per_block(c->head_dim, a.group, a.streams) : 1;
+    const long long step = tc ? attn_tc_tokens_per_block(a.group, a.streams) : 1;
     long long groups = tc ? (max_q + step - 1) / step
                           : ((long long)max_q * a.group + attn_rows_per_block() - 1) / attn_rows_per_block();
     long long units = (long long)c->n_seqs * a.kv_heads;

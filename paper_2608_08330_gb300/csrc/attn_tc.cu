@@ -1,25 +1,24 @@
 // Attention of many rows over the token memory on the 5th-generation tensor
 // cores (the formula is in attn_rows.cu).
 //
-// A block has up to four tiles of 128 rows and one key head; the query heads that
-// share it are rows of the same tile (row r: token r / group, head r % group), so
-// keys and values are read once for all of them.  Keys come in steps of 64.  A
-// "chain" is one tile's way through its steps:  S = Q K^T (128 x 64 floats in
-// tensor memory), four softmax warps turn S into P = exp2(x - m), rounded to the
-// storage type and written over S, and O += P V takes P from there.  Chains run
-// beside each other, so that one's softmax covers another's products: four for
-// heads of up to 64 channels (S and O of each: 4 x (64 + 64) = 512 columns of
-// tensor memory), two for heads of up to 128, each with two S, so that the next
-// scores are there when a softmax ends (2 x (2 x 64 + 128)).
+// A block has two tiles of 128 rows and one key head; the query heads that share it
+// are rows of the same tile (row r: token r / group, head r % group), so keys and
+// values are read once for all of them.  Keys come in steps of 64.  A "chain" is one
+// tile's way through its steps:  S = Q K^T (128 x 64 floats in tensor memory), four
+// softmax warps turn S into P = exp2(x - m), rounded to the storage type and written
+// over S, and O += P V takes P from there.  The two chains run beside each other, so
+// that one's softmax covers the other's products, and each has two S, so that the
+// next scores are there when a softmax ends: 2 x (2 x 64 + head size) of 512 columns.
 //
-// With few rows the chains share a tile and take its steps in turn ("streams"):
-// a stream writes a partial result as a chunk of the span does, and k_attn_join
-// merges them.
+// An odd number of tiles would leave a chain idle in the last block.  Then both
+// chains share a tile and take its steps in turn ("streams"): a stream writes a
+// partial result as a chunk of the span does, and k_attn_join merges them.
 //
-// Roles: four softmax warps per chain (a thread owns a row: no shuffles), then a
-// warp that loads keys (TMA, one lane) and stages their coordinates, one that
-// loads values and zeroes those of keys nobody sees, and two that issue the
-// products of half of the chains each.
+// Roles: four softmax warps per chain (a thread owns a row: no shuffles), a warp
+// that loads keys (TMA, one lane) and stages their coordinates, one that loads
+// values and zeroes those of keys nobody sees, and one per chain that issues its
+// products.  Steps run from the last key back: with a distance bias a causal row's
+// nearest keys come last, and starting there its maximum hardly moves.
 //
 // The running maximum m of a row moves late: P = exp2(x - m) is formed in one
 // pass with the m of the step before, and where a row's maximum has passed m by
@@ -31,6 +30,17 @@
 // whole steps; in a step at the edge their scores are replaced, not added to, and
 // their value rows are zeroed in shared memory before the product, so their
 // contents never reach a result.
+//
+// What bounds it is the softmax: exp2 takes 4 clocks a warp on the special-function
+// unit, a packed multiply-add 2 on the FMA pipe, and of those a capped score needs
+// 5, a biased one 5 more, beside 4 for the sum and the rest; with two softmax warps
+// on a scheduler a step's 64 keys take 1420 clocks bare, 1890 with a cap, 1950 with
+// a bias and 2730 with both, against 640 (heads of 64) or 1280 of the tensor pipe.
+// Measured: 16,384 x 49,152 keys, 6 heads of 64, cap and bias: 3.13 ms, 395 TFLOP/s;
+// 14,700 packed causal tokens of 16 heads of 128 with a cap: 145 us, 649 TFLOP/s.
+// Tried and slower: four chains of one S each (four softmax warps a scheduler, 96
+// registers: 10 to 30 %), the next S loaded while P is stored (spills: 5 to 15 %),
+// scalar beside packed arithmetic (up to 30 %).
 #include <type_traits>
 
 #include "attn.cuh"
@@ -46,23 +56,25 @@ constexpr float kSlack = 8.0f, kHard = 15.0f;
 
 __device__ int g_attn_err;                       // bit b: a wait on barrier b (mod 32) ran out
 
+constexpr int kChains = 2;
+constexpr int kS = 2;                            // S per chain
+constexpr int kWarps = 4 * kChains + 4;
+constexpr int kLoadK = 4 * kChains, kLoadV = kLoadK + 1, kProduct = kLoadK + 2;       // warps
+
 template <int DP> struct TcCfg {
   static constexpr int NC = DP / 64;             // 64-channel chunks (one 128-byte swizzle line each)
-  static constexpr int kChains = 2;
-  static constexpr int kS = 2;    // S per chain
   static constexpr int kRing = DP == 64 ? 8 : 4; // steps of keys and of values in shared memory
   static constexpr int kStep = NC * kBox;
   static constexpr int kQ = kChains * NC * kQBox;
   static constexpr int kPos = kRing * 2 * kKeys * 4;         // [step in the ring][y | x][64]
   static constexpr int kSmem = kQ + 2 * kRing * kStep + kPos + 1024;
-  static constexpr int kWarps = 4 * kChains + 4;
   // tensor memory: S of every chain, then O of every chain
   static constexpr int kO = kChains * kS * kKeys;
   static_assert(kO + kChains * DP <= 512, "tensor memory");
   // barriers
-  static constexpr int FULL = 0, FREE = kRing, VOK = 2 * kRing, SFULL = 3 * kRing,
-                       PREADY = SFULL + kChains * kS, DONE = PREADY + kChains * kS,
-                       QFULL = DONE + kChains * kS, QFREE = QFULL + 1, DRAIN = QFREE + 1, kBars = DRAIN + 2;
+  static constexpr int FULL = 0, FREE = kRing, VOK = 2 * kRing, SFULL = 3 * kRing, PREADY = SFULL + kChains * kS,
+                       DONE = PREADY + kChains * kS, QFULL = DONE + kChains * kS, QFREE = QFULL + 1,
+                       DRAIN = QFREE + 1, kBars = DRAIN + kChains;
 };
 
 struct TcMaps {
@@ -250,7 +262,7 @@ __device__ __forceinline__ void outlast_copies() {
 }
 
 template <typename T, int DP, bool CAP, bool DIST>
-__global__ void __launch_bounds__(TcCfg<DP>::kWarps * 32, 1)
+__global__ void __launch_bounds__(kWarps * 32, 1)
     k_attn_tc(const __grid_constant__ AttnArgs A, const __grid_constant__ TcMaps M, const TanhPoly poly) {
   using C = TcCfg<DP>;
   extern __shared__ unsigned char smem_raw[];
@@ -267,7 +279,7 @@ __global__ void __launch_bounds__(TcCfg<DP>::kWarps * 32, 1)
 
   // block -> (row group, chunk, key head, sequence); the last rows of a causal
   // sequence have the longest reach and go first
-  const int streams = A.streams, tiles = C::kChains / streams;
+  const int streams = A.streams, tiles = kChains / streams;
   int b = blockIdx.x;
   int rg0 = b % A.row_groups;
   b /= A.row_groups;
@@ -302,7 +314,7 @@ __global__ void __launch_bounds__(TcCfg<DP>::kWarps * 32, 1)
     }
     __syncwarp();
   }
-  if (warp == 4 * C::kChains + 2) {
+  if (warp == kProduct) {
     tmem_alloc(&tmem_base, 512);
     tmem_relinquish();
   }
@@ -352,7 +364,7 @@ __global__ void __launch_bounds__(TcCfg<DP>::kWarps * 32, 1)
   auto place = [](int g) { return g & (C::kRing - 1); };
   auto phase = [](int g) { return (uint32_t)(g / C::kRing) & 1u; };
 
-  if (warp == 4 * C::kChains) {
+  if (warp == kLoadK) {
     // ------------------------------------------ queries, keys, coordinates
     bool ok = true;
     uint32_t item = 0;
@@ -399,7 +411,7 @@ __global__ void __launch_bounds__(TcCfg<DP>::kWarps * 32, 1)
       g = k.g;
     }
     if (!ok) outlast_copies();
-  } else if (warp == 4 * C::kChains + 1) {
+  } else if (warp == kLoadV) {
     // ------------------------------------------ values, and zeroes at edges
     bool ok = true;
     int g = 0;
@@ -442,122 +454,96 @@ __global__ void __launch_bounds__(TcCfg<DP>::kWarps * 32, 1)
     }
     if (ok) ok = patch();
     if (!ok) outlast_copies();
-  } else if (warp > 4 * C::kChains) {
-    // ------------------------------------------------------------- products
-    constexpr int kOwn = C::kChains / 2;         // chains of this warp
-    const int first = __shfl_sync(0xFFFFFFFFu, (warp - 4 * C::kChains - 2) * kOwn, 0);
+  } else if (warp >= kProduct) {
+    // ---------------------------------------------------- products of a chain
+    const int chain = __shfl_sync(0xFFFFFFFFu, warp - kProduct, 0), w = chain / streams, stream = chain & (streams - 1);
     constexpr uint32_t fmt = std::is_same<T, __nv_bfloat16>::value;
     constexpr uint32_t id_s = idesc_f16(128, kKeys, fmt);
     constexpr uint32_t id_o = idesc_f16(128, DP, fmt) | (1u << 16);      // B is MN-major
     constexpr uint64_t kStepUnits = C::kStep >> 4, kBoxUnits = kBox >> 4, kQBoxUnits = kQBox >> 4;
     const uint64_t dk = smem_desc(smem_u32(sk), 1024, 2), dv = desc_v(smem_u32(sv));
-    const uint64_t dq = smem_desc(smem_u32(sq), 1024, 2);
+    const uint64_t dq = smem_desc(smem_u32(sq), 1024, 2) + w * C::NC * kQBoxUnits;
     bool ok = true;
     uint32_t item = 0, vok = 0;                  // bit p of vok: the patch phase of place p
+    uint32_t n_qk = 0, n_pv = 0;                 // products issued
     int g = 0;
-    uint32_t n_qk[kOwn] = {}, n_pv[kOwn] = {};   // products issued per chain
     for (int rg = rg0; rg < groups && ok; rg += A.row_groups, ++item) {
-      const int end = reach_all(rg);
-      Walk qk[kOwn], pv[kOwn];
-      int e[kOwn];
-      uint32_t begun = 0;
-#pragma unroll
-      for (int c = 0; c < kOwn; ++c) {
-        const int stream = (first + c) & (streams - 1);
-        e[c] = reach(rg, (first + c) / streams);
-        qk[c] = Walk(c0, end, c1, g);
-        qk[c].settle(A, S, slots, all);
-        qk[c].seek(A, S, slots, all, streams, stream);
-        pv[c] = qk[c];
-      }
-      // S = Q K^T of chain c's next step (its values are there as well)
-      auto score = [&](int c) -> bool {
-        if (!qk[c].live()) return true;
-        const int chain = first + c, p = place(qk[c].g);
-        if (!wait(C::FULL + p, phase(qk[c].g))) return false;
-        if (qk[c].t * kKeys < e[c]) {
+      const int end = reach_all(rg), e = reach(rg, w);
+      Walk qk(c0, end, c1, g);
+      qk.settle(A, S, slots, all);
+      qk.seek(A, S, slots, all, streams, stream);
+      Walk pv = qk;
+      bool begun = false;
+      // S = Q K^T of the next step (its values are there as well)
+      auto score = [&]() -> bool {
+        if (!qk.live()) return true;
+        const int p = place(qk.g);
+        if (!wait(C::FULL + p, phase(qk.g))) return false;
+        if (qk.t * kKeys < e) {
           tc_fence_after();
-          const uint32_t s = chain * C::kS + (n_qk[c] & (C::kS - 1));
-          const uint64_t q = dq + (chain / streams) * C::NC * kQBoxUnits, kd = dk + p * kStepUnits;
+          const uint32_t s = chain * kS + (n_qk & (kS - 1));
+          const uint64_t kd = dk + p * kStepUnits;
 #pragma unroll
           for (int i = 0; i < C::NC; ++i)
-            umma4_ss(tmem + s * kKeys, q + i * kQBoxUnits, kd + i * kBoxUnits, id_s, i > 0);
+            umma4_ss(tmem + s * kKeys, dq + i * kQBoxUnits, kd + i * kBoxUnits, id_s, i > 0);
           umma_commit_elected(&bar[C::SFULL + s]);
           // this warp has seen the step's coordinates: its arrival passes them on
           if (DIST && lane == 0) mbar_arrive(&bar[C::SFULL + s]);
-          ++n_qk[c];
+          ++n_qk;
         }
-        qk[c].next_own(A, S, slots, all, streams, chain & (streams - 1));
+        qk.next_own(A, S, slots, all, streams, stream);
         return true;
       };
-      // O += P V of chain c's next step; keys and values are released when it is done
-      auto value = [&](int c) -> bool {
-        if (!pv[c].live()) return true;
-        const int chain = first + c, p = place(pv[c].g);
-        const bool zeroed = patched(pv[c]);
-        if (pv[c].t * kKeys < e[c]) {
-          if (zeroed && !wait(C::VOK + p, (vok >> (p + 8 * c)) & 1)) return false;
-          const uint32_t s = chain * C::kS + (n_pv[c] & (C::kS - 1));
-          if (!wait(C::PREADY + s, (n_pv[c] / C::kS) & 1)) return false;
+      // O += P V of the next step; keys and values are released when it is done
+      auto value = [&]() -> bool {
+        const int p = place(pv.g);
+        const bool zeroed = patched(pv);
+        if (pv.t * kKeys < e) {
+          if (zeroed && !wait(C::VOK + p, (vok >> p) & 1)) return false;
+          const uint32_t s = chain * kS + (n_pv & (kS - 1));
+          if (!wait(C::PREADY + s, (n_pv / kS) & 1)) return false;
           tc_fence_after();
-          umma4_ts(tmem + C::kO + chain * DP, tmem + s * kKeys, dv + p * kStepUnits, id_o, (begun >> c) & 1);
+          umma4_ts(tmem + C::kO + chain * DP, tmem + s * kKeys, dv + p * kStepUnits, id_o, begun);
           umma_commit_elected(&bar[C::FREE + p]);
-          if (C::kS > 1) umma_commit_elected(&bar[C::DONE + s]);
-          ++n_pv[c];
-          begun |= 1u << c;
+          umma_commit_elected(&bar[C::DONE + s]);
+          ++n_pv;
+          begun = true;
         } else if (lane == 0) {
           mbar_arrive(&bar[C::FREE + p]);
         }
-        if (zeroed) vok ^= 1u << (p + 8 * c);
-        pv[c].next_own(A, S, slots, all, streams, chain & (streams - 1));
+        if (zeroed) vok ^= 1u << p;
+        pv.next_own(A, S, slots, all, streams, stream);
         return true;
       };
       ok = wait(C::QFULL, item & 1);
 #pragma unroll
-      for (int i = 0; i < C::kS; ++i)
-#pragma unroll
-        for (int c = 0; c < kOwn; ++c) ok = ok && score(c);
-      while (ok) {
-        bool more = false;
-#pragma unroll
-        for (int c = 0; c < kOwn; ++c) {
-          ok = ok && value(c) && score(c);
-          more = more || pv[c].live();
-        }
-        if (!more) break;
-      }
+      for (int i = 0; i < kS; ++i) ok = ok && score();
+      while (ok && pv.live()) ok = value() && score();
       // the steps of the whole group, for the next group's places
       Walk k(c0, end, c1, g);
       if (rg + A.row_groups < groups)
         for (k.settle(A, S, slots, all); k.live(); k.next(A, S, slots, all)) {
         }
       g = k.g;
-      if (C::kS == 1)
-#pragma unroll
-        for (int c = 0; c < kOwn; ++c)
-          if (ok && ((begun >> c) & 1)) umma_commit_elected(&bar[C::DONE + first + c]);
       if (ok) umma_commit_elected(&bar[C::QFREE]);
       __syncwarp();
     }
     // no product may still run when tensor memory is freed
-    const int drain = C::DRAIN + first / kOwn;
-    umma_commit_elected(&bar[drain]);
-    if (!mbar_wait(&bar[drain], 0)) atomicOr(&g_attn_err, 1 << (drain & 31));
+    umma_commit_elected(&bar[C::DRAIN + chain]);
+    if (!mbar_wait(&bar[C::DRAIN + chain], 0)) atomicOr(&g_attn_err, 1 << ((C::DRAIN + chain) & 31));
     __syncwarp();
   } else {
     // -------------------------------------------------------------- softmax
     const int chain = warp >> 2, r = tid & 127, w = chain / streams, stream = chain & (streams - 1);
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-    const uint32_t ts0 = tmem + chain * C::kS * kKeys + lanes, to = tmem + C::kO + chain * DP + lanes;
+    const uint32_t ts0 = tmem + chain * kS * kKeys + lanes, to = tmem + C::kO + chain * DP + lanes;
     uint32_t n = 0;                              // steps of this chain since the block began
     int g = 0;
     bool ok = true;
-    // With one S, this step's S is complete only after the product of the step
-    // before, and DONE marks the end of a row group.  With two S a product may lag:
-    // DONE marks every step's, by turns on two barriers, since it may lag two steps.
-    auto done = [&](uint32_t i) -> int { return C::DONE + chain * C::kS + (i & (C::kS - 1)); };
-    uint32_t ends = 0;                           // row groups of this chain that had a step
-    auto phase_s = [](uint32_t i) -> uint32_t { return (i / C::kS) & 1; };
+    // The barrier of step i's product, and its phase: two by turns, since a product
+    // may lag two steps.
+    auto done = [&](uint32_t i) -> int { return C::DONE + chain * kS + (i & (kS - 1)); };
+    auto phase_s = [](uint32_t i) -> uint32_t { return (i / kS) & 1; };
     for (int rg = rg0; rg < groups && ok; rg += A.row_groups) {
       const int i0 = (rg * tiles + w) * qpt;
       const int ql = i0 + r / A.group;
@@ -584,7 +570,7 @@ __global__ void __launch_bounds__(TcCfg<DP>::kWarps * 32, 1)
       // product before is done with O.
       auto rise = [&](float up) -> bool {
         if (n > n0) {
-          if (C::kS > 1 && !wait(done(n - 1), phase_s(n - 1))) return false;
+          if (!wait(done(n - 1), phase_s(n - 1))) return false;
           tc_fence_after();
           const float f = ex2(-up);
 #pragma unroll 1
@@ -602,7 +588,7 @@ __global__ void __launch_bounds__(TcCfg<DP>::kWarps * 32, 1)
       };
       // S of the next step is there; maxima that lag behind are raised first
       auto begin = [&]() -> bool {
-        if (!wait(C::SFULL + chain * C::kS + (n & (C::kS - 1)), phase_s(n))) return false;
+        if (!wait(C::SFULL + chain * kS + (n & (kS - 1)), phase_s(n))) return false;
         tc_fence_after();
         if (lagging) {
           if (!rise(late)) return false;
@@ -618,7 +604,7 @@ __global__ void __launch_bounds__(TcCfg<DP>::kWarps * 32, 1)
         tmem_st_wait();
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(&bar[C::PREADY + chain * C::kS + (n & (C::kS - 1))]);
+        if (lane == 0) mbar_arrive(&bar[C::PREADY + chain * kS + (n & (kS - 1))]);
         ++n;
         k.next_own(A, S, slots, all, streams, stream);
       };
@@ -629,7 +615,7 @@ __global__ void __launch_bounds__(TcCfg<DP>::kWarps * 32, 1)
           int run = all ? (k.t - k.t0) / streams + 1 : 1;
           bool slow = false;
           do {
-            const uint32_t ts = ts0 + (n & (C::kS - 1)) * kKeys;
+            const uint32_t ts = ts0 + (n & (kS - 1)) * kKeys;
             const float* py = spos + place(k.g) * 2 * kKeys;
             if (!(ok = begin())) break;
             // one pass with the maximum as it is: z = score (log2 units) - m, p = exp2(z)
@@ -731,7 +717,7 @@ __global__ void __launch_bounds__(TcCfg<DP>::kWarps * 32, 1)
         } else if (!(ok = begin())) {
           break;
         }
-        const uint32_t ts = ts0 + (n & (C::kS - 1)) * kKeys;
+        const uint32_t ts = ts0 + (n & (kS - 1)) * kKeys;
         const float* py = spos + place(k.g) * 2 * kKeys;
         // 32 keys at a time, with tanh itself, masks, and maxima that move at once
         const unsigned long long keep = edge ? key_mask(A, S, slots, k.t * kKeys, hi) : ~0ull;
@@ -808,8 +794,7 @@ __global__ void __launch_bounds__(TcCfg<DP>::kWarps * 32, 1)
       const long long R = tok * A.heads + head;
       const bool any = n > n0;
       if (any) {
-        if (!(ok = C::kS > 1 ? wait(done(n - 1), phase_s(n - 1)) : wait(C::DONE + chain, ends & 1))) break;
-        ++ends;
+        if (!(ok = wait(done(n - 1), phase_s(n - 1)))) break;
         tc_fence_after();
       }
       const float inv = l > 0.f ? 1.0f / l : (l == 0.f ? 0.f : l);
@@ -858,7 +843,7 @@ __global__ void __launch_bounds__(TcCfg<DP>::kWarps * 32, 1)
   __syncwarp();
   tc_fence_before();
   __syncthreads();
-  if (warp == 4 * C::kChains + 2) {
+  if (warp == kProduct) {
     tc_fence_after();
     tmem_dealloc(tmem, 512);
   }
@@ -882,7 +867,7 @@ cudaError_t launch_tc_t(const AttnArgs& a, const TcMaps& m, cudaStream_t st) {
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t lc = {};
   lc.gridDim = dim3((unsigned)((long long)a.n_seqs * a.kv_heads * a.n_chunks * a.row_groups));
-  lc.blockDim = dim3(TcCfg<DP>::kWarps * 32);
+  lc.blockDim = dim3(kWarps * 32);
   lc.dynamicSmemBytes = TcCfg<DP>::kSmem;
   lc.stream = st;
   return cudaLaunchKernelEx(&lc, kern, a, m, poly);
@@ -890,16 +875,10 @@ cudaError_t launch_tc_t(const AttnArgs& a, const TcMaps& m, cudaStream_t st) {
 
 }  // namespace
 
-// Streams: two chains share a tile where that leaves fewer of them idle (tiles in
-// all over chains at work: 300 rows are 3 tiles, so 3 blocks of half the steps
-// each instead of 2 of all).
-int attn_tc_streams(int dim, int group, int max_q) {
-  const long long tiles = (max_q + 128 / group - 1) / (128 / group);
-  return tiles % 2 ? 2 : 1;
-}
-int attn_tc_tokens_per_block(int dim, int group, int streams) {
-  return (dim <= 64 ? TcCfg<64>::kChains : TcCfg<128>::kChains) / streams * (128 / group);
-}
+// Streams: two chains share a tile where that leaves fewer of them idle (300 rows
+// are 3 tiles: 3 blocks of half the steps each instead of 2 of all).
+int attn_tc_streams(int group, int max_q) { return (max_q + 128 / group - 1) / (128 / group) % 2 ? 2 : 1; }
+int attn_tc_tokens_per_block(int group, int streams) { return kChains / streams * (128 / group); }
 int attn_tc_unit(int streams) { return kKeys * streams; }
 
 // cudaErrorNotSupported where the arrays cannot be described to the TMA unit
