@@ -19,11 +19,12 @@ constexpr int kTcRows = 32;
 // Chunks of the span for the few-rows kernel, two blocks of which run on an SM.  A
 // block costs about kBegin to begin and end, and a step of its four warps (32 KB of
 // keys and values) about kStep, the memory's share of it when all blocks run.
-// One sequence: whole rounds of blocks; 110,537 keys of 2 heads take 34 us in one
-// round, 53 in four.  Several sequences are taken to be ragged: blocks of unlike
-// lengths run into one another, so the number weighs what they cost to begin
+// One sequence: whole rounds of blocks; 110,537 keys of 2 heads take 30 us in one
+// round, 38 in two, 55 in four.  Several sequences are taken to be ragged: blocks of
+// unlike lengths run into one another, so the number weighs what they cost to begin
 // against the last one's length; 61 sequences of up to 16,384 keys and 8 heads take
-// 310 us in 3 chunks, 287 in 5.
+// 323 us in 3 chunks, 297 in 5 (the rule's) and 299 in 8; 8 sequences of up to
+// 20,000 keys and 4 heads 60, 23 (the rule's 22) and 32 us in 3, 22 and 8.
 long long rows_chunks(long long units, int n_seqs, long long steps, long long most, int sms) {
   constexpr double kBegin = 10.0, kStep = 1.5;
   const long long slots = 2LL * sms;

@@ -13,8 +13,15 @@
 // shared memory filled by 16-byte asynchronous copies (no block barrier in the
 // loop).  Rows of the memory that no query may see are never read: their place
 // in the tile is zero-filled, so stale or non-finite contents do not matter.
+// The probabilities go to the second product as the sum of two numbers of the
+// storage type: the tensor pipe has room for the second product, and a single
+// token's error then is the output's rounding alone.
+//
 // With few rows the memory's bytes bound it, and splitting the span into chunks
-// fills the GPU; k_attn_join merges the chunks in index order.
+// fills the GPU; k_attn_join merges the chunks in index order.  Measured: 61 tokens
+// over ragged histories of up to 16,384 keys, 8 key heads of 128, 1.9 GB: 297 us,
+// 6.45 TB/s, 95 % of a plain copy's; one token over 4097 keys of 6 heads of 64
+// takes 8.3 us, most of which is two launches and a block's first copies.
 #include "attn.cuh"
 #include "kernels.h"
 

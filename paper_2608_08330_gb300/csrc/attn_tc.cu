@@ -36,11 +36,13 @@
 // 5, a biased one 5 more, beside 4 for the sum and the rest; with two softmax warps
 // on a scheduler a step's 64 keys take 1420 clocks bare, 1890 with a cap, 1950 with
 // a bias and 2730 with both, against 640 (heads of 64) or 1280 of the tensor pipe.
-// Measured: 16,384 x 49,152 keys, 6 heads of 64, cap and bias: 3.13 ms, 395 TFLOP/s;
-// 14,700 packed causal tokens of 16 heads of 128 with a cap: 145 us, 649 TFLOP/s.
+// Measured: 16,384 x 49,152 keys, 6 heads of 64, cap and bias: 2.98 ms, 415 TFLOP/s;
+// 14,700 packed causal tokens of 16 heads of 128 with a cap: 143 us, 655 TFLOP/s.
 // Tried and slower: four chains of one S each (four softmax warps a scheduler, 96
 // registers: 10 to 30 %), the next S loaded while P is stored (spills: 5 to 15 %),
-// scalar beside packed arithmetic (up to 30 %).
+// scalar beside packed arithmetic (up to 30 %), a second form of the pass for steps
+// whose keys share one y (8 % faster where all do, 8 % slower where two thirds do:
+// the two forms push each other out of the instruction cache).
 #include <type_traits>
 
 #include "attn.cuh"
@@ -621,11 +623,15 @@ __global__ void __launch_bounds__(kWarps * 32, 1)
             // one pass with the maximum as it is: z = score (log2 units) - m, p = exp2(z)
             float2 x2[kKeys / 2];
             float* x = reinterpret_cast<float*>(x2);
-#pragma unroll
-            for (int c = 0; c < kKeys; c += 32) tmem_ld32_issue(ts + c, x + c);
+            // the second half comes while the first is worked on where that takes longest
+            // (cap and bias: 4 % faster; the bias alone would be 4 % slower)
+            constexpr bool kHalves = CAP && DIST;
+            tmem_ld32_issue(ts, x);
+            if (!kHalves) tmem_ld32_issue(ts + 32, x + 32);
             tmem_ld_wait();
-#pragma unroll
-            for (int c = 0; c < kKeys; c += 32) reg_fence32(x + c);
+            reg_fence32(x);
+            if (!kHalves) reg_fence32(x + 32);
+            if (kHalves) tmem_ld32_issue(ts + 32, x + 32);
             float b0 = 0.f, t0 = -INFINITY, t1 = -INFINITY;
             float2 s0 = both(0.f), s1 = both(0.f);
             uint32_t pk[kKeys / 2];
@@ -634,6 +640,10 @@ __global__ void __launch_bounds__(kWarps * 32, 1)
             for (int ii = 0; ii < kKeys / 2 + 2 * G; ii += G) {
               // group ii's scores, the exponentials of the group before, and the sums
               // and packing of the one before that: each waits on nothing recent
+              if (kHalves && ii == kKeys / 4) {
+                tmem_ld_wait();
+                reg_fence32(x + 32);
+              }
               if (ii < kKeys / 2) {
                 const int i = ii;
                 float2 a[G];                       // what is added to the capped score

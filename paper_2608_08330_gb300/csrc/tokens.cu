@@ -11,7 +11,8 @@
 //   and the span and length of every sequence afterwards.  One launch: the
 //   scan is short (at most 16,384 sequences, 64 KB), so every block repeats it
 //   in shared memory instead of waiting for another block, then fills its own
-//   share of the tokens.
+//   share of the tokens.  The launch and the scan's latency bound it:
+//   61 sequences take 2.6 us, 2048 with 409,000 token places (5 MB) 7.0 us.
 //
 // rtcc_qkv_prepare: for every token and head of q and k
 //   x^ = x * rsqrt(mean(x^2) + eps) * gain,
@@ -23,7 +24,10 @@
 //   registers for all heads.  Eight heads' vectors are on their way to a ring in
 //   shared memory, every thread's own places, so nothing is waited for but the
 //   copy itself.  With few tokens a token's heads are divided among several groups
-//   of lanes.
+//   of lanes.  Measured: 176,000 tokens of 18 heads of 64, 815 MB, 122 us: 6.7 TB/s,
+//   98 % of a plain copy's; 16,384 of them, one wave of blocks, 17.4 us, 64 %;
+//   12,345 tokens of 20 heads of 80 (10 of 16 lanes have channels) 19.2 us, 61 %;
+//   61 tokens 3.7 us.
 #include <math.h>
 
 #include <atomic>
