@@ -535,17 +535,24 @@ typedef struct {
  *   j >= d_prefix[s] (a prefix that every token sees; NULL = 0);
  *   out = sum of softmax(x) v over the visible keys, lse = ln sum exp(x).
  * A token that sees no key gets out = 0 and lse = -inf.  Sums and the softmax
- * are float32; the probabilities are rounded to the storage type for their
- * product with v, as out is.  Rows that no token of a sequence sees (outside
- * the span, in an absent slot) are not used: they may hold anything, infinities
- * and NaN included.  Tokens of no sequence are left untouched.  Offsets and
- * spans are cut to [0, n_q] and [0, n_rows].
+ * are float32; for their product with v the probabilities are rounded to the
+ * storage type, or to the sum of two of its numbers where a key head has few
+ * query rows; out is rounded once.  How a span is split depends on the sizes, the
+ * workspace and the GPU, and changes the order of float32 sums; the same call
+ * gives the same bits.  Rows that no token of a sequence sees (outside the span,
+ * in an absent slot) are not used: they may hold anything, infinities and NaN
+ * included.  (Seen by some of its tokens, a row whose v is not finite may make
+ * the sequence's other tokens NaN too: their probability for it is 0.)  Tokens of
+ * no sequence are left untouched.  Offsets and spans are cut to [0, n_q] and
+ * [0, n_rows].
  * d_lse float32 [n_q][heads] (may be NULL); d_present int32 [n_slots];
  * d_slopes float32 [heads], d_q_pos [n_q][q_pos_row], d_k_pos [n_rows][2], all
  * three or none; d_out may be d_q with the same strides.  d_workspace: scratch
  * for splitting long spans over the GPU, used until the work is done, any
- * content; more than chunks * n_q * heads * (head_dim + 2) * 4 bytes is of no
- * use, without it (NULL, or too small) spans are not split.  q, k, v, out and
+ * content.  Each part of a span takes n_q * heads * (head_dim + 2) * 4 bytes;
+ * more parts than fill the GPU are not made, and without room for two (NULL, or
+ * too small) spans are not split.  scale, cap and scale / cap are finite, cap not
+ * negative; n_q * heads is below 2^31, heads at most 4096.  q, k, v, out and
  * the workspace are 16-byte aligned, d_k_pos 8-byte, the rest 4-byte.
  */
 rtcc_status rtcc_memory_attention(const rtcc_attn_config* cfg, const void* d_q, const void* d_k,
