@@ -35,7 +35,7 @@
 // unit, a packed multiply-add 2 on the FMA pipe, and of those a capped score needs
 // 5, a biased one 5 more, beside 4 for the sum and the rest; with two softmax warps
 // on a scheduler a step's 64 keys take 1420 clocks bare, 1890 with a cap, 1950 with
-// a bias and 2730 with both, against 640 (heads of 64) or 1280 of the tensor pipe.
+// a bias and 2630 with both, against 640 (heads of 64) or 1280 of the tensor pipe.
 // Measured: 16,384 x 49,152 keys, 6 heads of 64, cap and bias: 2.98 ms, 415 TFLOP/s;
 // 14,700 packed causal tokens of 16 heads of 128 with a cap: 143 us, 655 TFLOP/s.
 // Tried and slower: four chains of one S each (four softmax warps a scheduler, 96
