@@ -26,6 +26,7 @@ struct AttnArgs {
   uint32_t slot_mul, slot_shift; // row / slot_rows = row * slot_mul >> slot_shift
   int n_chunks, chunk, unit;     // key chunks per sequence at most, keys per chunk at least, a multiple of unit
   int streams;                   // partial results per chunk
+  int cluster;                   // 1: the chunks are a cluster of blocks that joins them itself
   int row_groups;                // blocks along the rows of one sequence and key head
   float scale_log2;              // scale * log2(e); with a cap: scale / cap
   float cap_log2;                // cap * log2(e), 0 = no cap

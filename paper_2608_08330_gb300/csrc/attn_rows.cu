@@ -18,10 +18,11 @@
 // token's error then is the output's rounding alone.
 //
 // With few rows the memory's bytes bound it, and splitting the span into chunks
-// fills the GPU; k_attn_join merges the chunks in index order.  Measured: 61 tokens
+// fills the GPU; k_attn_join merges the chunks in index order, or, where the chunks
+// are few, the blocks of a cluster do it from one another's shared memory.  Measured: 61 tokens
 // over ragged histories of up to 16,384 keys, 8 key heads of 128, 1.9 GB: 297 us,
 // 6.45 TB/s, 95 % of a plain copy's; one token over 4097 keys of 6 heads of 64
-// takes 8.3 us, most of which is two launches and a block's first copies.
+// takes 8.1 us, most of which is the launch, a block's first copies and three steps.
 #include "attn.cuh"
 #include "kernels.h"
 
@@ -31,6 +32,7 @@ namespace {
 constexpr int kWarps = 4;
 constexpr int kStages = 3;
 constexpr int kRows = 16;
+constexpr int kCluster = 16;                     // blocks of a cluster at most
 
 template <int DP> struct RowsCfg {               // DP: head size padded to 64 or 128
   static constexpr int KT = DP == 64 ? 32 : 16;  // keys per tile: 4 KB of keys, 4 KB of values
@@ -38,8 +40,10 @@ template <int DP> struct RowsCfg {               // DP: head size padded to 64 o
   static constexpr int kPosBytes = KT * 8;
   static constexpr int kStageBytes = 2 * kTileBytes + kPosBytes;
   static constexpr int kRing = kWarps * kStages * kStageBytes;
-  static constexpr int kMerge = kWarps * kRows * (DP + 4) * 4;   // the warps' accumulators at the end
-  static constexpr int kSmem = kRing > kMerge ? kRing : kMerge;
+  // at the end the warps' accumulators, then the block's for its cluster: [row][DP + 4]
+  static constexpr int kState = kRows * (DP + 4);
+  static_assert((kWarps + 1) * kState * 4 <= kRing, "states at the end lie in the ring");
+  static constexpr int kSmem = kRing;
 };
 
 __device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool live) {
@@ -79,6 +83,21 @@ __device__ __forceinline__ void mma16816<__nv_bfloat16>(float (&d)[4], const uin
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
+// Shared memory of the cluster's blocks.
+__device__ __forceinline__ float4 cluster_ld4(uint32_t a) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+               : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
+               : "r"(a)
+               : "memory");
+  return v;
+}
+__device__ __forceinline__ float2 cluster_ld2(uint32_t a) {
+  float2 v;
+  asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(a) : "memory");
+  return v;
+}
+
 // Two floats as hi + lo of the storage type.
 template <typename T>
 __device__ __forceinline__ void split2(float a, float b, uint32_t& hi, uint32_t& lo) {
@@ -101,7 +120,20 @@ __device__ __forceinline__ uint32_t tile_off(int r, int c) {
   return (uint32_t)(r * DP * 2 + (c & ~7) * 16 + (((c ^ r) & 7) * 16));
 }
 
-template <typename T, int DP>
+// Four channels of a row's result: accumulators over the sum, and the lse.
+template <typename T>
+__device__ __forceinline__ void store_row(const AttnArgs& A, long long t, int h, int c, float4 acc, float mm, float ll) {
+  const float inv = ll > 0.f ? 1.0f / ll : (ll == 0.f ? 0.f : ll);
+  uint2 u;
+  u.x = Store<T>::pack2(acc.x * inv, acc.y * inv);
+  u.y = Store<T>::pack2(acc.z * inv, acc.w * inv);
+  *reinterpret_cast<uint2*>(static_cast<T*>(A.out) + t * A.out_row + (long long)h * A.out_head + c) = u;
+  if (c == 0 && A.lse) A.lse[t * A.heads + h] = ll == 0.f ? -INFINITY : (mm + log2f(ll)) * kLn2;
+}
+
+// CLUSTER: the chunks are the cluster's blocks, which join them (a kernel of its own:
+// the join's registers cost the long split 2 %).
+template <typename T, int DP, bool CLUSTER>
 __global__ void __launch_bounds__(kWarps * 32, 2) k_attn_rows(const __grid_constant__ AttnArgs A) {
   using C = RowsCfg<DP>;
   constexpr int KT = C::KT;
@@ -119,7 +151,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) k_attn_rows(const __grid_const
   const int rows_all = S.nq * A.group;
   const int per = attn_chunk(A, S.nk, A.unit);
   const int c0 = (int)min((long long)per * chunk, (long long)S.nk), c1 = min(S.nk - c0, per) + c0;
-  if (chunk > 0 && c0 >= S.nk) return;           // not in use; chunk 0 always answers
+  if (!CLUSTER && chunk > 0 && c0 >= S.nk) return;   // not in use; chunk 0 always answers
   const unsigned long long slots = attn_slot_mask(A, lane);
   const uint32_t ring = smem_u32(smem) + w * kStages * C::kStageBytes;
   const unsigned char* ring_g = smem + w * kStages * C::kStageBytes;
@@ -338,18 +370,57 @@ __global__ void __launch_bounds__(kWarps * 32, 2) k_attn_rows(const __grid_const
       const long long t = S.q0 + (r0 + r) / A.group;
       const int h = kvh * A.group + (r0 + r) % A.group;
       const long long R = t * A.heads + h;
-      if (A.n_chunks > 1) {
+      if (CLUSTER) {
+        float* dst = mo + kWarps * C::kState + r * P;
+        *reinterpret_cast<float4*>(dst + c) = acc;
+        if (c == 0) *reinterpret_cast<float2*>(dst + DP) = make_float2(mm, ll);
+      } else if (A.n_chunks > 1) {
         const long long at = (long long)chunk * A.n_q * A.heads + R;
         *reinterpret_cast<float4*>(A.part_o + at * A.dim + c) = acc;
         if (c == 0) A.part_ml[at] = make_float2(mm, ll);
       } else {
-        const float inv = ll > 0.f ? 1.0f / ll : (ll == 0.f ? 0.f : ll);
-        uint2 u;
-        u.x = Store<T>::pack2(acc.x * inv, acc.y * inv);
-        u.y = Store<T>::pack2(acc.z * inv, acc.w * inv);
-        *reinterpret_cast<uint2*>(static_cast<T*>(A.out) + t * A.out_row + (long long)h * A.out_head + c) = u;
-        if (c == 0 && A.lse) A.lse[R] = ll == 0.f ? -INFINITY : (mm + log2f(ll)) * kLn2;
+        store_row<T>(A, t, h, c, acc, mm, ll);
       }
+    }
+    if (CLUSTER) {
+      // every block joins its share of the rows, from the blocks' states in chunk order
+      __syncwarp();
+      cluster_sync_all();
+      const uint32_t state = smem_u32(mo + kWarps * C::kState);
+      const int blocks = (int)cluster_nctarank();
+      for (int idx = chunk * kWarps * 32 + threadIdx.x; idx < kRows * (DP / 4); idx += A.n_chunks * kWarps * 32) {
+        const int r = idx / (DP / 4), c = (idx % (DP / 4)) * 4;
+        if (r0 + r >= rows_all || c >= A.dim) continue;
+        float2 ml[kCluster];
+        float4 x[kCluster];
+        float mm = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < kCluster; ++i) {
+          const bool in = i < blocks;
+          const uint32_t at = mapa_shared(state + r * P * 4, in ? i : 0);
+          ml[i] = in ? cluster_ld2(at + DP * 4) : make_float2(-INFINITY, 0.f);
+          x[i] = in ? cluster_ld4(at + c * 4) : make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+#pragma unroll
+        for (int i = 0; i < kCluster; ++i) mm = fmaxf(mm, ml[i].x);
+        const float base = mm == -INFINITY ? 0.f : mm;
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+        float ll = 0.f;
+#pragma unroll
+        for (int i = 0; i < kCluster; ++i) {
+          const float f = exp2f(ml[i].x - base);
+          acc.x = fmaf(f, x[i].x, acc.x);
+          acc.y = fmaf(f, x[i].y, acc.y);
+          acc.z = fmaf(f, x[i].z, acc.z);
+          acc.w = fmaf(f, x[i].w, acc.w);
+          ll = fmaf(f, ml[i].y, ll);
+        }
+        const long long t = S.q0 + (r0 + r) / A.group;
+        const int h = kvh * A.group + (r0 + r) % A.group;
+        store_row<T>(A, t, h, c, acc, mm, ll);
+      }
+      __syncwarp();
+      cluster_sync_all();                        // before a block's state goes
     }
     __syncthreads();
   }
@@ -425,41 +496,48 @@ __global__ void __launch_bounds__(kJoinWarps * 32) k_attn_join(const __grid_cons
     if (W == 1 || w == 0) {
       const long long t = R / A.heads;
       const int h = (int)(R % A.heads);
-      const float inv = ll > 0.f ? 1.0f / ll : (ll == 0.f ? 0.f : ll);
-      if (on) {
-        uint2 u;
-        u.x = Store<T>::pack2(acc.x * inv, acc.y * inv);
-        u.y = Store<T>::pack2(acc.z * inv, acc.w * inv);
-        *reinterpret_cast<uint2*>(static_cast<T*>(A.out) + t * A.out_row + (long long)h * A.out_head + c4) = u;
-      }
-      if (lane == 0 && A.lse) A.lse[R] = ll == 0.f ? -INFINITY : (mm + log2f(ll)) * kLn2;
+      if (on) store_row<T>(A, t, h, c4, acc, mm, ll);
     }
     if (W > 1) __syncthreads();                  // before the next row's sums
   }
 }
 
-template <typename T, int DP>
+template <typename T, int DP, bool CLUSTER>
 cudaError_t launch_rows_t(const AttnArgs& a, cudaStream_t st) {
   using C = RowsCfg<DP>;
   static std::atomic<uint64_t> allowed{0};
-  const cudaError_t e = allow_smem(reinterpret_cast<const void*>(k_attn_rows<T, DP>), C::kSmem, &allowed);
+  const cudaError_t e = allow_smem(reinterpret_cast<const void*>(k_attn_rows<T, DP, CLUSTER>), C::kSmem, &allowed, CLUSTER && kCluster > 8);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t lc = {};
   lc.gridDim = dim3((unsigned)((long long)a.n_seqs * a.kv_heads * a.row_groups * a.n_chunks));
   lc.blockDim = dim3(kWarps * 32);
   lc.dynamicSmemBytes = C::kSmem;
   lc.stream = st;
-  return cudaLaunchKernelEx(&lc, k_attn_rows<T, DP>, a);
+  cudaLaunchAttribute at[1];
+  if (CLUSTER) {
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = a.n_chunks;
+    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    lc.attrs = at;
+    lc.numAttrs = 1;
+  }
+  return cudaLaunchKernelEx(&lc, k_attn_rows<T, DP, CLUSTER>, a);
 }
 
 }  // namespace
 
 int attn_rows_unit(int dim) { return kWarps * (dim <= 64 ? RowsCfg<64>::KT : RowsCfg<128>::KT); }
 int attn_rows_per_block() { return kRows; }
+int attn_rows_cluster() { return kCluster; }
 
+template <bool CLUSTER>
+static cudaError_t launch_rows(const AttnArgs& a, bool bf16, cudaStream_t st) {
+  if (a.dim <= 64)
+    return bf16 ? launch_rows_t<__nv_bfloat16, 64, CLUSTER>(a, st) : launch_rows_t<__half, 64, CLUSTER>(a, st);
+  return bf16 ? launch_rows_t<__nv_bfloat16, 128, CLUSTER>(a, st) : launch_rows_t<__half, 128, CLUSTER>(a, st);
+}
 cudaError_t launch_attn_rows(const AttnArgs& a, bool bf16, cudaStream_t st) {
-  if (a.dim <= 64) return bf16 ? launch_rows_t<__nv_bfloat16, 64>(a, st) : launch_rows_t<__half, 64>(a, st);
-  return bf16 ? launch_rows_t<__nv_bfloat16, 128>(a, st) : launch_rows_t<__half, 128>(a, st);
+  return a.cluster ? launch_rows<true>(a, bf16, st) : launch_rows<false>(a, bf16, st);
 }
 
 cudaError_t launch_attn_join(const AttnArgs& a, int max_q, bool bf16, cudaStream_t st) {

@@ -366,11 +366,13 @@ cudaError_t launch_nms(const NmsArgs& a, cudaStream_t st);
 int sm_count();
 // Let `kernel` use `bytes` of dynamic shared memory on the current device;
 // `devices` remembers where that is done already.
-cudaError_t allow_smem(const void* kernel, int bytes, std::atomic<uint64_t>* devices);
+cudaError_t allow_smem(const void* kernel, int bytes, std::atomic<uint64_t>* devices,
+                       bool wide_clusters = false);
 // Attention over the token memory: few rows (attn_rows.cu), many (attn_tc.cu).
 struct AttnArgs;
 int attn_rows_unit(int dim);       // chunks of the span are multiples of this many keys
 int attn_rows_per_block();         // (token, head) rows per block
+int attn_rows_cluster();           // blocks that can join their chunks
 cudaError_t launch_attn_rows(const AttnArgs& a, bool bf16, cudaStream_t st);
 // The tensor-core kernel for many rows (attn_tc.cu): partial results per chunk,
 // tokens per block, the chunks' unit, launch (cudaErrorNotSupported: the arrays do

@@ -394,13 +394,14 @@ int sm_count() {
   return n;
 }
 
-cudaError_t allow_smem(const void* kernel, int bytes, std::atomic<uint64_t>* devices) {
+cudaError_t allow_smem(const void* kernel, int bytes, std::atomic<uint64_t>* devices, bool wide_clusters) {
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
   const uint64_t bit = 1ull << (dev & 63);
   if (dev < 64 && (devices->load(std::memory_order_relaxed) & bit)) return cudaSuccess;
   e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == cudaSuccess && wide_clusters) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
   if (e == cudaSuccess && dev < 64) devices->fetch_or(bit, std::memory_order_relaxed);
   return e;
 }

@@ -417,6 +417,21 @@ def test_attention_split_and_hints(R, n, m):
         Case(n, m, heads=4, kv=2, dim=128, causal=True, dtype="bf16").run(R, **kw).check()
 
 
+@pytest.mark.parametrize("dim", [64, 80])
+@pytest.mark.parametrize("n,m", [([1], [130]), ([1], [1025]), ([3], [2049]), ([5], [4097]), ([1, 1, 1], [900, 0, 31]),
+                                 ([2, 0, 4, 1], [1, 700, 2000, 650])])
+def test_attention_joined_inside_clusters(R, n, m, dim):
+    """Few chunks: the blocks of a cluster join them, with and without a
+    workspace, over chunks that are empty, rows past the last and absent slots."""
+    for kw in (dict(heads=8, kv=2), dict(heads=6, kv=6, slot_rows=150, absent=(0, 2), cap=30.0, dist=True)):
+        if kw.get("absent"):                     # slots that the memory has
+            kw["absent"] = [a for a in kw["absent"] if a * 150 < sum(m)]
+        c = Case(n, m, dim=dim, causal=True, gap=3, **kw)
+        for run in (dict(), dict(workspace=0), dict(max_k=60 * 64)):
+            c.out.fill_(7.0)
+            c.run(R, **run).check()
+
+
 def test_attention_repeats_bit_for_bit(R):
     a = Case([1, 30], [9000, 4000], heads=4, kv=2, dim=64, causal=True).run(R).check()
     b = Case([1, 30], [9000, 4000], heads=4, kv=2, dim=64, causal=True).run(R)
