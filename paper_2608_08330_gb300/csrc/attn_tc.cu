@@ -279,12 +279,19 @@ __global__ void __launch_bounds__(kWarps * 32, 1)
   unsigned char* sv = sk + C::kRing * C::kStep;
   float* spos = reinterpret_cast<float*>(sv + C::kRing * C::kStep);
 
-  // block -> (row group, chunk, key head, sequence); the last rows of a causal
-  // sequence have the longest reach and go first
+  // block -> (row group, chunk, key head, sequence); the last rows of causal
+  // sequences have the longest reach and go first, those of all sequences together,
+  // so that short work is left for the end
   const int streams = A.streams, tiles = kChains / streams;
-  int b = blockIdx.x;
-  int rg0 = b % A.row_groups;
-  b /= A.row_groups;
+  int b = blockIdx.x, rg0;
+  if (A.causal) {
+    const int each = gridDim.x / A.row_groups;
+    rg0 = A.row_groups - 1 - b / each;
+    b %= each;
+  } else {
+    rg0 = b % A.row_groups;
+    b /= A.row_groups;
+  }
   const int chunk = b % A.n_chunks;
   b /= A.n_chunks;
   const int kvh = b % A.kv_heads;
@@ -292,7 +299,6 @@ __global__ void __launch_bounds__(kWarps * 32, 1)
   const AttnSpan S = attn_span(A, seq);
   const int qpt = 128 / A.group;                 // tokens per tile
   const int groups = (S.nq + tiles * qpt - 1) / (tiles * qpt);
-  if (A.causal) rg0 = A.row_groups - 1 - rg0;
   const int per = attn_chunk(A, S.nk, A.unit);
   const int c0 = (int)min((long long)per * chunk, (long long)S.nk), c1 = min(S.nk - c0, per) + c0;
   if (rg0 >= groups || (chunk > 0 && c0 >= S.nk)) return;   // not in use; chunk 0 always answers
