@@ -25,8 +25,9 @@
 //   shared memory, every thread's own places, so nothing is waited for but the
 //   copy itself.  With few tokens a token's heads are divided among several groups
 //   of lanes.  Measured: 176,000 tokens of 18 heads of 64, 815 MB, 122 us: 6.7 TB/s,
-//   98 % of a plain copy's; 16,384 of them, one wave of blocks, 17.4 us, 64 %;
-//   12,345 tokens of 20 heads of 80 (10 of 16 lanes have channels) 19.2 us, 61 %;
+//   98 % of a plain copy's; 16,384 of them, a wave of blocks, 16.6 us, 68 %, or
+//   14.2 us, 79 %, where pairs are neighbours and no lane needs another's vector;
+//   12,345 tokens of 20 heads of 80 (10 of 16 lanes have channels) 19.0 us, 61 %;
 //   61 tokens 3.7 us.
 #include <math.h>
 
@@ -256,14 +257,14 @@ __global__ void __launch_bounds__(kPrepThreads, 6) k_qkv_prepare(const __grid_co
   // pairs [j0, j1) are heads [0, n) of q or k, at src and dst
   auto heads = [&](int j0, int j1, int n, const T* src, long long src_step, T* dst, long long dst_step, bool write,
                    const float* gain) {
-    float2 gn[4], go[4];                         // gains: own, and the partner's
+    float2 gn[4], go[4];                         // gains: own, and the partner's, for all heads
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       gn[i] = gain && live ? make_float2(gain[e0 + 2 * i], gain[e0 + 2 * i + 1]) : make_float2(1.f, 1.f);
-      go[i] = make_float2(1.f, 1.f);
-      if (TURN == kTurnLanes && gain && live && in_rot) {
+      if (TURN == kTurnLanes) {                  // with the cosine and the sine
         const int o = e0 + 2 * i + (low ? A.n_rot : -A.n_rot);
-        go[i] = make_float2(gain[o], gain[o + 1]);
+        go[i] = gain && live && in_rot ? mul2(make_float2(gain[o], gain[o + 1]), sn[i]) : sn[i];
+        gn[i] = mul2(gn[i], cs[i]);
       }
     }
     for (int j = j0; j < j1; ++j, n -= 2, src += 2 * src_step, dst += 2 * dst_step) {
@@ -298,10 +299,12 @@ __global__ void __launch_bounds__(kPrepThreads, 6) k_qkv_prepare(const __grid_co
         if (u >= n) continue;                    // the same for the whole block
         const float2 rr = make_float2(rs[u], rs[u]);
         float2 y[4];
-        y[0] = mul2(mul2(Store<T>::unpack2(raw[u].x), rr), gn[0]);
-        y[1] = mul2(mul2(Store<T>::unpack2(raw[u].y), rr), gn[1]);
-        y[2] = mul2(mul2(Store<T>::unpack2(raw[u].z), rr), gn[2]);
-        y[3] = mul2(mul2(Store<T>::unpack2(raw[u].w), rr), gn[3]);
+        y[0] = mul2(Store<T>::unpack2(raw[u].x), rr);
+        y[1] = mul2(Store<T>::unpack2(raw[u].y), rr);
+        y[2] = mul2(Store<T>::unpack2(raw[u].z), rr);
+        y[3] = mul2(Store<T>::unpack2(raw[u].w), rr);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i] = mul2(y[i], gn[i]);
         if (TURN == kTurnInterleaved) {
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
@@ -317,7 +320,7 @@ __global__ void __launch_bounds__(kPrepThreads, 6) k_qkv_prepare(const __grid_co
           z[3] = Store<T>::unpack2(__shfl_sync(0xFFFFFFFFu, raw[u].w, from, LP));
           if (in_rot) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) y[i] = fma2(y[i], cs[i], mul2(mul2(mul2(z[i], rr), go[i]), sn[i]));
+            for (int i = 0; i < 4; ++i) y[i] = fma2(mul2(z[i], rr), go[i], y[i]);
           }
         } else if (TURN == kTurnAny) {
           if (live) {
