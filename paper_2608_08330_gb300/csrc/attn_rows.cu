@@ -19,10 +19,11 @@
 //
 // With few rows the memory's bytes bound it, and splitting the span into chunks
 // fills the GPU; k_attn_join merges the chunks in index order, or, where the chunks
-// are few, the blocks of a cluster do it from one another's shared memory.  Measured: 61 tokens
-// over ragged histories of up to 16,384 keys, 8 key heads of 128, 1.9 GB: 297 us,
-// 6.45 TB/s, 95 % of a plain copy's; one token over 4097 keys of 6 heads of 64
-// takes 8.1 us, most of which is the launch, a block's first copies and three steps.
+// are few, the blocks of a cluster do it from one another's shared memory.
+// Measured: 61 tokens over ragged histories of up to 16,384 keys, 8 key heads of
+// 128, 1.9 GB: 294 to 297 us, 6.5 TB/s, 95 % of a plain copy's; one token over 4097 keys of
+// 6 heads of 64 takes 8.1 us, most of which is the launch, a block's first copies
+// and three steps.
 #include "attn.cuh"
 #include "kernels.h"
 

@@ -37,12 +37,16 @@
 // on a scheduler a step's 64 keys take 1420 clocks bare, 1890 with a cap, 1950 with
 // a bias and 2630 with both, against 640 (heads of 64) or 1280 of the tensor pipe.
 // Measured: 16,384 x 49,152 keys, 6 heads of 64, cap and bias: 2.98 ms, 415 TFLOP/s;
-// 14,700 packed causal tokens of 16 heads of 128 with a cap: 143 us, 655 TFLOP/s.
+// 14,700 packed causal tokens of 16 heads of 128 with a cap: 130 us, 720 TFLOP/s
+// (of a block's 22 us there, 1 goes to its set-up, 2 to its first scores, 2 to the
+// masked step and 3 to its results).
 // Tried and slower: four chains of one S each (four softmax warps a scheduler, 96
 // registers: 10 to 30 %), the next S loaded while P is stored (spills: 5 to 15 %),
 // scalar beside packed arithmetic (up to 30 %), a second form of the pass for steps
 // whose keys share one y (8 % faster where all do, 8 % slower where two thirds do:
-// the two forms push each other out of the instruction cache).
+// the two forms push each other out of the instruction cache), blocks that take over
+// the work of those not yet begun (up to 30 %: the roles change over one after the
+// other), and results through shared memory to whole lines (4 %).
 #include <type_traits>
 
 #include "attn.cuh"

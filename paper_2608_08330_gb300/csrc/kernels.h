@@ -365,7 +365,8 @@ cudaError_t launch_nms(const NmsArgs& a, cudaStream_t st);
 // SMs of the current device, 0 on an error (tokens.cu).
 int sm_count();
 // Let `kernel` use `bytes` of dynamic shared memory on the current device;
-// `devices` remembers where that is done already.
+// `devices` remembers where that is done already.  wide_clusters: and launch in
+// clusters of more than 8 blocks.
 cudaError_t allow_smem(const void* kernel, int bytes, std::atomic<uint64_t>* devices,
                        bool wide_clusters = false);
 // Attention over the token memory: few rows (attn_rows.cu), many (attn_tc.cu).
