@@ -93,7 +93,7 @@ __global__ void __launch_bounds__(kAppendThreads) k_memory_append(const AppendAr
   if (tid == 0) off[A.n_seqs] = (int)min(carry, cap);
   __syncthreads();
   const int stride = gridDim.x * blockDim.x, first = blockIdx.x * blockDim.x + tid;
-  for (int s = first; s <= A.n_seqs; s += stride) {
+  for (int s = first; s <= A.n_seqs; s += stride) {   // at most kMaxSeqs + stride
     A.offsets[s] = off[s];
     if (s == A.n_seqs) break;
     const int slot = A.slot ? A.slot[s] : s;
@@ -106,7 +106,8 @@ __global__ void __launch_bounds__(kAppendThreads) k_memory_append(const AppendAr
     A.length[s] = len;
   }
   const int live = off[A.n_seqs];
-  for (int i = first; i < A.n_tokens; i += stride) {
+  for (long long t = first; t < A.n_tokens; t += stride) {   // in 64 bits: n_tokens + stride may pass 2^31
+    const int i = (int)t;
     int row = -1, seq = -1, pos = -1;
     if (i < live) {
       int lo = 0, hi = A.n_seqs;                 // the last sequence with off <= i
