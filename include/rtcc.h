@@ -550,8 +550,10 @@ typedef struct {
  * three or none; d_out may be d_q with the same strides.  d_workspace: scratch
  * for splitting long spans over the GPU, used until the work is done, any
  * content.  Each part of a span takes n_q * heads * (head_dim + 2) * 4 bytes;
- * more parts than fill the GPU are not made, and without room for two (NULL, or
- * too small) spans are not split.  scale, cap and scale / cap are finite, cap not
+ * more parts than fill the GPU, or than one for 65,536 keys, are not made, and
+ * without room for two (NULL, or too small) spans are not split.  A float32 sum
+ * over n equally weighted keys of a part may come out smaller by n 2^-28 of
+ * itself, so long spans want a workspace (and max_k).  scale, cap and scale / cap are finite, cap not
  * negative; n_q * heads is below 2^31, heads at most 4096.  q, k, v, out and
  * the workspace are 16-byte aligned, d_k_pos 8-byte, the rest 4-byte.
  */

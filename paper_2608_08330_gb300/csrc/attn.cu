@@ -16,6 +16,16 @@ namespace {
 // and 27 in blocks of 16 rows, 30 rows over 50,000 keys, heads of 64, 25 and 23.
 constexpr int kTcRows = 32;
 
+// The tensor cores cut what does not fit the float32 sum off at every 16 keys' addition
+// (a unit in the last place at most), so a sum over n keys of equal weight comes out
+// smaller by up to (n / 32) 2^-23: 2^-12 at 65,536 keys, half of fp16's rounding; measured
+// 0.1 % at 2^18 keys, 0.6 % at 2^20.  Parts of a span are no longer than this where the
+// workspace has room: kSumKeys per sum, a block of the few-rows kernel has a sum in each
+// of its four warps.  A call of the tensor-core kernel without room, whose parts would be
+// longer than kLongSum, goes to the few-rows kernel instead: slower, but a cluster of its
+// blocks has up to 64 sums.
+constexpr long long kSumKeys = 1 << 16, kLongSum = 1 << 20;
+
 // Chunks of the span for the few-rows kernel, two blocks of which run on an SM.  A
 // block costs about kBegin to begin and end, and a step of its four warps (32 KB of
 // keys and values) about kStep, the memory's share of it when all blocks run.
@@ -25,7 +35,7 @@ constexpr int kTcRows = 32;
 // against the last one's length; 61 sequences of up to 16,384 keys and 8 heads take
 // 323 us in 3 chunks, 297 in 5 (the rule's) and 299 in 8; 8 sequences of up to
 // 20,000 keys and 4 heads 60, 23 (the rule's 22) and 32 us in 3, 22 and 8.
-long long rows_chunks(long long units, int n_seqs, long long steps, long long most, int sms) {
+long long rows_chunks(long long units, int n_seqs, long long steps, long long least_chunks, long long most, int sms) {
   constexpr double kBegin = 10.0, kStep = 1.5;
   const long long slots = 2LL * sms;
   long long best = 1;
@@ -42,7 +52,7 @@ long long rows_chunks(long long units, int n_seqs, long long steps, long long mo
       }
     }
   }
-  return std::max(1LL, std::min(best, most));
+  return std::max(1LL, std::min(std::max(best, least_chunks), most));
 }
 
 // Chunks that a cluster of blocks joins by itself through shared memory (1: none),
@@ -52,9 +62,13 @@ long long rows_chunks(long long units, int n_seqs, long long steps, long long mo
 // 6.0 us against 7.2, 4097 8.1 against 8.9, 8000 9.5 and 9.2, and 12,000 would be
 // 11.5 against 10.1; every call from the host is 2.5 us shorter.  Four ragged
 // sequences of up to 4000 keys and 8 heads 10.1 against 13.0.
-long long rows_cluster(long long units, long long steps, long long split, int sms, int dim) {
+// Also taken, with blocks resident or not, where it gives more chunks than the
+// workspace has room for and the least number is not reached.
+long long rows_cluster(long long units, long long steps, long long split, long long least_chunks, int sms, int dim) {
   const long long kJoin = dim <= 64 ? 2 : 1;
   const long long wide = attn_rows_cluster();
+  const long long most = std::min(least_chunks, units * wide <= sms ? wide : 8LL);
+  if (split < most && units * most <= 0x7FFFFFFF) return most;
   const long long limit = units * wide <= sms ? wide : std::min(8LL, 2LL * sms / units);
   if (limit < 2) return 1;
   const long long per = (steps + limit - 1) / limit;
@@ -67,15 +81,16 @@ long long rows_cluster(long long units, long long steps, long long split, int sm
 // the merge two steps' time and the traffic of the partial results (a step takes
 // about 1.2 us).  With 384 units of 768 steps, one chunk leaves the third round
 // half empty, five fill 13 rounds.
-long long tc_chunks(long long units, long long steps, long long most, int sms, int streams, long long n_q, int heads,
-                    int dim) {
-  long long best = 1;
+long long tc_chunks(long long units, long long steps, long long least_chunks, long long most, int sms, int streams,
+                    long long n_q, int heads, int dim) {
+  const long long first = std::max(1LL, std::min(least_chunks, most));
+  long long best = first;
   double least = 0;
-  for (long long c = 1; c <= std::max(1LL, std::min(most, 64LL)); ++c) {
+  for (long long c = first; c <= std::max(first, std::min(most, 64LL)); ++c) {
     const double rounds = (double)((units * c + sms - 1) / sms);
     double cost = rounds * ((double)((steps + c - 1) / c) + 4);
     if (c * streams > 1) cost += 2 + 8e-6 * (double)(c * streams * n_q * heads) * dim / (6.8 * 1.2);
-    if (c == 1 || cost < least) {
+    if (c == first || cost < least) {
       least = cost;
       best = c;
     }
@@ -173,9 +188,12 @@ extern "C" rtcc_status rtcc_memory_attention(const rtcc_attn_config* c, const vo
     long long most = tc ? (steps + 3) / 4 : steps;
     if (most > room / a.streams) most = room / a.streams;
     if (most > 0x7FFFFFFF / units) most = 0x7FFFFFFF / units;
-    long long chunks = tc ? tc_chunks(units, steps, most, sms, a.streams, a.n_q, a.heads, a.dim)
-                          : rows_chunks(units, c->n_seqs, steps, most, sms);
-    const long long joined = tc ? 1 : rows_cluster(units, steps, chunks, sms, a.dim);
+    const long long sums = tc ? a.streams : 4;     // of a block
+    const long long least = (max_k + sums * kSumKeys - 1) / (sums * kSumKeys);
+    long long chunks = tc ? tc_chunks(units, steps, least, most, sms, a.streams, a.n_q, a.heads, a.dim)
+                          : rows_chunks(units, c->n_seqs, steps, least, most, sms);
+    if (tc && max_k / (chunks * sums) > kLongSum) continue;
+    const long long joined = tc ? 1 : rows_cluster(units, steps, chunks, least, sms, a.dim);
     a.cluster = joined > 1;
     if (a.cluster) chunks = joined;
     a.n_chunks = (int)chunks;

@@ -5,6 +5,8 @@ happens when a launch or a wait fails.
 Tolerances are those of test_gpu_tokens.py (u: the storage type's unit roundoff,
 d: a score's error, A = sum_j p_j |v_j|), unless a test derives its own.
 """
+import math
+
 import numpy as np
 import pytest
 
@@ -43,3 +45,47 @@ def test_append_token_places_up_to_2_to_the_31(R):
     for lo in range(5, n, 1 << 28):
         assert bool((rows[lo:lo + (1 << 28)] == -1).all()), lo
     assert bool((buf[:guard] == -77).all()) and bool((buf[guard + n:] == -77).all())
+
+
+# ---------------------------------------------------------------------------
+# attention
+# ---------------------------------------------------------------------------
+
+def attend(R, q, k, v, n=None, m=None, dtype="fp16", begin=None, prefix=None, workspace=0, lse=True, out=None, **kw):
+    """One call over whole tensors [rows][heads][dim]; `n` and `m` are the sequences'
+    tokens and keys (default: one sequence of everything).  Returns (out, lse)."""
+    n, m = [q.shape[0]] if n is None else n, [k.shape[0]] if m is None else m
+    off, b = i32(np.concatenate([[0], np.cumsum(n)])), i32(np.concatenate([[0], np.cumsum(m)[:-1]]) if begin is None else begin)
+    e = b + i32(m)
+    p = None if prefix is None else i32(prefix)
+    out = torch.full_like(q, 7.0) if out is None else out
+    ls = torch.full(q.shape[:2], 7.0, device="cuda")
+    ws = torch.full((max(workspace, 16),), 0xFF, dtype=torch.uint8, device="cuda")
+    cfg = R.attn_config(q.shape[1], k.shape[1], q.shape[2], R.BF16 if dtype == "bf16" else R.FP16, q.shape[0], k.shape[0],
+                        q.stride()[:2], k.stride()[:2], v.stride()[:2], out.stride()[:2], len(n), max(n), max(m), **kw)
+    R.check(R.rtcc_memory_attention(cfg, q.data_ptr(), k.data_ptr(), v.data_ptr(), off.data_ptr(), b.data_ptr(),
+                                    e.data_ptr(), None if p is None else p.data_ptr(), None, None, None, None,
+                                    out.data_ptr(), ls.data_ptr() if lse else None, ws.data_ptr() if workspace else None,
+                                    workspace, 0))
+    torch.cuda.synchronize()
+    return out, ls
+
+
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+@pytest.mark.parametrize("n,heads,lg,workspace", [(200, 1, 20, 64 << 20), (40, 2, 19, 64 << 20), (40, 1, 22, 0), (1, 1, 22, 1 << 20),
+                                                  (2, 8, 20, 0), (1, 160, 20, 64 << 20)])
+def test_attention_sums_over_many_equal_keys(R, n, heads, lg, workspace, dtype):
+    """Equal scores over 2^19 to 2^22 keys.  The sums lose at most a unit in the last
+    place per 16 keys: 2^-12 of a part of 65,536 keys, besides the usual 2 u + 2^-20."""
+    m, dt = 1 << lg, torch.float16 if dtype == "fp16" else torch.bfloat16
+    g = torch.Generator(device="cuda")
+    g.manual_seed(lg)
+    k = torch.zeros(m, heads, 8, device="cuda", dtype=dt)
+    v = torch.rand(m, heads, 8, generator=g, device="cuda").to(dt)
+    q = torch.zeros(n, heads, 8, device="cuda", dtype=dt)
+    out, lse = attend(R, q, k, v, dtype=dtype, workspace=workspace)
+    want = v.double().mean(0)
+    u = 2.0 ** -11 if dtype == "fp16" else 2.0 ** -8
+    err = (out.double() - want).abs() / want
+    assert float(err.max()) <= 2 * u + 2.0 ** -12 + 2.0 ** -20
+    assert float((lse.double() - lg * math.log(2)).abs().max()) <= 2.0 ** -20 * (1 + lg)
