@@ -553,9 +553,10 @@ typedef struct {
  * more parts than fill the GPU, or than one for 65,536 keys, are not made, and
  * without room for two (NULL, or too small) spans are not split.  A float32 sum
  * over n equally weighted keys of a part may come out smaller by n 2^-28 of
- * itself, so long spans want a workspace (and max_k).  scale, cap and scale / cap are finite, cap not
- * negative; n_q * heads is below 2^31, heads at most 4096.  q, k, v, out and
- * the workspace are 16-byte aligned, d_k_pos 8-byte, the rest 4-byte.
+ * itself, so long spans want a workspace (and max_k).  scale, cap and scale / cap
+ * are finite, cap not negative; n_rows and n_q * heads are at most 2^31 - 2^16,
+ * heads at most 4096.  q, k, v, out and the workspace are 16-byte aligned, d_k_pos
+ * 8-byte, the rest 4-byte.
  */
 rtcc_status rtcc_memory_attention(const rtcc_attn_config* cfg, const void* d_q, const void* d_k,
                                   const void* d_v, const int32_t* d_q_offsets,

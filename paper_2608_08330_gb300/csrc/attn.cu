@@ -118,7 +118,7 @@ extern "C" rtcc_status rtcc_memory_attention(const rtcc_attn_config* c, const vo
   if (c->heads < 1 || c->heads > 4096 || c->kv_heads < 1 || c->heads % c->kv_heads) return RTCC_E_ARG;
   if (c->head_dim < 8 || c->head_dim > 128 || c->head_dim % 8) return RTCC_E_ARG;
   if (c->n_q < 0 || c->n_rows < 0 || c->n_seqs < 0 || c->max_q < 0 || c->max_k < 0) return RTCC_E_ARG;
-  if ((long long)c->n_q * c->heads > 0x7FFFFFFFLL) return RTCC_E_ARG;
+  if ((long long)c->n_q * c->heads > kMaxRows || c->n_rows > kMaxRows) return RTCC_E_ARG;
   const int64_t strides[] = {c->q_row, c->q_head, c->k_row, c->k_head, c->v_row, c->v_head, c->out_row, c->out_head};
   for (int64_t s : strides)
     if (bad_stride(s)) return RTCC_E_ARG;

@@ -9,6 +9,9 @@ namespace rtcc {
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr int kMaxSlots = 64;
+// Largest row number, and number of (token, head) rows: 32-bit key and row numbers
+// go past the last one by less than a step of a block or of its copies' ring.
+constexpr long long kMaxRows = (1LL << 31) - (1 << 16);
 
 struct AttnArgs {
   const void *q, *k, *v;
@@ -53,7 +56,7 @@ __device__ __forceinline__ AttnSpan attn_span(const AttnArgs& A, int seq) {
 // Keys [0, n) of the span that token i of the sequence sees (slots aside).
 __device__ __forceinline__ int attn_visible(const AttnArgs& A, const AttnSpan& s, int i) {
   if (!A.causal) return s.nk;
-  return max(0, min(s.nk, max(s.prefix, i + 1 + s.nk - s.nq)));
+  return max(0, max(s.prefix, s.nk - (s.nq - 1 - i)));   // prefix <= nk, i < nq
 }
 
 // Slot of a memory row (there are at most 64).

@@ -160,7 +160,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) k_attn_rows(const __grid_const
   const T* kbase = static_cast<const T*>(A.k) + (long long)kvh * A.k_head;
   const T* vbase = static_cast<const T*>(A.v) + (long long)kvh * A.v_head;
 
-  for (int rg = rg0; rg * kRows < rows_all; rg += A.row_groups) {
+  for (int rg = rg0; (long long)rg * kRows < rows_all; rg += A.row_groups) {
     const int r0 = rg * kRows;
     // this lane's two rows: lane / 4 and 8 further
     int hi[2], head[2];

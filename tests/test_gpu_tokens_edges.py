@@ -89,3 +89,17 @@ def test_attention_sums_over_many_equal_keys(R, n, heads, lg, workspace, dtype):
     err = (out.double() - want).abs() / want
     assert float(err.max()) <= 2 * u + 2.0 ** -12 + 2.0 ** -20
     assert float((lse.double() - lg * math.log(2)).abs().max()) <= 2.0 ** -20 * (1 + lg)
+
+
+@pytest.mark.parametrize("n,workspace", [(1, 0), (1, 1 << 20), (3, 1 << 20), (40, 0), (40, 32 << 20), (200, 32 << 20)])
+def test_attention_spans_up_to_the_limit(R, n, workspace):
+    """2^31 - 2^16 equal keys and values: out is the value, lse the visible keys' logarithm (causal).
+    Few rows read one row over and over (strides of 0); many need the rows themselves."""
+    m = 2 ** 31 - 2 ** 16
+    k = torch.full((1 if n <= 32 else m, 1, 8), 0.5, device="cuda", dtype=torch.float16)
+    k = k.expand(m, 1, 8)
+    q = torch.zeros(n, 1, 8, device="cuda", dtype=torch.float16)
+    out, lse = attend(R, q, k, k, workspace=workspace, causal=True)
+    assert bool((out == 0.5).all())
+    want = torch.log(torch.arange(m - n + 1, m + 1, device="cuda", dtype=torch.float64))
+    assert float((lse[:, 0].double() - want).abs().max()) <= 2.0 ** -20 * 23

@@ -1,0 +1,22 @@
+"""Refusals of the token-memory calls at the edges of their ranges, without a GPU."""
+import pytest
+
+from tests.test_tokens_cpu import P, attend, attn_cfg
+from paper_2608_08330_gb300 import build as B
+
+
+@pytest.fixture(scope="module")
+def R():
+    B.build()
+    from paper_2608_08330_gb300 import rtcc
+    rtcc.load()
+    return rtcc
+
+
+def test_attention_refuses_row_numbers_that_would_wrap(R):
+    limit = 2 ** 31 - 2 ** 16
+    for kw in (dict(n_rows=limit + 1), dict(n_rows=2 ** 31 - 1), dict(n_q=limit // 4 + 1), dict(n_q=(2 ** 31 - 1) // 4)):
+        assert attend(R, attn_cfg(R, **kw)) == R.E_ARG, kw
+    # a call of the largest sizes with nothing to do is none of these
+    assert attend(R, attn_cfg(R, n_rows=limit, n_q=limit // 4, n_seqs=0)) == R.OK
+    assert attend(R, attn_cfg(R, n_rows=limit, n_q=0), q=None, out=None, present=P) == R.E_ARG    # no slots given
