@@ -108,9 +108,10 @@ __device__ __forceinline__ void split2(float a, float b, uint32_t& hi, uint32_t&
 }
 
 // tanh(u) = 1 - 2 / (1 + e^2u): its absolute error (about 2e-7) is what counts
-// here, since the cap multiplies it into a score.
+// here, since the cap multiplies it into a score.  An infinite e^2u gives 1, a NaN
+// stays one (a minimum in its place would turn it into a score of the cap).
 __device__ __forceinline__ float tanh_abs(float u) {
-  return 1.0f - __fdividef(2.0f, 1.0f + exp2f(fminf(2.0f * kLog2e * u, 64.0f)));
+  return 1.0f - __fdividef(2.0f, 1.0f + exp2f(2.0f * kLog2e * u));
 }
 
 // Byte offset of 16-byte unit c of row r in a tile of DP-channel rows; units

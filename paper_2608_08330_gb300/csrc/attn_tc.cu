@@ -189,7 +189,7 @@ __device__ __forceinline__ float ex2(float x) {
   return y;
 }
 __device__ __forceinline__ float tanh_abs(float u) {
-  return 1.0f - __fdividef(2.0f, 1.0f + ex2(fminf(2.0f * kLog2e * u, 64.0f)));
+  return 1.0f - __fdividef(2.0f, 1.0f + ex2(2.0f * kLog2e * u));   // a NaN stays one
 }
 __device__ __forceinline__ float2 both(float a) { return make_float2(a, a); }
 

@@ -11,6 +11,7 @@ import numpy as np
 import pytest
 
 from tests import gpu_util as U
+from tests.test_gpu_tokens import Case
 
 pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
@@ -103,3 +104,36 @@ def test_attention_spans_up_to_the_limit(R, n, workspace):
     assert bool((out == 0.5).all())
     want = torch.log(torch.arange(m - n + 1, m + 1, device="cuda", dtype=torch.float64))
     assert float((lse[:, 0].double() - want).abs().max()) <= 2.0 ** -20 * 23
+
+
+@pytest.mark.parametrize("n", [1, 200])
+@pytest.mark.parametrize("m", [40, 300])
+@pytest.mark.parametrize("dist", [False, True])
+def test_attention_nan_stays_nan_under_a_cap(R, n, m, dist):
+    """A NaN in a query makes its row NaN, and one in a key every row of its head, also where scores are
+    capped; other rows keep their bits."""
+    ref = Case([n, 5], [m, 300], heads=2, kv=2, cap=30.0, dist=dist).run(R).check()
+    c = Case([n, 5], [m, 300], heads=2, kv=2, cap=30.0, dist=dist)
+    c.q[0, 0, 3] = float("nan")
+    c.k[m // 2, 1, 7] = float("nan")                 # of the first sequence
+    c.run(R)
+    torch.cuda.synchronize()
+    bad = torch.zeros(n + 5, 2, dtype=torch.bool, device="cuda")
+    bad[0, 0] = True
+    bad[:n, 1] = True
+    assert bool(torch.isnan(c.out[bad]).all()) and bool(torch.isnan(c.lse[bad]).all())
+    assert torch.equal(c.out[~bad], ref.out[~bad]) and torch.equal(c.lse[~bad], ref.lse[~bad])
+
+
+@pytest.mark.parametrize("n", [1, 200])
+def test_attention_infinite_scores_reach_the_cap(R, n):
+    """Scores of +-infinity are the cap and its negative."""
+    q = torch.zeros(n, 1, 64, device="cuda", dtype=torch.bfloat16)
+    k = torch.zeros(130, 1, 64, device="cuda", dtype=torch.bfloat16)
+    q[:, 0, 0], k[7, 0, 0], k[100, 0, 0] = 3e38, 3e38, -3e38
+    v = torch.zeros_like(k)
+    v[7] = 1
+    out, lse = attend(R, q, k, v, dtype="bf16", scale=1.0, cap=3.0)
+    total = 128 + math.exp(3) + math.exp(-3)
+    assert float((out.double() - math.exp(3) / total).abs().max()) <= 2 * 2.0 ** -8 * math.exp(3) / total
+    assert float((lse.double() - math.log(total)).abs().max()) <= 4e-7 * 3 + 2.0 ** -20 * (1 + math.log(total))
