@@ -165,11 +165,8 @@ extern "C" rtcc_status rtcc_memory_attention(const rtcc_attn_config* c, const vo
   const int max_k = c->max_k < 1 ? 1 : c->max_k > c->n_rows ? (c->n_rows < 1 ? 1 : c->n_rows) : c->max_k;
   const bool bf16 = c->dtype == RTCC_BF16;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  // The tensor-core kernel from kTcRows (token, head) rows per key head on.  It
-  // needs a positive scale (its maximum is taken over unscaled scores) and a cap
-  // its polynomial's coefficients can express.
-  bool tc = (long long)max_q * a.group > kTcRows && a.group <= 128 && c->scale > 0.f && a.scale_log2 < 1e4f &&
-            c->n_rows > 0;
+  // the tensor-core kernel from kTcRows (token, head) rows per key head on
+  bool tc = (long long)max_q * a.group > kTcRows && a.group <= 128 && c->n_rows > 0;
   const size_t part = (size_t)c->n_q * c->heads * (c->head_dim * sizeof(float) + sizeof(float2));
   const long long room = d_workspace ? (long long)(workspace_bytes / part) : 0;
   for (;; tc = false) {

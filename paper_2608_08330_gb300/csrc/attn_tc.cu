@@ -47,6 +47,9 @@
 // the two forms push each other out of the instruction cache), blocks that take over
 // the work of those not yet begun (up to 30 %: the roles change over one after the
 // other), and results through shared memory to whole lines (4 %).
+#include <float.h>
+#include <math.h>
+
 #include <type_traits>
 
 #include "attn.cuh"
@@ -87,9 +90,13 @@ struct TcMaps {
   CUtensorMap q, k, v;
 };
 
-// coefficients of cap tanh(x scale / cap) log2(e) = x (c0 + w (c1 + w (c2 + w c3))), w = x^2
+// coefficients of cap tanh(x scale / cap) log2(e) = x (c0 + w (c1 + w (c2 + w c3))), w = x^2,
+// for |x| <= limit.  They work on scores before the scale, which saves a product, so
+// with a small scale / cap (1e-5, say) they leave float32's range: the limit is 0 then,
+// and every step takes the form with tanh itself.
 struct TanhPoly {
   float c[4];
+  float limit;
 };
 
 __device__ __forceinline__ void tmem_ld32_issue(uint32_t a, float* x) {
@@ -622,7 +629,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1)
       };
       while (k.live()) {
         const bool edge = k.partial || k.t * kKeys + kKeys > all_see;
-        if (begun && !edge) {
+        if (begun && !edge && (!CAP || poly.limit > 0.f)) {
           // going back, no further step is at the edge unless a slot is absent
           int run = all ? (k.t - k.t0) / streams + 1 : 1;
           bool slow = false;
@@ -685,7 +692,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1)
 #pragma unroll
                   for (int u = 0; u < G; ++u) x2[i + u] = fma2(x2[i + u], both(A.scale_log2), a[u]);
                 } else {
-                  // an odd polynomial: |error| <= 1.5e-7 cap for |x| <= cap / 2
+                  // an odd polynomial: |error| <= 2e-7 cap for scaled |x| <= cap / 2
                   float2 w2[G], p[G];
 #pragma unroll
                   for (int u = 0; u < G; ++u) {
@@ -721,9 +728,9 @@ __global__ void __launch_bounds__(kWarps * 32, 1)
               }
             }
             const float top = fmaxf(t0, t1);
-            if (__any_sync(0xFFFFFFFFu, valid && ((CAP && !(b0 * A.scale_log2 <= 0.5f)) || top > kSlack))) {
+            if (__any_sync(0xFFFFFFFFu, valid && ((CAP && !(b0 <= poly.limit)) || top > kSlack))) {
               // too large for the polynomial, or for P; or m lags behind from here on
-              slow = __any_sync(0xFFFFFFFFu, valid && ((CAP && !(b0 * A.scale_log2 <= 0.5f)) || top > kHard));
+              slow = __any_sync(0xFFFFFFFFu, valid && ((CAP && !(b0 <= poly.limit)) || top > kHard));
               if (slow) break;
               if (valid && top > kSlack) late = fmaxf(late, top);
               lagging = true;
@@ -871,13 +878,16 @@ __global__ void __launch_bounds__(kWarps * 32, 1)
 
 template <typename T, int DP>
 cudaError_t launch_tc_t(const AttnArgs& a, const TcMaps& m, cudaStream_t st) {
-  // tanh(u) / u on |u| <= 1/2 in w = u^2, least largest |error| of u p(w): 1.4e-7
+  // tanh(u) / u on |u| <= 1/2 in w = u^2, least largest |error| of u p(w): 1.4e-7, and
+  // up to 2e-7 as float32 computes it
   constexpr double kTanh[4] = {0.9999974621104636, -0.3331988899884361, 0.13138806507278963,
                                 -0.04322690737438131};
   TanhPoly poly{};
   if (a.cap_log2 > 0.f) {
     double f = (double)a.cap_log2 * a.scale_log2;
     for (int i = 0; i < 4; ++i, f *= (double)a.scale_log2 * a.scale_log2) poly.c[i] = (float)(f * kTanh[i]);
+    const float limit = fabsf(0.5f / a.scale_log2), c3 = fabsf(poly.c[3]);
+    poly.limit = c3 >= FLT_MIN && c3 <= FLT_MAX && limit * limit <= FLT_MAX ? limit : 0.f;
   }
   const bool cap = a.cap_log2 > 0.f, dist = a.slopes != nullptr;
   auto kern = cap ? (dist ? k_attn_tc<T, DP, true, true> : k_attn_tc<T, DP, true, false>)

@@ -137,3 +137,35 @@ def test_attention_infinite_scores_reach_the_cap(R, n):
     total = 128 + math.exp(3) + math.exp(-3)
     assert float((out.double() - math.exp(3) / total).abs().max()) <= 2 * 2.0 ** -8 * math.exp(3) / total
     assert float((lse.double() - math.log(total)).abs().max()) <= 4e-7 * 3 + 2.0 ** -20 * (1 + math.log(total))
+
+
+@pytest.mark.parametrize("n", [3, 200])
+@pytest.mark.parametrize("dist", [False, True])
+@pytest.mark.parametrize("scale,sq,sk,dtype", [
+    (1e-4, 150, 4, "fp16"), (1e-5, 150, 100, "fp16"), (1e-6, 500, 300, "fp16"), (1e-9, 1e4, 1e4, "bf16"),
+    (1e-19, 1e9, 1e9, "bf16"), (-0.3, 3, 3, "fp16"), (-1e-5, 150, 100, "fp16")])
+def test_attention_scales_and_caps(R, n, dist, scale, sq, sk, dtype):
+    """Capped scores of up to 0.45 of the cap from queries and keys of any size, with scales down to 1e-19."""
+    c = Case([n], [700], heads=2, kv=1, cap=30.0, dtype=dtype, dim=8, dist=dist)
+    a = 0.45 * c.cap / (8 * abs(scale) * sq * sk)
+    c.q.copy_(torch.sign(c.q) * sq * a)
+    c.k.copy_(torch.sign(c.k) * sk)
+    c.scale = scale
+    c.run(R).check()
+
+
+@pytest.mark.parametrize("n", [3, 200])
+@pytest.mark.parametrize("scale,cap", [(-0.2, 0.0), (0.0, 0.0), (0.0, 20.0), (2.0, 1e-4), (30.0, 1e-4), (0.1, 1e-8)])
+def test_attention_scales_of_any_sign_and_size(R, n, scale, cap):
+    for dist in (False, True):
+        c = Case([n, 3], [700, 90], heads=2, kv=1, cap=cap, dist=dist)
+        c.scale = scale
+        if scale < 0:                                # the check's score size is a magnitude
+            c.q.neg_()
+            ref = Case([n, 3], [700, 90], heads=2, kv=1, cap=cap, dist=dist)
+            ref.scale = -scale
+            c.run(R)
+            ref.run(R).check()
+            assert torch.equal(c.out, ref.out) and torch.equal(c.lse, ref.lse)
+        else:
+            c.run(R).check()
