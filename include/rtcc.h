@@ -554,7 +554,9 @@ typedef struct {
  * without room for two (NULL, or too small) spans are not split.  A float32 sum
  * over n equally weighted keys of a part may come out smaller by n 2^-28 of
  * itself, so long spans want a workspace (and max_k).  scale, cap and scale / cap
- * are finite, cap not negative; n_rows and n_q * heads are at most 2^31 - 2^16,
+ * are finite, cap between 0 and 1e38, scale / cap 0 or at least 2^-126 in
+ * magnitude; capped scores are good to 2e-7 of the cap for caps up to 256, to 1e-6 of
+ * themselves above.  n_rows and n_q * heads are at most 2^31 - 2^16,
  * heads at most 4096.  q, k, v, out and the workspace are 16-byte aligned, d_k_pos
  * 8-byte, the rest 4-byte.
  */

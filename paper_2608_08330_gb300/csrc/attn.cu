@@ -1,5 +1,6 @@
 // Host side of the attention over the token memory: argument checks, the
 // choice of kernel and of the split of long spans.
+#include <float.h>
 #include <math.h>
 
 #include <algorithm>
@@ -123,7 +124,10 @@ extern "C" rtcc_status rtcc_memory_attention(const rtcc_attn_config* c, const vo
   for (int64_t s : strides)
     if (bad_stride(s)) return RTCC_E_ARG;
   if (!isfinite(c->scale) || !isfinite(c->cap) || c->cap < 0.f) return RTCC_E_ARG;
-  if (c->cap > 0.f && !isfinite(c->scale / c->cap)) return RTCC_E_ARG;
+  if (c->cap > 0.f) {
+    const float ratio = fabsf(c->scale / c->cap);
+    if (c->cap > 1e38f || !isfinite(ratio) || (ratio < FLT_MIN && c->scale != 0.f)) return RTCC_E_ARG;
+  }
   if (c->n_slots < 0 || c->n_slots > kMaxSlots || (c->n_slots > 0) != (d_present != nullptr)) return RTCC_E_ARG;
   if (c->n_slots > 0 && (c->slot_rows < 1 || (long long)c->n_slots * c->slot_rows < c->n_rows)) return RTCC_E_ARG;
   if ((d_slopes != nullptr) != (d_q_pos != nullptr) || (d_slopes != nullptr) != (d_k_pos != nullptr)) return RTCC_E_ARG;

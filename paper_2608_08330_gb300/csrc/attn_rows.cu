@@ -107,13 +107,6 @@ __device__ __forceinline__ void split2(float a, float b, uint32_t& hi, uint32_t&
   lo = Store<T>::pack2(a - h.x, b - h.y);
 }
 
-// tanh(u) = 1 - 2 / (1 + e^2u): its absolute error (about 2e-7) is what counts
-// here, since the cap multiplies it into a score.  An infinite e^2u gives 1, a NaN
-// stays one (a minimum in its place would turn it into a score of the cap).
-__device__ __forceinline__ float tanh_abs(float u) {
-  return 1.0f - __fdividef(2.0f, 1.0f + exp2f(2.0f * kLog2e * u));
-}
-
 // Byte offset of 16-byte unit c of row r in a tile of DP-channel rows; units
 // are permuted within 128-byte lines so that ldmatrix reads 8 rows without
 // bank conflicts.
@@ -157,7 +150,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) k_attn_rows(const __grid_const
   const unsigned long long slots = attn_slot_mask(A, lane);
   const uint32_t ring = smem_u32(smem) + w * kStages * C::kStageBytes;
   const unsigned char* ring_g = smem + w * kStages * C::kStageBytes;
-  const bool dist = A.slopes != nullptr;
+  const bool dist = A.slopes != nullptr, far_cap = A.cap_log2 > kAbsCap * kLog2e;
   const T* kbase = static_cast<const T*>(A.k) + (long long)kvh * A.k_head;
   const T* vbase = static_cast<const T*>(A.v) + (long long)kvh * A.v_head;
 
@@ -270,7 +263,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) k_attn_rows(const __grid_const
           for (int i = 0; i < 4; ++i) {
             const int key = n * 8 + (lane & 3) * 2 + (i & 1), rr = i >> 1;
             float x = s[n][i] * A.scale_log2;
-            if (A.cap_log2 > 0.f) x = A.cap_log2 * tanh_abs(x);
+            if (A.cap_log2 > 0.f) x = A.cap_log2 * (far_cap ? tanh_rel(x) : tanh_abs(x));
             if (dist) {
               const float2 p = ps[key];
               x = fmaf(-slope[rr], fabsf(qy[rr] - p.x) + fabsf(qx[rr] - p.y), x);

@@ -93,7 +93,7 @@ struct TcMaps {
 // coefficients of cap tanh(x scale / cap) log2(e) = x (c0 + w (c1 + w (c2 + w c3))), w = x^2,
 // for |x| <= limit.  They work on scores before the scale, which saves a product, so
 // with a small scale / cap (1e-5, say) they leave float32's range: the limit is 0 then,
-// and every step takes the form with tanh itself.
+// as for caps above kAbsCap, and every step takes the form with tanh itself.
 struct TanhPoly {
   float c[4];
   float limit;
@@ -190,14 +190,6 @@ __device__ __forceinline__ uint64_t desc_v(uint32_t saddr) {
   return d;
 }
 
-__device__ __forceinline__ float ex2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-__device__ __forceinline__ float tanh_abs(float u) {
-  return 1.0f - __fdividef(2.0f, 1.0f + ex2(2.0f * kLog2e * u));   // a NaN stays one
-}
 __device__ __forceinline__ float2 both(float a) { return make_float2(a, a); }
 
 // A walk over the steps of a chunk that have a key in a present slot, and their
@@ -758,9 +750,16 @@ __global__ void __launch_bounds__(kWarps * 32, 1)
           const uint32_t bits = (uint32_t)(keep >> c);
           float top = -INFINITY;
 #pragma unroll
+          for (int i = 0; i < 32; ++i) y[i] *= A.scale_log2;
+          if (CAP && A.cap_log2 <= kAbsCap * kLog2e) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) y[i] = A.cap_log2 * tanh_abs(y[i]);
+          } else if (CAP) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) y[i] = A.cap_log2 * tanh_rel(y[i]);
+          }
+#pragma unroll
           for (int i = 0; i < 32; ++i) {
-            y[i] *= A.scale_log2;
-            if (CAP) y[i] = A.cap_log2 * tanh_abs(y[i]);
             if (DIST) y[i] = fmaf(fabsf(py[c + i] + qy) + fabsf(py[kKeys + c + i] + qx), slope, y[i]);
             y[i] = (bits >> i) & 1 ? y[i] - m0 : -INFINITY;
             top = fmaxf(top, y[i]);
@@ -887,7 +886,8 @@ cudaError_t launch_tc_t(const AttnArgs& a, const TcMaps& m, cudaStream_t st) {
     double f = (double)a.cap_log2 * a.scale_log2;
     for (int i = 0; i < 4; ++i, f *= (double)a.scale_log2 * a.scale_log2) poly.c[i] = (float)(f * kTanh[i]);
     const float limit = fabsf(0.5f / a.scale_log2), c3 = fabsf(poly.c[3]);
-    poly.limit = c3 >= FLT_MIN && c3 <= FLT_MAX && limit * limit <= FLT_MAX ? limit : 0.f;
+    const bool range = c3 >= FLT_MIN && c3 <= FLT_MAX && limit * limit <= FLT_MAX;
+    poly.limit = range && a.cap_log2 <= kAbsCap * kLog2e ? limit : 0.f;
   }
   const bool cap = a.cap_log2 > 0.f, dist = a.slopes != nullptr;
   auto kern = cap ? (dist ? k_attn_tc<T, DP, true, true> : k_attn_tc<T, DP, true, false>)

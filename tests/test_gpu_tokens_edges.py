@@ -169,3 +169,24 @@ def test_attention_scales_of_any_sign_and_size(R, n, scale, cap):
             assert torch.equal(c.out, ref.out) and torch.equal(c.lse, ref.lse)
         else:
             c.run(R).check()
+
+
+@pytest.mark.parametrize("n", [2, 200])
+@pytest.mark.parametrize("cap", [300.0, 1e4, 1e5, 1e6, 1e30])
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+def test_attention_large_caps_keep_relative_scores(R, n, cap, dtype):
+    """Far above the scores a cap does next to nothing.  A capped score's error is 2^-20 of itself (tanh) and
+    three roundings of 2^-24, besides the product's (float32 sums of 64 terms); no part of the cap."""
+    c = Case([n], [700], heads=2, kv=1, cap=cap, dtype=dtype, spread=8.0).run(R)
+    torch.cuda.synchronize()
+    u = 2.0 ** -11 if dtype == "fp16" else 2.0 ** -8
+    for h in range(2):
+        q, k, v = c.q[:, h].double(), c.k[:, 0].double(), c.v[:, 0].double()
+        x = cap * torch.tanh(c.scale * (q @ k.T) / cap)
+        lse = torch.logsumexp(x, 1)
+        p = torch.exp(x - lse[:, None])
+        size = c.scale * float((q.abs() @ k.abs().T).max())
+        d = 2.0 ** -23 * 8 * size + (2.0 ** -20 + 3 * 2.0 ** -24) * float(x.abs().max()) + 2.0 ** -21
+        err = (c.out[:, h].double() - p @ v).abs()
+        assert bool((err <= (2 * u + 2 * d + 2.0 ** -20) * (p @ v.abs())).all())
+        assert bool(((c.lse[:, h].double() - lse).abs() <= d + 2.0 ** -20 * (1 + lse.abs())).all())

@@ -20,3 +20,10 @@ def test_attention_refuses_row_numbers_that_would_wrap(R):
     # a call of the largest sizes with nothing to do is none of these
     assert attend(R, attn_cfg(R, n_rows=limit, n_q=limit // 4, n_seqs=0)) == R.OK
     assert attend(R, attn_cfg(R, n_rows=limit, n_q=0), q=None, out=None, present=P) == R.E_ARG    # no slots given
+
+
+def test_attention_refuses_caps_out_of_range(R):
+    for kw in (dict(cap=1.1e38), dict(cap=1e30, scale=1e-19), dict(cap=1e-38, scale=100.0)):
+        assert attend(R, attn_cfg(R, **kw)) == R.E_ARG, kw
+    for kw in (dict(cap=1e38, scale=2.0), dict(cap=1e30, scale=0.0), dict(cap=1e-38, scale=1.0)):
+        assert attend(R, attn_cfg(R, n_seqs=0, **kw)) == R.OK, kw
