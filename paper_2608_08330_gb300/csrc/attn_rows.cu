@@ -290,13 +290,18 @@ __global__ void __launch_bounds__(kWarps * 32, 2) k_attn_rows(const __grid_const
             }
           }
         }
+        // a tile's sum first: one by one, small probabilities behind a large one would
+        // round to nothing (2^-25 of it each)
+        float sum[2] = {0.f, 0.f};
 #pragma unroll
         for (int n = 0; n < KT / 8; ++n)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             s[n][i] = exp2f(s[n][i] - top[i >> 1]);
-            l[i >> 1] += s[n][i];
+            sum[i >> 1] += s[n][i];
           }
+        l[0] += sum[0];
+        l[1] += sum[1];
 #pragma unroll
         for (int kk = 0; kk < KT / 16; ++kk) {
           // probabilities as two terms of the storage type, so that their rounding

@@ -793,12 +793,14 @@ __global__ void __launch_bounds__(kWarps * 32, 1)
             m = up;
           }
           uint32_t pk[16];
+          float sum = 0.f;
 #pragma unroll
           for (int i = 0; i < 32; i += 2) {
             const float v0 = ex2(y[i] - up), v1 = ex2(y[i + 1] - up);
-            l += v0 + v1;
+            sum += v0 + v1;
             pk[i / 2] = Store<T>::pack2(v0, v1);
           }
+          l += sum;
           tmem_st16(ts + c / 2, pk);
           tmem_st_wait();
           if (l != l && m == -INFINITY) m = 0.f;         // a NaN row never gets a maximum: it is done with

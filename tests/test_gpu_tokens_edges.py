@@ -190,3 +190,18 @@ def test_attention_large_caps_keep_relative_scores(R, n, cap, dtype):
         err = (c.out[:, h].double() - p @ v).abs()
         assert bool((err <= (2 * u + 2 * d + 2.0 ** -20) * (p @ v.abs())).all())
         assert bool(((c.lse[:, h].double() - lse).abs() <= d + 2.0 ** -20 * (1 + lse.abs())).all())
+
+
+@pytest.mark.parametrize("dim", [8, 72])
+@pytest.mark.parametrize("heads,n,cap", [(160, 1, 0.0), (1, 200, 0.0), (1, 200, 1e6)])
+def test_attention_sums_keep_small_probabilities(R, heads, n, cap, dim):
+    """262,143 keys 2^-25 below the first one in the sum of their exponentials.  A warp (of four, few rows)
+    or a row (many) adds n keys to one float32 sum: n 2^-28 of it may go, besides the usual 2^-20."""
+    m = 1 << 18
+    q = torch.zeros(n, heads, dim, device="cuda", dtype=torch.bfloat16)
+    k = torch.zeros(m, heads, dim, device="cuda", dtype=torch.bfloat16)
+    q[:, :, 0], k[0, :, 0] = 1, 25
+    _, lse = attend(R, q, k, k, dtype="bf16", scale=math.log(2), cap=cap)
+    want = 25 * math.log(2) + math.log1p((m - 1) * 2.0 ** -25)
+    lim = m * 2.0 ** -28 / (4 if n == 1 else 1) + 2.0 ** -20 * (1 + want) + 25 * 2.0 ** -20 + 2.0 ** -21
+    assert float((lse.double() - want).abs().max()) <= lim
