@@ -537,7 +537,8 @@ typedef struct {
  * A token that sees no key gets out = 0 and lse = -inf.  Sums and the softmax
  * are float32; for their product with v the probabilities are rounded to the
  * storage type, or to the sum of two of its numbers where a key head has few
- * query rows; out is rounded once.  How a span is split depends on the sizes, the
+ * query rows; out is rounded once.  In fp16, whose range is short, a key of a small
+ * probability loses up to 2^-30 (2^-40 with few query rows) of the largest.  How a span is split depends on the sizes, the
  * workspace and the GPU, and changes the order of float32 sums; the same call
  * gives the same bits.  Rows that no token of a sequence sees (outside the span,
  * in an absent slot) are not used: they may hold anything, infinities and NaN

@@ -15,7 +15,9 @@
 // in the tile is zero-filled, so stale or non-finite contents do not matter.
 // The probabilities go to the second product as the sum of two numbers of the
 // storage type: the tensor pipe has room for the second product, and a single
-// token's error then is the output's rounding alone.
+// token's error then is the output's rounding alone.  fp16 ends at 2^-24, so there
+// the largest probability is 2^15 instead of 1: what is lost of a key is 2^-40 of
+// the largest, not 2^-25, which over 280,000 keys would be up to 0.8 % of the weight.
 //
 // With few rows the memory's bytes bound it, and splitting the span into chunks
 // fills the GPU; k_attn_join merges the chunks in index order, or, where the chunks
@@ -24,6 +26,8 @@
 // 128, 1.9 GB: 294 to 297 us, 6.5 TB/s, 95 % of a plain copy's; one token over 4097 keys of
 // 6 heads of 64 takes 8.1 us, most of which is the launch, a block's first copies
 // and three steps.
+#include <type_traits>
+
 #include "attn.cuh"
 #include "kernels.h"
 
@@ -34,6 +38,9 @@ constexpr int kWarps = 4;
 constexpr int kStages = 3;
 constexpr int kRows = 16;
 constexpr int kCluster = 16;                     // blocks of a cluster at most
+
+// log2 of the largest probability (a row's m is its largest score less this)
+template <typename T> constexpr float kLift = std::is_same<T, __half>::value ? 15.0f : 0.0f;
 
 template <int DP> struct RowsCfg {               // DP: head size padded to 64 or 128
   static constexpr int KT = DP == 64 ? 32 : 16;  // keys per tile: 4 KB of keys, 4 KB of values
@@ -276,7 +283,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) k_attn_rows(const __grid_const
         for (int rr = 0; rr < 2; ++rr) {
           top[rr] = fmaxf(top[rr], __shfl_xor_sync(0xFFFFFFFFu, top[rr], 1));
           top[rr] = fmaxf(top[rr], __shfl_xor_sync(0xFFFFFFFFu, top[rr], 2));
-          const float mn = fmaxf(m[rr], top[rr]);
+          const float mn = fmaxf(m[rr], top[rr] - kLift<T>);
           const float base = mn == -INFINITY ? 0.f : mn;
           const float f = exp2f(m[rr] - base);   // m = -inf: 0
           m[rr] = mn;

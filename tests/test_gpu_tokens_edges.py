@@ -205,3 +205,30 @@ def test_attention_sums_keep_small_probabilities(R, heads, n, cap, dim):
     want = 25 * math.log(2) + math.log1p((m - 1) * 2.0 ** -25)
     lim = m * 2.0 ** -28 / (4 if n == 1 else 1) + 2.0 ** -20 * (1 + want) + 25 * 2.0 ** -20 + 2.0 ** -21
     assert float((lse.double() - want).abs().max()) <= lim
+
+
+@pytest.mark.parametrize("heads,n", [(160, 1), (1, 200)])
+@pytest.mark.parametrize("depth", [24.6, 25.1, 30.0])
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+def test_attention_long_tails_count(R, heads, n, depth, dtype):
+    """One key far above 281,599 others, which together hold up to 1 % of the weight.  fp16 may lose 2^-40
+    (few rows) or 2^-30 (many) of the largest probability per key, and a float32 sum over n keys (all of them,
+    or a warp's quarter) n 2^-28 of itself."""
+    m, dt = 281600, torch.float16 if dtype == "fp16" else torch.bfloat16
+    q = torch.zeros(n, heads, 8, device="cuda", dtype=dt)
+    q[:, :, :2] = 1
+    u = 2.0 ** -11 if dtype == "fp16" else 2.0 ** -8
+    for near in (0, 150000, m - 1):
+        k = torch.zeros(m, heads, 8, device="cuda", dtype=dt)
+        k[near, :, 0], k[near, :, 1] = math.floor(depth), depth - math.floor(depth)
+        x = float(k[near, 0, :2].double().sum())
+        v = torch.full_like(k, -1.0)
+        v[near] = 1
+        out, lse = attend(R, q, k, v, dtype=dtype, scale=math.log(2))
+        rest = (m - 1) * 2.0 ** -x
+        d = 2.0 ** -23 * math.sqrt(8) * x + 2.0 ** -21
+        lost = 0 if dtype == "bf16" else m * (2.0 ** -40 if n == 1 else 2.0 ** -30)
+        sums = m * 2.0 ** -28 / (4 if n == 1 else 1)
+        assert float((out.double() - (1 - rest) / (1 + rest)).abs().max()) <= 2 * u + 2 * d + 2.0 ** -20 + lost + 2 * sums
+        want = x * math.log(2) + math.log1p(rest)
+        assert float((lse.double() - want).abs().max()) <= d + 2.0 ** -20 * (1 + want) + sums
