@@ -771,8 +771,10 @@ __global__ void __launch_bounds__(kWarps * 32, 1)
             y[i] = (bits >> i) & 1 ? y[i] - m0 : -INFINITY;
             top = fmaxf(top, y[i]);
           }
-          // from nothing at once, later past the slack
-          const float up = (m == -INFINITY ? top > -INFINITY : top > kSlack<T>) ? top - kLift<T> : 0.f;
+          // from nothing at once, later past the slack and by whole powers of two: the
+          // probabilities that this step has rounded already are scaled exactly
+          const float rest = top - kLift<T>;
+          const float up = m == -INFINITY ? (top > -INFINITY ? rest : 0.f) : top > kSlack<T> ? ceilf(rest) : 0.f;
           if (__any_sync(0xFFFFFFFFu, up != 0.f && l > 0.f)) {
             const float f = l > 0.f ? up : 0.f;
             if (!(ok = rise(f))) break;

@@ -232,3 +232,21 @@ def test_attention_long_tails_count(R, heads, n, depth, dtype):
         assert float((out.double() - (1 - rest) / (1 + rest)).abs().max()) <= 2 * u + 2 * d + 2.0 ** -20 + lost + 2 * sums
         want = x * math.log(2) + math.log1p(rest)
         assert float((lse.double() - want).abs().max()) <= d + 2.0 ** -20 * (1 + want) + sums
+
+
+def test_attention_rounds_each_probability_once(R):
+    """A row whose maximum rises within a masked-form step, after the step's first 32 probabilities were
+    rounded: 32 keys at 2^7.04, one at 2^8.03, the others, met before, at 1.  (Row 5's scores are twice as
+    large, which makes its warp take that form.)  These values round up by 0.9 u again if scaled by 2^-8.03."""
+    n, u = 200, 2.0 ** -8
+    q = torch.zeros(n, 1, 64, device="cuda", dtype=torch.bfloat16)
+    q[:, 0, :2] = 1
+    q[5, 0, :2] = 2
+    k = torch.zeros(128, 1, 64, device="cuda", dtype=torch.bfloat16)
+    k[:32, 0, 0], k[:32, 0, 1] = 7, 10 / 256
+    k[32, 0, 0], k[32, 0, 1] = 8, 7 / 256
+    d = 2.0 ** -23 * 8 * 16 + 2.0 ** -21
+    for j in range(128):
+        v = torch.full_like(k, 1 + j / 128)
+        out, _ = attend(R, q, k, v, dtype="bf16", scale=math.log(2))
+        assert float((out.double() / (1 + j / 128) - 1).abs().max()) <= 2 * u + 2 * d + 2.0 ** -20, j
