@@ -444,7 +444,8 @@ rtcc_status rtcc_pillarise_noalloc(const rtcc_model_config* cfg, const float* d_
  *   d_seq, d_pos int32 [n_tokens] its sequence and its place in it (may be NULL)
  *   d_begin, d_end int32 [n_seqs] the sequence's rows once its tokens are in
  *   d_length  int32 [n_seqs]      their number, at most capacity
- * A token past its slot's capacity gets row -1; entries past the total get -1
+ * A token past its slot's capacity gets row -1 (causal attention of such a step
+ * wants d_held as its d_q_start); entries past the total get -1
  * in all three token arrays.  Tokens that do not fit into n_tokens are dropped:
  * offsets are cut there, and they do not count towards the length.  Negative
  * counts read as 0, held counts are cut to the capacity, and a negative slot
@@ -520,6 +521,10 @@ typedef struct {
                                        next, >= 2                            */
   float scale;                      /* of q.k, usually 1 / sqrt(head_dim)    */
   float cap;                        /* scores are capped at +-cap; 0: no cap */
+  const int32_t* d_q_start;         /* [n_seqs] place of the sequence's first
+                                       token among its keys, for the causal mask;
+                                       NULL: its tokens are the span's last
+                                       rows                                  */
 } rtcc_attn_config;
 
 /*
@@ -531,8 +536,11 @@ typedef struct {
  *   x = x - slopes[h] * (|dy| + |dx|) if d_slopes is given, with the difference
  *       of the token's d_q_pos and the row's d_k_pos;
  *   key j is visible unless its row lies in a slot whose d_present is 0, or
- *   causal is set and j > i + m - n (the tokens are the span's last rows) and
- *   j >= d_prefix[s] (a prefix that every token sees; NULL = 0);
+ *   causal is set and j > i + start and j >= d_prefix[s] (a prefix that every
+ *   token sees; NULL = 0), with start = m - n (the tokens are the span's last
+ *   rows) or cfg->d_q_start[s], at least 0.  Where slots may fill up, a start of
+ *   rtcc_memory_append's d_held keeps it right: tokens that got no row are tokens
+ *   here, but add no key;
  *   out = sum of softmax(x) v over the visible keys, lse = ln sum exp(x).
  * A token that sees no key gets out = 0 and lse = -inf.  Sums and the softmax
  * are float32; for their product with v the probabilities are rounded to the

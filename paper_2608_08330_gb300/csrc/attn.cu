@@ -138,7 +138,7 @@ extern "C" rtcc_status rtcc_memory_attention(const rtcc_attn_config* c, const vo
   const void* by16[] = {d_q, d_k, d_v, d_out, d_workspace};
   for (const void* p : by16)
     if (misaligned(p, 16)) return RTCC_E_ARG;
-  const void* by4[] = {d_q_offsets, d_k_begin, d_k_end, d_prefix, d_present, d_slopes, d_q_pos, d_lse};
+  const void* by4[] = {d_q_offsets, d_k_begin, d_k_end, d_prefix, d_present, d_slopes, d_q_pos, d_lse, c->d_q_start};
   for (const void* p : by4)
     if (misaligned(p, 4)) return RTCC_E_ARG;
   if (misaligned(d_k_pos, 8)) return RTCC_E_ARG;
@@ -149,7 +149,7 @@ extern "C" rtcc_status rtcc_memory_attention(const rtcc_attn_config* c, const vo
   AttnArgs a{};
   a.q = d_q; a.k = d_k; a.v = d_v; a.out = d_out; a.lse = d_lse;
   a.q_offsets = d_q_offsets; a.k_begin = d_k_begin; a.k_end = d_k_end;
-  a.prefix = d_prefix; a.present = d_present;
+  a.prefix = d_prefix; a.present = d_present; a.q_start = c->d_q_start;
   a.slopes = d_slopes; a.q_pos = d_q_pos; a.k_pos = d_k_pos;
   a.q_row = c->q_row; a.q_head = c->q_head; a.k_row = c->k_row; a.k_head = c->k_head;
   a.v_row = c->v_row; a.v_head = c->v_head; a.out_row = c->out_row; a.out_head = c->out_head;

@@ -19,6 +19,7 @@ struct AttnArgs {
   float* lse;                    // [n_q][heads], may be null
   const int *q_offsets, *k_begin, *k_end;
   const int* prefix;             // may be null
+  const int* q_start;            // may be null: the tokens are the span's last rows
   const int* present;            // [n_slots], may be null
   const float *slopes, *q_pos, *k_pos;
   float* part_o;                 // [n_chunks * streams][n_q * heads][dim] when there are several
@@ -35,10 +36,12 @@ struct AttnArgs {
   float cap_log2;                // cap * log2(e), 0 = no cap
 };
 
-// One sequence: its tokens [q0, q0 + nq) and memory rows [kb, kb + nk).  Offsets
-// come from device memory, so they are cut to the arrays' extents.
+// One sequence: its tokens [q0, q0 + nq) and memory rows [kb, kb + nk), the first
+// token's place among the keys (a causal token i sees keys up to first + i; negative
+// where there are more tokens than keys).  Offsets come from device memory, so they
+// are cut to the arrays' extents; keys after the last token's are left out.
 struct AttnSpan {
-  int q0, nq, kb, nk, prefix;
+  int q0, nq, kb, nk, prefix, first;
 };
 
 __device__ __forceinline__ AttnSpan attn_span(const AttnArgs& A, int seq) {
@@ -50,13 +53,19 @@ __device__ __forceinline__ AttnSpan attn_span(const AttnArgs& A, int seq) {
   s.kb = min(max(kb, 0), A.n_rows);
   s.nk = min(max(ke, s.kb), A.n_rows) - s.kb;
   s.prefix = A.prefix ? min(max(A.prefix[seq], 0), s.nk) : 0;
+  s.first = s.nk - s.nq;
+  if (A.causal && A.q_start) {
+    s.first = min(max(A.q_start[seq], 0), s.nk);
+    if (s.nk - s.first > s.nq) s.nk = max(s.prefix, s.first + s.nq);
+  }
   return s;
 }
 
 // Keys [0, n) of the span that token i of the sequence sees (slots aside).
-__device__ __forceinline__ int attn_visible(const AttnArgs& A, const AttnSpan& s, int i) {
+__device__ __forceinline__ int attn_visible(const AttnArgs& A, const AttnSpan& s, int first, int i) {
   if (!A.causal) return s.nk;
-  return max(0, max(s.prefix, s.nk - (s.nq - 1 - i)));   // prefix <= nk, i < nq
+  const int own = i < s.nk - first ? first + i + 1 : s.nk;
+  return max(0, max(s.prefix, own));
 }
 
 // Slot of a memory row (there are at most 64).

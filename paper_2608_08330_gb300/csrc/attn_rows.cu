@@ -175,7 +175,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) k_attn_rows(const __grid_const
       const int ql = row_ok[i] ? r / A.group : 0;
       head[i] = kvh * A.group + (row_ok[i] ? r % A.group : 0);
       tok[i] = S.q0 + ql;
-      hi[i] = row_ok[i] ? attn_visible(A, S, ql) : 0;
+      hi[i] = row_ok[i] ? attn_visible(A, S, S.first, ql) : 0;
       slope[i] = dist ? A.slopes[head[i]] * kLog2e : 0.f;
       qy[i] = dist && row_ok[i] ? A.q_pos[tok[i] * A.q_pos_row] : 0.f;
       qx[i] = dist && row_ok[i] ? A.q_pos[tok[i] * A.q_pos_row + 1] : 0.f;

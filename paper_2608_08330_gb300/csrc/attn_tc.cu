@@ -280,7 +280,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1)
   extern __shared__ unsigned char smem_raw[];
   __shared__ uint64_t bar[C::kBars];
   __shared__ uint32_t tmem_base;
-  __shared__ int gave_up;
+  __shared__ int gave_up, first_place;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   unsigned char* smem =
       reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
@@ -326,6 +326,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1)
       }
       fence_barrier_init();
       gave_up = 0;
+      first_place = S.first;
       tma_prefetch_desc(&M.q);
       tma_prefetch_desc(&M.k);
       tma_prefetch_desc(&M.v);
@@ -347,6 +348,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1)
     all = ((slots >> s0) & want) == want;
   }
   volatile int* stop = &gave_up;
+  volatile int* first = &first_place;            // read once a group: registers are short
   // A wait by a whole warp; one that runs out marks the block, and every role then
   // leaves its loops.  A slot's barrier is waited for at every use by each role
   // that waits on it at all (a slot belongs to one stream), so parities suffice.
@@ -370,7 +372,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1)
   auto reach = [&](int rg, int w) -> int {
     const int i0 = (rg * tiles + w) * qpt;
     if (i0 >= S.nq) return c0;
-    return max(c0, min(c1, attn_visible(A, S, min(i0 + qpt, S.nq) - 1)));
+    return max(c0, min(c1, attn_visible(A, S, *first, min(i0 + qpt, S.nq) - 1)));
   };
   auto reach_all = [&](int rg) -> int {
     int e = reach(rg, 0);
@@ -568,8 +570,9 @@ __global__ void __launch_bounds__(kWarps * 32, 1)
       const bool valid = r < qpt * A.group && ql < S.nq;
       const int head = kvh * A.group + r % A.group;
       const long long tok = S.q0 + min(ql, S.nq - 1);        // a row without a token computes nothing
-      const int hi = valid ? min(c1, attn_visible(A, S, ql)) : 0;
-      const int all_see = i0 < S.nq ? min(c1, attn_visible(A, S, i0)) : 0;   // every row sees the keys before this
+      const int place0 = *first;
+      const int hi = valid ? min(c1, attn_visible(A, S, place0, ql)) : 0;
+      const int all_see = i0 < S.nq ? min(c1, attn_visible(A, S, place0, i0)) : 0;   // every row sees the keys before this
       float qy = 0.f, qx = 0.f, slope = 0.f;
       if (DIST) {
         qy = -A.q_pos[tok * A.q_pos_row];

@@ -95,13 +95,13 @@ class rtcc_attn_config(C.Structure):
         ("v_row", C.c_int64), ("v_head", C.c_int64), ("out_row", C.c_int64), ("out_head", C.c_int64),
         ("n_seqs", C.c_int32), ("max_q", C.c_int32), ("max_k", C.c_int32), ("causal", C.c_int32),
         ("n_slots", C.c_int32), ("slot_rows", C.c_int32), ("q_pos_row", C.c_int32),
-        ("scale", C.c_float), ("cap", C.c_float),
+        ("scale", C.c_float), ("cap", C.c_float), ("d_q_start", C.c_void_p),
     ]
 
 
 # the two structs' fields in order, packed in one go (field by field takes twice as long)
 _PREPARE = struct.Struct("=6i12q3i2i2f4x")
-_ATTN = struct.Struct("=6i8q7i2f4x")
+_ATTN = struct.Struct("=6i8q7i2f4xQ")
 assert _PREPARE.size == C.sizeof(rtcc_prepare_config) and _ATTN.size == C.sizeof(rtcc_attn_config)
 
 BOX_DTYPE = np.dtype([("x", "<f4"), ("y", "<f4"), ("z", "<f4"), ("l", "<f4"), ("w", "<f4"),
@@ -481,12 +481,13 @@ def rtcc_qkv_prepare(cfg: rtcc_prepare_config, d_q, d_k, d_v, d_q_gain, d_k_gain
 def attn_config(heads: int, kv_heads: int, head_dim: int, dtype: int, n_q: int, n_rows: int, q, k, v,
                 out, n_seqs: int, max_q: int, max_k: int, causal: bool = False, n_slots: int = 0,
                 slot_rows: int = 0, q_pos_row: int = 2, scale: Optional[float] = None,
-                cap: float = 0.0) -> rtcc_attn_config:
+                cap: float = 0.0, q_start: Optional[int] = None) -> rtcc_attn_config:
     """Shapes of rtcc_memory_attention; q .. out are the arrays' (row, head)
-    strides in elements; scale None = 1 / sqrt(head_dim)."""
+    strides in elements; scale None = 1 / sqrt(head_dim); q_start is a device
+    address."""
     return rtcc_attn_config.from_buffer_copy(_ATTN.pack(
         heads, kv_heads, head_dim, dtype, n_q, n_rows, *q, *k, *v, *out, n_seqs, max_q, max_k, causal, n_slots,
-        slot_rows, q_pos_row, head_dim ** -0.5 if scale is None else scale, cap))
+        slot_rows, q_pos_row, head_dim ** -0.5 if scale is None else scale, cap, q_start or 0))
 
 
 def rtcc_memory_attention(cfg: rtcc_attn_config, d_q, d_k, d_v, d_q_offsets, d_k_begin, d_k_end, d_prefix,

@@ -250,3 +250,90 @@ def test_attention_rounds_each_probability_once(R):
         v = torch.full_like(k, 1 + j / 128)
         out, _ = attend(R, q, k, v, dtype="bf16", scale=math.log(2))
         assert float((out.double() / (1 + j / 128) - 1).abs().max()) <= 2 * u + 2 * d + 2.0 ** -20, j
+
+
+def check_causal(out, lse, q, k, v, n, m, begin, start, prefix, u):
+    """float64 attention with key j of a sequence visible to its token i where j <= start + i or j < prefix."""
+    at, group = 0, q.shape[1] // k.shape[1]
+    for s in range(len(n)):
+        i, j = torch.arange(n[s], device="cuda")[:, None], torch.arange(m[s], device="cuda")[None]
+        see = (j <= i + start[s]) | (j < prefix[s])
+        for h in range(q.shape[1]):
+            kk, vv = k[begin[s]:begin[s] + m[s], h // group].double(), v[begin[s]:begin[s] + m[s], h // group].double()
+            some = see.any(0)[:, None]
+            kk, vv = torch.where(some, kk, 0.0), torch.where(some, vv, 0.0)
+            qq = q[at:at + n[s], h].double()
+            x = torch.where(see, qq @ kk.T / math.sqrt(q.shape[2]), -math.inf)
+            want_lse = torch.logsumexp(x, 1) if m[s] else torch.full((n[s],), -math.inf, device="cuda", dtype=torch.float64)
+            none = torch.isinf(want_lse)
+            p = torch.exp(x - torch.where(none, 0.0, want_lse)[:, None])
+            size = float((qq.abs() @ kk.abs().T).max()) / math.sqrt(q.shape[2]) if n[s] and m[s] else 0.0
+            d = 2.0 ** -23 * math.sqrt(q.shape[2]) * size + 2.0 ** -21
+            err = (out[at:at + n[s], h].double() - p @ vv).abs()
+            assert bool((err <= (2 * u + 2 * d + 2.0 ** -20) * (p @ vv.abs()) + 2.0 ** -25).all()), (s, h)
+            got = lse[at:at + n[s], h].double()
+            assert bool((got[none] == -math.inf).all())
+            assert bool(((got - want_lse).abs()[~none] <= d + 2.0 ** -20 * (1 + want_lse[~none].abs())).all()), (s, h)
+        at += n[s]
+
+
+@pytest.mark.parametrize("n,m", [([4, 1, 3], [12, 40, 3]), ([30, 200], [64, 130]), ([150, 0, 300], [400, 10, 90])])
+@pytest.mark.parametrize("kind", ["held", "behind", "ahead"])
+@pytest.mark.parametrize("prefixed", [False, True])
+def test_attention_starts(R, n, m, kind, prefixed):
+    """Starts at any place among the keys; keys that no token sees then hold NaN."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(len(n) + n[0])
+    start = {"held": [max(0, b - a + 2) for a, b in zip(n, m)], "behind": [max(0, b - a - 37) // 2 for a, b in zip(n, m)],
+             "ahead": [b + 10 for b in m]}[kind]
+    prefix = [min(b, 29) for b in m] if prefixed else [0] * len(m)
+    q = torch.randn(sum(n), 4, 64, generator=g, device="cuda").half()
+    k = torch.randn(sum(m), 2, 64, generator=g, device="cuda").half()
+    v = torch.randn(sum(m), 2, 64, generator=g, device="cuda").half()
+    begin = np.concatenate([[0], np.cumsum(m)[:-1]]).tolist()
+    for a, b, s, p, at in zip(n, m, start, prefix, begin):
+        seen = min(b, max(p, s + a))
+        k[at + seen:at + b], v[at + seen:at + b] = float("nan"), float("inf")
+    st = i32(start)
+    for workspace in (0, 16 << 20):
+        out, lse = attend(R, q, k, v, n=n, m=m, prefix=prefix if prefixed else None, workspace=workspace, causal=True,
+                          q_start=st.data_ptr())
+        check_causal(out, lse, q, k, v, n, m, begin, start, prefix, 2.0 ** -11)
+
+
+def test_attention_negative_starts_read_as_zero(R):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(8)
+    for n, m in (([3], [9]), ([150], [400])):
+        q = torch.randn(n[0], 2, 64, generator=g, device="cuda").half()
+        k, v = (torch.randn(m[0], 2, 64, generator=g, device="cuda").half() for _ in range(2))
+        st = i32([-5])
+        out, lse = attend(R, q, k, v, causal=True, q_start=st.data_ptr())
+        check_causal(out, lse, q, k, v, n, m, [0], [0], [0], 2.0 ** -11)
+
+
+@pytest.mark.parametrize("n_new", [[4, 3, 0], [60, 2, 90]])
+def test_append_into_slots_that_fill_up_then_attend(R, n_new):
+    """Tokens that still got a row see it and what came before it; those past the capacity see the slot."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(sum(n_new))
+    seqs, capacity, held_h = 3, 80, [78, 20, 10]
+    n = sum(n_new)
+    e = lambda c: torch.empty(c, dtype=torch.int32, device="cuda")  # noqa: E731
+    off, rows, begin, end, length = e(seqs + 1), e(n), e(seqs), e(seqs), e(seqs)
+    held, fresh = i32(held_h), i32(n_new)
+    R.check(R.rtcc_memory_append(seqs, capacity, n, fresh.data_ptr(), held.data_ptr(), None, off.data_ptr(), rows.data_ptr(),
+                                 None, None, begin.data_ptr(), end.data_ptr(), length.data_ptr()))
+    k = torch.randn(seqs * capacity, 2, 64, generator=g, device="cuda").half()
+    v = torch.randn(seqs * capacity, 2, 64, generator=g, device="cuda").half()
+    q = torch.randn(n, 2, 64, generator=g, device="cuda").half()
+    out, lse = torch.empty_like(q), torch.empty(n, 2, device="cuda")
+    st = (128, 64)
+    cfg = R.attn_config(2, 2, 64, R.FP16, n, seqs * capacity, st, st, st, st, seqs, max(n_new), capacity, causal=True,
+                        q_start=held.data_ptr())
+    R.check(R.rtcc_memory_attention(cfg, q.data_ptr(), k.data_ptr(), v.data_ptr(), off.data_ptr(), begin.data_ptr(),
+                                    end.data_ptr(), None, None, None, None, None, out.data_ptr(), lse.data_ptr(), None, 0))
+    torch.cuda.synchronize()
+    m = [min(capacity, h + a) for h, a in zip(held_h, n_new)]
+    assert length.tolist() == m
+    check_causal(out, lse, q, k, v, n_new, m, [s * capacity for s in range(seqs)], held_h, [0] * seqs, 2.0 ** -11)

@@ -27,3 +27,9 @@ def test_attention_refuses_caps_out_of_range(R):
         assert attend(R, attn_cfg(R, **kw)) == R.E_ARG, kw
     for kw in (dict(cap=1e38, scale=2.0), dict(cap=1e30, scale=0.0), dict(cap=1e-38, scale=1.0)):
         assert attend(R, attn_cfg(R, n_seqs=0, **kw)) == R.OK, kw
+
+
+def test_attention_start_is_checked_and_passed_on(R):
+    c = attn_cfg(R, causal=True, q_start=P + 64)
+    assert c.d_q_start == P + 64 and attn_cfg(R).d_q_start is None
+    assert attend(R, attn_cfg(R, causal=True, q_start=P + 2)) == R.E_ARG
