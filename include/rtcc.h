@@ -584,6 +584,16 @@ rtcc_status rtcc_memory_attention(const rtcc_attn_config* cfg, const void* d_q, 
  */
 rtcc_status rtcc_memory_attention_status(void* stream);
 
+/*
+ * Test hook of the attention calls of this process, until the next one (0: none).
+ * RTCC_TEST_UNREACHABLE_WAIT: the tensor-core kernel (many rows) never loads its
+ * queries and gives its waits up after about 10 ms; it sets the error that
+ * rtcc_memory_attention_status reports, and winds down without trapping.
+ * RTCC_E_ARG for other bits.
+ */
+#define RTCC_TEST_UNREACHABLE_WAIT 1
+rtcc_status rtcc_test_attention(int32_t what);
+
 /* ------------------------------------------------------------------------ */
 /* Release controller alone (host only; no GPU needed)                      */
 /* ------------------------------------------------------------------------ */

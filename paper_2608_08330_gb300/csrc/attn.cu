@@ -4,6 +4,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <atomic>
 
 #include "attn.cuh"
 #include "kernels.h"
@@ -99,6 +100,8 @@ long long tc_chunks(long long units, long long steps, long long least_chunks, lo
   return best;
 }
 
+std::atomic<int> g_test{0};                      // bits of rtcc_test_attention
+
 bool misaligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
 bool bad_stride(int64_t s) { return s < 0 || s % 8 != 0; }
 
@@ -165,6 +168,8 @@ extern "C" rtcc_status rtcc_memory_attention(const rtcc_attn_config* c, const vo
   a.cap_log2 = c->cap * kLog2e;
   a.scale_log2 = c->cap > 0.f ? c->scale / c->cap : c->scale * kLog2e;
 
+  a.stall = (g_test.load(std::memory_order_relaxed) & RTCC_TEST_UNREACHABLE_WAIT) != 0;
+  a.budget = a.stall ? kWaitBudgetCycles / 100 : kWaitBudgetCycles;
   const int max_q = c->max_q < 1 ? 1 : c->max_q > c->n_q ? c->n_q : c->max_q;
   const int max_k = c->max_k < 1 ? 1 : c->max_k > c->n_rows ? (c->n_rows < 1 ? 1 : c->n_rows) : c->max_k;
   const bool bf16 = c->dtype == RTCC_BF16;
@@ -213,4 +218,10 @@ extern "C" rtcc_status rtcc_memory_attention_status(void* stream) {
   int err = 0;
   if (attn_tc_error(&err, static_cast<cudaStream_t>(stream)) != cudaSuccess) return RTCC_E_CUDA;
   return err ? RTCC_E_DEVICE : RTCC_OK;
+}
+
+extern "C" rtcc_status rtcc_test_attention(int32_t what) {
+  if (what & ~RTCC_TEST_UNREACHABLE_WAIT) return RTCC_E_ARG;
+  g_test.store(what, std::memory_order_relaxed);
+  return RTCC_OK;
 }

@@ -34,6 +34,8 @@ struct AttnArgs {
   int row_groups;                // blocks along the rows of one sequence and key head
   float scale_log2;              // scale * log2(e); with a cap: scale / cap
   float cap_log2;                // cap * log2(e), 0 = no cap
+  long long budget;              // cycles of a bounded wait
+  int stall;                     // test hook: the queries are never loaded
 };
 
 // One sequence: its tokens [q0, q0 + nq) and memory rows [kb, kb + nk), the first

@@ -361,7 +361,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1)
         : "r"(bar0 + i * 8), "r"(parity)
         : "memory");
     if (__all_sync(0xFFFFFFFFu, in)) return true;
-    bool ok = mbar_wait(&bar[i], parity);
+    bool ok = mbar_wait(&bar[i], parity, A.budget);
     if (!ok) {
       *stop = 1;
       atomicOr(&g_attn_err, 1 << (i & 31));
@@ -386,7 +386,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1)
 
   if (warp == kLoadK) {
     // ------------------------------------------ queries, keys, coordinates
-    bool ok = true;
+    bool ok = !A.stall;
     uint32_t item = 0;
     int g = 0;
     for (int rg = rg0; rg < groups && ok; rg += A.row_groups, ++item) {
@@ -550,7 +550,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1)
     }
     // no product may still run when tensor memory is freed
     umma_commit_elected(&bar[C::DRAIN + chain]);
-    if (!mbar_wait(&bar[C::DRAIN + chain], 0)) atomicOr(&g_attn_err, 1 << ((C::DRAIN + chain) & 31));
+    if (!mbar_wait(&bar[C::DRAIN + chain], 0, A.budget)) atomicOr(&g_attn_err, 1 << ((C::DRAIN + chain) & 31));
     __syncwarp();
   } else {
     // -------------------------------------------------------------- softmax

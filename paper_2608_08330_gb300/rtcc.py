@@ -188,6 +188,7 @@ def load(path: Optional[str] = None) -> C.CDLL:
         "rtcc_memory_attention": (S, [C.POINTER(rtcc_attn_config)] + [C.c_void_p] * 14 +
                                   [C.c_size_t, C.c_void_p]),
         "rtcc_memory_attention_status": (S, [C.c_void_p]),
+        "rtcc_test_attention": (S, [C.c_int32]),
     }
     for name, (res, args) in sig.items():
         f = getattr(lib, name)
@@ -502,6 +503,14 @@ def rtcc_memory_attention(cfg: rtcc_attn_config, d_q, d_k, d_v, d_q_offsets, d_k
 def rtcc_memory_attention_status(stream: int = 0) -> int:
     """Wait for `stream`; E_DEVICE if an attention kernel gave up a wait."""
     return load().rtcc_memory_attention_status(stream or None)
+
+
+TEST_UNREACHABLE_WAIT = 1
+
+
+def rtcc_test_attention(what: int) -> int:
+    """Test hook of the attention calls of this process (see rtcc.h)."""
+    return load().rtcc_test_attention(what)
 
 
 # --------------------------------------------------------------------------

@@ -337,3 +337,33 @@ def test_append_into_slots_that_fill_up_then_attend(R, n_new):
     m = [min(capacity, h + a) for h, a in zip(held_h, n_new)]
     assert length.tolist() == m
     check_causal(out, lse, q, k, v, n_new, m, [s * capacity for s in range(seqs)], held_h, [0] * seqs, 2.0 ** -11)
+
+
+# ---------------------------------------------------------------------------
+# waits and launches that fail
+# ---------------------------------------------------------------------------
+
+@pytest.fixture
+def hook(R):
+    yield R.rtcc_test_attention
+    R.rtcc_test_attention(0)
+
+
+@pytest.mark.parametrize("kw", [
+    dict(n=[300], m=[500], heads=2, kv=2), dict(n=[40, 200], m=[5000, 130], heads=4, kv=2, dim=128, causal=True, dtype="bf16"),
+    dict(n=[200], m=[20000], heads=1, kv=1, cap=20.0, dist=True, slot_rows=1000, absent=(3, 7)), dict(n=[256], m=[64], heads=1, kv=1)])
+def test_attention_wait_that_runs_out_is_reported(R, hook, kw):
+    """A kernel whose queries never come gives its waits up; the report says so once, and the calls before and
+    after are right."""
+    assert R.rtcc_memory_attention_status() == R.OK
+    c = Case(**kw).run(R).check()
+    assert R.rtcc_memory_attention_status() == R.OK
+    first = c.out.clone()
+    assert hook(R.TEST_UNREACHABLE_WAIT) == R.OK
+    c.run(R)
+    assert R.rtcc_memory_attention_status() == R.E_DEVICE
+    assert hook(0) == R.OK
+    assert R.rtcc_memory_attention_status() == R.OK
+    c.out.fill_(7.0)
+    c.run(R).check()
+    assert torch.equal(c.out, first) and R.rtcc_memory_attention_status() == R.OK

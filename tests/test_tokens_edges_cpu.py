@@ -33,3 +33,8 @@ def test_attention_start_is_checked_and_passed_on(R):
     c = attn_cfg(R, causal=True, q_start=P + 64)
     assert c.d_q_start == P + 64 and attn_cfg(R).d_q_start is None
     assert attend(R, attn_cfg(R, causal=True, q_start=P + 2)) == R.E_ARG
+
+
+def test_attention_test_hook_refuses_unknown_bits(R):
+    assert R.rtcc_test_attention(1 << 20) == R.E_ARG and R.rtcc_test_attention(-1) == R.E_ARG
+    assert R.rtcc_test_attention(R.TEST_UNREACHABLE_WAIT) == R.OK and R.rtcc_test_attention(0) == R.OK
