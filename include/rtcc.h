@@ -578,9 +578,13 @@ rtcc_status rtcc_memory_attention(const rtcc_attn_config* cfg, const void* d_q, 
                                   void* d_workspace, size_t workspace_bytes, void* stream);
 
 /*
- * Wait for `stream` and report on the attention calls of this device since the
- * last report: RTCC_E_DEVICE if a kernel gave up one of its bounded waits (its
- * outputs are then not valid), else RTCC_OK.  Not during a stream capture.
+ * Wait for `stream` and report on the attention calls of this device since the last
+ * report on this stream (since the start for its first): RTCC_E_DEVICE if a kernel
+ * gave up one of its bounded waits (the outputs of its call are then not valid), else
+ * RTCC_OK.  A failure is the device's, not a stream's: every stream's next report
+ * tells of it, also where another stream's call failed, and a report takes nothing
+ * from another's.  Calls of other streams still running may not have failed yet.
+ * Not during a stream capture.
  */
 rtcc_status rtcc_memory_attention_status(void* stream);
 

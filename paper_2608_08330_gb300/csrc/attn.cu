@@ -5,6 +5,9 @@
 
 #include <algorithm>
 #include <atomic>
+#include <map>
+#include <mutex>
+#include <utility>
 
 #include "attn.cuh"
 #include "kernels.h"
@@ -214,10 +217,22 @@ extern "C" rtcc_status rtcc_memory_attention(const rtcc_attn_config* c, const vo
   }
 }
 
-extern "C" rtcc_status rtcc_memory_attention_status(void* stream) {
-  int err = 0;
-  if (attn_tc_error(&err, static_cast<cudaStream_t>(stream)) != cudaSuccess) return RTCC_E_CUDA;
-  return err ? RTCC_E_DEVICE : RTCC_OK;
+// The device counts and nothing clears the count, so no failure is lost between a read
+// and a clear; each stream remembers the count of its last report.
+extern "C" rtcc_status rtcc_memory_attention_status(void* stream) try {
+  static std::mutex mu;
+  static std::map<std::pair<int, void*>, unsigned> reported;
+  unsigned count = 0;
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return RTCC_E_CUDA;
+  if (attn_tc_errors(&count, static_cast<cudaStream_t>(stream)) != cudaSuccess) return RTCC_E_CUDA;
+  std::lock_guard<std::mutex> lk(mu);
+  unsigned& last = reported[{dev, stream}];
+  if ((int)(count - last) <= 0) return RTCC_OK;
+  last = count;
+  return RTCC_E_DEVICE;
+} catch (...) {
+  return RTCC_E_NOMEM;
 }
 
 extern "C" rtcc_status rtcc_test_attention(int32_t what) {

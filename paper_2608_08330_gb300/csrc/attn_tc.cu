@@ -70,7 +70,7 @@ constexpr float kHard = 15.9f;
 // Measured on 300 queries over 281,600 keys with a bias, fp16, (lift, slack): (0, 8) 325 us,
 // (6, 11) 325, (8, 11) 333, (8, 12) with kHard 15 367: what is short of kHard is done again.
 
-__device__ int g_attn_err;                       // bit b: a wait on barrier b (mod 32) ran out
+__device__ unsigned g_attn_err;                  // threads whose waits ran out, since the start
 
 constexpr int kChains = 2;
 constexpr int kS = 2;                            // S per chain
@@ -364,7 +364,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1)
     bool ok = mbar_wait(&bar[i], parity, A.budget);
     if (!ok) {
       *stop = 1;
-      atomicOr(&g_attn_err, 1 << (i & 31));
+      atomicAdd(&g_attn_err, 1u);
     }
     return __all_sync(0xFFFFFFFFu, ok && *stop == 0);
   };
@@ -550,7 +550,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1)
     }
     // no product may still run when tensor memory is freed
     umma_commit_elected(&bar[C::DRAIN + chain]);
-    if (!mbar_wait(&bar[C::DRAIN + chain], 0, A.budget)) atomicOr(&g_attn_err, 1 << ((C::DRAIN + chain) & 31));
+    if (!mbar_wait(&bar[C::DRAIN + chain], 0, A.budget)) atomicAdd(&g_attn_err, 1u);
     __syncwarp();
   } else {
     // -------------------------------------------------------------- softmax
@@ -938,12 +938,11 @@ cudaError_t launch_attn_tc(const AttnArgs& a, bool bf16, cudaStream_t st) {
   return bf16 ? launch_tc_t<__nv_bfloat16, 128>(a, m, st) : launch_tc_t<__half, 128>(a, m, st);
 }
 
-cudaError_t attn_tc_error(int* err, cudaStream_t st) {
+cudaError_t attn_tc_errors(unsigned* count, cudaStream_t st) {
   void* p = nullptr;
   cudaError_t e = cudaGetSymbolAddress(&p, g_attn_err);
-  if (e == cudaSuccess) e = cudaMemcpyAsync(err, p, sizeof(int), cudaMemcpyDeviceToHost, st);
+  if (e == cudaSuccess) e = cudaMemcpyAsync(count, p, sizeof(*count), cudaMemcpyDeviceToHost, st);
   if (e == cudaSuccess) e = cudaStreamSynchronize(st);
-  if (e == cudaSuccess && *err) e = cudaMemsetAsync(p, 0, sizeof(int), st);
   return e;
 }
 

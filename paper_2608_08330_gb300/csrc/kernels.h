@@ -377,12 +377,12 @@ int attn_rows_cluster();           // blocks that can join their chunks
 cudaError_t launch_attn_rows(const AttnArgs& a, bool bf16, cudaStream_t st);
 // The tensor-core kernel for many rows (attn_tc.cu): partial results per chunk,
 // tokens per block, the chunks' unit, launch (cudaErrorNotSupported: the arrays do
-// not fit a tensor map), and the error word of its bounded waits, read and cleared.
+// not fit a tensor map), and the device's count of its waits that ran out.
 int attn_tc_streams(int group, int max_q);
 int attn_tc_tokens_per_block(int group, int streams);
 int attn_tc_unit(int streams);
 cudaError_t launch_attn_tc(const AttnArgs& a, bool bf16, cudaStream_t st);
-cudaError_t attn_tc_error(int* err, cudaStream_t st);
+cudaError_t attn_tc_errors(unsigned* count, cudaStream_t st);
 // Merge of the chunks' partial results into out and lse.
 cudaError_t launch_attn_join(const AttnArgs& a, int max_q, bool bf16, cudaStream_t st);
 

@@ -367,3 +367,22 @@ def test_attention_wait_that_runs_out_is_reported(R, hook, kw):
     c.out.fill_(7.0)
     c.run(R).check()
     assert torch.equal(c.out, first) and R.rtcc_memory_attention_status() == R.OK
+
+
+def test_attention_failure_is_reported_to_every_stream(R, hook):
+    a, b = torch.cuda.Stream(), torch.cuda.Stream()
+    R.rtcc_memory_attention_status(a.cuda_stream), R.rtcc_memory_attention_status(b.cuda_stream)
+    c = Case([300], [500], heads=2, kv=2)
+    torch.cuda.synchronize()
+    hook(R.TEST_UNREACHABLE_WAIT)
+    with torch.cuda.stream(a):
+        c.run(R, stream=a.cuda_stream)
+    a.synchronize()
+    hook(0)
+    # the report on b does not take a's away
+    assert R.rtcc_memory_attention_status(b.cuda_stream) == R.E_DEVICE
+    assert R.rtcc_memory_attention_status(a.cuda_stream) == R.E_DEVICE
+    assert R.rtcc_memory_attention_status(a.cuda_stream) == R.OK
+    assert R.rtcc_memory_attention_status(b.cuda_stream) == R.OK
+    assert R.rtcc_memory_attention_status() == R.E_DEVICE
+    assert R.rtcc_memory_attention_status() == R.OK
