@@ -489,7 +489,8 @@ typedef struct {
  * coordinates (y, x) go to the memory row d_rows[i] of token i (d_rows NULL:
  * row i); a token whose row is outside [0, n_rows) writes its query only.  Rows
  * of one call must differ.
- * d_q, d_k, d_v: each may be NULL together with its output.  d_q_gain,
+ * d_q, d_k, d_v: each may be NULL together with its output, all of them to write
+ * coordinates alone.  d_q_gain,
  * d_k_gain float32 [head_dim], NULL = 1.  d_pos float32 [n_tokens][3] = (t, y,
  * x).  d_coord float32 [n_rows][2].  Vectors are 16-byte aligned, d_coord
  * 8-byte, the rest 4-byte.  d_q_out may be d_q with the same strides.

@@ -483,7 +483,7 @@ extern "C" rtcc_status rtcc_qkv_prepare(const rtcc_prepare_config* c, const void
       misaligned(d_k_mem, 16) || misaligned(d_v_mem, 16) || misaligned(d_coord, 8) || misaligned(d_pos, 4) ||
       misaligned(d_rows, 4) || misaligned(d_q_gain, 4) || misaligned(d_k_gain, 4))
     return RTCC_E_ARG;
-  if (c->n_tokens == 0 || (!d_q && !d_k && !d_v)) return RTCC_OK;
+  if (c->n_tokens == 0 || (!d_q && !d_k && !d_v && !d_coord)) return RTCC_OK;
   const int sms = sm_count();
   if (sms < 1) return RTCC_E_CUDA;
 
@@ -520,6 +520,7 @@ extern "C" rtcc_status rtcc_qkv_prepare(const rtcc_prepare_config* c, const void
   const long long threads = (long long)a.n_tokens * lp;
   long long parts = (512LL * sms + threads - 1) / threads;
   if (parts > heads) parts = heads;
+  if (parts < 1) parts = 1;                      // coordinates alone
   cudaLaunchConfig_t lc = {};
   lc.gridDim = dim3((unsigned)((threads + kPrepThreads - 1) / kPrepThreads), (unsigned)parts);
   lc.blockDim = dim3(kPrepThreads);

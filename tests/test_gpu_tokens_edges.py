@@ -49,6 +49,26 @@ def test_append_token_places_up_to_2_to_the_31(R):
 
 
 # ---------------------------------------------------------------------------
+# prepare
+# ---------------------------------------------------------------------------
+
+@pytest.mark.parametrize("n", [1, 700])
+@pytest.mark.parametrize("dim,pairs", [(64, (8, 12, 12)), (8, (0, 0, 0)), (80, (3, 4, 4))])
+def test_prepare_writes_coordinates_alone(R, n, dim, pairs):
+    pos = torch.rand(n, 3, device="cuda")
+    rows = torch.randperm(n + 5, device="cuda")[:n].int()
+    rows[0] = -1
+    coord = torch.full((n + 5, 2), 9.0, device="cuda")
+    cfg = R.prepare_config(4, 2, dim, R.FP16, n, n + 5, *[(4 * dim, dim)] * 6, pairs)
+    R.check(R.rtcc_qkv_prepare(cfg, None, None, None, None, None, pos.data_ptr(), rows.data_ptr(), None, None, None,
+                               coord.data_ptr()))
+    torch.cuda.synchronize()
+    want = torch.full_like(coord, 9.0)
+    want[rows[1:].long()] = pos[1:, 1:]
+    assert torch.equal(coord, want)
+
+
+# ---------------------------------------------------------------------------
 # attention
 # ---------------------------------------------------------------------------
 
