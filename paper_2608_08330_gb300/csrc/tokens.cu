@@ -310,7 +310,8 @@ __global__ void __launch_bounds__(kPrepThreads, 6) k_qkv_prepare(const __grid_co
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const float c = i & 1 ? cs[i / 2].y : cs[i / 2].x, s = i & 1 ? sn[i / 2].y : sn[i / 2].x;
-            y[i] = make_float2(y[i].x * c - y[i].y * s, y[i].x * s + y[i].y * c);
+            // a pair that is not turned (1 and 0) keeps its channels, whatever the other holds
+            if (s != 0.f || c < 0.f) y[i] = make_float2(y[i].x * c - y[i].y * s, y[i].x * s + y[i].y * c);
           }
         } else if (TURN == kTurnLanes) {
           const int from = lane + (low ? A.n_rot / 8 : -(A.n_rot / 8));

@@ -68,6 +68,26 @@ def test_prepare_writes_coordinates_alone(R, n, dim, pairs):
     assert torch.equal(coord, want)
 
 
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("dim,pairs", [(64, (8, 4, 4)), (64, (5, 3, 3)), (64, (0, 0, 0)), (40, (1, 0, 6)), (128, (0, 3, 0))])
+def test_prepare_leaves_unturned_channels_alone(R, interleaved, dim, pairs):
+    """Channels past the turned pairs keep their bits without a norm, beside infinities and NaN too."""
+    n, rot = 9, 2 * sum(pairs)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(dim + rot)
+    q = torch.randn(n, 2, dim, generator=g, device="cuda").half()
+    for e in range(rot, dim, 3):
+        q[e % n, e % 2, e] = float("inf") if e % 4 else float("nan")
+    pos, out = 9 * torch.rand(n, 3, generator=g, device="cuda"), torch.empty_like(q)
+    cfg = R.prepare_config(2, 1, dim, R.FP16, n, 0, *[(2 * dim, dim)] * 6, pairs, interleaved=interleaved, norm=False)
+    R.check(R.rtcc_qkv_prepare(cfg, q.data_ptr(), None, None, None, None, pos.data_ptr(), None, out.data_ptr(), None, None,
+                               None))
+    torch.cuda.synchronize()
+    a, b = out[..., rot:], q[..., rot:]
+    assert torch.equal(torch.isnan(a), torch.isnan(b)) and torch.equal(a[~torch.isnan(b)], b[~torch.isnan(b)])
+    assert bool(torch.isfinite(out[..., :rot]).all())
+
+
 # ---------------------------------------------------------------------------
 # attention
 # ---------------------------------------------------------------------------
