@@ -492,7 +492,8 @@ typedef struct {
  * d_q, d_k, d_v: each may be NULL together with its output, all of them to write
  * coordinates alone.  d_q_gain,
  * d_k_gain float32 [head_dim], NULL = 1.  d_pos float32 [n_tokens][3] = (t, y,
- * x).  d_coord float32 [n_rows][2].  Vectors are 16-byte aligned, d_coord
+ * x), NULL where no pair turns and d_coord is NULL.  Angles are good to 4e-7 up to
+ * positions of 10^8, beyond in proportion to them.  d_coord float32 [n_rows][2].  Vectors are 16-byte aligned, d_coord
  * 8-byte, the rest 4-byte.  d_q_out may be d_q with the same strides.
  */
 rtcc_status rtcc_qkv_prepare(const rtcc_prepare_config* cfg, const void* d_q, const void* d_k,

@@ -215,7 +215,11 @@ __global__ void __launch_bounds__(kPrepThreads, 6) k_qkv_prepare(const __grid_co
   for (int j = 0; j < kPrepPairs; ++j) issue(j);
   const long long row = A.rows ? A.rows[tok] : tok;
   const bool stored = live && row >= 0 && row < A.n_rows;
-  const float pos[3] = {A.pos[3 * tok], A.pos[3 * tok + 1], A.pos[3 * tok + 2]};
+  float pos[3] = {0.f, 0.f, 0.f};
+  if (TURN != kTurnNone || A.coord) {            // else d_pos may be null
+#pragma unroll
+    for (int i = 0; i < 3; ++i) pos[i] = A.pos[3 * tok + i];
+  }
   if (A.coord && blockIdx.y == 0 && stored && lane == 0)
     *reinterpret_cast<float2*>(A.coord + 2 * row) = make_float2(pos[1], pos[2]);
   __syncthreads();                               // the table of turns
@@ -470,7 +474,7 @@ extern "C" rtcc_status rtcc_qkv_prepare(const rtcc_prepare_config* c, const void
   if ((d_q != nullptr) != (d_q_out != nullptr) || (d_k != nullptr) != (d_k_mem != nullptr) ||
       (d_v != nullptr) != (d_v_mem != nullptr))
     return RTCC_E_ARG;
-  if (c->n_tokens > 0 && !d_pos) return RTCC_E_ARG;
+  if (c->n_tokens > 0 && !d_pos && (pairs > 0 || d_coord)) return RTCC_E_ARG;
   if (d_q && (c->heads < 1 || bad_stride(c->q_row) || bad_stride(c->q_head) || bad_stride(c->qo_row) ||
               bad_stride(c->qo_head)))
     return RTCC_E_ARG;

@@ -88,6 +88,26 @@ def test_prepare_leaves_unturned_channels_alone(R, interleaved, dim, pairs):
     assert bool(torch.isfinite(out[..., :rot]).all())
 
 
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_prepare_without_positions(R, interleaved):
+    """Where nothing turns and no coordinates are kept, positions may be NULL."""
+    n = 33
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+    x = torch.randn(n, 6, 64, generator=g, device="cuda").half()
+    q, km, vm = torch.empty(n, 4, 64, dtype=torch.float16, device="cuda"), *(torch.empty(n, 1, 64, dtype=torch.float16,
+                                                                                         device="cuda") for _ in range(2))
+    st = (6 * 64, 64)
+    cfg = R.prepare_config(4, 1, 64, R.FP16, n, n, st, st, st, (256, 64), (64, 64), (64, 64), (0, 0, 0), interleaved=interleaved)
+    R.check(R.rtcc_qkv_prepare(cfg, x.data_ptr(), x[:, 4:].data_ptr(), x[:, 5:].data_ptr(), None, None, None, None, q.data_ptr(),
+                               km.data_ptr(), vm.data_ptr(), None))
+    torch.cuda.synchronize()
+    y = x.double() / torch.sqrt((x.double() ** 2).mean(-1, keepdim=True) + 1e-6)
+    for got, want in ((q, y[:, :4]), (km, y[:, 4:5])):
+        assert bool(((got.double() - want).abs() <= (2.0 ** -11 + 2.0 ** -19) * want.abs() + 2.0 ** -25).all())
+    assert torch.equal(vm, x[:, 5:])
+
+
 # ---------------------------------------------------------------------------
 # attention
 # ---------------------------------------------------------------------------

@@ -1,7 +1,7 @@
 """Refusals of the token-memory calls at the edges of their ranges, without a GPU."""
 import pytest
 
-from tests.test_tokens_cpu import P, attend, attn_cfg
+from tests.test_tokens_cpu import P, attend, attn_cfg, prep_cfg, prepare
 from paper_2608_08330_gb300 import build as B
 
 
@@ -38,3 +38,10 @@ def test_attention_start_is_checked_and_passed_on(R):
 def test_attention_test_hook_refuses_unknown_bits(R):
     assert R.rtcc_test_attention(1 << 20) == R.E_ARG and R.rtcc_test_attention(-1) == R.E_ARG
     assert R.rtcc_test_attention(R.TEST_UNREACHABLE_WAIT) == R.OK and R.rtcc_test_attention(0) == R.OK
+
+
+def test_prepare_needs_positions_to_turn_or_keep_them(R):
+    plain = prep_cfg(R, axis_pairs=(0, 0, 0))
+    assert prepare(R, plain, pos=None, coord=P) == R.E_ARG
+    assert prepare(R, prep_cfg(R), pos=None) == R.E_ARG
+    assert prepare(R, prep_cfg(R, axis_pairs=(0, 0, 0), n_tokens=0), pos=None) == R.OK
