@@ -595,9 +595,12 @@ rtcc_status rtcc_memory_attention_status(void* stream);
  * RTCC_TEST_UNREACHABLE_WAIT: the tensor-core kernel (many rows) never loads its
  * queries and gives its waits up after about 10 ms; it sets the error that
  * rtcc_memory_attention_status reports, and winds down without trapping.
- * RTCC_E_ARG for other bits.
+ * RTCC_TEST_NO_CLUSTERS: launches of clusters (few rows, short spans) are taken as
+ * refused, as by a part of a GPU that has no room for them; the call then splits its
+ * spans in the workspace.  RTCC_E_ARG for other bits.
  */
 #define RTCC_TEST_UNREACHABLE_WAIT 1
+#define RTCC_TEST_NO_CLUSTERS 2
 rtcc_status rtcc_test_attention(int32_t what);
 
 /* ------------------------------------------------------------------------ */

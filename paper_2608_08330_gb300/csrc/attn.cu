@@ -171,7 +171,8 @@ extern "C" rtcc_status rtcc_memory_attention(const rtcc_attn_config* c, const vo
   a.cap_log2 = c->cap * kLog2e;
   a.scale_log2 = c->cap > 0.f ? c->scale / c->cap : c->scale * kLog2e;
 
-  a.stall = (g_test.load(std::memory_order_relaxed) & RTCC_TEST_UNREACHABLE_WAIT) != 0;
+  const int test = g_test.load(std::memory_order_relaxed);
+  a.stall = (test & RTCC_TEST_UNREACHABLE_WAIT) != 0;
   a.budget = a.stall ? kWaitBudgetCycles / 100 : kWaitBudgetCycles;
   const int max_q = c->max_q < 1 ? 1 : c->max_q > c->n_q ? c->n_q : c->max_q;
   const int max_k = c->max_k < 1 ? 1 : c->max_k > c->n_rows ? (c->n_rows < 1 ? 1 : c->n_rows) : c->max_k;
@@ -181,6 +182,7 @@ extern "C" rtcc_status rtcc_memory_attention(const rtcc_attn_config* c, const vo
   bool tc = (long long)max_q * a.group > kTcRows && a.group <= 128 && c->n_rows > 0;
   const size_t part = (size_t)c->n_q * c->heads * (c->head_dim * sizeof(float) + sizeof(float2));
   const long long room = d_workspace ? (long long)(workspace_bytes / part) : 0;
+  bool clusters = true;
   for (;; tc = false) {
     a.streams = tc ? attn_tc_streams(a.group, max_q) : 1;
     if (a.streams > room) a.streams = 1;
@@ -202,15 +204,21 @@ extern "C" rtcc_status rtcc_memory_attention(const rtcc_attn_config* c, const vo
     long long chunks = tc ? tc_chunks(units, steps, least, most, sms, a.streams, a.n_q, a.heads, a.dim)
                           : rows_chunks(units, c->n_seqs, steps, least, most, sms);
     if (tc && max_k / (chunks * sums) > kLongSum) continue;
-    const long long joined = tc ? 1 : rows_cluster(units, steps, chunks, least, sms, a.dim);
+    const long long joined = tc || !clusters ? 1 : rows_cluster(units, steps, chunks, least, sms, a.dim);
     a.cluster = joined > 1;
     if (a.cluster) chunks = joined;
     a.n_chunks = (int)chunks;
     a.chunk = (int)((max_k + chunks - 1) / chunks);
     a.part_o = static_cast<float*>(d_workspace);
     a.part_ml = reinterpret_cast<float2*>(a.part_o + (size_t)chunks * a.streams * c->n_q * c->heads * c->head_dim);
-    const cudaError_t e = tc ? launch_attn_tc(a, bf16, st) : launch_attn_rows(a, bf16, st);
+    cudaError_t e = a.cluster && (test & RTCC_TEST_NO_CLUSTERS) ? cudaErrorInvalidClusterSize
+                    : tc ? launch_attn_tc(a, bf16, st) : launch_attn_rows(a, bf16, st);
     if (tc && e == cudaErrorNotSupported) continue;
+    if (a.cluster && e != cudaSuccess) {           // no room for such clusters (a part of a GPU): two launches
+      cudaGetLastError();
+      clusters = false;
+      continue;
+    }
     if (e != cudaSuccess) return RTCC_E_CUDA;
     if (!a.cluster && chunks * a.streams > 1 && launch_attn_join(a, max_q, bf16, st) != cudaSuccess) return RTCC_E_CUDA;
     return RTCC_OK;
@@ -236,7 +244,7 @@ extern "C" rtcc_status rtcc_memory_attention_status(void* stream) try {
 }
 
 extern "C" rtcc_status rtcc_test_attention(int32_t what) {
-  if (what & ~RTCC_TEST_UNREACHABLE_WAIT) return RTCC_E_ARG;
+  if (what & ~(RTCC_TEST_UNREACHABLE_WAIT | RTCC_TEST_NO_CLUSTERS)) return RTCC_E_ARG;
   g_test.store(what, std::memory_order_relaxed);
   return RTCC_OK;
 }

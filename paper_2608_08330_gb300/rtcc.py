@@ -505,7 +505,7 @@ def rtcc_memory_attention_status(stream: int = 0) -> int:
     return load().rtcc_memory_attention_status(stream or None)
 
 
-TEST_UNREACHABLE_WAIT = 1
+TEST_UNREACHABLE_WAIT, TEST_NO_CLUSTERS = 1, 2
 
 
 def rtcc_test_attention(what: int) -> int:

@@ -446,3 +446,15 @@ def test_attention_failure_is_reported_to_every_stream(R, hook):
     assert R.rtcc_memory_attention_status(b.cuda_stream) == R.OK
     assert R.rtcc_memory_attention_status() == R.E_DEVICE
     assert R.rtcc_memory_attention_status() == R.OK
+
+
+@pytest.mark.parametrize("workspace", [0, 32 << 20])
+def test_attention_without_clusters(R, hook, workspace):
+    """A refused cluster launch is made up for by split spans, and with no workspace by whole ones."""
+    for n, m, dim in (([1], [4097], 64), ([2, 0, 4, 1], [1, 700, 2000, 650], 80), ([3], [2049], 128)):
+        c = Case(n, m, heads=6, kv=2, dim=dim, causal=True)
+        hook(R.TEST_NO_CLUSTERS)
+        c.run(R, workspace=workspace).check()
+        hook(0)
+        c.out.fill_(7.0)
+        c.run(R, workspace=workspace).check()
