@@ -399,6 +399,26 @@ def test_append_into_slots_that_fill_up_then_attend(R, n_new):
     check_causal(out, lse, q, k, v, n_new, m, [s * capacity for s in range(seqs)], held_h, [0] * seqs, 2.0 ** -11)
 
 
+@pytest.mark.parametrize("max_q", [40, 129, 200])
+@pytest.mark.parametrize("n,m", [([400], [1000]), ([700, 0, 333], [777, 64, 1500]), ([1500], [700]), ([401, 399], [0, 2177])])
+@pytest.mark.parametrize("kw", [
+    dict(heads=2, kv=2, dim=64), dict(heads=3, kv=1, dim=128, causal=True, prefixed=90, dtype="bf16"),
+    dict(heads=2, kv=1, dim=64, cap=20.0, dist=True), dict(heads=4, kv=2, dim=128, slot_rows=150, absent=(0, 2, 3), cap=30.0),
+    dict(heads=1, kv=1, dim=80, causal=True, dist=True, slot_rows=100, absent=(1, 4), dtype="bf16")])
+def test_attention_longer_sequences_than_stated(R, max_q, n, m, kw):
+    """The blocks of the many-rows kernel then take several groups of rows, one after another: with one or two
+    streams, other groups' masks, steps and ring places."""
+    kw = dict(kw)
+    if kw.get("absent"):
+        kw["absent"] = [a for a in kw["absent"] if a * kw["slot_rows"] < sum(m) + 7 * (len(m) + 1)]
+    prefix = kw.pop("prefixed", None)
+    c = Case(n, m, gap=7, prefix=None if prefix is None else [min(prefix, x) for x in m], seed=max_q, **kw)
+    for run in (dict(workspace=0), dict(), dict(max_k=300), dict(workspace=0, max_k=64)):
+        c.out.fill_(7.0)
+        c.run(R, max_q=max_q, **run).check()
+    assert R.rtcc_memory_attention_status() == R.OK
+
+
 # ---------------------------------------------------------------------------
 # waits and launches that fail
 # ---------------------------------------------------------------------------
