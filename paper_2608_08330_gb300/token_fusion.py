@@ -29,6 +29,8 @@ THETA, EPS, CAP = 10000.0, 1e-6, 30.0
 
 def head_layout(channels: int):
     """(heads, channels per head): heads of 64, or 32 for narrow maps."""
+    if channels < 32 or channels % 32:
+        raise ValueError(f"{channels} channels are not heads of 64 or 32")
     dim = 64 if channels % 64 == 0 else 32
     return channels // dim, dim
 
@@ -59,6 +61,8 @@ def fuse(maps, dtype: str, feat_h: int, feat_w: int, cell: float):
     import torch
 
     from . import rtcc as R
+    if not maps or maps[0] is None:
+        raise ValueError("the ego's map (agent 0) is needed")
     dev = torch.device("cuda")
     kind = torch.bfloat16 if dtype == "bf16" else torch.float16
     code = R.BF16 if dtype == "bf16" else R.FP16
@@ -137,6 +141,10 @@ def main(argv=None) -> int:
     ap.add_argument("--frame", type=int, default=0)
     ap.add_argument("--absent", type=int, nargs="*", default=[], help="agents that do not report (not the ego)")
     a = ap.parse_args(argv)
+    import synth
+    agents = synth.get_config(a.workload).n_agents
+    if any(not 0 < k < agents for k in a.absent):
+        ap.error(f"--absent takes agents 1 to {agents - 1}: agent 0 is the ego")
     cfg, maps = frame_maps(a.workload, a.frame, a.absent)
     out, lse = fuse(maps, cfg.dtype, cfg.feat_h, cfg.feat_w, cfg.pillar * cfg.feat_stride)
     print(f"{a.workload}: {cfg.feat_h} x {cfg.feat_w} cells over {sum(m is not None for m in maps)} maps, "
