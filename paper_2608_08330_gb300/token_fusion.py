@@ -41,6 +41,11 @@ def axis_pairs(dim: int):
     return t, (dim // 2 - t) // 2, dim // 2 - t - (dim // 2 - t) // 2
 
 
+def workspace_bytes(tokens: int, keys: int, heads: int, dim: int) -> int:
+    """Room for a part per 65,536 keys, and one more, so that no float32 sum of the attention gets long."""
+    return (-(-keys // 65536) + 1) * tokens * heads * (dim + 2) * 4
+
+
 def slopes(heads: int) -> np.ndarray:
     """Distance slopes per head, 1/4 per metre down to 1/256."""
     return (0.25 * 2.0 ** (-6.0 * np.arange(heads) / max(heads, 1))).astype(np.float32)
@@ -100,7 +105,7 @@ def fuse(maps, dtype: str, feat_h: int, feat_w: int, cell: float):
     slope = torch.from_numpy(slopes(heads)).to(dev)
     present = i32([int(m is not None) for m in maps])
     q_offsets, first, last = i32([0, cells]), i32([0]), i32([rows_all])
-    workspace = empty(32 << 20, t=torch.uint8)
+    workspace = empty(workspace_bytes(cells, rows_all, heads, dim), t=torch.uint8)
     cfg = R.attn_config(heads, heads, dim, code, cells, rows_all, st, st, st, st, 1, cells, rows_all, n_slots=agents,
                         slot_rows=cells, q_pos_row=3, cap=CAP)
     R.check(R.rtcc_memory_attention(cfg, q.data_ptr(), k_mem.data_ptr(), v_mem.data_ptr(), q_offsets.data_ptr(),

@@ -22,3 +22,9 @@ def test_the_ego_is_needed():
     for maps in ([], [None, 1]):
         with pytest.raises(ValueError):
             F.fuse(maps, "fp16", 4, 4, 0.8)
+
+
+def test_workspace_has_a_part_per_65536_keys():
+    part = 35200 * 6 * 66 * 4
+    assert F.workspace_bytes(35200, 176000, 6, 64) == 4 * part
+    assert F.workspace_bytes(1, 65536, 1, 32) == 2 * 34 * 4 and F.workspace_bytes(1, 65537, 1, 32) == 3 * 34 * 4
