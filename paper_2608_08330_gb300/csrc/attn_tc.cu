@@ -759,17 +759,11 @@ __global__ void __launch_bounds__(kWarps * 32, 1)
           reg_fence32(y);
           const uint32_t bits = (uint32_t)(keep >> c);
           float top = -INFINITY;
-#pragma unroll
-          for (int i = 0; i < 32; ++i) y[i] *= A.scale_log2;
-          if (CAP && A.cap_log2 <= kAbsCap * kLog2e) {
-#pragma unroll
-            for (int i = 0; i < 32; ++i) y[i] = A.cap_log2 * tanh_abs(y[i]);
-          } else if (CAP) {
-#pragma unroll
-            for (int i = 0; i < 32; ++i) y[i] = A.cap_log2 * tanh_rel(y[i]);
-          }
+          const bool far_cap = CAP && A.cap_log2 > kAbsCap * kLog2e;
 #pragma unroll
           for (int i = 0; i < 32; ++i) {
+            y[i] *= A.scale_log2;
+            if (CAP) y[i] = A.cap_log2 * (far_cap ? tanh_rel(y[i]) : tanh_abs(y[i]));
             if (DIST) y[i] = fmaf(fabsf(py[c + i] + qy) + fabsf(py[kKeys + c + i] + qx), slope, y[i]);
             y[i] = (bits >> i) & 1 ? y[i] - m0 : -INFINITY;
             top = fmaxf(top, y[i]);
