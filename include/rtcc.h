@@ -443,13 +443,14 @@ rtcc_status rtcc_pillarise_noalloc(const rtcc_model_config* cfg, const float* d_
  *   d_rows    int32 [n_tokens]    memory row of each token, -1 = none
  *   d_seq, d_pos int32 [n_tokens] its sequence and its place in it (may be NULL)
  *   d_begin, d_end int32 [n_seqs] the sequence's rows once its tokens are in
- *   d_length  int32 [n_seqs]      their number, at most capacity
+ *   d_length  int32 [n_seqs]      the tokens held and new, at most capacity
  * A token past its slot's capacity gets row -1 (causal attention of such a step
  * wants d_held as its d_q_start); entries past the total get -1
  * in all three token arrays.  Tokens that do not fit into n_tokens are dropped:
  * offsets are cut there, and they do not count towards the length.  Negative
  * counts read as 0, held counts are cut to the capacity, and a negative slot
- * or one whose rows pass 2^31 gets no rows and an empty span.
+ * or one whose rows pass 2^31 gets no rows and an empty span (its length is
+ * counted all the same).
  * 0 <= n_seqs <= 16384, capacity >= 1, n_tokens >= 0; d_length may be neither
  * d_held nor d_new.
  */
@@ -547,10 +548,10 @@ typedef struct {
  * A token that sees no key gets out = 0 and lse = -inf.  Sums and the softmax
  * are float32; for their product with v the probabilities are rounded to the
  * storage type, or to the sum of two of its numbers where a key head has few
- * query rows; out is rounded once.  In fp16, whose range is short, a key of a small
- * probability loses up to 2^-30 (2^-40 with few query rows) of the largest.  How a span is split depends on the sizes, the
- * workspace and the GPU, and changes the order of float32 sums; the same call
- * gives the same bits.  Rows that no token of a sequence sees (outside the span,
+ * query rows; out is rounded once.  In fp16, whose range is short, a key of a
+ * small probability loses up to 2^-30 (2^-40 with few query rows) of the largest.
+ * How a span is split depends on the sizes, the workspace and the GPU, and changes
+ * the order of float32 sums; the same call gives the same bits.  Rows that no token of a sequence sees (outside the span,
  * in an absent slot) are not used: they may hold anything, infinities and NaN
  * included.  (Seen by some of its tokens, a row whose v is not finite may make
  * the sequence's other tokens NaN too: their probability for it is 0.)  Tokens of
@@ -561,15 +562,18 @@ typedef struct {
  * three or none; d_out may be d_q with the same strides.  d_workspace: scratch
  * for splitting long spans over the GPU, used until the work is done, any
  * content.  Each part of a span takes n_q * heads * (head_dim + 2) * 4 bytes;
- * more parts than fill the GPU, or than one for 65,536 keys, are not made, and
- * without room for two (NULL, or too small) spans are not split.  A float32 sum
- * over n equally weighted keys of a part may come out smaller by n 2^-28 of
- * itself, so long spans want a workspace (and max_k).  scale, cap and scale / cap
- * are finite, cap between 0 and 1e38, scale / cap 0 or at least 2^-126 in
- * magnitude; capped scores are good to 2e-7 of the cap for caps up to 256, to 1e-6 of
- * themselves above.  n_rows and n_q * heads are at most 2^31 - 2^16,
- * heads at most 4096.  q, k, v, out and the workspace are 16-byte aligned, d_k_pos
- * 8-byte, the rest 4-byte.
+ * more parts than fill the GPU, or than keep sums within 65,536 keys, are not
+ * made, and without room for two (NULL, or too small) spans are not split.  A
+ * float32 sum over n equally weighted keys may come out smaller by n 2^-28 of
+ * itself, so long spans want a workspace (and max_k): room for max_k / 65,536 + 2
+ * parts keeps sums that short.  Calls with more than 128 query heads to a key head,
+ * or with a stride of 0 (several heads or rows at one place), take the kernel for
+ * few query rows whatever their size, several times slower at many rows.
+ * scale, cap and scale / cap are finite, cap between 0 and 1e38, scale / cap 0 or at
+ * least 2^-126 in magnitude; capped scores are good to 2e-7 of the cap for caps up
+ * to 256, to 1e-6 of themselves above.  n_rows and n_q * heads are at most
+ * 2^31 - 2^16, heads at most 4096.  q, k, v, out and the workspace are 16-byte
+ * aligned, d_k_pos 8-byte, the rest 4-byte.
  */
 rtcc_status rtcc_memory_attention(const rtcc_attn_config* cfg, const void* d_q, const void* d_k,
                                   const void* d_v, const int32_t* d_q_offsets,

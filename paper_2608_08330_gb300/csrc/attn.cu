@@ -84,8 +84,9 @@ long long rows_cluster(long long units, long long steps, long long split, long l
 // number of least cost, in steps of 64 keys.  Rounds of blocks over the SMs, each
 // with its share of the steps and about four steps' time to begin and end, and for
 // the merge two steps' time and the traffic of the partial results (a step takes
-// about 1.2 us).  With 384 units of 768 steps, one chunk leaves the third round
-// half empty, five fill 13 rounds.
+// about 1.2 us).  With 384 units of 768 steps, one chunk leaves the third round half
+// empty and five would fill 13 rounds, if the workspace has room for them: at 16,384
+// tokens of 6 heads of 64 a part takes 26 MB.
 long long tc_chunks(long long units, long long steps, long long least_chunks, long long most, int sms, int streams,
                     long long n_q, int heads, int dim) {
   const long long first = std::max(1LL, std::min(least_chunks, most));

@@ -23,8 +23,8 @@
 // fills the GPU; k_attn_join merges the chunks in index order, or, where the chunks
 // are few, the blocks of a cluster do it from one another's shared memory.
 // Measured: 61 tokens over ragged histories of up to 16,384 keys, 8 key heads of
-// 128, 1.9 GB: 294 to 297 us, 6.5 TB/s, 95 % of a plain copy's; one token over 4097 keys of
-// 6 heads of 64 takes 8.1 us, most of which is the launch, a block's first copies
+// 128, 1.9 GB: 300 us, 6.4 TB/s, 94 % of a plain copy's; one token over 4097 keys of
+// 6 heads of 64 takes 8.2 us, most of which is the launch, a block's first copies
 // and three steps.
 #include <type_traits>
 

@@ -34,15 +34,17 @@
 // their value rows are zeroed in shared memory before the product, so their
 // contents never reach a result.
 //
-// What bounds it is the softmax: exp2 takes 4 clocks a warp on the special-function
-// unit, a packed multiply-add 2 on the FMA pipe, and of those a capped score needs
-// 5, a biased one 5 more, beside 4 for the sum and the rest; with two softmax warps
-// on a scheduler a step's 64 keys take 1420 clocks bare, 1890 with a cap, 1950 with
-// a bias and 2630 with both, against 640 (heads of 64) or 1280 of the tensor pipe.
-// Measured: 16,384 x 49,152 keys, 6 heads of 64, cap and bias: 2.98 ms, 415 TFLOP/s;
-// 14,700 packed causal tokens of 16 heads of 128 with a cap: 130 us, 720 TFLOP/s
-// (of a block's 22 us there, 1 goes to its set-up, 2 to its first scores, 2 to the
-// masked step and 3 to its results).
+// What bounds it is the softmax warps' latency, no pipe alone.  Two of them share a
+// scheduler.  Their 64 keys take 1,420 clocks bare, 1,890 with a cap, 1,950 with a bias
+// and 2,630 with both, against 640 (heads of 64) or 1,280 of the tensor pipe.  A pair of
+// keys costs 1 packed multiply-add bare or 5 with a cap, 3 and two single adds for a
+// bias, and 1 for the sum: with both 1,280 clocks of the FMA pipe (packed ones take 2),
+// and 512 for exp2 (4 a warp).  The rest is waiting for scores from tensor memory and for
+// results.  Measured: 16,384 x 49,152 keys, 6 heads of 64: 1.54 ms bare (802 TFLOP/s),
+// 2.17 with a cap, 2.16 with a bias, 3.00 with both (412), each with a sixth of the SMs'
+// time lost to a half-empty third round of blocks; 12,036 packed causal tokens of 16
+// heads of 128 with a cap: 132 us, 711 TFLOP/s (of a block's 22 us there, 1 goes to its
+// set-up, 2 to its first scores, 2 to the masked step and 3 to its results).
 // Tried and slower: four chains of one S each (four softmax warps a scheduler, 96
 // registers: 10 to 30 %), the next S loaded while P is stored (spills: 5 to 15 %),
 // scalar beside packed arithmetic (up to 30 %), a second form of the pass for steps

@@ -24,11 +24,10 @@
 //   registers for all heads.  Eight heads' vectors are on their way to a ring in
 //   shared memory, every thread's own places, so nothing is waited for but the
 //   copy itself.  With few tokens a token's heads are divided among several groups
-//   of lanes.  Measured: 176,000 tokens of 18 heads of 64, 815 MB, 122 us: 6.7 TB/s,
-//   98 % of a plain copy's; 16,384 of them, a wave of blocks, 16.6 us, 68 %, or
-//   14.2 us, 79 %, where pairs are neighbours and no lane needs another's vector;
-//   12,345 tokens of 20 heads of 80 (10 of 16 lanes have channels) 19.0 us, 61 %;
-//   61 tokens 3.7 us.
+//   of lanes.  Measured: 176,000 tokens of 18 heads of 64, 815 MB, 121.5 us: 6.7 TB/s,
+//   99 % of a plain copy's; 16,384 of them 16.9 us, 66 %, or 14.6 us, 77 %, where pairs
+//   are neighbours and no lane needs another's vector; 12,345 tokens of 20 heads of 80
+//   (10 of 16 lanes have channels) 19.7 us, 59 %; 61 tokens 3.7 us.
 #include <math.h>
 
 #include <atomic>
