@@ -567,8 +567,9 @@ typedef struct {
  * float32 sum over n equally weighted keys may come out smaller by n 2^-28 of
  * itself, so long spans want a workspace (and max_k): room for max_k / 65,536 + 2
  * parts keeps sums that short.  Calls with more than 128 query heads to a key head,
- * or with a stride of 0 (several heads or rows at one place), take the kernel for
- * few query rows whatever their size, several times slower at many rows.
+ * with a stride of 0 (several heads or rows at one place), or without room and with
+ * a max_k above 2^20 (so do not overstate it) take the kernel for few query rows
+ * whatever their size, several times slower at many rows.
  * scale, cap and scale / cap are finite, cap between 0 and 1e38, scale / cap 0 or at
  * least 2^-126 in magnitude; capped scores are good to 2e-7 of the cap for caps up
  * to 256, to 1e-6 of themselves above.  n_rows and n_q * heads are at most
