@@ -630,7 +630,10 @@ def _exact_write(s, c):
                 lo, hi = max(h, b * BLOCK), min(h + n, (b + 1) * BLOCK)
                 page, row = table[q][b * BLOCK // pr], b * BLOCK % pr
                 y = x[off[q] + lo - h:off[q] + hi - h].double().transpose(0, 1)              # [kv, rows, d]
-                e = torch.ceil(torch.log2(y.abs().amax((1, 2)) / 448)).clamp(E_MIN, E_MAX)
+                top = y.abs().amax((1, 2))
+                e = torch.ceil(torch.log2(top / 448))                    # a logarithm next to a whole number may miss it
+                e = torch.where(448 * torch.exp2(e - 1) >= top, e - 1, e)
+                e = torch.where(448 * torch.exp2(e) < top, e + 1, e).clamp(E_MIN, E_MAX)
                 if lo > b * BLOCK:
                     was = scales[page, :, row // BLOCK, which]
                     e = torch.maximum(e, was)
