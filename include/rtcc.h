@@ -608,6 +608,212 @@ rtcc_status rtcc_memory_attention_status(void* stream);
 #define RTCC_TEST_NO_CLUSTERS 2
 rtcc_status rtcc_test_attention(int32_t what);
 
+/*
+ * rtcc_memory_attention with a sliding window: key j (of the span, from 0) is visible
+ * to token i at place p = i + start where
+ *   (j <= p and (j > p - window or j < sinks)) or j < d_prefix[s],
+ * in a present slot; everything else is as there, the workspace and its parts included.
+ * The first `sinks` keys thus stay visible to all later tokens.  cfg->causal is 1;
+ * window >= 1, sinks >= 0.  Keys between the sinks (or the prefix) and the window of a
+ * sequence's first token are neither read nor paid for; their rows may hold anything.
+ */
+rtcc_status rtcc_memory_window_attention(const rtcc_attn_config* cfg, int32_t window, int32_t sinks,
+                                         const void* d_q, const void* d_k, const void* d_v,
+                                         const int32_t* d_q_offsets, const int32_t* d_k_begin,
+                                         const int32_t* d_k_end, const int32_t* d_prefix,
+                                         const int32_t* d_present, const float* d_slopes,
+                                         const float* d_q_pos, const float* d_k_pos, void* d_out,
+                                         float* d_lse, void* d_workspace, size_t workspace_bytes,
+                                         void* stream);
+
+/* ------------------------------------------------------------------------ */
+/* Paged token memory: keys and values in 8 bits, on pages that branch      */
+/* ------------------------------------------------------------------------ */
+
+/*
+ * Histories of tokens that branch and age (hypotheses of tracked objects, streams of
+ * frames) are kept on pages of a pool instead of in slots.  A page holds the keys and
+ * values of page_rows consecutive places of a sequence; a table names the page of every
+ * page_rows places of each sequence (-1: none), and sequences may share pages.  Keys and
+ * values are e4m3 numbers (4 exponent bits, 3 fraction bits, largest 448) times a power
+ * of two for each block of 16 places and key head:
+ *   value = number * 2^exponent, exponent in [-120, 120].
+ * Arrays of a pool, which the caller owns:
+ *   keys, values  uint8 [n_pages][kv_heads][page_rows][head_dim]
+ *   exponents     int8  [n_pages][kv_heads][page_rows / 16][2], of keys and of values
+ * The tables and reference counts serve any number of pools (one per layer) alike.
+ *
+ * rtcc_pages_fork, rtcc_pages_extend and rtcc_pages_compact decide which pages sequences
+ * have, rtcc_pages_copy moves what they list, rtcc_pages_write rounds new tokens into
+ * their pages, rtcc_pages_attention attends to them.  All work is queued on the caller's
+ * stream (capturable), nothing is allocated, arrays live on the current device, and the
+ * same call gives the same bits.  Entries and page numbers come from device memory and
+ * are checked there: one outside [0, n_pages) is no page.
+ */
+
+/* Shapes of the pools and tables. */
+typedef struct {
+  int32_t kv_heads;                 /* 1..4096                               */
+  int32_t head_dim;                 /* a multiple of 16 in 16..128           */
+  int32_t page_rows;                /* 32, 64 or 128                         */
+  int32_t n_pages;                  /* pages of a pool, at most 2^26         */
+  int32_t n_seqs;                   /* sequences of the table                */
+  int32_t table_row;                /* pages of a sequence at most; table_row *
+                                       page_rows and n_seqs * table_row are at
+                                       most 2^30                             */
+  int64_t page_bytes;               /* bytes from a page's keys (values) to the
+                                       next page's, a multiple of 16; 0: dense */
+  int64_t scale_bytes;              /* the same of its exponents, a multiple of
+                                       4; 0: dense                           */
+} rtcc_page_config;
+
+/*
+ * Sequences take over pages: sequence s of the new table continues from sequence
+ * d_parent[s] of the old one (n_from rows of table_row entries), with its first
+ * min(d_length[parent], d_keep[s]) tokens (d_keep NULL: all of them); any number may
+ * continue from one parent.  A parent outside [0, n_from) leaves the sequence empty.
+ * With window > 0, pages whose places are all at or past `sinks` and behind the window
+ * of every later token (place + window <= tokens held) are dropped: -1.
+ *   d_length_out int32 [n_seqs]             tokens held
+ *   d_table_out  int32 [n_seqs][table_row]  pages, -1 from the last held place on
+ *   d_refs       int32 [n_pages]            entries of d_table_out that name each page
+ * Pages that nobody took over are thus free (0).  No output may overlap an input.
+ */
+rtcc_status rtcc_pages_fork(const rtcc_page_config* cfg, int32_t n_from, const int32_t* d_parent,
+                            const int32_t* d_keep, int32_t window, int32_t sinks,
+                            const int32_t* d_length, const int32_t* d_table,
+                            int32_t* d_length_out, int32_t* d_table_out, int32_t* d_refs,
+                            void* stream);
+
+/* Bytes of workspace that rtcc_pages_extend and rtcc_pages_compact need; 0 where cfg is
+ * not valid. */
+size_t rtcc_pages_workspace(const rtcc_page_config* cfg);
+
+/*
+ * Pages for the d_new[s] tokens that follow the d_length[s] held ones (at most up to
+ * place table_row * page_rows).  Wanted are, sequence by sequence in order of places, a
+ * page of its own for the last held place's page if that page has room left and others
+ * have it too when the call begins (or if there is none), and a page for every page_rows
+ * places after it; earlier contents of those entries are ignored.  The k-th wanted page
+ * is the k-th lowest-numbered page without references.  Where there are none left,
+ * entries are -1, the shared page stays, and the sequence's tokens end before.
+ *   d_table, d_refs                    as above, changed in place; d_refs of a page
+ *                                      that was given up goes down by one
+ *   d_length_out int32 [n_seqs]        places that the sequence has now (its new tokens
+ *                                      up to here have pages); may be d_length
+ *   d_copy_src, d_copy_dst int32 [n_seqs]  page given up and the page in its place,
+ *                                      whose first d_copy_rows [n_seqs] places are to
+ *                                      be copied (rtcc_pages_copy); -1, -1, 0: none
+ *   d_short int32 [1]                  wanted pages that there were not; may be NULL
+ * d_workspace: 16-byte aligned, rtcc_pages_workspace bytes, any content.
+ */
+rtcc_status rtcc_pages_extend(const rtcc_page_config* cfg, const int32_t* d_new,
+                              const int32_t* d_length, int32_t* d_table, int32_t* d_refs,
+                              int32_t* d_length_out, int32_t* d_copy_src, int32_t* d_copy_dst,
+                              int32_t* d_copy_rows, int32_t* d_short, void* d_workspace,
+                              size_t workspace_bytes, void* stream);
+
+/*
+ * The pages in use (references > 0), L of them, brought to numbers below L: the k-th
+ * page in use at or past L goes to the k-th free number below L.
+ *   d_move_src, d_move_dst int32 [n_pages]  from and to, the rest -1
+ *   d_count int32 [1]                       moves
+ *   d_table_out, d_refs_out                 with the new numbers; entries that name no
+ *                                           page in use become -1
+ * d_table_out may be d_table; no other output may overlap an input.  The workspace is
+ * that of rtcc_pages_extend.
+ */
+rtcc_status rtcc_pages_compact(const rtcc_page_config* cfg, const int32_t* d_table,
+                               const int32_t* d_refs, int32_t* d_table_out, int32_t* d_refs_out,
+                               int32_t* d_move_src, int32_t* d_move_dst, int32_t* d_count,
+                               void* d_workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Copies page d_src[i] of one pool to page d_dst[i] of another (or the same one) of
+ * n_pages_dst pages, for i below n and, if given, d_count[0]: keys and values of its
+ * first d_rows[i] places (d_rows NULL: of all), and the exponents of their blocks.
+ * Pairs with a number that is no page are left out.  A page may be listed once as a
+ * destination, and not as a source too; else what the page then holds is not defined.
+ * Both pools have the strides of cfg; cfg->n_pages is the source's.
+ */
+rtcc_status rtcc_pages_copy(const rtcc_page_config* cfg, int32_t n, const int32_t* d_count,
+                            const int32_t* d_src, const int32_t* d_dst, const int32_t* d_rows,
+                            const void* d_k_src, const void* d_v_src, const void* d_scales_src,
+                            int32_t n_pages_dst, void* d_k_dst, void* d_v_dst, void* d_scales_dst,
+                            void* stream);
+
+/* New tokens for rtcc_pages_write; strides in elements as in rtcc_prepare_config. */
+typedef struct {
+  int32_t dtype;                    /* rtcc_dtype of k and v                 */
+  int32_t n_tokens;                 /* tokens of all sequences               */
+  int32_t max_new;                  /* the most of one sequence; sizes the
+                                       launch only                           */
+  int32_t reserved;                 /* 0                                     */
+  int64_t k_row, k_head, v_row, v_head;
+} rtcc_write_config;
+
+/*
+ * Keys and values of new tokens into their pages.  Sequence s has the tokens
+ * [d_offsets[s], d_offsets[s + 1]); token i of it goes to place d_held[s] + i, if that
+ * is below d_length[s] (NULL: table_row * page_rows) and its entry of the table is a
+ * page; else it is left out.  A block's exponent is the least e with
+ * |x| <= 448 * 2^e for its new tokens' values x, or the block's own where tokens that
+ * it holds already (places below d_held[s]) have a larger one; those tokens' numbers are
+ * rounded again where e rises.  Numbers are x * 2^-e, rounded to nearest, ties to even;
+ * infinities and NaN become NaN and do not count for e.  Other rows are left untouched.
+ * The pages that one call writes to belong to one sequence each.
+ * k and v are 16-byte aligned, pages 16-byte, exponents 4-byte, the rest 4-byte.
+ */
+rtcc_status rtcc_pages_write(const rtcc_page_config* cfg, const rtcc_write_config* tokens,
+                             const void* d_k, const void* d_v, const int32_t* d_offsets,
+                             const int32_t* d_held, const int32_t* d_length,
+                             const int32_t* d_table, void* d_k_pages, void* d_v_pages,
+                             void* d_scales, void* stream);
+
+/* Queries for rtcc_pages_attention; strides in elements. */
+typedef struct {
+  int32_t heads;                    /* a multiple of kv_heads, at most 4096  */
+  int32_t dtype;                    /* rtcc_dtype of q and out               */
+  int32_t n_q;                      /* tokens of all sequences               */
+  int32_t max_q, max_k;             /* tokens and keys of a sequence at most:
+                                       its tokens from max_q on and keys from
+                                       max_k on are left out                 */
+  int32_t causal;                   /* 0: every token sees every key         */
+  int32_t window, sinks;            /* as in rtcc_memory_window_attention;
+                                       window 0: none (causal otherwise)     */
+  int64_t q_row, q_head, out_row, out_head;
+  float scale;                      /* of q.k, usually 1 / sqrt(head_dim)    */
+  float cap;                        /* scores are capped at +-cap; 0: no cap */
+} rtcc_page_attn_config;
+
+/*
+ * rtcc_memory_attention over the pages: sequence s has the tokens
+ * [d_q_offsets[s], d_q_offsets[s + 1]) and the keys at places [0, d_length[s]), its
+ * first token is at place d_start[s] (NULL: its tokens are the last places).  Key j is
+ * visible to the token at place p where
+ *   not causal, or j <= p and (no window, or j > p - window or j < sinks),
+ *   or j < d_prefix[s] (NULL = 0),
+ * and its page is one.  out and lse as there; pages that no token sees may hold
+ * anything.  Products are exact in the 8-bit numbers; queries of bf16 are scaled by a
+ * power of two per row and lose what is below 2^-39 of the row's largest where a key
+ * head has few query rows.
+ * Many rows (tokens times heads to a key head) want room in the workspace: besides the
+ * parts of rtcc_memory_attention the keys and values that tokens see are widened to
+ * 16 bits once, n_seqs * S * kv_heads * head_dim * 4 bytes and n_seqs * S / 64 + 256 more
+ * with S = max_k, or, with a window and no prefix, sinks + window + max_q + 192 if that
+ * is less, rounded up to a multiple of 64.  Without that room they take the kernel for few
+ * rows, several times slower.  With fp16, values that a pool got from bf16 tokens and
+ * that fp16 cannot hold are taken as its largest or smallest there.
+ * Limits and alignment as in rtcc_memory_attention; errors of its waits are reported by
+ * rtcc_memory_attention_status.
+ */
+rtcc_status rtcc_pages_attention(const rtcc_page_config* cfg, const rtcc_page_attn_config* rows,
+                                 const void* d_q, const int32_t* d_q_offsets, const int32_t* d_start,
+                                 const int32_t* d_length, const int32_t* d_prefix,
+                                 const int32_t* d_table, const void* d_k_pages,
+                                 const void* d_v_pages, const void* d_scales, void* d_out,
+                                 float* d_lse, void* d_workspace, size_t workspace_bytes, void* stream);
+
 /* ------------------------------------------------------------------------ */
 /* Release controller alone (host only; no GPU needed)                      */
 /* ------------------------------------------------------------------------ */

@@ -11,6 +11,7 @@
 
 #include "attn.cuh"
 #include "kernels.h"
+#include "pages.cuh"
 #include "rtcc.h"
 
 namespace rtcc {
@@ -20,6 +21,8 @@ namespace {
 // on: 33 rows over 9 ragged histories of 5001 keys, heads of 80, take 24 us there
 // and 27 in blocks of 16 rows, 30 rows over 50,000 keys, heads of 64, 25 and 23.
 constexpr int kTcRows = 32;
+// Over pages, whose keys and values are widened first, from this many on.
+constexpr int kTcPageRows = 64;
 
 // The tensor cores cut what does not fit the float32 sum off at every 16 keys' addition
 // (a unit in the last place at most), so a sum over n keys of equal weight comes out
@@ -112,29 +115,129 @@ bool bad_stride(int64_t s) { return s < 0 || s % 8 != 0; }
 }  // namespace
 }  // namespace rtcc
 
-using namespace rtcc;
+namespace rtcc {
+namespace {
 
-extern "C" rtcc_status rtcc_memory_attention(const rtcc_attn_config* c, const void* d_q, const void* d_k,
-                                             const void* d_v, const int32_t* d_q_offsets,
-                                             const int32_t* d_k_begin, const int32_t* d_k_end,
-                                             const int32_t* d_prefix, const int32_t* d_present,
-                                             const float* d_slopes, const float* d_q_pos,
-                                             const float* d_k_pos, void* d_out, float* d_lse,
-                                             void* d_workspace, size_t workspace_bytes, void* stream) {
+// Shapes and scores that 16-bit rows and pages have in common.
+bool bad_scores(int dtype, int heads, int kv_heads, float scale, float cap) {
+  if (dtype != RTCC_FP16 && dtype != RTCC_BF16) return true;
+  if (heads < 1 || heads > 4096 || kv_heads < 1 || heads % kv_heads) return true;
+  if (!isfinite(scale) || !isfinite(cap) || cap < 0.f) return true;
+  if (cap > 0.f) {
+    const float ratio = fabsf(scale / cap);
+    if (cap > 1e38f || !isfinite(ratio) || (ratio < FLT_MIN && scale != 0.f)) return true;
+  }
+  return false;
+}
+
+// Bytes of the workspace for keys and values widened from pages: both, then the steps' halves on no page.
+size_t widened_bytes(long long rows, const AttnArgs& a) {
+  return (size_t)rows * a.kv_heads * a.dim * 4 + ((size_t)rows / 64 + 255) / 256 * 256;
+}
+
+// Chooses kernel and split, and launches.  max_q, max_k size the launch; `pages`: the
+// keys and values are on pages (else NULL).
+rtcc_status run_attention(AttnArgs& a, const PagesArgs* pages, int max_q, int max_k, bool bf16, void* d_workspace,
+                          size_t workspace_bytes, cudaStream_t st) {
+  const int sms = sm_count();
+  if (sms < 1) return RTCC_E_CUDA;
+  const int test = g_test.load(std::memory_order_relaxed);
+  a.stall = (test & RTCC_TEST_UNREACHABLE_WAIT) != 0;
+  a.budget = a.stall ? kWaitBudgetCycles / 100 : kWaitBudgetCycles;
+  // keys of a sequence that its tokens see: with a window no more than the sinks, the
+  // tokens and a window, in whole steps
+  long long most_k = max_k;
+  if (a.window > 0 && !a.prefix) {
+    const long long seen = ((long long)a.sinks + 63) / 64 * 64 + a.window + max_q + 63LL;
+    if (seen < most_k) most_k = seen;
+  }
+  // the tensor-core kernel from kTcRows (token, head) rows per key head on
+  bool tc = (long long)max_q * a.group > (pages ? kTcPageRows : kTcRows) && a.group <= 128 && a.n_rows > 0;
+  const size_t part = (size_t)a.n_q * a.heads * (a.dim * sizeof(float) + sizeof(float2));
+  const long long span = (most_k + 63) / 64 * 64, span_rows = span * a.n_seqs;
+  size_t wide = pages ? widened_bytes(span_rows, a) : 0;
+  if (pages && (wide > workspace_bytes || !d_workspace || span_rows > kMaxRows)) tc = false;
+  bool clusters = true, widened = false;
+  for (;; tc = false) {
+    AttnArgs w = a;                              // as the kernel gets it
+    char* space = static_cast<char*>(d_workspace);
+    size_t left = d_workspace ? workspace_bytes : 0;
+    if (pages && tc) {
+      w.k = space;
+      w.v = space + (size_t)span_rows * a.kv_heads * a.dim * 2;
+      w.hidden = reinterpret_cast<unsigned char*>(space) + (size_t)span_rows * a.kv_heads * a.dim * 4;
+      w.k_row = w.v_row = (long long)a.kv_heads * a.dim;
+      w.k_head = w.v_head = a.dim;
+      w.span_rows = (int)span;
+      w.n_rows = (int)span_rows;
+      space += wide;
+      left -= wide;
+    }
+    const long long room = (long long)(left / part);
+    w.streams = tc ? attn_tc_streams(w.group, max_q) : 1;
+    if (w.streams > room) w.streams = 1;
+    w.unit = tc ? attn_tc_unit(w.streams) : pages ? attn_pages_unit() : attn_rows_unit(w.dim);
+    const long long step = tc ? attn_tc_tokens_per_block(w.group, w.streams) : 1;
+    long long groups = tc ? (max_q + step - 1) / step
+                          : ((long long)max_q * w.group + attn_rows_per_block() - 1) / attn_rows_per_block();
+    long long units = (long long)w.n_seqs * w.kv_heads;
+    if (units > 0x3FFFFFFF) return RTCC_E_ARG;
+    while (units * groups > 0x3FFFFFFF && groups > 1) groups = (groups + 1) / 2;   // blocks then loop
+    units *= groups;
+    w.row_groups = (int)groups;
+    const long long steps = (most_k + w.unit - 1LL) / w.unit;
+    long long most = tc ? (steps + 3) / 4 : steps;
+    // tokens that see mostly other keys than one another's leave nothing to split
+    if (tc && w.window > 0 && max_q > w.window) most = 1;
+    if (most > room / w.streams) most = room / w.streams;
+    if (most > 0x7FFFFFFF / units) most = 0x7FFFFFFF / units;
+    const long long sums = tc ? w.streams : 4;     // of a block
+    const long long least = (most_k + sums * kSumKeys - 1) / (sums * kSumKeys);
+    long long chunks = tc ? tc_chunks(units, steps, least, most, sms, w.streams, w.n_q, w.heads, w.dim)
+                          : rows_chunks(units, w.n_seqs, steps, least, most, sms);
+    if (tc && most_k / (chunks * sums) > kLongSum) continue;
+    const long long joined = tc || !clusters ? 1 : rows_cluster(units, steps, chunks, least, sms, w.dim);
+    w.cluster = joined > 1;
+    if (w.cluster) chunks = joined;
+    w.n_chunks = (int)chunks;
+    w.chunk = (int)((most_k + chunks - 1) / chunks);
+    w.part_o = reinterpret_cast<float*>(space);
+    w.part_ml = reinterpret_cast<float2*>(w.part_o + (size_t)chunks * w.streams * w.n_q * w.heads * w.dim);
+    if (pages && tc && !widened) {
+      const cudaError_t e = launch_pages_widen(a, *pages, const_cast<void*>(w.k), const_cast<void*>(w.v),
+                                               const_cast<unsigned char*>(w.hidden), (int)span, bf16, st);
+      if (e == cudaErrorNotSupported) continue;
+      if (e != cudaSuccess) return RTCC_E_CUDA;
+      widened = true;
+    }
+    cudaError_t e = w.cluster && (test & RTCC_TEST_NO_CLUSTERS) ? cudaErrorInvalidClusterSize
+                    : tc ? launch_attn_tc(w, bf16, st)
+                    : pages ? launch_attn_pages(w, *pages, bf16, st) : launch_attn_rows(w, bf16, st);
+    if (tc && e == cudaErrorNotSupported) continue;
+    if (w.cluster && e != cudaSuccess) {           // no room for such clusters (a part of a GPU): two launches
+      cudaGetLastError();
+      clusters = false;
+      continue;
+    }
+    if (e != cudaSuccess) return RTCC_E_CUDA;
+    if (!w.cluster && chunks * w.streams > 1 && launch_attn_join(w, max_q, bf16, st) != cudaSuccess) return RTCC_E_CUDA;
+    return RTCC_OK;
+  }
+}
+
+rtcc_status memory_attention(const rtcc_attn_config* c, int window, int sinks, const void* d_q, const void* d_k,
+                             const void* d_v, const int32_t* d_q_offsets, const int32_t* d_k_begin,
+                             const int32_t* d_k_end, const int32_t* d_prefix, const int32_t* d_present,
+                             const float* d_slopes, const float* d_q_pos, const float* d_k_pos, void* d_out,
+                             float* d_lse, void* d_workspace, size_t workspace_bytes, void* stream) {
   if (!c) return RTCC_E_ARG;
-  if (c->dtype != RTCC_FP16 && c->dtype != RTCC_BF16) return RTCC_E_ARG;
-  if (c->heads < 1 || c->heads > 4096 || c->kv_heads < 1 || c->heads % c->kv_heads) return RTCC_E_ARG;
+  if (bad_scores(c->dtype, c->heads, c->kv_heads, c->scale, c->cap)) return RTCC_E_ARG;
   if (c->head_dim < 8 || c->head_dim > 128 || c->head_dim % 8) return RTCC_E_ARG;
   if (c->n_q < 0 || c->n_rows < 0 || c->n_seqs < 0 || c->max_q < 0 || c->max_k < 0) return RTCC_E_ARG;
   if ((long long)c->n_q * c->heads > kMaxRows || c->n_rows > kMaxRows) return RTCC_E_ARG;
   const int64_t strides[] = {c->q_row, c->q_head, c->k_row, c->k_head, c->v_row, c->v_head, c->out_row, c->out_head};
   for (int64_t s : strides)
     if (bad_stride(s)) return RTCC_E_ARG;
-  if (!isfinite(c->scale) || !isfinite(c->cap) || c->cap < 0.f) return RTCC_E_ARG;
-  if (c->cap > 0.f) {
-    const float ratio = fabsf(c->scale / c->cap);
-    if (c->cap > 1e38f || !isfinite(ratio) || (ratio < FLT_MIN && c->scale != 0.f)) return RTCC_E_ARG;
-  }
   if (c->n_slots < 0 || c->n_slots > kMaxSlots || (c->n_slots > 0) != (d_present != nullptr)) return RTCC_E_ARG;
   if (c->n_slots > 0 && (c->slot_rows < 1 || (long long)c->n_slots * c->slot_rows < c->n_rows)) return RTCC_E_ARG;
   if ((d_slopes != nullptr) != (d_q_pos != nullptr) || (d_slopes != nullptr) != (d_k_pos != nullptr)) return RTCC_E_ARG;
@@ -151,8 +254,6 @@ extern "C" rtcc_status rtcc_memory_attention(const rtcc_attn_config* c, const vo
   if (misaligned(d_k_pos, 8)) return RTCC_E_ARG;
   if (c->n_q == 0 || c->n_seqs == 0) return RTCC_OK;
 
-  const int sms = sm_count();
-  if (sms < 1) return RTCC_E_CUDA;
   AttnArgs a{};
   a.q = d_q; a.k = d_k; a.v = d_v; a.out = d_out; a.lse = d_lse;
   a.q_offsets = d_q_offsets; a.k_begin = d_k_begin; a.k_end = d_k_end;
@@ -172,58 +273,86 @@ extern "C" rtcc_status rtcc_memory_attention(const rtcc_attn_config* c, const vo
   a.cap_log2 = c->cap * kLog2e;
   a.scale_log2 = c->cap > 0.f ? c->scale / c->cap : c->scale * kLog2e;
 
-  const int test = g_test.load(std::memory_order_relaxed);
-  a.stall = (test & RTCC_TEST_UNREACHABLE_WAIT) != 0;
-  a.budget = a.stall ? kWaitBudgetCycles / 100 : kWaitBudgetCycles;
+  a.window = window; a.sinks = sinks;
   const int max_q = c->max_q < 1 ? 1 : c->max_q > c->n_q ? c->n_q : c->max_q;
   const int max_k = c->max_k < 1 ? 1 : c->max_k > c->n_rows ? (c->n_rows < 1 ? 1 : c->n_rows) : c->max_k;
-  const bool bf16 = c->dtype == RTCC_BF16;
-  cudaStream_t st = static_cast<cudaStream_t>(stream);
-  // the tensor-core kernel from kTcRows (token, head) rows per key head on
-  bool tc = (long long)max_q * a.group > kTcRows && a.group <= 128 && c->n_rows > 0;
-  const size_t part = (size_t)c->n_q * c->heads * (c->head_dim * sizeof(float) + sizeof(float2));
-  const long long room = d_workspace ? (long long)(workspace_bytes / part) : 0;
-  bool clusters = true;
-  for (;; tc = false) {
-    a.streams = tc ? attn_tc_streams(a.group, max_q) : 1;
-    if (a.streams > room) a.streams = 1;
-    a.unit = tc ? attn_tc_unit(a.streams) : attn_rows_unit(c->head_dim);
-    const long long step = tc ? attn_tc_tokens_per_block(a.group, a.streams) : 1;
-    long long groups = tc ? (max_q + step - 1) / step
-                          : ((long long)max_q * a.group + attn_rows_per_block() - 1) / attn_rows_per_block();
-    long long units = (long long)c->n_seqs * a.kv_heads;
-    if (units > 0x3FFFFFFF) return RTCC_E_ARG;
-    while (units * groups > 0x3FFFFFFF && groups > 1) groups = (groups + 1) / 2;   // blocks then loop
-    units *= groups;
-    a.row_groups = (int)groups;
-    const long long steps = (max_k + a.unit - 1LL) / a.unit;
-    long long most = tc ? (steps + 3) / 4 : steps;
-    if (most > room / a.streams) most = room / a.streams;
-    if (most > 0x7FFFFFFF / units) most = 0x7FFFFFFF / units;
-    const long long sums = tc ? a.streams : 4;     // of a block
-    const long long least = (max_k + sums * kSumKeys - 1) / (sums * kSumKeys);
-    long long chunks = tc ? tc_chunks(units, steps, least, most, sms, a.streams, a.n_q, a.heads, a.dim)
-                          : rows_chunks(units, c->n_seqs, steps, least, most, sms);
-    if (tc && max_k / (chunks * sums) > kLongSum) continue;
-    const long long joined = tc || !clusters ? 1 : rows_cluster(units, steps, chunks, least, sms, a.dim);
-    a.cluster = joined > 1;
-    if (a.cluster) chunks = joined;
-    a.n_chunks = (int)chunks;
-    a.chunk = (int)((max_k + chunks - 1) / chunks);
-    a.part_o = static_cast<float*>(d_workspace);
-    a.part_ml = reinterpret_cast<float2*>(a.part_o + (size_t)chunks * a.streams * c->n_q * c->heads * c->head_dim);
-    cudaError_t e = a.cluster && (test & RTCC_TEST_NO_CLUSTERS) ? cudaErrorInvalidClusterSize
-                    : tc ? launch_attn_tc(a, bf16, st) : launch_attn_rows(a, bf16, st);
-    if (tc && e == cudaErrorNotSupported) continue;
-    if (a.cluster && e != cudaSuccess) {           // no room for such clusters (a part of a GPU): two launches
-      cudaGetLastError();
-      clusters = false;
-      continue;
-    }
-    if (e != cudaSuccess) return RTCC_E_CUDA;
-    if (!a.cluster && chunks * a.streams > 1 && launch_attn_join(a, max_q, bf16, st) != cudaSuccess) return RTCC_E_CUDA;
-    return RTCC_OK;
-  }
+  return run_attention(a, nullptr, max_q, max_k, c->dtype == RTCC_BF16, d_workspace, workspace_bytes,
+                       static_cast<cudaStream_t>(stream));
+}
+
+}  // namespace
+}  // namespace rtcc
+
+using namespace rtcc;
+
+extern "C" rtcc_status rtcc_memory_attention(const rtcc_attn_config* c, const void* d_q, const void* d_k,
+                                             const void* d_v, const int32_t* d_q_offsets,
+                                             const int32_t* d_k_begin, const int32_t* d_k_end,
+                                             const int32_t* d_prefix, const int32_t* d_present,
+                                             const float* d_slopes, const float* d_q_pos,
+                                             const float* d_k_pos, void* d_out, float* d_lse,
+                                             void* d_workspace, size_t workspace_bytes, void* stream) {
+  return memory_attention(c, 0, 0, d_q, d_k, d_v, d_q_offsets, d_k_begin, d_k_end, d_prefix, d_present, d_slopes,
+                          d_q_pos, d_k_pos, d_out, d_lse, d_workspace, workspace_bytes, stream);
+}
+
+extern "C" rtcc_status rtcc_memory_window_attention(const rtcc_attn_config* c, int32_t window, int32_t sinks,
+                                                    const void* d_q, const void* d_k, const void* d_v,
+                                                    const int32_t* d_q_offsets, const int32_t* d_k_begin,
+                                                    const int32_t* d_k_end, const int32_t* d_prefix,
+                                                    const int32_t* d_present, const float* d_slopes,
+                                                    const float* d_q_pos, const float* d_k_pos, void* d_out,
+                                                    float* d_lse, void* d_workspace, size_t workspace_bytes,
+                                                    void* stream) {
+  if (!c || !c->causal || window < 1 || sinks < 0) return RTCC_E_ARG;
+  return memory_attention(c, window, sinks, d_q, d_k, d_v, d_q_offsets, d_k_begin, d_k_end, d_prefix, d_present,
+                          d_slopes, d_q_pos, d_k_pos, d_out, d_lse, d_workspace, workspace_bytes, stream);
+}
+
+extern "C" rtcc_status rtcc_pages_attention(const rtcc_page_config* cfg, const rtcc_page_attn_config* c, const void* d_q,
+                                            const int32_t* d_q_offsets, const int32_t* d_start, const int32_t* d_length,
+                                            const int32_t* d_prefix, const int32_t* d_table, const void* d_k_pages,
+                                            const void* d_v_pages, const void* d_scales, void* d_out, float* d_lse,
+                                            void* d_workspace, size_t workspace_bytes, void* stream) {
+  PagesArgs p{};
+  if (!page_shape(cfg, &p.s) || !c) return RTCC_E_ARG;
+  if (bad_scores(c->dtype, c->heads, p.s.kv_heads, c->scale, c->cap)) return RTCC_E_ARG;
+  if (c->n_q < 0 || c->max_q < 0 || c->max_k < 0 || (long long)c->n_q * c->heads > kMaxRows) return RTCC_E_ARG;
+  const int64_t strides[] = {c->q_row, c->q_head, c->out_row, c->out_head};
+  for (int64_t s : strides)
+    if (bad_stride(s)) return RTCC_E_ARG;
+  if (c->window < 0 || c->sinks < 0 || (c->window > 0 && !c->causal)) return RTCC_E_ARG;
+  const long long cells = (long long)p.s.n_seqs * p.s.table_row;
+  if (p.s.n_seqs > 0 && (!d_q_offsets || !d_length || (cells > 0 && !d_table))) return RTCC_E_ARG;
+  if (c->n_q > 0 && (!d_q || !d_out)) return RTCC_E_ARG;
+  if (p.s.n_pages > 0 && (!d_k_pages || !d_v_pages || !d_scales)) return RTCC_E_ARG;
+  const void* by16[] = {d_q, d_k_pages, d_v_pages, d_out, d_workspace};
+  for (const void* x : by16)
+    if (misaligned(x, 16)) return RTCC_E_ARG;
+  const void* by4[] = {d_q_offsets, d_start, d_length, d_prefix, d_table, d_scales, d_lse};
+  for (const void* x : by4)
+    if (misaligned(x, 4)) return RTCC_E_ARG;
+  if (c->n_q == 0 || p.s.n_seqs == 0) return RTCC_OK;
+
+  p.table = d_table;
+  p.k = static_cast<const unsigned char*>(d_k_pages);
+  p.v = static_cast<const unsigned char*>(d_v_pages);
+  p.scales = static_cast<const signed char*>(d_scales);
+  const int places = p.s.table_row << p.s.shift;
+  const int max_q = c->max_q > c->n_q ? c->n_q : c->max_q, max_k = c->max_k > places ? places : c->max_k;
+  AttnArgs a{};
+  a.q = d_q; a.out = d_out; a.lse = d_lse;
+  a.q_offsets = d_q_offsets; a.k_end = d_length; a.prefix = d_prefix; a.q_start = d_start;
+  a.q_row = c->q_row; a.q_head = c->q_head; a.out_row = c->out_row; a.out_head = c->out_head;
+  a.n_q = c->n_q; a.n_rows = places; a.heads = c->heads; a.kv_heads = p.s.kv_heads;
+  a.group = c->heads / p.s.kv_heads; a.dim = p.s.dim; a.n_seqs = p.s.n_seqs; a.causal = c->causal != 0;
+  a.slot_rows = 1;
+  a.cap_log2 = c->cap * kLog2e;
+  a.scale_log2 = c->cap > 0.f ? c->scale / c->cap : c->scale * kLog2e;
+  a.window = c->window; a.sinks = c->sinks;
+  a.most_q = max_q; a.most_k = max_k;
+  return run_attention(a, &p, max_q < 1 ? 1 : max_q, max_k < 1 ? 1 : max_k, c->dtype == RTCC_BF16, d_workspace,
+                       workspace_bytes, static_cast<cudaStream_t>(stream));
 }
 
 // The device counts and nothing clears the count, so no failure is lost between a read

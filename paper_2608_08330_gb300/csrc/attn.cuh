@@ -36,38 +36,90 @@ struct AttnArgs {
   float cap_log2;                // cap * log2(e), 0 = no cap
   long long budget;              // cycles of a bounded wait
   int stall;                     // test hook: the queries are never loaded
+  // Kernels with WIN (a window, or pages) look at these as well.
+  int window, sinks;             // window 0: none
+  int most_q, most_k;            // pages: tokens and keys of a sequence past these are left out
+  int span_rows;                 // > 0: keys widened from pages, a sequence's from row seq * span_rows on
+  const unsigned char* hidden;   // then [n_seqs][span_rows / 64]: bit h set: half h of a step is on no page
 };
 
 // One sequence: its tokens [q0, q0 + nq) and memory rows [kb, kb + nk), the first
 // token's place among the keys (a causal token i sees keys up to first + i; negative
 // where there are more tokens than keys).  Offsets come from device memory, so they
 // are cut to the arrays' extents; keys after the last token's are left out.
+//
+// With a window, keys behind the first token's, past the sinks and the prefix, are seen
+// by nobody.  Whole steps of them (64 keys) are taken out of the span: keys are numbered
+// without them from there on (nk and first too), `dead` is the first number after the
+// gap and `shift` its length; attn_row gives a number's row.  Every token's window then
+// begins past `dead`, so that masks need no gap.
 struct AttnSpan {
   int q0, nq, kb, nk, prefix, first;
+  int dead, shift;
 };
 
+template <bool WIN = false>
 __device__ __forceinline__ AttnSpan attn_span(const AttnArgs& A, int seq) {
   AttnSpan s;
   const int q0 = A.q_offsets[seq], q1 = A.q_offsets[seq + 1];
-  const int kb = A.k_begin[seq], ke = A.k_end[seq];
   s.q0 = min(max(q0, 0), A.n_q);
   s.nq = min(max(q1, s.q0), A.n_q) - s.q0;
-  s.kb = min(max(kb, 0), A.n_rows);
-  s.nk = min(max(ke, s.kb), A.n_rows) - s.kb;
+  s.dead = 0x7FFFFFFF;
+  s.shift = 0;
+  if (WIN && !A.k_begin) {                       // pages: places from 0 on
+    s.kb = 0;
+    s.nk = min(max(A.k_end[seq], 0), A.most_k);
+  } else {
+    const int kb = A.k_begin[seq], ke = A.k_end[seq];
+    s.kb = min(max(kb, 0), A.n_rows);
+    s.nk = min(max(ke, s.kb), A.n_rows) - s.kb;
+  }
   s.prefix = A.prefix ? min(max(A.prefix[seq], 0), s.nk) : 0;
   s.first = s.nk - s.nq;
   if (A.causal && A.q_start) {
     s.first = min(max(A.q_start[seq], 0), s.nk);
     if (s.nk - s.first > s.nq) s.nk = max(s.prefix, s.first + s.nq);
   }
+  if (WIN) {
+    if (!A.k_begin) s.nq = min(s.nq, A.most_q);
+    if (A.window > 0) {
+      const int own = s.nq < s.nk - s.first ? s.first + s.nq : s.nk;
+      const int seen = max(s.prefix, min(A.sinks, own));                 // keys before this are seen from afar
+      const int low = (int)max(0LL, (long long)s.first + 1 - A.window);
+      const int dead = (seen + 63) & ~63;
+      if ((low & ~63) > dead) {
+        s.dead = dead;
+        s.shift = (low & ~63) - dead;
+        s.nk -= s.shift;
+        s.first -= s.shift;
+      }
+    }
+    if (A.span_rows > 0) {                       // widened keys lie without the gap
+      s.kb = seq * A.span_rows;
+      s.dead = 0x7FFFFFFF;
+    }
+  }
   return s;
 }
+
+// Memory row of key j.
+__device__ __forceinline__ int attn_row(const AttnSpan& s, int j) { return s.kb + j + (j >= s.dead ? s.shift : 0); }
 
 // Keys [0, n) of the span that token i of the sequence sees (slots aside).
 __device__ __forceinline__ int attn_visible(const AttnArgs& A, const AttnSpan& s, int first, int i) {
   if (!A.causal) return s.nk;
   const int own = i < s.nk - first ? first + i + 1 : s.nk;
   return max(0, max(s.prefix, own));
+}
+
+// With a window, token i sees keys [0, seen) and [low, attn_visible) instead.
+struct AttnView {
+  int seen, low;
+};
+__device__ __forceinline__ AttnView attn_view(const AttnArgs& A, const AttnSpan& s, int first, int i) {
+  if (A.window == 0) return {0, 0};
+  const int own = i < s.nk - first ? first + i + 1 : s.nk;
+  return {max(s.prefix, min(A.sinks, own)), (int)max(0LL, (long long)first + i + 1 - A.window)};
 }
 
 // Slot of a memory row (there are at most 64).

@@ -1,0 +1,447 @@
+// Attention of a few rows over pages of 8-bit keys and values, and the widening of
+// pages to 16 bits for the tensor-core kernel of many rows.
+//
+// The formula is attn_rows.cu's, with k = 2^e_k k8 and v = 2^e_v v8: e4m3 numbers and an
+// exponent for every 16 places of a page and key head.  e4m3 numbers are fp16 numbers, so
+// both products run on them exactly (mma.m16n8k16 fp16, float32 sums), for queries of
+// either type, and the exponents go where they cost least: e_k into the factor of the
+// scores, e_v into the probabilities, relative to the largest e_v that the warp has met
+// (E; its accumulators are in units of 2^E).  bf16 queries are scaled by a power of two
+// per row so that the largest is below 2^15; what is more than 2^39 below it is lost.
+//
+// As in attn_rows.cu a block has 16 (token, head) rows of one key head and a chunk of the
+// keys, its four warps take tiles of 32 keys in turn through rings of their own, and
+// rows of the memory that no query sees are not read.  A tile lies in one page, whose
+// number is fetched a round ahead of the copies.  Channels are permuted within groups
+// of 16 so that what ldmatrix gives a lane (4 bytes of a key; 2 bytes of two keys'
+// values) is what its products need: no number crosses lanes.
+#include <type_traits>
+
+#include "attn_rows.cuh"
+#include "kernels.h"
+#include "pages.cuh"
+
+namespace rtcc {
+namespace {
+
+constexpr int KT = 32;                           // keys of a tile
+
+template <int DP> struct PagesCfg {              // DP: head size padded to 64 or 128
+  static constexpr int kStages = DP == 64 ? 6 : 3;
+  static constexpr int kTileBytes = KT * DP;
+  static constexpr int kStageBytes = 2 * kTileBytes;
+  static constexpr int kRing = kWarps * kStages * kStageBytes;
+  static constexpr int kNotes = kWarps * kStages * 8;        // per stage: exponents, keys that may be read
+  static constexpr int kSmem = kRing + kNotes;
+  static_assert((kWarps + 1) * kRows * (DP + 4) * 4 <= kRing, "states at the end lie in the ring");
+};
+
+__device__ __forceinline__ void cp4(uint32_t dst, const void* src) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void cp16z(uint32_t dst, const void* src, bool live) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(live ? 16 : 0) : "memory");
+}
+
+// Byte offset of 16-byte unit c of row r in a tile of DP-byte rows; units are permuted
+// within 128-byte lines so that ldmatrix reads 8 rows without bank conflicts.
+template <int DP>
+__device__ __forceinline__ uint32_t tile8_off(int r, int c) {
+  if (DP == 128) return (uint32_t)(r * 128 + ((c ^ (r & 7)) * 16));
+  return (uint32_t)((r >> 1) * 128 + ((((r & 1) * 4 + c) ^ ((r >> 1) & 3)) * 16));
+}
+
+// 2^e, 0 below the float range.
+__device__ __forceinline__ float pow2_or_0(int e) { return e < -126 ? 0.f : pow2(e); }
+
+template <typename T, int DP, bool CLUSTER>
+__global__ void __launch_bounds__(kWarps * 32, 2)
+    k_attn_pages(const __grid_constant__ AttnArgs A, const __grid_constant__ PagesArgs P) {
+  using C = PagesCfg<DP>;
+  constexpr int kStages = C::kStages;
+  extern __shared__ __align__(128) unsigned char smem[];
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+  // block -> (sequence, key head, first row group, chunk), chunks fastest
+  int b = blockIdx.x;
+  const int chunk = b % A.n_chunks;
+  b /= A.n_chunks;
+  const int rg0 = b % A.row_groups;
+  b /= A.row_groups;
+  const int kvh = b % A.kv_heads;
+  const int seq = b / A.kv_heads;
+  const AttnSpan S = attn_span<true>(A, seq);
+  const int rows_all = S.nq * A.group;
+  const int per = attn_chunk(A, S.nk, A.unit);
+  const int c0 = (int)min((long long)per * chunk, (long long)S.nk), c1 = min(S.nk - c0, per) + c0;
+  if (!CLUSTER && chunk > 0 && c0 >= S.nk) return;   // not in use; chunk 0 always answers
+  const uint32_t ring = smem_u32(smem) + w * kStages * C::kStageBytes;
+  const uint32_t notes = smem_u32(smem) + C::kRing + w * kStages * 8;
+  uint32_t* notes_g = reinterpret_cast<uint32_t*>(smem + C::kRing + w * kStages * 8);
+  const bool far_cap = A.cap_log2 > kAbsCap * kLog2e;
+  const int* table = P.table + (long long)seq * P.s.table_row;
+  const long long head_at = (long long)kvh * P.s.page_rows * A.dim;
+  const long long scale_at = (long long)kvh * (P.s.page_rows / kPageBlock) * 2;
+
+  for (int rg = rg0; (long long)rg * kRows < rows_all; rg += A.row_groups) {
+    const int r0 = rg * kRows;
+    // this lane's two rows: lane / 4 and 8 further
+    int hi[2], head[2];
+    AttnView view[2];
+    bool row_ok[2];
+    long long tok[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int r = r0 + lane / 4 + 8 * i;
+      row_ok[i] = r < rows_all;
+      const int ql = row_ok[i] ? r / A.group : 0;
+      head[i] = kvh * A.group + (row_ok[i] ? r % A.group : 0);
+      tok[i] = S.q0 + ql;
+      hi[i] = row_ok[i] ? attn_visible(A, S, S.first, ql) : 0;
+      view[i] = attn_view(A, S, S.first, ql);
+    }
+    // the rows' reach, and what some or all of them see of keys behind their windows
+    const int ql0 = r0 / A.group, ql1 = (min(r0 + kRows, rows_all) - 1) / A.group;
+    const int end = min(c1, attn_visible(A, S, S.first, ql1)), least = attn_visible(A, S, S.first, ql0);
+    const AttnView first = attn_view(A, S, S.first, ql0), last = attn_view(A, S, S.first, ql1);
+    // A fragments of Q: step s has channels 16 s + 4 (lane % 4) + {0, 1 | 2, 3}
+    uint32_t qa[DP / 16][4];
+    float qs[2];                                 // what the scores are multiplied by
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      uint2 x[DP / 16];
+      const T* q = static_cast<const T*>(A.q) + tok[i] * A.q_row + (long long)head[i] * A.q_head;
+#pragma unroll
+      for (int s = 0; s < DP / 16; ++s) {
+        const int col = s * 16 + (lane % 4) * 4;
+        x[s] = row_ok[i] && col < A.dim ? *reinterpret_cast<const uint2*>(q + col) : make_uint2(0u, 0u);
+      }
+      qs[i] = A.scale_log2;
+      if (std::is_same<T, __nv_bfloat16>::value) {
+        float top = 0.f;
+#pragma unroll
+        for (int s = 0; s < DP / 16; ++s) {
+          const float2 f = Store<T>::unpack2(x[s].x), g = Store<T>::unpack2(x[s].y);
+          const float v[4] = {fabsf(f.x), fabsf(f.y), fabsf(g.x), fabsf(g.y)};
+#pragma unroll
+          for (int k = 0; k < 4; ++k) top = fmaxf(top, v[k] < INFINITY ? v[k] : 0.f);
+        }
+        top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+        top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
+        const int e = max((int)(__float_as_uint(top) >> 23) - 127 - 14, -110);   // top 2^-e in [2^14, 2^15)
+        const float down = pow2(-e);
+        qs[i] *= pow2(e);
+#pragma unroll
+        for (int s = 0; s < DP / 16; ++s) {
+          const float2 f = Store<T>::unpack2(x[s].x), g = Store<T>::unpack2(x[s].y);
+          qa[s][i] = Store<__half>::pack2(f.x * down, f.y * down);
+          qa[s][i + 2] = Store<__half>::pack2(g.x * down, g.y * down);
+        }
+      } else {
+#pragma unroll
+        for (int s = 0; s < DP / 16; ++s) {
+          qa[s][i] = x[s].x;
+          qa[s][i + 2] = x[s].y;
+        }
+      }
+    }
+    float o[DP / 8][4];                          // [2 u], [2 u + 1]: even, odd channels of unit u
+#pragma unroll
+    for (int n = 0; n < DP / 8; ++n) o[n][0] = o[n][1] = o[n][2] = o[n][3] = 0.f;
+    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+    int unit = kExpMin;                          // o is in units of 2^unit
+
+    const int n_tiles = end > c0 ? (end - c0 + KT - 1) / KT : 0;
+    auto page_of = [&](int t) -> int {           // of tile t, -1: none
+      if (t >= n_tiles) return -1;
+      const int page = table[attn_row(S, c0 + t * KT) >> P.s.shift];
+      return (unsigned)page < (unsigned)P.s.n_pages ? page : -1;
+    };
+    auto load = [&](int t, int stage, int page) {
+      const int j = c0 + t * KT + lane;
+      const bool ok = page >= 0 && j < end && (j < last.seen || j >= first.low);
+      const unsigned bits = __ballot_sync(0xFFFFFFFFu, ok);
+      if (bits) {
+        const uint32_t ks = ring + stage * C::kStageBytes, vs = ks + C::kTileBytes;
+        const int row = attn_row(S, c0 + t * KT) & (P.s.page_rows - 1);
+        const long long at = page * P.s.page_bytes + head_at + (long long)row * A.dim;
+        constexpr int U = DP / 16;               // 16-byte units of a row
+#pragma unroll
+        for (int i = 0; i < KT * U / 32; ++i) {
+          const int idx = i * 32 + lane, r = idx / U, c = idx % U;
+          const bool live = (bits >> r) & 1 && c * 16 < A.dim;
+          const int off = live ? r * A.dim + c * 16 : 0;
+          const uint32_t to = tile8_off<DP>(r, c);
+          cp16z(ks + to, P.k + at + off, live);
+          cp16z(vs + to, P.v + at + off, live);
+        }
+        if (lane == 0)
+          cp4(notes + stage * 8, P.scales + page * P.s.scale_bytes + scale_at + (row / kPageBlock) * 2);
+      }
+      if (lane == 0) notes_g[stage * 2 + 1] = bits;
+      cp_async_commit();
+    };
+#pragma unroll
+    for (int s = 0; s < kStages - 1; ++s) load(w + s * kWarps, s, page_of(w + s * kWarps));
+    int page = page_of(w + (kStages - 1) * kWarps);
+    int stage = 0;
+    for (int t = w; t < n_tiles; t += kWarps) {
+      cp_async_wait<kStages - 2>();
+      __syncwarp();
+      load(t + (kStages - 1) * kWarps, (stage + kStages - 1) % kStages, page);
+      page = page_of(t + kStages * kWarps);
+      const unsigned bits = notes_g[stage * 2 + 1];
+      if (bits) {
+        const uint32_t ks = ring + stage * C::kStageBytes, vs = ks + C::kTileBytes;
+        const uint32_t exps = notes_g[stage * 2];
+        float s[KT / 8][4];
+#pragma unroll
+        for (int n = 0; n < KT / 8; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f;
+#pragma unroll
+        for (int d = 0; d < DP / 64; ++d)        // 64 channels: four k16 steps, one ldmatrix.x4 per 8 keys
+#pragma unroll
+          for (int n = 0; n < KT / 8; ++n) {
+            uint32_t k4[4];
+            ldm4(ks + tile8_off<DP>(n * 8 + (lane & 7), d * 4 + (lane >> 3)), k4);
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+              mma16816<__half>(s[n], qa[d * 4 + u], widen_e4m3x2(k4[u]), widen_e4m3x2(k4[u] >> 16));
+          }
+        const int j0 = c0 + t * KT;
+        const bool edge = bits != 0xFFFFFFFFu || j0 + KT > least || (j0 < last.low && j0 + KT > first.seen);
+        float top[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+        for (int n = 0; n < KT / 8; ++n) {
+          const float ke = pow2(max((int)(signed char)(exps >> (n / 2 * 16)), kExpMin));
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int key = n * 8 + (lane & 3) * 2 + (i & 1), rr = i >> 1;
+            float x = s[n][i] * qs[rr] * ke;
+            if (A.cap_log2 > 0.f) x = A.cap_log2 * (far_cap ? tanh_rel(x) : tanh_abs(x));
+            if (edge) {
+              const int j = j0 + key;
+              if (!((bits >> key) & 1) || j >= hi[rr] || (j >= view[rr].seen && j < view[rr].low)) x = -INFINITY;
+            }
+            s[n][i] = x;
+            top[rr] = fmaxf(top[rr], x);
+          }
+        }
+        constexpr float kLift = 15.0f;           // log2 of the largest probability, for fp16's range
+#pragma unroll
+        for (int rr = 0; rr < 2; ++rr) {
+          top[rr] = fmaxf(top[rr], __shfl_xor_sync(0xFFFFFFFFu, top[rr], 1));
+          top[rr] = fmaxf(top[rr], __shfl_xor_sync(0xFFFFFFFFu, top[rr], 2));
+          const float mn = fmaxf(m[rr], top[rr] - kLift);
+          const float base = mn == -INFINITY ? 0.f : mn;
+          const float f = exp2f(m[rr] - base);   // m = -inf: 0
+          m[rr] = mn;
+          l[rr] *= f;
+          top[rr] = base;
+          if (__any_sync(0xFFFFFFFFu, f != 1.0f)) {
+#pragma unroll
+            for (int n = 0; n < DP / 8; ++n) {
+              o[n][2 * rr] *= f;
+              o[n][2 * rr + 1] *= f;
+            }
+          }
+        }
+        float sum[2] = {0.f, 0.f};               // a tile's sum first, as in attn_rows.cu
+#pragma unroll
+        for (int n = 0; n < KT / 8; ++n)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            s[n][i] = exp2f(s[n][i] - top[i >> 1]);
+            sum[i >> 1] += s[n][i];
+          }
+        l[0] += sum[0];
+        l[1] += sum[1];
+        // values' exponents; a block that nobody sees has none
+        int ve[2];
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk)
+          ve[kk] = (bits >> (kk * 16)) & 0xFFFFu ? max((int)(signed char)(exps >> (kk * 16 + 8)), kExpMin) : kExpMin;
+        const int up = max(ve[0], ve[1]);
+        if (up > unit) {
+          const float f = pow2_or_0(unit - up);
+#pragma unroll
+          for (int n = 0; n < DP / 8; ++n) {
+            o[n][0] *= f;
+            o[n][1] *= f;
+            o[n][2] *= f;
+            o[n][3] *= f;
+          }
+          unit = up;
+        }
+#pragma unroll
+        for (int kk = 0; kk < KT / 16; ++kk) {
+          const float f = pow2_or_0(ve[kk] - unit);
+          // probabilities as two terms, as in attn_rows.cu
+          uint32_t pa[4], pl[4];
+          split2<__half>(s[2 * kk][0] * f, s[2 * kk][1] * f, pa[0], pl[0]);
+          split2<__half>(s[2 * kk][2] * f, s[2 * kk][3] * f, pa[1], pl[1]);
+          split2<__half>(s[2 * kk + 1][0] * f, s[2 * kk + 1][1] * f, pa[2], pl[2]);
+          split2<__half>(s[2 * kk + 1][2] * f, s[2 * kk + 1][3] * f, pa[3], pl[3]);
+#pragma unroll
+          for (int u = 0; u < DP / 16; u += 2) {
+            uint32_t v4[4];                      // units u, u + 1: keys 2c, 2c + 1 and 8 further, channels 2g, 2g + 1
+            ldm4t(vs + tile8_off<DP>(kk * 16 + (lane & 15), u + (lane >> 4)), v4);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const uint32_t even = __byte_perm(v4[2 * h], v4[2 * h + 1], 0x6420);
+              const uint32_t odd = __byte_perm(v4[2 * h], v4[2 * h + 1], 0x7531);
+              const uint32_t e0 = widen_e4m3x2(even), e1 = widen_e4m3x2(even >> 16);
+              const uint32_t d0 = widen_e4m3x2(odd), d1 = widen_e4m3x2(odd >> 16);
+              mma16816<__half>(o[2 * (u + h)], pa, e0, e1);
+              mma16816<__half>(o[2 * (u + h) + 1], pa, d0, d1);
+              mma16816<__half>(o[2 * (u + h)], pl, e0, e1);
+              mma16816<__half>(o[2 * (u + h) + 1], pl, d0, d1);
+            }
+          }
+        }
+      }
+      stage = (stage + 1) % kStages;
+    }
+    cp_async_wait<0>();
+#pragma unroll
+    for (int rr = 0; rr < 2; ++rr) {
+      l[rr] += __shfl_xor_sync(0xFFFFFFFFu, l[rr], 1);
+      l[rr] += __shfl_xor_sync(0xFFFFFFFFu, l[rr], 2);
+    }
+    // the states leave with probabilities of at most 1 and without units
+    __syncthreads();
+    float* mo = reinterpret_cast<float*>(smem);
+    constexpr float kDrop = 1.0f / 32768.0f;
+    const float back = pow2(unit);
+#pragma unroll
+    for (int rr = 0; rr < 2; ++rr) {
+      float* dst = mo + (w * kRows + lane / 4 + 8 * rr) * (DP + 4);
+#pragma unroll
+      for (int u = 0; u < DP / 16; ++u)
+        *reinterpret_cast<float4*>(dst + u * 16 + (lane & 3) * 4) =
+            make_float4(o[2 * u][2 * rr] * kDrop * back, o[2 * u + 1][2 * rr] * kDrop * back,
+                        o[2 * u][2 * rr + 1] * kDrop * back, o[2 * u + 1][2 * rr + 1] * kDrop * back);
+      if ((lane & 3) == 0) {
+        dst[DP] = m[rr] + 15.0f;
+        dst[DP + 1] = l[rr] * kDrop;
+      }
+    }
+    merge_states<T, DP, CLUSTER>(A, S, mo, r0, rows_all, kvh, chunk);
+    __syncthreads();
+  }
+}
+
+// ---------------------------------------------------------------------------
+// widening
+// ---------------------------------------------------------------------------
+
+template <typename T> __device__ __forceinline__ float in_range(float x) { return x; }
+template <> __device__ __forceinline__ float in_range<__half>(float x) {
+  return fabsf(x) > 65504.f ? copysignf(65504.f, x) : x;     // NaN stays
+}
+
+constexpr int kWidenThreads = 256;
+
+// Keys and values that a sequence's tokens see, as 16-bit rows [key without the gap]
+// [kv_heads][dim] from row seq * span on: a warp per 16 keys and key head.  bf16 holds the
+// numbers exactly, and fp16 those that came from fp16.
+template <typename T>
+__global__ void __launch_bounds__(kWidenThreads)
+    k_pages_widen(const __grid_constant__ AttnArgs A, const __grid_constant__ PagesArgs P, T* k, T* v,
+                  unsigned char* hidden, int span) {
+  const int lane = threadIdx.x & 31;
+  long long item = (long long)blockIdx.x * (kWidenThreads / 32) + (threadIdx.x >> 5);
+  const int head = (int)(item % A.kv_heads);
+  item /= A.kv_heads;
+  const int blocks = span / kPageBlock, j0 = (int)(item % blocks) * kPageBlock, seq = (int)(item / blocks);
+  if (seq >= A.n_seqs) return;
+  const AttnSpan S = attn_span<true>(A, seq);
+  if (S.nq == 0 || j0 >= S.nk) return;
+  auto page_at = [&](int j) -> int {
+    const int page = P.table[(long long)seq * P.s.table_row + (attn_row(S, j) >> P.s.shift)];
+    return (unsigned)page < (unsigned)P.s.n_pages ? page : -1;
+  };
+  const int page = page_at(j0);
+  if (head == 0 && lane == 0 && j0 % 64 == 0)
+    hidden[((long long)seq * span + j0) / 64] =
+        (unsigned char)((page < 0) | (j0 + 32 < S.nk && page_at(j0 + 32) < 0 ? 2 : 0));
+  if (page < 0) return;
+  const int row = attn_row(S, j0) & (P.s.page_rows - 1);
+  const long long at = page * P.s.page_bytes + ((long long)head * P.s.page_rows + row) * A.dim;
+  const signed char* e =
+      P.scales + page * P.s.scale_bytes + ((long long)head * (P.s.page_rows / kPageBlock) + row / kPageBlock) * 2;
+  const float fk = pow2(max((int)e[0], kExpMin)), fv = pow2(max((int)e[1], kExpMin));
+  const int units = A.dim / 16;                  // of a row
+  for (int i = lane; i < kPageBlock * units; i += 32) {
+    const int r = i / units, c = i % units;
+    const uint4 x[2] = {__ldcs(reinterpret_cast<const uint4*>(P.k + at) + i),
+                        __ldcs(reinterpret_cast<const uint4*>(P.v + at) + i)};
+    const long long to = (((long long)seq * span + j0 + r) * A.kv_heads + head) * A.dim + c * 16;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const uint32_t u[4] = {x[h].x, x[h].y, x[h].z, x[h].w};
+      const float f = h ? fv : fk;
+      uint32_t y[8];
+#pragma unroll
+      for (int n = 0; n < 4; ++n) {
+        const float2 p = Store<__half>::unpack2(widen_e4m3x2(u[n])), q = Store<__half>::unpack2(widen_e4m3x2(u[n] >> 16));
+        y[2 * n] = Store<T>::pack2(in_range<T>(p.x * f), in_range<T>(p.y * f));
+        y[2 * n + 1] = Store<T>::pack2(in_range<T>(q.x * f), in_range<T>(q.y * f));
+      }
+      uint4* dst = reinterpret_cast<uint4*>((h ? v : k) + to);
+      dst[0] = make_uint4(y[0], y[1], y[2], y[3]);
+      dst[1] = make_uint4(y[4], y[5], y[6], y[7]);
+    }
+  }
+}
+
+template <typename T, int DP, bool CLUSTER>
+cudaError_t launch_pages_t(const AttnArgs& a, const PagesArgs& p, cudaStream_t st) {
+  using C = PagesCfg<DP>;
+  static std::atomic<uint64_t> allowed{0};
+  const cudaError_t e = allow_smem(reinterpret_cast<const void*>(k_attn_pages<T, DP, CLUSTER>), C::kSmem, &allowed, CLUSTER && kCluster > 8);
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t lc = {};
+  lc.gridDim = dim3((unsigned)((long long)a.n_seqs * a.kv_heads * a.row_groups * a.n_chunks));
+  lc.blockDim = dim3(kWarps * 32);
+  lc.dynamicSmemBytes = C::kSmem;
+  lc.stream = st;
+  cudaLaunchAttribute at[1];
+  if (CLUSTER) {
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = a.n_chunks;
+    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    lc.attrs = at;
+    lc.numAttrs = 1;
+  }
+  return cudaLaunchKernelEx(&lc, k_attn_pages<T, DP, CLUSTER>, a, p);
+}
+
+template <bool CLUSTER>
+cudaError_t launch_pages(const AttnArgs& a, const PagesArgs& p, bool bf16, cudaStream_t st) {
+  if (a.dim <= 64)
+    return bf16 ? launch_pages_t<__nv_bfloat16, 64, CLUSTER>(a, p, st) : launch_pages_t<__half, 64, CLUSTER>(a, p, st);
+  return bf16 ? launch_pages_t<__nv_bfloat16, 128, CLUSTER>(a, p, st) : launch_pages_t<__half, 128, CLUSTER>(a, p, st);
+}
+
+}  // namespace
+
+int attn_pages_unit() { return kWarps * KT; }
+
+cudaError_t launch_attn_pages(const AttnArgs& a, const PagesArgs& p, bool bf16, cudaStream_t st) {
+  return a.cluster ? launch_pages<true>(a, p, bf16, st) : launch_pages<false>(a, p, bf16, st);
+}
+
+cudaError_t launch_pages_widen(const AttnArgs& a, const PagesArgs& p, void* k, void* v, unsigned char* hidden, int span,
+                               bool bf16, cudaStream_t st) {
+  const long long warps = (long long)a.n_seqs * (span / kPageBlock) * a.kv_heads;
+  const long long grid = (warps + kWidenThreads / 32 - 1) / (kWidenThreads / 32);
+  if (grid > 0x7FFFFFFF) return cudaErrorNotSupported;
+  if (bf16)
+    k_pages_widen<__nv_bfloat16><<<(unsigned)grid, kWidenThreads, 0, st>>>(a, p, static_cast<__nv_bfloat16*>(k),
+                                                                         static_cast<__nv_bfloat16*>(v), hidden, span);
+  else
+    k_pages_widen<__half><<<(unsigned)grid, kWidenThreads, 0, st>>>(a, p, static_cast<__half*>(k), static_cast<__half*>(v),
+                                                                  hidden, span);
+  return cudaGetLastError();
+}
+
+}  // namespace rtcc

@@ -26,18 +26,13 @@
 // 128, 1.9 GB: 300 us, 6.4 TB/s, 94 % of a plain copy's; one token over 4097 keys of
 // 6 heads of 64 takes 8.2 us, most of which is the launch, a block's first copies
 // and three steps.
-#include <type_traits>
-
-#include "attn.cuh"
+#include "attn_rows.cuh"
 #include "kernels.h"
 
 namespace rtcc {
 namespace {
 
-constexpr int kWarps = 4;
 constexpr int kStages = 3;
-constexpr int kRows = 16;
-constexpr int kCluster = 16;                     // blocks of a cluster at most
 
 // log2 of the largest probability (a row's m is its largest score less this)
 template <typename T> constexpr float kLift = std::is_same<T, __half>::value ? 15.0f : 0.0f;
@@ -54,66 +49,6 @@ template <int DP> struct RowsCfg {               // DP: head size padded to 64 o
   static constexpr int kSmem = kRing;
 };
 
-__device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool live) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(live ? 16 : 0) : "memory");
-}
-__device__ __forceinline__ void cp8(uint32_t dst, const void* src, bool live) {
-  asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst), "l"(src), "r"(live ? 8 : 0) : "memory");
-}
-__device__ __forceinline__ void ldm4(uint32_t a, uint32_t (&r)[4]) {
-  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
-               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
-               : "r"(a)
-               : "memory");
-}
-__device__ __forceinline__ void ldm4t(uint32_t a, uint32_t (&r)[4]) {
-  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
-               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
-               : "r"(a)
-               : "memory");
-}
-
-template <typename T>
-__device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1);
-template <>
-__device__ __forceinline__ void mma16816<__half>(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm volatile(
-      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-template <>
-__device__ __forceinline__ void mma16816<__nv_bfloat16>(float (&d)[4], const uint32_t (&a)[4], uint32_t b0,
-                                                        uint32_t b1) {
-  asm volatile(
-      "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-
-// Shared memory of the cluster's blocks.
-__device__ __forceinline__ float4 cluster_ld4(uint32_t a) {
-  float4 v;
-  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
-               : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
-               : "r"(a)
-               : "memory");
-  return v;
-}
-__device__ __forceinline__ float2 cluster_ld2(uint32_t a) {
-  float2 v;
-  asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(a) : "memory");
-  return v;
-}
-
-// Two floats as hi + lo of the storage type.
-template <typename T>
-__device__ __forceinline__ void split2(float a, float b, uint32_t& hi, uint32_t& lo) {
-  hi = Store<T>::pack2(a, b);
-  const float2 h = Store<T>::unpack2(hi);
-  lo = Store<T>::pack2(a - h.x, b - h.y);
-}
-
 // Byte offset of 16-byte unit c of row r in a tile of DP-channel rows; units
 // are permuted within 128-byte lines so that ldmatrix reads 8 rows without
 // bank conflicts.
@@ -122,20 +57,9 @@ __device__ __forceinline__ uint32_t tile_off(int r, int c) {
   return (uint32_t)(r * DP * 2 + (c & ~7) * 16 + (((c ^ r) & 7) * 16));
 }
 
-// Four channels of a row's result: accumulators over the sum, and the lse.
-template <typename T>
-__device__ __forceinline__ void store_row(const AttnArgs& A, long long t, int h, int c, float4 acc, float mm, float ll) {
-  const float inv = ll > 0.f ? 1.0f / ll : (ll == 0.f ? 0.f : ll);
-  uint2 u;
-  u.x = Store<T>::pack2(acc.x * inv, acc.y * inv);
-  u.y = Store<T>::pack2(acc.z * inv, acc.w * inv);
-  *reinterpret_cast<uint2*>(static_cast<T*>(A.out) + t * A.out_row + (long long)h * A.out_head + c) = u;
-  if (c == 0 && A.lse) A.lse[t * A.heads + h] = ll == 0.f ? -INFINITY : (mm + log2f(ll)) * kLn2;
-}
-
 // CLUSTER: the chunks are the cluster's blocks, which join them (a kernel of its own:
 // the join's registers cost the long split 2 %).
-template <typename T, int DP, bool CLUSTER>
+template <typename T, int DP, bool CLUSTER, bool WIN>
 __global__ void __launch_bounds__(kWarps * 32, 2) k_attn_rows(const __grid_constant__ AttnArgs A) {
   using C = RowsCfg<DP>;
   constexpr int KT = C::KT;
@@ -149,7 +73,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) k_attn_rows(const __grid_const
   b /= A.row_groups;
   const int kvh = b % A.kv_heads;
   const int seq = b / A.kv_heads;
-  const AttnSpan S = attn_span(A, seq);
+  const AttnSpan S = attn_span<WIN>(A, seq);
   const int rows_all = S.nq * A.group;
   const int per = attn_chunk(A, S.nk, A.unit);
   const int c0 = (int)min((long long)per * chunk, (long long)S.nk), c1 = min(S.nk - c0, per) + c0;
@@ -165,6 +89,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) k_attn_rows(const __grid_const
     const int r0 = rg * kRows;
     // this lane's two rows: lane / 4 and 8 further
     int hi[2], head[2];
+    AttnView view[2];
     bool row_ok[2];
     long long tok[2];
     float slope[2], qy[2], qx[2];
@@ -176,6 +101,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) k_attn_rows(const __grid_const
       head[i] = kvh * A.group + (row_ok[i] ? r % A.group : 0);
       tok[i] = S.q0 + ql;
       hi[i] = row_ok[i] ? attn_visible(A, S, S.first, ql) : 0;
+      if (WIN) view[i] = attn_view(A, S, S.first, ql);
       slope[i] = dist ? A.slopes[head[i]] * kLog2e : 0.f;
       qy[i] = dist && row_ok[i] ? A.q_pos[tok[i] * A.q_pos_row] : 0.f;
       qx[i] = dist && row_ok[i] ? A.q_pos[tok[i] * A.q_pos_row + 1] : 0.f;
@@ -188,6 +114,13 @@ __global__ void __launch_bounds__(kWarps * 32, 2) k_attn_rows(const __grid_const
       least = min(least, __shfl_xor_sync(0xFFFFFFFFu, least, d));
     }
     const int end = min(c1, reach);
+    // with a window: keys [seen, low) are seen by no row, keys before seen_all and from low_all on by all
+    int seen = 0, low = 0, seen_all = 0, low_all = 0;
+    if (WIN) {
+      const AttnView f = attn_view(A, S, S.first, r0 / A.group);
+      const AttnView l = attn_view(A, S, S.first, (min(r0 + kRows, rows_all) - 1) / A.group);
+      seen = l.seen; low = f.low; seen_all = f.seen; low_all = l.low;
+    }
     // A fragments of Q
     uint32_t qa[DP / 16][4];
 #pragma unroll
@@ -211,19 +144,21 @@ __global__ void __launch_bounds__(kWarps * 32, 2) k_attn_rows(const __grid_const
     auto key_bits = [&](int t) -> unsigned {
       const int j = c0 + t * KT + lane;
       bool ok = t < n_tiles && lane < KT && j < end;
-      if (ok && A.present) ok = (slots >> slot_of(A, S.kb + j)) & 1;
+      if (WIN) ok = ok && (j < seen || j >= low);
+      if (ok && A.present) ok = (slots >> slot_of(A, WIN ? attn_row(S, j) : S.kb + j)) & 1;
       return __ballot_sync(0xFFFFFFFFu, ok);
     };
     auto load = [&](int t, int stage) {
       const unsigned bits = key_bits(t);
       if (bits) {
+        const long long at_row = WIN ? attn_row(S, c0 + t * KT) : S.kb + c0 + t * KT;   // a tile lies on one side of a gap
         const uint32_t ks = ring + stage * C::kStageBytes, vs = ks + C::kTileBytes, ps = vs + C::kTileBytes;
         constexpr int U = DP / 8;                // 16-byte units of a row
 #pragma unroll
         for (int i = 0; i < KT * U / 32; ++i) {
           const int idx = i * 32 + lane, r = idx / U, c = idx % U;
           const bool live = (bits >> r) & 1 && c * 8 < A.dim;
-          const long long row = live ? (long long)S.kb + c0 + t * KT + r : 0;
+          const long long row = live ? at_row + r : 0;
           const int col = live ? c * 8 : 0;
           const uint32_t at = tile_off<DP>(r, c);
           cp16(ks + at, kbase + row * A.k_row + col, live);
@@ -231,7 +166,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) k_attn_rows(const __grid_const
         }
         if (dist && lane < KT) {
           const bool live = (bits >> lane) & 1;
-          const long long row = live ? (long long)S.kb + c0 + t * KT + lane : 0;
+          const long long row = live ? at_row + lane : 0;
           cp8(ps + lane * 8, A.k_pos + 2 * row, live);
         }
       }
@@ -262,7 +197,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) k_attn_rows(const __grid_const
           }
         const int j0 = c0 + t * KT;
         const unsigned full = KT == 32 ? 0xFFFFFFFFu : (1u << KT) - 1u;
-        const bool edge = bits != full || j0 + KT > least;
+        const bool edge = bits != full || j0 + KT > least || (WIN && j0 < low_all && j0 + KT > seen_all);
         float top[2] = {-INFINITY, -INFINITY};
 #pragma unroll
         for (int n = 0; n < KT / 8; ++n)
@@ -276,6 +211,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) k_attn_rows(const __grid_const
               x = fmaf(-slope[rr], fabsf(qy[rr] - p.x) + fabsf(qx[rr] - p.y), x);
             }
             if (edge && !(((bits >> key) & 1) && j0 + key < hi[rr])) x = -INFINITY;
+            if (WIN && edge && j0 + key >= view[rr].seen && j0 + key < view[rr].low) x = -INFINITY;
             s[n][i] = x;
             top[rr] = fmaxf(top[rr], x);
           }
@@ -352,83 +288,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) k_attn_rows(const __grid_const
         dst[DP + 1] = l[rr];
       }
     }
-    __syncthreads();
-    for (int idx = threadIdx.x; idx < kRows * (DP / 4); idx += kWarps * 32) {
-      const int r = idx / (DP / 4), c = (idx % (DP / 4)) * 4;
-      if (r0 + r >= rows_all) continue;
-      float mm = -INFINITY;
-#pragma unroll
-      for (int i = 0; i < kWarps; ++i) mm = fmaxf(mm, mo[(i * kRows + r) * P + DP]);
-      const float base = mm == -INFINITY ? 0.f : mm;
-      float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-      float ll = 0.f;
-#pragma unroll
-      for (int i = 0; i < kWarps; ++i) {
-        const float* src = mo + (i * kRows + r) * P;
-        const float f = exp2f(src[DP] - base);
-        const float4 x = *reinterpret_cast<const float4*>(src + c);
-        acc.x = fmaf(f, x.x, acc.x);
-        acc.y = fmaf(f, x.y, acc.y);
-        acc.z = fmaf(f, x.z, acc.z);
-        acc.w = fmaf(f, x.w, acc.w);
-        ll = fmaf(f, src[DP + 1], ll);
-      }
-      if (c >= A.dim) continue;
-      const long long t = S.q0 + (r0 + r) / A.group;
-      const int h = kvh * A.group + (r0 + r) % A.group;
-      const long long R = t * A.heads + h;
-      if (CLUSTER) {
-        float* dst = mo + kWarps * C::kState + r * P;
-        *reinterpret_cast<float4*>(dst + c) = acc;
-        if (c == 0) *reinterpret_cast<float2*>(dst + DP) = make_float2(mm, ll);
-      } else if (A.n_chunks > 1) {
-        const long long at = (long long)chunk * A.n_q * A.heads + R;
-        *reinterpret_cast<float4*>(A.part_o + at * A.dim + c) = acc;
-        if (c == 0) A.part_ml[at] = make_float2(mm, ll);
-      } else {
-        store_row<T>(A, t, h, c, acc, mm, ll);
-      }
-    }
-    if (CLUSTER) {
-      // every block joins its share of the rows, from the blocks' states in chunk order
-      __syncwarp();
-      cluster_sync_all();
-      const uint32_t state = smem_u32(mo + kWarps * C::kState);
-      const int blocks = (int)cluster_nctarank();
-      for (int idx = chunk * kWarps * 32 + threadIdx.x; idx < kRows * (DP / 4); idx += A.n_chunks * kWarps * 32) {
-        const int r = idx / (DP / 4), c = (idx % (DP / 4)) * 4;
-        if (r0 + r >= rows_all || c >= A.dim) continue;
-        float2 ml[kCluster];
-        float4 x[kCluster];
-        float mm = -INFINITY;
-#pragma unroll
-        for (int i = 0; i < kCluster; ++i) {
-          const bool in = i < blocks;
-          const uint32_t at = mapa_shared(state + r * P * 4, in ? i : 0);
-          ml[i] = in ? cluster_ld2(at + DP * 4) : make_float2(-INFINITY, 0.f);
-          x[i] = in ? cluster_ld4(at + c * 4) : make_float4(0.f, 0.f, 0.f, 0.f);
-        }
-#pragma unroll
-        for (int i = 0; i < kCluster; ++i) mm = fmaxf(mm, ml[i].x);
-        const float base = mm == -INFINITY ? 0.f : mm;
-        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-        float ll = 0.f;
-#pragma unroll
-        for (int i = 0; i < kCluster; ++i) {
-          const float f = exp2f(ml[i].x - base);
-          acc.x = fmaf(f, x[i].x, acc.x);
-          acc.y = fmaf(f, x[i].y, acc.y);
-          acc.z = fmaf(f, x[i].z, acc.z);
-          acc.w = fmaf(f, x[i].w, acc.w);
-          ll = fmaf(f, ml[i].y, ll);
-        }
-        const long long t = S.q0 + (r0 + r) / A.group;
-        const int h = kvh * A.group + (r0 + r) % A.group;
-        store_row<T>(A, t, h, c, acc, mm, ll);
-      }
-      __syncwarp();
-      cluster_sync_all();                        // before a block's state goes
-    }
+    merge_states<T, DP, CLUSTER>(A, S, mo, r0, rows_all, kvh, chunk);
     __syncthreads();
   }
 }
@@ -445,7 +305,7 @@ __global__ void __launch_bounds__(kJoinWarps * 32) k_attn_join(const __grid_cons
   pdl_wait();
   const int seq = blockIdx.x / blocks_per_seq, b = blockIdx.x % blocks_per_seq;
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
-  const AttnSpan S = attn_span(A, seq);
+  const AttnSpan S = attn_span<true>(A, seq);
   const int per = attn_chunk(A, S.nk, A.unit);
   const int used = max(1, (int)(((long long)S.nk + per - 1) / per)) * A.streams;
   const long long rows = (long long)S.nq * A.heads, stride = (long long)A.n_q * A.heads;
@@ -509,11 +369,11 @@ __global__ void __launch_bounds__(kJoinWarps * 32) k_attn_join(const __grid_cons
   }
 }
 
-template <typename T, int DP, bool CLUSTER>
+template <typename T, int DP, bool CLUSTER, bool WIN>
 cudaError_t launch_rows_t(const AttnArgs& a, cudaStream_t st) {
   using C = RowsCfg<DP>;
   static std::atomic<uint64_t> allowed{0};
-  const cudaError_t e = allow_smem(reinterpret_cast<const void*>(k_attn_rows<T, DP, CLUSTER>), C::kSmem, &allowed, CLUSTER && kCluster > 8);
+  const cudaError_t e = allow_smem(reinterpret_cast<const void*>(k_attn_rows<T, DP, CLUSTER, WIN>), C::kSmem, &allowed, CLUSTER && kCluster > 8);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t lc = {};
   lc.gridDim = dim3((unsigned)((long long)a.n_seqs * a.kv_heads * a.row_groups * a.n_chunks));
@@ -528,7 +388,7 @@ cudaError_t launch_rows_t(const AttnArgs& a, cudaStream_t st) {
     lc.attrs = at;
     lc.numAttrs = 1;
   }
-  return cudaLaunchKernelEx(&lc, k_attn_rows<T, DP, CLUSTER>, a);
+  return cudaLaunchKernelEx(&lc, k_attn_rows<T, DP, CLUSTER, WIN>, a);
 }
 
 }  // namespace
@@ -537,14 +397,15 @@ int attn_rows_unit(int dim) { return kWarps * (dim <= 64 ? RowsCfg<64>::KT : Row
 int attn_rows_per_block() { return kRows; }
 int attn_rows_cluster() { return kCluster; }
 
-template <bool CLUSTER>
+template <bool CLUSTER, bool WIN>
 static cudaError_t launch_rows(const AttnArgs& a, bool bf16, cudaStream_t st) {
   if (a.dim <= 64)
-    return bf16 ? launch_rows_t<__nv_bfloat16, 64, CLUSTER>(a, st) : launch_rows_t<__half, 64, CLUSTER>(a, st);
-  return bf16 ? launch_rows_t<__nv_bfloat16, 128, CLUSTER>(a, st) : launch_rows_t<__half, 128, CLUSTER>(a, st);
+    return bf16 ? launch_rows_t<__nv_bfloat16, 64, CLUSTER, WIN>(a, st) : launch_rows_t<__half, 64, CLUSTER, WIN>(a, st);
+  return bf16 ? launch_rows_t<__nv_bfloat16, 128, CLUSTER, WIN>(a, st) : launch_rows_t<__half, 128, CLUSTER, WIN>(a, st);
 }
 cudaError_t launch_attn_rows(const AttnArgs& a, bool bf16, cudaStream_t st) {
-  return a.cluster ? launch_rows<true>(a, bf16, st) : launch_rows<false>(a, bf16, st);
+  if (a.window > 0) return a.cluster ? launch_rows<true, true>(a, bf16, st) : launch_rows<false, true>(a, bf16, st);
+  return a.cluster ? launch_rows<true, false>(a, bf16, st) : launch_rows<false, false>(a, bf16, st);
 }
 
 cudaError_t launch_attn_join(const AttnArgs& a, int max_q, bool bf16, cudaStream_t st) {

@@ -383,6 +383,16 @@ int attn_tc_tokens_per_block(int group, int streams);
 int attn_tc_unit(int streams);
 cudaError_t launch_attn_tc(const AttnArgs& a, bool bf16, cudaStream_t st);
 cudaError_t attn_tc_errors(unsigned* count, cudaStream_t st);
+// The same with windows and over widened pages (attn_win.cu).
+cudaError_t launch_attn_win(const AttnArgs& a, bool bf16, cudaStream_t st);
+cudaError_t attn_win_errors(unsigned* count, cudaStream_t st);
+// Attention of few rows over pages, and the pages' keys and values widened to 16
+// bits for many (attn_pages.cu).
+struct PagesArgs;
+int attn_pages_unit();
+cudaError_t launch_attn_pages(const AttnArgs& a, const PagesArgs& p, bool bf16, cudaStream_t st);
+cudaError_t launch_pages_widen(const AttnArgs& a, const PagesArgs& p, void* k, void* v, unsigned char* hidden, int span,
+                               bool bf16, cudaStream_t st);
 // Merge of the chunks' partial results into out and lse.
 cudaError_t launch_attn_join(const AttnArgs& a, int max_q, bool bf16, cudaStream_t st);
 

@@ -99,10 +99,38 @@ class rtcc_attn_config(C.Structure):
     ]
 
 
-# the two structs' fields in order, packed in one go (field by field takes twice as long)
+class rtcc_page_config(C.Structure):
+    _fields_ = [
+        ("kv_heads", C.c_int32), ("head_dim", C.c_int32), ("page_rows", C.c_int32), ("n_pages", C.c_int32),
+        ("n_seqs", C.c_int32), ("table_row", C.c_int32), ("page_bytes", C.c_int64), ("scale_bytes", C.c_int64),
+    ]
+
+
+class rtcc_write_config(C.Structure):
+    _fields_ = [
+        ("dtype", C.c_int32), ("n_tokens", C.c_int32), ("max_new", C.c_int32), ("reserved", C.c_int32),
+        ("k_row", C.c_int64), ("k_head", C.c_int64), ("v_row", C.c_int64), ("v_head", C.c_int64),
+    ]
+
+
+class rtcc_page_attn_config(C.Structure):
+    _fields_ = [
+        ("heads", C.c_int32), ("dtype", C.c_int32), ("n_q", C.c_int32), ("max_q", C.c_int32), ("max_k", C.c_int32),
+        ("causal", C.c_int32), ("window", C.c_int32), ("sinks", C.c_int32),
+        ("q_row", C.c_int64), ("q_head", C.c_int64), ("out_row", C.c_int64), ("out_head", C.c_int64),
+        ("scale", C.c_float), ("cap", C.c_float),
+    ]
+
+
+# the structs' fields in order, packed in one go (field by field takes twice as long)
 _PREPARE = struct.Struct("=6i12q3i2i2f4x")
 _ATTN = struct.Struct("=6i8q7i2f4xQ")
-assert _PREPARE.size == C.sizeof(rtcc_prepare_config) and _ATTN.size == C.sizeof(rtcc_attn_config)
+_PAGE = struct.Struct("=6i2q")
+_WRITE = struct.Struct("=4i4q")
+_PAGE_ATTN = struct.Struct("=8i4q2f")
+for _packed, _c in ((_PREPARE, rtcc_prepare_config), (_ATTN, rtcc_attn_config), (_PAGE, rtcc_page_config),
+                    (_WRITE, rtcc_write_config), (_PAGE_ATTN, rtcc_page_attn_config)):
+    assert _packed.size == C.sizeof(_c)
 
 BOX_DTYPE = np.dtype([("x", "<f4"), ("y", "<f4"), ("z", "<f4"), ("l", "<f4"), ("w", "<f4"),
                       ("h", "<f4"), ("yaw", "<f4"), ("score", "<f4"), ("anchor", "<i4")])
@@ -187,6 +215,18 @@ def load(path: Optional[str] = None) -> C.CDLL:
         "rtcc_qkv_prepare": (S, [C.POINTER(rtcc_prepare_config)] + [C.c_void_p] * 12),
         "rtcc_memory_attention": (S, [C.POINTER(rtcc_attn_config)] + [C.c_void_p] * 14 +
                                   [C.c_size_t, C.c_void_p]),
+        "rtcc_memory_window_attention": (S, [C.POINTER(rtcc_attn_config), C.c_int32, C.c_int32] +
+                                         [C.c_void_p] * 14 + [C.c_size_t, C.c_void_p]),
+        "rtcc_pages_fork": (S, [C.POINTER(rtcc_page_config), C.c_int32, C.c_void_p, C.c_void_p, C.c_int32,
+                                C.c_int32] + [C.c_void_p] * 6),
+        "rtcc_pages_workspace": (C.c_size_t, [C.POINTER(rtcc_page_config)]),
+        "rtcc_pages_extend": (S, [C.POINTER(rtcc_page_config)] + [C.c_void_p] * 10 + [C.c_size_t, C.c_void_p]),
+        "rtcc_pages_compact": (S, [C.POINTER(rtcc_page_config)] + [C.c_void_p] * 8 + [C.c_size_t, C.c_void_p]),
+        "rtcc_pages_copy": (S, [C.POINTER(rtcc_page_config), C.c_int32] + [C.c_void_p] * 7 + [C.c_int32] +
+                            [C.c_void_p] * 4),
+        "rtcc_pages_write": (S, [C.POINTER(rtcc_page_config), C.POINTER(rtcc_write_config)] + [C.c_void_p] * 10),
+        "rtcc_pages_attention": (S, [C.POINTER(rtcc_page_config), C.POINTER(rtcc_page_attn_config)] +
+                                 [C.c_void_p] * 12 + [C.c_size_t, C.c_void_p]),
         "rtcc_memory_attention_status": (S, [C.c_void_p]),
         "rtcc_test_attention": (S, [C.c_int32]),
     }
@@ -500,6 +540,15 @@ def rtcc_memory_attention(cfg: rtcc_attn_config, d_q, d_k, d_v, d_q_offsets, d_k
                                         workspace_bytes, stream or None)
 
 
+def rtcc_memory_window_attention(cfg: rtcc_attn_config, window: int, sinks: int, d_q, d_k, d_v, d_q_offsets,
+                                 d_k_begin, d_k_end, d_prefix, d_present, d_slopes, d_q_pos, d_k_pos, d_out,
+                                 d_lse, d_workspace, workspace_bytes: int, stream: int = 0) -> int:
+    """Attention over a sliding window and the first keys of a span (see rtcc.h)."""
+    return load().rtcc_memory_window_attention(cfg, window, sinks, d_q, d_k, d_v, d_q_offsets, d_k_begin,
+                                               d_k_end, d_prefix, d_present, d_slopes, d_q_pos, d_k_pos, d_out,
+                                               d_lse, d_workspace, workspace_bytes, stream or None)
+
+
 def rtcc_memory_attention_status(stream: int = 0) -> int:
     """Wait for `stream`; E_DEVICE if an attention kernel gave up a wait."""
     return load().rtcc_memory_attention_status(stream or None)
@@ -511,6 +560,84 @@ TEST_UNREACHABLE_WAIT, TEST_NO_CLUSTERS = 1, 2
 def rtcc_test_attention(what: int) -> int:
     """Test hook of the attention calls of this process (see rtcc.h)."""
     return load().rtcc_test_attention(what)
+
+
+# --------------------------------------------------------------------------
+# paged token memory; every d_* is a device address (0 or None: NULL)
+# --------------------------------------------------------------------------
+
+def page_config(kv_heads: int, head_dim: int, page_rows: int, n_pages: int, n_seqs: int, table_row: int,
+                page_bytes: int = 0, scale_bytes: int = 0) -> rtcc_page_config:
+    """Shapes of pools and tables; page_bytes, scale_bytes 0: dense."""
+    return rtcc_page_config.from_buffer_copy(_PAGE.pack(kv_heads, head_dim, page_rows, n_pages, n_seqs, table_row,
+                                                        page_bytes, scale_bytes))
+
+
+def rtcc_pages_fork(cfg: rtcc_page_config, n_from: int, d_parent, d_keep, window: int, sinks: int, d_length,
+                    d_table, d_length_out, d_table_out, d_refs, stream: int = 0) -> int:
+    """Sequences take over their parents' pages (see rtcc.h)."""
+    return load().rtcc_pages_fork(cfg, n_from, d_parent, d_keep, window, sinks, d_length, d_table, d_length_out,
+                                  d_table_out, d_refs, stream or None)
+
+
+def rtcc_pages_workspace(cfg: rtcc_page_config) -> int:
+    """Bytes of workspace of rtcc_pages_extend and rtcc_pages_compact."""
+    return load().rtcc_pages_workspace(cfg)
+
+
+def rtcc_pages_extend(cfg: rtcc_page_config, d_new, d_length, d_table, d_refs, d_length_out, d_copy_src,
+                      d_copy_dst, d_copy_rows, d_short, d_workspace, workspace_bytes: int, stream: int = 0) -> int:
+    """Pages for new tokens (see rtcc.h)."""
+    return load().rtcc_pages_extend(cfg, d_new, d_length, d_table, d_refs, d_length_out, d_copy_src, d_copy_dst,
+                                    d_copy_rows, d_short, d_workspace, workspace_bytes, stream or None)
+
+
+def rtcc_pages_compact(cfg: rtcc_page_config, d_table, d_refs, d_table_out, d_refs_out, d_move_src, d_move_dst,
+                       d_count, d_workspace, workspace_bytes: int, stream: int = 0) -> int:
+    """Pages in use to the pool's front (see rtcc.h)."""
+    return load().rtcc_pages_compact(cfg, d_table, d_refs, d_table_out, d_refs_out, d_move_src, d_move_dst, d_count,
+                                     d_workspace, workspace_bytes, stream or None)
+
+
+def rtcc_pages_copy(cfg: rtcc_page_config, n: int, d_count, d_src, d_dst, d_rows, d_k_src, d_v_src, d_scales_src,
+                    n_pages_dst: int, d_k_dst, d_v_dst, d_scales_dst, stream: int = 0) -> int:
+    """Copies of listed pages (see rtcc.h)."""
+    return load().rtcc_pages_copy(cfg, n, d_count, d_src, d_dst, d_rows, d_k_src, d_v_src, d_scales_src, n_pages_dst,
+                                  d_k_dst, d_v_dst, d_scales_dst, stream or None)
+
+
+def write_config(dtype: int, n_tokens: int, max_new: int, k, v) -> rtcc_write_config:
+    """New tokens of rtcc_pages_write; k, v are the arrays' (row, head) strides
+    in elements."""
+    return rtcc_write_config.from_buffer_copy(_WRITE.pack(dtype, n_tokens, max_new, 0, *k, *v))
+
+
+def rtcc_pages_write(cfg: rtcc_page_config, tokens: rtcc_write_config, d_k, d_v, d_offsets, d_held, d_length,
+                     d_table, d_k_pages, d_v_pages, d_scales, stream: int = 0) -> int:
+    """Keys and values of new tokens into their pages (see rtcc.h)."""
+    return load().rtcc_pages_write(cfg, tokens, d_k, d_v, d_offsets, d_held, d_length, d_table, d_k_pages, d_v_pages,
+                                   d_scales, stream or None)
+
+
+def page_attn_config(heads: int, dtype: int, n_q: int, q, out, max_q: int, max_k: int, causal: bool = True,
+                     window: int = 0, sinks: int = 0, scale: Optional[float] = None, cap: float = 0.0,
+                     head_dim: Optional[int] = None) -> rtcc_page_attn_config:
+    """Queries of rtcc_pages_attention; q and out are the arrays' (row, head)
+    strides in elements; scale None = 1 / sqrt(head_dim)."""
+    if scale is None:
+        if head_dim is None:
+            raise ValueError("a scale, or head_dim to take it from, is needed")
+        scale = head_dim ** -0.5
+    return rtcc_page_attn_config.from_buffer_copy(_PAGE_ATTN.pack(heads, dtype, n_q, max_q, max_k, causal, window, sinks,
+                                                                  *q, *out, scale, cap))
+
+
+def rtcc_pages_attention(cfg: rtcc_page_config, rows: rtcc_page_attn_config, d_q, d_q_offsets, d_start, d_length,
+                         d_prefix, d_table, d_k_pages, d_v_pages, d_scales, d_out, d_lse, d_workspace,
+                         workspace_bytes: int, stream: int = 0) -> int:
+    """Attention over pages (see rtcc.h)."""
+    return load().rtcc_pages_attention(cfg, rows, d_q, d_q_offsets, d_start, d_length, d_prefix, d_table, d_k_pages,
+                                       d_v_pages, d_scales, d_out, d_lse, d_workspace, workspace_bytes, stream or None)
 
 
 # --------------------------------------------------------------------------
