@@ -8,13 +8,20 @@
 // scores, e_v into the probabilities, relative to the largest e_v that the warp has met
 // (E; its accumulators are in units of 2^E).  bf16 queries are scaled by a power of two
 // per row so that the largest is below 2^15; what is more than 2^39 below it is lost.
+// Probabilities are rounded to fp16's 11 bits, seven more than the values have; the
+// largest is 2^15, so that 2^-40 of it still counts.
 //
-// As in attn_rows.cu a block has 16 (token, head) rows of one key head and a chunk of the
-// keys, its four warps take tiles of 32 keys in turn through rings of their own, and
-// rows of the memory that no query sees are not read.  A tile lies in one page, whose
-// number is fetched a round ahead of the copies.  Channels are permuted within groups
-// of 16 so that what ldmatrix gives a lane (4 bytes of a key; 2 bytes of two keys'
-// values) is what its products need: no number crosses lanes.
+// Keys and channels are the products' 16-wide side, query rows the 8-wide one,
+//   S^T = K Q^T,   O^T = V^T P^T,
+// so that a block with up to 8 (token, head) rows of a key head pays for 8; with more it
+// has two such groups for each widened number.  What bounds it is instructions, not
+// bytes alone: 4 KB of keys and values are 64 conversions, 32 shuffled bytes, 16 products
+// of 16 x 8 x 16 and the softmax of 4 numbers a lane.  As in attn_rows.cu the block's
+// four warps take tiles of 32 keys in turn through rings of their own, and rows of the
+// memory that no query sees are not read.  A tile lies in one page, whose number is
+// fetched a round ahead of the copies.  Channels are permuted within groups of 16 so
+// that what ldmatrix gives a lane (4 bytes of a key; 2 bytes of two keys' values) is
+// what its products need: no number crosses lanes but P, transposed once.
 #include <type_traits>
 
 #include "attn_rows.cuh"
@@ -27,7 +34,7 @@ namespace {
 constexpr int KT = 32;                           // keys of a tile
 
 template <int DP> struct PagesCfg {              // DP: head size padded to 64 or 128
-  static constexpr int kStages = DP == 64 ? 6 : 3;
+  static constexpr int kStages = DP == 64 ? 4 : 2;
   static constexpr int kTileBytes = KT * DP;
   static constexpr int kStageBytes = 2 * kTileBytes;
   static constexpr int kRing = kWarps * kStages * kStageBytes;
@@ -54,8 +61,16 @@ __device__ __forceinline__ uint32_t tile8_off(int r, int c) {
 // 2^e, 0 below the float range.
 __device__ __forceinline__ float pow2_or_0(int e) { return e < -126 ? 0.f : pow2(e); }
 
-template <typename T, int DP, bool CLUSTER>
-__global__ void __launch_bounds__(kWarps * 32, 2)
+// Transposes an 8 x 8 matrix of 16-bit numbers, two of a row per lane.
+__device__ __forceinline__ uint32_t transpose8(uint32_t x) {
+  uint32_t y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+
+// NR: groups of 8 rows of a block.
+template <typename T, int DP, int NR, bool CLUSTER>
+__global__ void __launch_bounds__(kWarps * 32, NR == 1 ? 3 : 2)
     k_attn_pages(const __grid_constant__ AttnArgs A, const __grid_constant__ PagesArgs P) {
   using C = PagesCfg<DP>;
   constexpr int kStages = C::kStages;
@@ -84,38 +99,23 @@ __global__ void __launch_bounds__(kWarps * 32, 2)
 
   for (int rg = rg0; (long long)rg * kRows < rows_all; rg += A.row_groups) {
     const int r0 = rg * kRows;
-    // this lane's two rows: lane / 4 and 8 further
-    int hi[2], head[2];
-    AttnView view[2];
-    bool row_ok[2];
-    long long tok[2];
+    // B fragments of Q: this lane's row is lane / 4 of a group, and step s has channels
+    // 16 s + 4 (lane % 4) + {0, 1 | 2, 3}
+    uint32_t qb[NR][DP / 16][2];
+    float qscale[NR];                            // what the row's scores are multiplied by
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int r = r0 + lane / 4 + 8 * i;
-      row_ok[i] = r < rows_all;
-      const int ql = row_ok[i] ? r / A.group : 0;
-      head[i] = kvh * A.group + (row_ok[i] ? r % A.group : 0);
-      tok[i] = S.q0 + ql;
-      hi[i] = row_ok[i] ? attn_visible(A, S, S.first, ql) : 0;
-      view[i] = attn_view(A, S, S.first, ql);
-    }
-    // the rows' reach, and what some or all of them see of keys behind their windows
-    const int ql0 = r0 / A.group, ql1 = (min(r0 + kRows, rows_all) - 1) / A.group;
-    const int end = min(c1, attn_visible(A, S, S.first, ql1)), least = attn_visible(A, S, S.first, ql0);
-    const AttnView first = attn_view(A, S, S.first, ql0), last = attn_view(A, S, S.first, ql1);
-    // A fragments of Q: step s has channels 16 s + 4 (lane % 4) + {0, 1 | 2, 3}
-    uint32_t qa[DP / 16][4];
-    float qs[2];                                 // what the scores are multiplied by
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < NR; ++i) {
+      const int r = r0 + i * 8 + lane / 4;
+      const bool row_ok = r < rows_all;
       uint2 x[DP / 16];
-      const T* q = static_cast<const T*>(A.q) + tok[i] * A.q_row + (long long)head[i] * A.q_head;
+      const T* q = static_cast<const T*>(A.q);
+      if (row_ok) q += (long long)(S.q0 + r / A.group) * A.q_row + (long long)(kvh * A.group + r % A.group) * A.q_head;
 #pragma unroll
       for (int s = 0; s < DP / 16; ++s) {
         const int col = s * 16 + (lane % 4) * 4;
-        x[s] = row_ok[i] && col < A.dim ? *reinterpret_cast<const uint2*>(q + col) : make_uint2(0u, 0u);
+        x[s] = row_ok && col < A.dim ? *reinterpret_cast<const uint2*>(q + col) : make_uint2(0u, 0u);
       }
-      qs[i] = A.scale_log2;
+      qscale[i] = A.scale_log2;
       if (std::is_same<T, __nv_bfloat16>::value) {
         float top = 0.f;
 #pragma unroll
@@ -129,25 +129,46 @@ __global__ void __launch_bounds__(kWarps * 32, 2)
         top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
         const int e = max((int)(__float_as_uint(top) >> 23) - 127 - 14, -110);   // top 2^-e in [2^14, 2^15)
         const float down = pow2(-e);
-        qs[i] *= pow2(e);
+        qscale[i] *= pow2(e);
 #pragma unroll
         for (int s = 0; s < DP / 16; ++s) {
           const float2 f = Store<T>::unpack2(x[s].x), g = Store<T>::unpack2(x[s].y);
-          qa[s][i] = Store<__half>::pack2(f.x * down, f.y * down);
-          qa[s][i + 2] = Store<__half>::pack2(g.x * down, g.y * down);
+          qb[i][s][0] = Store<__half>::pack2(f.x * down, f.y * down);
+          qb[i][s][1] = Store<__half>::pack2(g.x * down, g.y * down);
         }
       } else {
 #pragma unroll
         for (int s = 0; s < DP / 16; ++s) {
-          qa[s][i] = x[s].x;
-          qa[s][i + 2] = x[s].y;
+          qb[i][s][0] = x[s].x;
+          qb[i][s][1] = x[s].y;
         }
       }
     }
-    float o[DP / 8][4];                          // [2 u], [2 u + 1]: even, odd channels of unit u
+    // of scores and results a lane has two rows of each group: 2 (lane % 4) and the next
+    constexpr int N = 2 * NR;
+    int hi[N];
+    AttnView view[N];
+    float qs[N];
 #pragma unroll
-    for (int n = 0; n < DP / 8; ++n) o[n][0] = o[n][1] = o[n][2] = o[n][3] = 0.f;
-    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+    for (int i = 0; i < N; ++i) {
+      const int r = r0 + (i >> 1) * 8 + (lane & 3) * 2 + (i & 1);
+      const int ql = r < rows_all ? r / A.group : 0;
+      hi[i] = r < rows_all ? attn_visible(A, S, S.first, ql) : 0;
+      view[i] = attn_view(A, S, S.first, ql);
+      qs[i] = __shfl_sync(0xFFFFFFFFu, qscale[i >> 1], ((lane & 3) * 2 + (i & 1)) * 4);
+    }
+    // the rows' reach, and what some or all of them see of keys behind their windows
+    const int ql0 = r0 / A.group, ql1 = (min(r0 + 8 * NR, rows_all) - 1) / A.group;
+    const int end = min(c1, attn_visible(A, S, S.first, ql1)), least = attn_visible(A, S, S.first, ql0);
+    const AttnView first = attn_view(A, S, S.first, ql0), last = attn_view(A, S, S.first, ql1);
+    float o[NR][DP / 16][4];                     // channels 16 u + 2 (lane / 4) + {0, 1} of two rows: 00 01 10 11
+#pragma unroll
+    for (int i = 0; i < NR; ++i)
+#pragma unroll
+      for (int u = 0; u < DP / 16; ++u) o[i][u][0] = o[i][u][1] = o[i][u][2] = o[i][u][3] = 0.f;
+    float m[N], l[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) m[i] = -INFINITY, l[i] = 0.f;
     int unit = kExpMin;                          // o is in units of 2^unit
 
     const int n_tiles = end > c0 ? (end - c0 + KT - 1) / KT : 0;
@@ -156,6 +177,8 @@ __global__ void __launch_bounds__(kWarps * 32, 2)
       const int page = table[attn_row(S, c0 + t * KT) >> P.s.shift];
       return (unsigned)page < (unsigned)P.s.n_pages ? page : -1;
     };
+    constexpr int U = DP / 16;                   // 16-byte units of a row
+    const int lr = lane / U, lc = lane % U;      // this lane's first unit of a tile
     auto load = [&](int t, int stage, int page) {
       const int j = c0 + t * KT + lane;
       const bool ok = page >= 0 && j < end && (j < last.seen || j >= first.low);
@@ -164,15 +187,24 @@ __global__ void __launch_bounds__(kWarps * 32, 2)
         const uint32_t ks = ring + stage * C::kStageBytes, vs = ks + C::kTileBytes;
         const int row = attn_row(S, c0 + t * KT) & (P.s.page_rows - 1);
         const long long at = page * P.s.page_bytes + head_at + (long long)row * A.dim;
-        constexpr int U = DP / 16;               // 16-byte units of a row
+        if (bits == 0xFFFFFFFFu && A.dim == DP) {
+          const unsigned char *kg = P.k + at + lane * 16, *vg = P.v + at + lane * 16;
 #pragma unroll
-        for (int i = 0; i < KT * U / 32; ++i) {
-          const int idx = i * 32 + lane, r = idx / U, c = idx % U;
-          const bool live = (bits >> r) & 1 && c * 16 < A.dim;
-          const int off = live ? r * A.dim + c * 16 : 0;
-          const uint32_t to = tile8_off<DP>(r, c);
-          cp16z(ks + to, P.k + at + off, live);
-          cp16z(vs + to, P.v + at + off, live);
+          for (int i = 0; i < U; ++i) {
+            const uint32_t to = tile8_off<DP>(i * (32 / U) + lr, lc);
+            cp16z(ks + to, kg + i * 512, true);
+            cp16z(vs + to, vg + i * 512, true);
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < U; ++i) {
+            const int r = i * (32 / U) + lr;
+            const bool live = (bits >> r) & 1 && lc * 16 < A.dim;
+            const int off = live ? r * A.dim + lc * 16 : 0;
+            const uint32_t to = tile8_off<DP>(r, lc);
+            cp16z(ks + to, P.k + at + off, live);
+            cp16z(vs + to, P.v + at + off, live);
+          }
         }
         if (lane == 0)
           cp4(notes + stage * 8, P.scales + page * P.s.scale_bytes + scale_at + (row / kPageBlock) * 2);
@@ -185,126 +217,139 @@ __global__ void __launch_bounds__(kWarps * 32, 2)
     int page = page_of(w + (kStages - 1) * kWarps);
     int stage = 0;
     for (int t = w; t < n_tiles; t += kWarps) {
-      cp_async_wait<kStages - 2>();
-      __syncwarp();
       load(t + (kStages - 1) * kWarps, (stage + kStages - 1) % kStages, page);
+      cp_async_wait<kStages - 1>();
+      __syncwarp();
       page = page_of(t + kStages * kWarps);
       const unsigned bits = notes_g[stage * 2 + 1];
       if (bits) {
         const uint32_t ks = ring + stage * C::kStageBytes, vs = ks + C::kTileBytes;
         const uint32_t exps = notes_g[stage * 2];
-        float s[KT / 8][4];
+        float s[NR][KT / 16][4];                 // keys lane / 4 and 8 further of 16, two rows: 00 01 10 11
 #pragma unroll
-        for (int n = 0; n < KT / 8; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f;
+        for (int i = 0; i < NR; ++i)
 #pragma unroll
-        for (int d = 0; d < DP / 64; ++d)        // 64 channels: four k16 steps, one ldmatrix.x4 per 8 keys
+          for (int n = 0; n < KT / 16; ++n) s[i][n][0] = s[i][n][1] = s[i][n][2] = s[i][n][3] = 0.f;
 #pragma unroll
-          for (int n = 0; n < KT / 8; ++n) {
-            uint32_t k4[4];
-            ldm4(ks + tile8_off<DP>(n * 8 + (lane & 7), d * 4 + (lane >> 3)), k4);
+        for (int u = 0; u < DP / 16; u += 2)     // 32 channels: two k16 steps, one ldmatrix.x4 per 16 keys
 #pragma unroll
-            for (int u = 0; u < 4; ++u)
-              mma16816<__half>(s[n], qa[d * 4 + u], widen_e4m3x2(k4[u]), widen_e4m3x2(k4[u] >> 16));
+          for (int n = 0; n < KT / 16; ++n) {
+            uint32_t k4[4];                      // keys of unit u, 8 further, of unit u + 1, 8 further
+            ldm4(ks + tile8_off<DP>(n * 16 + (lane & 15), u + (lane >> 4)), k4);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const uint32_t a[4] = {widen_e4m3x2(k4[2 * h]), widen_e4m3x2(k4[2 * h + 1]), widen_e4m3x2(k4[2 * h] >> 16),
+                                     widen_e4m3x2(k4[2 * h + 1] >> 16)};
+#pragma unroll
+              for (int i = 0; i < NR; ++i) mma16816<__half>(s[i][n], a, qb[i][u + h][0], qb[i][u + h][1]);
+            }
           }
         const int j0 = c0 + t * KT;
         const bool edge = bits != 0xFFFFFFFFu || j0 + KT > least || (j0 < last.low && j0 + KT > first.seen);
-        float top[2] = {-INFINITY, -INFINITY};
+        float top[N];
 #pragma unroll
-        for (int n = 0; n < KT / 8; ++n) {
-          const float ke = pow2(max((int)(signed char)(exps >> (n / 2 * 16)), kExpMin));
+        for (int i = 0; i < N; ++i) top[i] = -INFINITY;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int key = n * 8 + (lane & 3) * 2 + (i & 1), rr = i >> 1;
-            float x = s[n][i] * qs[rr] * ke;
-            if (A.cap_log2 > 0.f) x = A.cap_log2 * (far_cap ? tanh_rel(x) : tanh_abs(x));
-            if (edge) {
-              const int j = j0 + key;
-              if (!((bits >> key) & 1) || j >= hi[rr] || (j >= view[rr].seen && j < view[rr].low)) x = -INFINITY;
+        for (int n = 0; n < KT / 16; ++n) {
+          const float ke = pow2(max((int)(signed char)(exps >> (n * 16)), kExpMin));
+#pragma unroll
+          for (int i = 0; i < N; ++i) {
+            // finite: a score of 0 stays 0 whatever the factor
+            const float f = fminf(fmaxf(qs[i] * ke, -3e38f), 3e38f);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              float& y = s[i >> 1][n][2 * h + (i & 1)];
+              float x = y * f;
+              if (A.cap_log2 > 0.f) x = A.cap_log2 * (far_cap ? tanh_rel(x) : tanh_abs(x));
+              if (edge) {
+                const int key = n * 16 + h * 8 + lane / 4, j = j0 + key;
+                if (!((bits >> key) & 1) || j >= hi[i] || (j >= view[i].seen && j < view[i].low)) x = -INFINITY;
+              }
+              y = x;
+              top[i] = fmaxf(top[i], x);
             }
-            s[n][i] = x;
-            top[rr] = fmaxf(top[rr], x);
           }
         }
         constexpr float kLift = 15.0f;           // log2 of the largest probability, for fp16's range
+        bool moved = false;
+        float f[N];
 #pragma unroll
-        for (int rr = 0; rr < 2; ++rr) {
-          top[rr] = fmaxf(top[rr], __shfl_xor_sync(0xFFFFFFFFu, top[rr], 1));
-          top[rr] = fmaxf(top[rr], __shfl_xor_sync(0xFFFFFFFFu, top[rr], 2));
-          const float mn = fmaxf(m[rr], top[rr] - kLift);
+        for (int i = 0; i < N; ++i) {
+          top[i] = fmaxf(top[i], __shfl_xor_sync(0xFFFFFFFFu, top[i], 4));
+          top[i] = fmaxf(top[i], __shfl_xor_sync(0xFFFFFFFFu, top[i], 8));
+          top[i] = fmaxf(top[i], __shfl_xor_sync(0xFFFFFFFFu, top[i], 16));
+          const float mn = fmaxf(m[i], top[i] - kLift);
           const float base = mn == -INFINITY ? 0.f : mn;
-          const float f = exp2f(m[rr] - base);   // m = -inf: 0
-          m[rr] = mn;
-          l[rr] *= f;
-          top[rr] = base;
-          if (__any_sync(0xFFFFFFFFu, f != 1.0f)) {
-#pragma unroll
-            for (int n = 0; n < DP / 8; ++n) {
-              o[n][2 * rr] *= f;
-              o[n][2 * rr + 1] *= f;
-            }
-          }
+          f[i] = exp2f(m[i] - base);             // m = -inf: 0
+          moved = moved || f[i] != 1.0f;
+          m[i] = mn;
+          l[i] *= f[i];
+          top[i] = base;
         }
-        float sum[2] = {0.f, 0.f};               // a tile's sum first, as in attn_rows.cu
-#pragma unroll
-        for (int n = 0; n < KT / 8; ++n)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            s[n][i] = exp2f(s[n][i] - top[i >> 1]);
-            sum[i >> 1] += s[n][i];
-          }
-        l[0] += sum[0];
-        l[1] += sum[1];
         // values' exponents; a block that nobody sees has none
         int ve[2];
 #pragma unroll
         for (int kk = 0; kk < 2; ++kk)
           ve[kk] = (bits >> (kk * 16)) & 0xFFFFu ? max((int)(signed char)(exps >> (kk * 16 + 8)), kExpMin) : kExpMin;
         const int up = max(ve[0], ve[1]);
-        if (up > unit) {
-          const float f = pow2_or_0(unit - up);
+        if (__any_sync(0xFFFFFFFFu, moved) || up > unit) {
+          const float g = pow2_or_0(min(unit - up, 0));
+          unit = max(unit, up);
 #pragma unroll
-          for (int n = 0; n < DP / 8; ++n) {
-            o[n][0] *= f;
-            o[n][1] *= f;
-            o[n][2] *= f;
-            o[n][3] *= f;
+          for (int i = 0; i < NR; ++i)
+#pragma unroll
+            for (int u = 0; u < DP / 16; ++u) {
+              o[i][u][0] *= f[2 * i] * g;
+              o[i][u][1] *= f[2 * i + 1] * g;
+              o[i][u][2] *= f[2 * i] * g;
+              o[i][u][3] *= f[2 * i + 1] * g;
+            }
+        }
+        uint32_t pb[NR][KT / 16][2];             // B fragments of P^T
+        float sum[N];                            // a tile's sum first, as in attn_rows.cu
+#pragma unroll
+        for (int i = 0; i < N; ++i) sum[i] = 0.f;
+#pragma unroll
+        for (int n = 0; n < KT / 16; ++n) {
+          const float g = pow2_or_0(ve[n] - unit);
+#pragma unroll
+          for (int i = 0; i < NR; ++i) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const float p0 = exp2f(s[i][n][2 * h] - top[2 * i]), p1 = exp2f(s[i][n][2 * h + 1] - top[2 * i + 1]);
+              sum[2 * i] += p0;
+              sum[2 * i + 1] += p1;
+              pb[i][n][h] = transpose8(Store<__half>::pack2(p0 * g, p1 * g));
+            }
           }
-          unit = up;
         }
 #pragma unroll
-        for (int kk = 0; kk < KT / 16; ++kk) {
-          const float f = pow2_or_0(ve[kk] - unit);
-          // probabilities as two terms, as in attn_rows.cu
-          uint32_t pa[4], pl[4];
-          split2<__half>(s[2 * kk][0] * f, s[2 * kk][1] * f, pa[0], pl[0]);
-          split2<__half>(s[2 * kk][2] * f, s[2 * kk][3] * f, pa[1], pl[1]);
-          split2<__half>(s[2 * kk + 1][0] * f, s[2 * kk + 1][1] * f, pa[2], pl[2]);
-          split2<__half>(s[2 * kk + 1][2] * f, s[2 * kk + 1][3] * f, pa[3], pl[3]);
+        for (int i = 0; i < N; ++i) l[i] += sum[i];
+#pragma unroll
+        for (int n = 0; n < KT / 16; ++n)
 #pragma unroll
           for (int u = 0; u < DP / 16; u += 2) {
             uint32_t v4[4];                      // units u, u + 1: keys 2c, 2c + 1 and 8 further, channels 2g, 2g + 1
-            ldm4t(vs + tile8_off<DP>(kk * 16 + (lane & 15), u + (lane >> 4)), v4);
+            ldm4t(vs + tile8_off<DP>(n * 16 + (lane & 15), u + (lane >> 4)), v4);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
               const uint32_t even = __byte_perm(v4[2 * h], v4[2 * h + 1], 0x6420);
               const uint32_t odd = __byte_perm(v4[2 * h], v4[2 * h + 1], 0x7531);
-              const uint32_t e0 = widen_e4m3x2(even), e1 = widen_e4m3x2(even >> 16);
-              const uint32_t d0 = widen_e4m3x2(odd), d1 = widen_e4m3x2(odd >> 16);
-              mma16816<__half>(o[2 * (u + h)], pa, e0, e1);
-              mma16816<__half>(o[2 * (u + h) + 1], pa, d0, d1);
-              mma16816<__half>(o[2 * (u + h)], pl, e0, e1);
-              mma16816<__half>(o[2 * (u + h) + 1], pl, d0, d1);
+              const uint32_t a[4] = {widen_e4m3x2(even), widen_e4m3x2(odd), widen_e4m3x2(even >> 16), widen_e4m3x2(odd >> 16)};
+#pragma unroll
+              for (int i = 0; i < NR; ++i) mma16816<__half>(o[i][u + h], a, pb[i][n][0], pb[i][n][1]);
             }
           }
-        }
       }
+      __syncwarp();                              // the tile is done with: the next round's copies take its place
       stage = (stage + 1) % kStages;
     }
     cp_async_wait<0>();
 #pragma unroll
-    for (int rr = 0; rr < 2; ++rr) {
-      l[rr] += __shfl_xor_sync(0xFFFFFFFFu, l[rr], 1);
-      l[rr] += __shfl_xor_sync(0xFFFFFFFFu, l[rr], 2);
+    for (int i = 0; i < N; ++i) {
+      l[i] += __shfl_xor_sync(0xFFFFFFFFu, l[i], 4);
+      l[i] += __shfl_xor_sync(0xFFFFFFFFu, l[i], 8);
+      l[i] += __shfl_xor_sync(0xFFFFFFFFu, l[i], 16);
     }
     // the states leave with probabilities of at most 1 and without units
     __syncthreads();
@@ -312,16 +357,15 @@ __global__ void __launch_bounds__(kWarps * 32, 2)
     constexpr float kDrop = 1.0f / 32768.0f;
     const float back = pow2(unit);
 #pragma unroll
-    for (int rr = 0; rr < 2; ++rr) {
-      float* dst = mo + (w * kRows + lane / 4 + 8 * rr) * (DP + 4);
+    for (int i = 0; i < N; ++i) {
+      float* dst = mo + (w * kRows + (i >> 1) * 8 + (lane & 3) * 2 + (i & 1)) * (DP + 4);
 #pragma unroll
       for (int u = 0; u < DP / 16; ++u)
-        *reinterpret_cast<float4*>(dst + u * 16 + (lane & 3) * 4) =
-            make_float4(o[2 * u][2 * rr] * kDrop * back, o[2 * u + 1][2 * rr] * kDrop * back,
-                        o[2 * u][2 * rr + 1] * kDrop * back, o[2 * u + 1][2 * rr + 1] * kDrop * back);
-      if ((lane & 3) == 0) {
-        dst[DP] = m[rr] + 15.0f;
-        dst[DP + 1] = l[rr] * kDrop;
+        *reinterpret_cast<float2*>(dst + u * 16 + (lane / 4) * 2) =
+            make_float2(o[i >> 1][u][i & 1] * kDrop * back, o[i >> 1][u][2 + (i & 1)] * kDrop * back);
+      if (lane / 4 == 0) {
+        dst[DP] = m[i] + 15.0f;
+        dst[DP + 1] = l[i] * kDrop;
       }
     }
     merge_states<T, DP, CLUSTER>(A, S, mo, r0, rows_all, kvh, chunk);
@@ -393,11 +437,12 @@ __global__ void __launch_bounds__(kWidenThreads)
   }
 }
 
-template <typename T, int DP, bool CLUSTER>
+template <typename T, int DP, int NR, bool CLUSTER>
 cudaError_t launch_pages_t(const AttnArgs& a, const PagesArgs& p, cudaStream_t st) {
   using C = PagesCfg<DP>;
+  const auto kern = k_attn_pages<T, DP, NR, CLUSTER>;
   static std::atomic<uint64_t> allowed{0};
-  const cudaError_t e = allow_smem(reinterpret_cast<const void*>(k_attn_pages<T, DP, CLUSTER>), C::kSmem, &allowed, CLUSTER && kCluster > 8);
+  const cudaError_t e = allow_smem(reinterpret_cast<const void*>(kern), C::kSmem, &allowed, CLUSTER && kCluster > 8);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t lc = {};
   lc.gridDim = dim3((unsigned)((long long)a.n_seqs * a.kv_heads * a.row_groups * a.n_chunks));
@@ -412,14 +457,21 @@ cudaError_t launch_pages_t(const AttnArgs& a, const PagesArgs& p, cudaStream_t s
     lc.attrs = at;
     lc.numAttrs = 1;
   }
-  return cudaLaunchKernelEx(&lc, k_attn_pages<T, DP, CLUSTER>, a, p);
+  return cudaLaunchKernelEx(&lc, kern, a, p);
 }
 
+template <int DP, int NR, bool CLUSTER>
+cudaError_t launch_pages(const AttnArgs& a, const PagesArgs& p, bool bf16, cudaStream_t st) {
+  return bf16 ? launch_pages_t<__nv_bfloat16, DP, NR, CLUSTER>(a, p, st) : launch_pages_t<__half, DP, NR, CLUSTER>(a, p, st);
+}
+template <int DP, bool CLUSTER>
+cudaError_t launch_pages(const AttnArgs& a, const PagesArgs& p, bool bf16, cudaStream_t st) {
+  return (long long)a.most_q * a.group <= 8 ? launch_pages<DP, 1, CLUSTER>(a, p, bf16, st)
+                                            : launch_pages<DP, 2, CLUSTER>(a, p, bf16, st);
+}
 template <bool CLUSTER>
 cudaError_t launch_pages(const AttnArgs& a, const PagesArgs& p, bool bf16, cudaStream_t st) {
-  if (a.dim <= 64)
-    return bf16 ? launch_pages_t<__nv_bfloat16, 64, CLUSTER>(a, p, st) : launch_pages_t<__half, 64, CLUSTER>(a, p, st);
-  return bf16 ? launch_pages_t<__nv_bfloat16, 128, CLUSTER>(a, p, st) : launch_pages_t<__half, 128, CLUSTER>(a, p, st);
+  return a.dim <= 64 ? launch_pages<64, CLUSTER>(a, p, bf16, st) : launch_pages<128, CLUSTER>(a, p, bf16, st);
 }
 
 }  // namespace
