@@ -34,26 +34,42 @@ constexpr int kTcPageRows = 64;
 // blocks has up to 64 sums.
 constexpr long long kSumKeys = 1 << 16, kLongSum = 1 << 20;
 
-// Chunks of the span for the few-rows kernel, two blocks of which run on an SM.  A
-// block costs about kBegin to begin and end, and a step of its four warps (32 KB of
-// keys and values) about kStep, the memory's share of it when all blocks run.
+// Chunks of the span for the few-rows kernels, `resident` blocks of which run on an SM
+// (2, or 3 over pages where a key head has up to 8 rows).  A block costs about `begin` to
+// begin and end, and a step of its four warps (32 KB of keys and values) about kStep, the
+// memory's share of it when all blocks run.
 // One sequence: whole rounds of blocks; 110,537 keys of 2 heads take 30 us in one
 // round, 38 in two, 55 in four.  Several sequences are taken to be ragged: blocks of
 // unlike lengths run into one another, so the number weighs what they cost to begin
 // against the last one's length; 61 sequences of up to 16,384 keys and 8 heads take
 // 323 us in 3 chunks, 297 in 5 (the rule's) and 299 in 8; 8 sequences of up to
-// 20,000 keys and 4 heads 60, 23 (the rule's 22) and 32 us in 3, 22 and 8.
-long long rows_chunks(long long units, int n_seqs, long long steps, long long least_chunks, long long most, int sms) {
-  constexpr double kBegin = 10.0, kStep = 1.5;
-  const long long slots = 2LL * sms;
+// 20,000 keys and 4 heads 60, 23 (the rule's 22) and 32 us in 3, 22 and 8; over pages
+// the 61 take 163 us in 4 chunks, 157 in 5 (the rule's) and 156 in 8.  Behind a window
+// most are as long as one another (`equal`): rounds again, the last one of which may
+// overhang by a quarter, since some are shorter; the 61 over windows of 5000 take 206,
+// 175 (the rule's 2 chunks), 190 and 197 us in 1, 2, 3 and 8, 30 of them over windows of
+// 2000 47, 57 and 59 in 1 (the rule's), 2 and 3.
+long long rows_chunks(long long units, bool several, bool equal, long long steps, long long least_chunks, long long most,
+                      int sms, int resident, double begin) {
+  constexpr double kStep = 1.5;
+  const long long slots = (long long)resident * sms;
   long long best = 1;
-  if (n_seqs > 1) {
-    best = (long long)(sqrt((double)steps * kStep * slots / (units * kBegin)) + 0.5);
+  double least = 0;
+  if (several && equal) {
+    for (long long c = 1; c <= std::min(most, 64LL); ++c) {
+      const double rounds = std::max(1.0, ceil((double)(units * c) / slots - 0.25));
+      const double cost = rounds * (6.0 + kStep * ((steps + c - 1) / c));
+      if (c == 1 || cost < least) {
+        least = cost;
+        best = c;
+      }
+    }
+  } else if (several) {
+    best = (long long)(sqrt((double)steps * kStep * slots / (units * begin)) + 0.5);
   } else {
-    double least = 0;
     for (long long k = 1; k <= 8; ++k) {
       const long long c = std::max(1LL, std::min(most, slots * k / units));
-      const double cost = (double)((units * c + slots - 1) / slots) * (kBegin + kStep * ((steps + c - 1) / c)) + 0.02 * c;
+      const double cost = (double)((units * c + slots - 1) / slots) * (begin + kStep * ((steps + c - 1) / c)) + 0.02 * c;
       if (k == 1 || cost < least) {
         least = cost;
         best = c;
@@ -194,7 +210,8 @@ rtcc_status run_attention(AttnArgs& a, const PagesArgs* pages, int max_q, int ma
     const long long sums = tc ? w.streams : 4;     // of a block
     const long long least = (most_k + sums * kSumKeys - 1) / (sums * kSumKeys);
     long long chunks = tc ? tc_chunks(units, steps, least, most, sms, w.streams, w.n_q, w.heads, w.dim)
-                          : rows_chunks(units, w.n_seqs, steps, least, most, sms);
+                          : rows_chunks(units, w.n_seqs > 1, most_k < max_k, steps, least, most, sms,
+                                        pages && (long long)max_q * w.group <= 8 ? 3 : 2, pages ? 8.0 : 10.0);
     if (tc && most_k / (chunks * sums) > kLongSum) continue;
     const long long joined = tc || !clusters ? 1 : rows_cluster(units, steps, chunks, least, sms, w.dim);
     w.cluster = joined > 1;

@@ -16,6 +16,7 @@
 //
 // copy and write move every byte once and are bound by HBM.
 #include <atomic>
+#include <type_traits>
 
 #include "common.cuh"
 #include "kernels.h"
@@ -73,17 +74,25 @@ __device__ __forceinline__ int block_sum(int v, int* warp_sum, int* total) {
   return before + x - v;
 }
 
-// The cluster's sums of one value per block: before this block, and of all.
-__device__ __forceinline__ int cluster_sum(int mine, int* slot, int rank, int blocks, int* all) {
+// The cluster's sums of two values per block: before this block, and of all.  Peers'
+// shared memory is read before the next barrier of the cluster, which there has to be.
+__device__ __forceinline__ int2 cluster_sum(int2 mine, int2* slot, int rank, int blocks, int2* all) {
   if (threadIdx.x == 0) *slot = mine;
   __syncthreads();
   cluster_sync_all();
-  int before = 0, sum = 0;
+  int2 before = make_int2(0, 0), sum = make_int2(0, 0);
   for (int i = 0; i < blocks; ++i) {
-    int v;
-    asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(mapa_shared(smem_u32(slot), i)) : "memory");
-    if (i < rank) before += v;
-    sum += v;
+    int2 v;
+    asm volatile("ld.shared::cluster.v2.s32 {%0, %1}, [%2];"
+                 : "=r"(v.x), "=r"(v.y)
+                 : "r"(mapa_shared(smem_u32(slot), i))
+                 : "memory");
+    if (i < rank) {
+      before.x += v.x;
+      before.y += v.y;
+    }
+    sum.x += v.x;
+    sum.y += v.y;
   }
   *all = sum;
   return before;
@@ -119,44 +128,53 @@ __device__ __forceinline__ int fork_entry(const ForkArgs& A, int seq, int i) {
   return (unsigned)page < (unsigned)A.s.n_pages ? page : -1;
 }
 
-// References to `page`, counted together where lanes of a warp name the same one.
-__device__ __forceinline__ void count_page(int* refs, int page) {
-  if (page >= 0) atomicAdd(&refs[page], 1);      // whole numbers: the order does not matter
-}
-
-// One block for small tables: the counts are cleared, then entries counted.
-__global__ void __launch_bounds__(kThreads) k_fork_small(const __grid_constant__ ForkArgs A) {
-  for (int p = threadIdx.x; p < A.s.n_pages; p += kThreads) A.refs[p] = 0;
-  __syncthreads();
-  const int cells = A.s.n_seqs * A.s.table_row;
-  for (int c = threadIdx.x; c < cells; c += kThreads) {
-    const int page = fork_entry(A, c / A.s.table_row, c % A.s.table_row);
-    A.table_out[c] = page;
-    count_page(A.refs, page);
-  }
-  for (int s = threadIdx.x; s < A.s.n_seqs; s += kThreads) {
-    int p;
-    A.length_out[s] = fork_length(A, s, &p);
-  }
-}
-
-// Larger ones in two launches: entries are written and counts cleared, then counted.
-__global__ void __launch_bounds__(256) k_fork_table(const __grid_constant__ ForkArgs A) {
-  pdl_trigger();
-  const long long step = (long long)gridDim.x * blockDim.x, first = (long long)blockIdx.x * blockDim.x + threadIdx.x;
-  for (long long p = first; p < A.s.n_pages; p += step) A.refs[p] = 0;
+// Four entries at a time, step apart: their chains of loads (parent, length, entry) run
+// beside one another.
+__device__ __forceinline__ void fork_cells(const ForkArgs& A, long long first, long long step, bool count) {
   const long long cells = (long long)A.s.n_seqs * A.s.table_row;
-  for (long long c = first; c < cells; c += step)
-    A.table_out[c] = fork_entry(A, (int)(c / A.s.table_row), (int)(c % A.s.table_row));
+  for (long long c0 = first; c0 < cells; c0 += 4 * step) {
+    int page[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const long long c = c0 + u * step;
+      page[u] = c < cells ? fork_entry(A, (int)(c / A.s.table_row), (int)(c % A.s.table_row)) : -1;
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (c0 + u * step < cells) {
+        A.table_out[c0 + u * step] = page[u];
+        if (count && page[u] >= 0) atomicAdd(&A.refs[page[u]], 1);       // whole numbers: the order does not matter
+      }
+  }
   for (long long s = first; s < A.s.n_seqs; s += step) {
     int p;
     A.length_out[s] = fork_length(A, (int)s, &p);
   }
 }
+
+// Small tables in one launch of a cluster: counts are cleared, then entries counted.
+__global__ void __launch_bounds__(kThreads) k_fork(const __grid_constant__ ForkArgs A) {
+  const int rank = (int)cluster_ctarank(), blocks = (int)cluster_nctarank();
+  for (int p = rank * kThreads + threadIdx.x; p < A.s.n_pages; p += blocks * kThreads) A.refs[p] = 0;
+  __threadfence();
+  cluster_sync_all();
+  fork_cells(A, rank * kThreads + threadIdx.x, blocks * kThreads, true);
+}
+
+// Larger ones in two: entries are written and counts cleared, then counted.
+__global__ void __launch_bounds__(256) k_fork_table(const __grid_constant__ ForkArgs A) {
+  pdl_trigger();
+  const long long step = (long long)gridDim.x * blockDim.x, first = (long long)blockIdx.x * blockDim.x + threadIdx.x;
+  for (long long p = first; p < A.s.n_pages; p += step) A.refs[p] = 0;
+  fork_cells(A, first, step, false);
+}
 __global__ void __launch_bounds__(256) k_fork_count(const int* table, int* refs, long long cells) {
   pdl_wait();
   const long long step = (long long)gridDim.x * blockDim.x;
-  for (long long c = (long long)blockIdx.x * blockDim.x + threadIdx.x; c < cells; c += step) count_page(refs, table[c]);
+  for (long long c = (long long)blockIdx.x * blockDim.x + threadIdx.x; c < cells; c += step) {
+    const int page = table[c];
+    if (page >= 0) atomicAdd(&refs[page], 1);
+  }
 }
 
 // ---------------------------------------------------------------------------
@@ -198,12 +216,16 @@ __device__ __forceinline__ Want want_of(const ExtendArgs& A, int seq) {
 }
 
 __global__ void __launch_bounds__(kThreads) k_extend(const __grid_constant__ ExtendArgs A) {
-  __shared__ int warp_sum[kWarps], slot_w, slot_f;
+  __shared__ int warp_sum[kWarps];
+  __shared__ int2 slot;
   const int tid = threadIdx.x, lane = tid & 31;
   const int rank = (int)cluster_ctarank(), blocks = (int)cluster_nctarank();
   // ---- what is wanted, and which pages are free, each block over its share
   const int s0 = (int)((long long)A.s.n_seqs * rank / blocks), s1 = (int)((long long)A.s.n_seqs * (rank + 1) / blocks);
-  int wanted = 0;
+  const int p0 = (int)((long long)A.s.n_pages * rank / blocks), p1 = (int)((long long)A.s.n_pages * (rank + 1) / blocks);
+  int n_free = 0, wanted = 0, total;
+#pragma unroll 4
+  for (int p = p0 + tid; p < p1; p += kThreads) n_free += A.refs[p] == 0;
   for (int s = s0; s < s1; s += kThreads) {
     int n = 0;
     Want w{};
@@ -212,63 +234,57 @@ __global__ void __launch_bounds__(kThreads) k_extend(const __grid_constant__ Ext
       n = w.count();
       A.src[s + tid] = w.src;                    // the counts as the call began: kept for later
     }
-    int total;
     const int at = wanted + block_sum(n, warp_sum, &total);
     // whether its own last page is asked for rides along in the sign
     if (s + tid < s1) A.offset[s + tid] = w.own ? ~at : at;
     wanted += total;
   }
-  const int p0 = (int)((long long)A.s.n_pages * rank / blocks), p1 = (int)((long long)A.s.n_pages * (rank + 1) / blocks);
-  int n_free = 0;
-  for (int p = p0 + tid; p < p1; p += kThreads) n_free += A.refs[p] == 0;
-  int total;
   block_sum(n_free, warp_sum, &total);
-  n_free = total;
-  int all_wanted, all_free;
-  const int want_base = cluster_sum(wanted, &slot_w, rank, blocks, &all_wanted);
-  const int free_base = cluster_sum(n_free, &slot_f, rank, blocks, &all_free);
+  int2 all;
+  const int2 base = cluster_sum(make_int2(wanted, total), &slot, rank, blocks, &all);
   // ---- the free pages that will be given, in order
-  int at_free = free_base;
-  for (int p = p0; p < p1 && at_free < all_wanted; p += kThreads) {
+  int at_free = base.y;
+  for (int p = p0; p < p1 && at_free < all.x; p += kThreads) {
     const bool is = p + tid < p1 && A.refs[p + tid] == 0;
     const int k = at_free + block_sum(is, warp_sum, &total);
-    if (is && k < all_wanted) A.free_list[k] = p + tid;
+    if (is && k < all.x) A.free_list[k] = p + tid;
     at_free += total;
   }
   __threadfence();
   cluster_sync_all();
-  // ---- given out, a warp per sequence
-  const int given = min(all_free, all_wanted);
-  for (int s = s0 + (tid >> 5); s < s1; s += kWarps) {
-    const int off = A.offset[s], own = off < 0, src = A.src[s];
-    const int base = want_base + (own ? ~off : off);
-    const int cap = A.s.table_row << A.s.shift, pr = A.s.page_rows;
-    const int held = min(max(A.length[s], 0), cap);
-    const int end = (int)min((long long)cap, (long long)held + max(A.fresh[s], 0));
-    const int first = (held + pr - 1) >> A.s.shift, last = max(first, (end + pr - 1) >> A.s.shift);
-    int* row = A.table + (long long)s * A.s.table_row;
-    for (int i = first + lane; i < last; i += 32) {
-      const int k = base + own + i - first;
-      const int page = k < given ? A.free_list[k] : -1;
-      row[i] = page;
-      if (page >= 0) A.refs[page] = 1;
-    }
-    __syncwarp();
-    if (lane == 0) {
+  // ---- given out: a thread per sequence for its own page and the first few, its warp
+  // for what is left of long ones
+  const int given = min(all.x, all.y);
+  constexpr int kFew = 4;
+  for (int s = s0 + tid; s - lane < s1; s += kThreads) {
+    int k0 = 0, i0 = 0, i1 = 0;                  // wanted page i0 + n is number k0 + n
+    if (s < s1) {
+      const int off = A.offset[s], own = off < 0, src = A.src[s];
+      const int cap = A.s.table_row << A.s.shift, pr = A.s.page_rows;
+      const int held = min(max(A.length[s], 0), cap);
+      const int end = (int)min((long long)cap, (long long)held + max(A.fresh[s], 0));
+      const int first = (held + pr - 1) >> A.s.shift, last = max(first, (end + pr - 1) >> A.s.shift);
+      const int k = base.x + (own ? ~off : off);
+      int* row = A.table + (long long)s * A.s.table_row;
+      k0 = k + own;
+      i0 = first;
+      i1 = last;
+      int page[kFew + 1];
+#pragma unroll
+      for (int u = 0; u <= kFew; ++u) page[u] = u < own + last - first && k + u < given ? A.free_list[k + u] : -1;
       // places that have pages: up to the first one that was not given
-      const int got = min(max(given - base, 0), own + last - first);
+      const int got = min(max(given - k, 0), own + last - first);
       int n = end;
       if (got < own + last - first) n = got < own ? held : max(held, (first + got - own) << A.s.shift);
       int from = -1, to = -1, rows = 0;
       if (own) {
-        const int page = got > 0 ? A.free_list[base] : -1;
-        if (page >= 0) {
-          row[held >> A.s.shift] = page;
-          A.refs[page] = 1;
+        if (page[0] >= 0) {
+          row[held >> A.s.shift] = page[0];
+          A.refs[page[0]] = 1;
           if (src >= 0) {
             atomicSub(&A.refs[src], 1);
             from = src;
-            to = page;
+            to = page[0];
             rows = held & (pr - 1);
           }
         } else if (src < 0) {
@@ -279,10 +295,27 @@ __global__ void __launch_bounds__(kThreads) k_extend(const __grid_constant__ Ext
       A.dst[s] = to;
       A.rows[s] = rows;
       A.length_out[s] = n;
+#pragma unroll
+      for (int u = 0; u < kFew; ++u) {
+        if (i0 >= i1) break;
+        const int p = own ? page[u + 1] : page[u];
+        row[i0++] = p;
+        ++k0;
+        if (p >= 0) A.refs[p] = 1;
+      }
+    }
+    for (unsigned left = __ballot_sync(0xFFFFFFFFu, i0 < i1); left; left &= left - 1) {
+      const int l = __ffs(left) - 1;
+      const int k = __shfl_sync(0xFFFFFFFFu, k0, l), a = __shfl_sync(0xFFFFFFFFu, i0, l), b = __shfl_sync(0xFFFFFFFFu, i1, l);
+      int* row = A.table + (long long)(s - lane + l) * A.s.table_row;
+      for (int i = a + lane; i < b; i += 32) {
+        const int p = k + i - a < given ? A.free_list[k + i - a] : -1;
+        row[i] = p;
+        if (p >= 0) A.refs[p] = 1;
+      }
     }
   }
-  if (rank == 0 && tid == 0 && A.missing) *A.missing = all_wanted - given;
-  cluster_sync_all();                            // no block's sums go while another reads them
+  if (rank == 0 && tid == 0 && A.missing) *A.missing = all.x - given;
 }
 
 // ---------------------------------------------------------------------------
@@ -292,72 +325,84 @@ __global__ void __launch_bounds__(kThreads) k_extend(const __grid_constant__ Ext
 struct CompactArgs {
   const int *table, *refs;
   int *table_out, *refs_out, *src, *dst, *count;
-  int *to, *n_live;                              // workspace: [n_pages], [1]
+  int *to, *n_live;                              // workspace: [n_pages], [2]
   int remap;                                     // 1: the table is written here too
   PageShape s;
 };
 
-__device__ __forceinline__ int new_number(const CompactArgs& A, int page, int n_live) {
+// refs > 0 and number at or past n_live: `to` has the page's number among those in use.
+__device__ __forceinline__ int new_number(const CompactArgs& A, int page, int n_live, int below) {
   if ((unsigned)page >= (unsigned)A.s.n_pages || A.refs[page] <= 0) return -1;
-  return page < n_live ? page : A.to[page];
+  return page < n_live ? page : A.dst[A.to[page] - below];
+}
+
+// Four entries at a time, as in fork_cells.
+__device__ __forceinline__ void compact_cells(const CompactArgs& A, int n_live, int below, long long first, long long step) {
+  const long long cells = (long long)A.s.n_seqs * A.s.table_row;
+  for (long long c0 = first; c0 < cells; c0 += 4 * step) {
+    int page[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) page[u] = c0 + u * step < cells ? A.table[c0 + u * step] : -1;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) page[u] = new_number(A, page[u], n_live, below);
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (c0 + u * step < cells) A.table_out[c0 + u * step] = page[u];
+  }
 }
 
 __global__ void __launch_bounds__(kThreads) k_compact(const __grid_constant__ CompactArgs A) {
-  __shared__ int warp_sum[kWarps], slot_l, slot_b;
+  __shared__ int warp_sum[kWarps];
+  __shared__ int2 slot, slot_below;
   const int tid = threadIdx.x;
   const int rank = (int)cluster_ctarank(), blocks = (int)cluster_nctarank(), n = A.s.n_pages;
   pdl_trigger();
   const int p0 = (int)((long long)n * rank / blocks), p1 = (int)((long long)n * (rank + 1) / blocks);
-  int v = 0, total, live, below;
+  int v = 0, total;
+#pragma unroll 4
   for (int p = p0 + tid; p < p1; p += kThreads) v += A.refs[p] > 0;
   block_sum(v, warp_sum, &total);
-  const int live_base = cluster_sum(total, &slot_l, rank, blocks, &live);
-  v = 0;
-  for (int p = p0 + tid; p < min(p1, live); p += kThreads) v += A.refs[p] > 0;
-  block_sum(v, warp_sum, &total);
-  cluster_sum(total, &slot_b, rank, blocks, &below);
-  const int moves = live - below;
+  int2 all;
+  const int base = cluster_sum(make_int2(total, 0), &slot, rank, blocks, &all).x, live = all.x;
   // page p is the at-th in use: a free one below `live` is hole p - at, one in use past
-  // it is number at - below among those that move
-  int at0 = live_base;
+  // it the at-th of all, that is number at - below among those that move, where `below`
+  // pages in use stay
+  int at0 = base, stay = 0;
   for (int p = p0; p < p1; p += kThreads) {
-    const int i = p + tid;
-    const bool in = i < p1, is = in && A.refs[i] > 0;
-    const int at = at0 + block_sum(is, warp_sum, &total);
+    const int i = p + tid, count = i < p1 ? A.refs[i] : 0;
+    const int at = at0 + block_sum(count > 0, warp_sum, &total);
     at0 += total;
-    if (!in) continue;
-    if (is && i >= live) A.src[at - below] = i;
-    if (!is && i < live) A.dst[i - at] = i;
-    if (is || i >= live) A.refs_out[i] = i < live ? A.refs[i] : 0;     // holes get theirs below
-    if (i >= moves) A.src[i] = A.dst[i] = -1;
+    if (i >= p1) continue;
+    if (count > 0) {
+      A.to[i] = at;
+      stay += i < live;
+    }
+    if (count <= 0 && i < live) A.dst[i - at] = i;
+    if (count > 0 || i >= live) A.refs_out[i] = i < live ? count : 0;    // holes get theirs below
   }
+  block_sum(stay, warp_sum, &total);
   __threadfence();
-  cluster_sync_all();
-  for (int k = rank * kThreads + tid; k < moves; k += blocks * kThreads) {
-    const int from = A.src[k], hole = A.dst[k];
-    A.to[from] = hole;
-    A.refs_out[hole] = A.refs[from];
+  const int below = (cluster_sum(make_int2(total, 0), &slot_below, rank, blocks, &all), all.x), moves = live - below;
+  for (int i = p0 + tid; i < p1; i += kThreads) {
+    if (i >= live && A.refs[i] > 0) {
+      const int k = A.to[i] - below, hole = A.dst[k];
+      A.src[k] = i;
+      A.refs_out[hole] = A.refs[i];
+    }
+    if (i >= moves) A.src[i] = A.dst[i] = -1;    // no hole's number: those are below `moves`
   }
   if (rank == 0 && tid == 0) {
     *A.count = moves;
-    *A.n_live = live;
+    A.n_live[0] = live;
+    A.n_live[1] = below;
   }
-  if (A.remap) {
-    __threadfence();
-    cluster_sync_all();
-    const int cells = A.s.n_seqs * A.s.table_row;
-    for (int c = rank * kThreads + tid; c < cells; c += blocks * kThreads)
-      A.table_out[c] = new_number(A, A.table[c], live);
-  }
-  cluster_sync_all();
+  if (A.remap) compact_cells(A, live, below, rank * kThreads + tid, blocks * kThreads);
+  cluster_sync_all();                            // no block's sums go while another reads them
 }
 
 __global__ void __launch_bounds__(256) k_compact_table(const __grid_constant__ CompactArgs A) {
   pdl_wait();
-  const int live = *A.n_live;
-  const long long cells = (long long)A.s.n_seqs * A.s.table_row, step = (long long)gridDim.x * blockDim.x;
-  for (long long c = (long long)blockIdx.x * blockDim.x + threadIdx.x; c < cells; c += step)
-    A.table_out[c] = new_number(A, A.table[c], live);
+  compact_cells(A, A.n_live[0], A.n_live[1], (long long)blockIdx.x * blockDim.x + threadIdx.x, (long long)gridDim.x * blockDim.x);
 }
 
 // ---------------------------------------------------------------------------
@@ -372,35 +417,46 @@ struct CopyArgs {
   PageShape s;
 };
 
-constexpr int kCopyThreads = 256, kCopyVecs = 8; // 16-byte vectors of a thread and tile
+constexpr int kCopyThreads = 256;
 
-// A tile is 32 KB of a page's keys or values; every thread has eight loads under way
-// before its first store.  The listed pages' bytes bound it.
+// A tile is kCopyVecs 16-byte vectors of every thread, of a page's keys or values: up to 32 KB,
+// eight loads under way before the first store.  The listed pages' bytes bound it.
+template <int kCopyVecs>
 __global__ void __launch_bounds__(kCopyThreads) k_pages_copy(const __grid_constant__ CopyArgs A) {
   const int n = A.count ? min(A.n, *A.count) : A.n;
   const int head = A.s.page_rows * A.s.dim / 16, vecs = A.s.kv_heads * head;   // of a head, of a page's keys
-  const long long tiles = (long long)n * A.tiles;
-  for (long long t = blockIdx.x; t < tiles; t += gridDim.x) {
-    const int pair = (int)(t / A.tiles), part = (int)(t % A.tiles);
+  // block b takes tile b % tiles of pairs b / tiles, ...: gridDim.x is a multiple of the tiles
+  const int part = (int)blockIdx.x % A.tiles;
+  const bool values = part >= A.tiles / 2;
+  const unsigned char* k_src = values ? A.v_src : A.k_src;
+  unsigned char* k_dst = values ? A.v_dst : A.k_dst;
+  const int v0 = (values ? part - A.tiles / 2 : part) * kCopyThreads * kCopyVecs + (int)threadIdx.x;
+  const int step = (int)gridDim.x / A.tiles;
+  for (int pair = (int)blockIdx.x / A.tiles; pair < n; pair += step) {
     const int from = A.src[pair], to = A.dst[pair];
     if ((unsigned)from >= (unsigned)A.s.n_pages || (unsigned)to >= (unsigned)A.n_dst) continue;
     const int rows = A.rows ? min(max(A.rows[pair], 0), A.s.page_rows) : A.s.page_rows;
-    const int keep = rows * A.s.dim / 16;        // vectors of a head that are copied
-    const bool values = part >= A.tiles / 2;
-    const uint4* a = reinterpret_cast<const uint4*>((values ? A.v_src : A.k_src) + from * A.s.page_bytes);
-    uint4* b = reinterpret_cast<uint4*>((values ? A.v_dst : A.k_dst) + to * A.s.page_bytes);
-    const int v0 = (values ? part - A.tiles / 2 : part) * kCopyThreads * kCopyVecs + threadIdx.x;
+    const uint4* a = reinterpret_cast<const uint4*>(k_src + from * A.s.page_bytes) + v0;
+    uint4* b = reinterpret_cast<uint4*>(k_dst + to * A.s.page_bytes) + v0;
     uint4 x[kCopyVecs];
-    bool on[kCopyVecs];
+    if (rows == A.s.page_rows && v0 + (kCopyVecs - 1) * kCopyThreads < vecs) {
 #pragma unroll
-    for (int u = 0; u < kCopyVecs; ++u) {
-      const int v = v0 + u * kCopyThreads;
-      on[u] = v < vecs && v % head < keep;
-      if (on[u]) x[u] = __ldcs(a + v);
+      for (int u = 0; u < kCopyVecs; ++u) x[u] = __ldcs(a + u * kCopyThreads);
+#pragma unroll
+      for (int u = 0; u < kCopyVecs; ++u) __stcs(b + u * kCopyThreads, x[u]);
+    } else {
+      const int keep = rows * A.s.dim / 16;      // vectors of a head that are copied
+      bool on[kCopyVecs];
+#pragma unroll
+      for (int u = 0; u < kCopyVecs; ++u) {
+        const int v = v0 + u * kCopyThreads;
+        on[u] = v < vecs && v % head < keep;
+        if (on[u]) x[u] = __ldcs(a + u * kCopyThreads);
+      }
+#pragma unroll
+      for (int u = 0; u < kCopyVecs; ++u)
+        if (on[u]) __stcs(b + u * kCopyThreads, x[u]);
     }
-#pragma unroll
-    for (int u = 0; u < kCopyVecs; ++u)
-      if (on[u]) __stcs(b + v0 + u * kCopyThreads, x[u]);
     if (part == 0) {
       const int blocks = A.s.page_rows / kPageBlock, live = (rows + kPageBlock - 1) / kPageBlock;
       const uint16_t* sa = reinterpret_cast<const uint16_t*>(A.s_src + from * A.s.scale_bytes);
@@ -443,23 +499,59 @@ __device__ __forceinline__ uint32_t to_e4m3x2(float lo, float hi) {
 }
 __device__ __forceinline__ float2 from_e4m3x2(uint32_t v) { return Store<__half>::unpack2(widen_e4m3x2(v)); }
 
+// Eight numbers x of type T, finite, as 8 bits each of x 2^-e.
+template <typename T> struct Narrow;
+// fp16 all the way: a power of two changes no digits where the product is at least 2^-14,
+// and what is smaller rounds to 0 in 8 bits anyway.  2^-e is two factors, since fp16 ends
+// at 2^15: e from kLeast on; larger e than 40 leave 0 as 40 does.
+template <> struct Narrow<__half> {
+  static constexpr int kLeast = -30;
+  __half2 f, g;
+  __device__ __forceinline__ explicit Narrow(int e) {
+    const int n = max(-e, -40), a = n / 2;
+    f = __float2half2_rn(pow2(a));
+    g = __float2half2_rn(pow2(n - a));
+  }
+  __device__ __forceinline__ uint32_t two(uint32_t x) const {
+    __half2 h = __hmul2(__hmul2(*reinterpret_cast<__half2*>(&x), f), g);
+    uint16_t r;
+    asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(r) : "r"(*reinterpret_cast<uint32_t*>(&h)));
+    return r;
+  }
+};
+template <> struct Narrow<__nv_bfloat16> {
+  static constexpr int kLeast = kExpMin;
+  float2 f;
+  __device__ __forceinline__ explicit Narrow(int e) { f = make_float2(pow2(-e), pow2(-e)); }
+  __device__ __forceinline__ uint32_t two(uint32_t x) const {
+    const float2 y = mul2(Store<__nv_bfloat16>::unpack2(x), f);
+    return to_e4m3x2(y.x, y.y);
+  }
+};
+__device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("max.u16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+template <typename T> constexpr uint32_t kInfBits = std::is_same<T, __half>::value ? 0x7C00u : 0x7F80u;
+
 // A warp per block of 16 places, key head, and keys or values: 16 x dim numbers stay in
 // registers between the search for the largest and the rounding.  Lane l has the
 // 8-number units l, l + 32, ... of the block, row by row, so loads and stores of
 // neighbouring lanes are neighbours.  Keys and values of neighbouring heads are
-// neighbouring warps' work, as they are neighbours in a packed projection.
+// neighbouring warps' work, as they are neighbours in a packed projection.  The largest
+// is found among the numbers' bits without their signs, two at a time; a block with an
+// infinity or a NaN in it looks again.
 template <typename T, int J>                     // J = dim / 16 units of a lane
-__global__ void __launch_bounds__(kWriteThreads) k_pages_write(const __grid_constant__ WriteArgs A) {
+__global__ void __launch_bounds__(kWriteThreads, 3) k_pages_write(const __grid_constant__ WriteArgs A) {
   constexpr int U = 2 * J;                       // units of a row
   const int lane = threadIdx.x & 31;
-  long long item = (long long)blockIdx.x * (kWriteThreads / 32) + (threadIdx.x >> 5);
-  const int head = (int)(item % A.s.kv_heads);
-  item /= A.s.kv_heads;
-  const bool values = item & 1;
-  item >>= 1;
-  const int b0 = (int)(item % A.blocks);
-  const long long seq = item / A.blocks;
-  if (seq >= A.s.n_seqs) return;
+  const unsigned item = blockIdx.x * (kWriteThreads / 32) + (threadIdx.x >> 5);
+  const int head = (int)(item % (unsigned)A.s.kv_heads), rest = (int)(item / (unsigned)A.s.kv_heads);
+  const bool values = rest & 1;
+  const int b0 = rest >> 1;
+  if (b0 >= A.blocks) return;
+  for (long long seq = blockIdx.y; seq < A.s.n_seqs; seq += gridDim.y) {
   const int t0 = min(max(A.offsets[seq], 0), A.n_tokens), t1 = min(max(A.offsets[seq + 1], t0), A.n_tokens);
   const int cap = A.s.table_row << A.s.shift;
   const int held = min(max(A.held[seq], 0), cap);
@@ -474,40 +566,63 @@ __global__ void __launch_bounds__(kWriteThreads) k_pages_write(const __grid_cons
     if ((unsigned)page >= (unsigned)A.s.n_pages) continue;
     const int r0 = place & (A.s.page_rows - 1);
     const int lo = max(held - place, 0), hi = min(end - place, kPageBlock);      // rows [0, lo) are old, [lo, hi) new
+    const T* src = x0 + (long long)(t0 + place - held) * row;                    // row 0's; not read before row lo
     uint4 x[J];
-    float top = 0.f;
 #pragma unroll
     for (int j = 0; j < J; ++j) {
       const int i = j * 32 + lane, r = i / U, c = i % U;
       x[j] = make_uint4(0u, 0u, 0u, 0u);
-      if (r >= lo && r < hi)
-        x[j] = __ldcs(reinterpret_cast<const uint4*>(x0 + (long long)(t0 + place + r - held) * row + c * 8));
+      if (r >= lo && r < hi) x[j] = __ldcs(reinterpret_cast<const uint4*>(src + r * row + c * 8));
     }
     unsigned char* block = pages + page * A.s.page_bytes + ((long long)head * A.s.page_rows + r0) * A.s.dim;
     signed char* scale = A.scales + page * A.s.scale_bytes +
                          ((long long)head * (A.s.page_rows / kPageBlock) + r0 / kPageBlock) * 2 + values;
-    const int was = lo > 0 ? *scale : kExpMin;
+    const int was = lo > 0 ? min(max((int)*scale, kExpMin), kExpMax) : kExpMin;
+    uint32_t most = 0;
 #pragma unroll
     for (int j = 0; j < J; ++j) {
       const uint32_t u[4] = {x[j].x, x[j].y, x[j].z, x[j].w};
 #pragma unroll
-      for (int h = 0; h < 4; ++h) {
-        const float2 f = Store<T>::unpack2(u[h]);
-        const float a = fabsf(f.x), c = fabsf(f.y);
-        top = fmaxf(top, a < INFINITY ? a : 0.f);
-        top = fmaxf(top, c < INFINITY ? c : 0.f);
-      }
+      for (int h = 0; h < 4; ++h) most = max_u16x2(most, u[h] & 0x7FFF7FFFu);
     }
-    top = __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(top)));
-    const int e = max(least_exponent(top), min(max(was, kExpMin), kExpMax));
-    const float down = pow2(-e);
-    if (lane == 0) *scale = (signed char)e;
+    most = __reduce_max_sync(0xFFFFFFFFu, max(most & 0xFFFFu, most >> 16));
+    const bool finite = most < kInfBits<T>;
+    if (!finite) {
+      most = 0;
 #pragma unroll
-    for (int j = 0; j < J; ++j) {
-      const int i = j * 32 + lane, r = i / U, c = i % U;
-      uint2* dst = reinterpret_cast<uint2*>(block + r * A.s.dim + c * 8);
-      if (r >= lo && r < hi) {
+      for (int j = 0; j < J; ++j) {
         const uint32_t u[4] = {x[j].x, x[j].y, x[j].z, x[j].w};
+#pragma unroll
+        for (int h = 0; h < 4; ++h) {
+          const uint32_t p = u[h] & 0x7FFFu, q = u[h] >> 16 & 0x7FFFu;
+          most = max(most, max(p < kInfBits<T> ? p : 0u, q < kInfBits<T> ? q : 0u));
+        }
+      }
+      most = __reduce_max_sync(0xFFFFFFFFu, most);
+    }
+    const int e = max(least_exponent(Store<T>::unpack2(most).x), was);
+    if (lane == 0) *scale = (signed char)e;
+    const Narrow<T> narrow(e);
+    if (finite && e >= Narrow<T>::kLeast) {
+#pragma unroll
+      for (int j = 0; j < J; ++j) {
+        const int i = j * 32 + lane, r = i / U;
+        if (r >= lo && r < hi)                   // unit i of the block
+          *reinterpret_cast<uint2*>(block + i * 8) =
+              make_uint2(__byte_perm(narrow.two(x[j].x), narrow.two(x[j].y), 0x5410),
+                         __byte_perm(narrow.two(x[j].z), narrow.two(x[j].w), 0x5410));
+      }
+    } else {
+      const float down = pow2(-e);
+#pragma unroll 1
+      for (int j = 0; j < J; ++j) {
+        const int i = j * 32 + lane, r = i / U;
+        if (r < lo || r >= hi) continue;
+        uint4 z = x[0];
+#pragma unroll
+        for (int k = 1; k < J; ++k)
+          if (k == j) z = x[k];
+        const uint32_t u[4] = {z.x, z.y, z.z, z.w};
         uint32_t y[4];
 #pragma unroll
         for (int h = 0; h < 4; ++h) {
@@ -516,11 +631,15 @@ __global__ void __launch_bounds__(kWriteThreads) k_pages_write(const __grid_cons
           f.y = fabsf(f.y) < INFINITY ? f.y * down : NAN;
           y[h] = to_e4m3x2(f.x, f.y);
         }
-        *dst = make_uint2(y[0] | y[1] << 16, y[2] | y[3] << 16);
-      } else if (r < lo && e > was) {
-        // numbers of before, whose exponent rose: 2^(was - e) below 2^-30 leaves 0
+        *reinterpret_cast<uint2*>(block + i * 8) = make_uint2(y[0] | y[1] << 16, y[2] | y[3] << 16);
+      }
+    }
+    if (lo > 0 && e > was) {
+      // numbers of before, whose exponent rose: 2^-60 leaves 0 as what is smaller does
+      const float f = pow2(max(was - e, -60));
+      for (int i = lane; i < lo * U; i += 32) {
+        uint2* dst = reinterpret_cast<uint2*>(block + i * 8);
         const uint2 z = *dst;
-        const float f = pow2(max(was - e, -60));
         const uint32_t u[2] = {z.x, z.y};
         uint32_t y[2];
 #pragma unroll
@@ -532,11 +651,12 @@ __global__ void __launch_bounds__(kWriteThreads) k_pages_write(const __grid_cons
       }
     }
   }
+  }
 }
 
 template <typename T>
 cudaError_t launch_write(const WriteArgs& a, long long grid, cudaStream_t st) {
-  const dim3 g((unsigned)grid), b(kWriteThreads);
+  const dim3 g((unsigned)grid, (unsigned)(a.s.n_seqs < 65535 ? a.s.n_seqs : 65535)), b(kWriteThreads);
   switch (a.s.dim / 16) {
     case 1: k_pages_write<T, 1><<<g, b, 0, st>>>(a); break;
     case 2: k_pages_write<T, 2><<<g, b, 0, st>>>(a); break;
@@ -614,10 +734,8 @@ extern "C" rtcc_status rtcc_pages_fork(const rtcc_page_config* cfg, int32_t n_fr
   if (sms < 1) return RTCC_E_CUDA;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const long long work = cells > a.s.n_pages ? (cells > n ? cells : n) : (a.s.n_pages > n ? a.s.n_pages : n);
-  if (work <= 4 * kThreads) {
-    k_fork_small<<<1, kThreads, 0, st>>>(a);
-    return cudaGetLastError() == cudaSuccess ? RTCC_OK : RTCC_E_CUDA;
-  }
+  if (work <= 8LL * kBlocks * kThreads)
+    return launch_cluster(k_fork, a, work, st) == cudaSuccess ? RTCC_OK : RTCC_E_CUDA;
   long long grid = (work + 255) / 256;
   if (grid > sms * 8LL) grid = sms * 8LL;
   k_fork_table<<<(unsigned)grid, 256, 0, st>>>(a);
@@ -727,10 +845,17 @@ extern "C" rtcc_status rtcc_pages_copy(const rtcc_page_config* cfg, int32_t n, c
   a.s_dst = static_cast<unsigned char*>(d_scales_dst);
   a.n = n; a.n_dst = n_pages_dst;
   const int vecs = a.s.kv_heads * a.s.page_rows * a.s.dim / 16;
-  a.tiles = 2 * ((vecs + kCopyThreads * kCopyVecs - 1) / (kCopyThreads * kCopyVecs));
-  long long grid = (long long)n * a.tiles;
-  if (grid > sms * 8LL) grid = sms * 8LL;
-  k_pages_copy<<<(unsigned)grid, kCopyThreads, 0, static_cast<cudaStream_t>(stream)>>>(a);
+  const int per = vecs >= 8 * kCopyThreads ? 8 : vecs >= 4 * kCopyThreads ? 4 : vecs >= 2 * kCopyThreads ? 2 : 1;
+  a.tiles = 2 * ((vecs + kCopyThreads * per - 1) / (kCopyThreads * per));
+  long long at_once = sms * 32LL / a.tiles;      // pairs
+  if (at_once > n) at_once = n;
+  if (at_once < 1) at_once = 1;
+  const dim3 grid((unsigned)(at_once * a.tiles)), block(kCopyThreads);
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (per == 8) k_pages_copy<8><<<grid, block, 0, st>>>(a);
+  else if (per == 4) k_pages_copy<4><<<grid, block, 0, st>>>(a);
+  else if (per == 2) k_pages_copy<2><<<grid, block, 0, st>>>(a);
+  else k_pages_copy<1><<<grid, block, 0, st>>>(a);
   return cudaGetLastError() == cudaSuccess ? RTCC_OK : RTCC_E_CUDA;
 }
 
@@ -760,10 +885,8 @@ extern "C" rtcc_status rtcc_pages_write(const rtcc_page_config* cfg, const rtcc_
   a.n_tokens = t->n_tokens;
   const int most = t->max_new < 1 ? 1 : t->max_new > t->n_tokens ? t->n_tokens : t->max_new;
   long long blocks = (most + 14LL) / kPageBlock + 1;       // that they touch at most, wherever they begin
-  const long long each = (long long)a.s.n_seqs * a.s.kv_heads * 2;
-  constexpr long long kMostWarps = (1LL << 31) * (kWriteThreads / 32) - 64;
-  while (each * blocks > kMostWarps && blocks > 1) blocks = (blocks + 1) / 2;      // warps then loop
-  if (each * blocks > kMostWarps) return RTCC_E_ARG;
+  const long long each = a.s.kv_heads * 2LL;
+  while (each * blocks > 0x3FFFFFFF) blocks = (blocks + 1) / 2;     // warps then loop
   a.blocks = (int)blocks;
   const long long grid = (each * blocks + kWriteThreads / 32 - 1) / (kWriteThreads / 32);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
