@@ -742,7 +742,8 @@ rtcc_status rtcc_pages_copy(const rtcc_page_config* cfg, int32_t n, const int32_
                             int32_t n_pages_dst, void* d_k_dst, void* d_v_dst, void* d_scales_dst,
                             void* stream);
 
-/* New tokens for rtcc_pages_write; strides in elements as in rtcc_prepare_config. */
+/* New tokens for rtcc_pages_write; strides in elements as in rtcc_prepare_config, below
+ * 2^31. */
 typedef struct {
   int32_t dtype;                    /* rtcc_dtype of k and v                 */
   int32_t n_tokens;                 /* tokens of all sequences               */

@@ -528,9 +528,16 @@ template <> struct Narrow<__nv_bfloat16> {
     return to_e4m3x2(y.x, y.y);
   }
 };
-__device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b) {
+// The larger magnitudes of two pairs (signs are anything), NaN where there is one.
+template <typename T> __device__ __forceinline__ uint32_t larger2(uint32_t a, uint32_t b);
+template <> __device__ __forceinline__ uint32_t larger2<__half>(uint32_t a, uint32_t b) {
   uint32_t r;
-  asm("max.u16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  asm("max.NaN.xorsign.abs.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+template <> __device__ __forceinline__ uint32_t larger2<__nv_bfloat16>(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("max.NaN.xorsign.abs.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
   return r;
 }
 template <typename T> constexpr uint32_t kInfBits = std::is_same<T, __half>::value ? 0x7C00u : 0x7F80u;
@@ -540,10 +547,9 @@ template <typename T> constexpr uint32_t kInfBits = std::is_same<T, __half>::val
 // 8-number units l, l + 32, ... of the block, row by row, so loads and stores of
 // neighbouring lanes are neighbours.  Keys and values of neighbouring heads are
 // neighbouring warps' work, as they are neighbours in a packed projection.  The largest
-// is found among the numbers' bits without their signs, two at a time; a block with an
-// infinity or a NaN in it looks again.
+// is found two at a time; a block with an infinity or a NaN in it looks again.
 template <typename T, int J>                     // J = dim / 16 units of a lane
-__global__ void __launch_bounds__(kWriteThreads, 3) k_pages_write(const __grid_constant__ WriteArgs A) {
+__global__ void __launch_bounds__(kWriteThreads, 2) k_pages_write(const __grid_constant__ WriteArgs A) {
   constexpr int U = 2 * J;                       // units of a row
   const int lane = threadIdx.x & 31;
   const unsigned item = blockIdx.x * (kWriteThreads / 32) + (threadIdx.x >> 5);
@@ -559,21 +565,25 @@ __global__ void __launch_bounds__(kWriteThreads, 3) k_pages_write(const __grid_c
   if (A.length) end = min(end, max(A.length[seq], 0));
   const T* x0 = static_cast<const T*>(values ? A.v : A.k) + head * (values ? A.v_head : A.k_head);
   const long long row = values ? A.v_row : A.k_row;
+  const unsigned row_bytes = (unsigned)row * 2u;
   unsigned char* pages = values ? A.v_pages : A.k_pages;
-  for (long long b = held / kPageBlock + b0; b * kPageBlock < end; b += A.blocks) {
-    const int place = (int)b * kPageBlock;
-    const int page = A.table[seq * A.s.table_row + (place >> A.s.shift)];
-    if ((unsigned)page >= (unsigned)A.s.n_pages) continue;
-    const int r0 = place & (A.s.page_rows - 1);
-    const int lo = max(held - place, 0), hi = min(end - place, kPageBlock);      // rows [0, lo) are old, [lo, hi) new
-    const T* src = x0 + (long long)(t0 + place - held) * row;                    // row 0's; not read before row lo
-    uint4 x[J];
+  // the numbers of block b's new rows, on their way
+  auto fetch = [&](long long b, uint4 (&x)[J]) {
+    const int place = (int)b * kPageBlock, lo = max(held - place, 0), hi = min(end - place, kPageBlock);
+    const char* src = reinterpret_cast<const char*>(x0 + (long long)(t0 + place - held) * row);   // row 0's
 #pragma unroll
     for (int j = 0; j < J; ++j) {
       const int i = j * 32 + lane, r = i / U, c = i % U;
       x[j] = make_uint4(0u, 0u, 0u, 0u);
-      if (r >= lo && r < hi) x[j] = __ldcs(reinterpret_cast<const uint4*>(src + r * row + c * 8));
+      if (r >= lo && r < hi)
+        x[j] = __ldcs(reinterpret_cast<const uint4*>(src + (unsigned long long)(unsigned)r * row_bytes + c * 16));
     }
+  };
+  auto page_at = [&](long long b) -> int { return A.table[seq * A.s.table_row + (b * kPageBlock >> A.s.shift)]; };
+  auto store = [&](long long b, int page, const uint4 (&x)[J]) {
+    if ((unsigned)page >= (unsigned)A.s.n_pages) return;
+    const int place = (int)b * kPageBlock, r0 = place & (A.s.page_rows - 1);
+    const int lo = max(held - place, 0), hi = min(end - place, kPageBlock);      // rows [0, lo) are old, [lo, hi) new
     unsigned char* block = pages + page * A.s.page_bytes + ((long long)head * A.s.page_rows + r0) * A.s.dim;
     signed char* scale = A.scales + page * A.s.scale_bytes +
                          ((long long)head * (A.s.page_rows / kPageBlock) + r0 / kPageBlock) * 2 + values;
@@ -583,9 +593,9 @@ __global__ void __launch_bounds__(kWriteThreads, 3) k_pages_write(const __grid_c
     for (int j = 0; j < J; ++j) {
       const uint32_t u[4] = {x[j].x, x[j].y, x[j].z, x[j].w};
 #pragma unroll
-      for (int h = 0; h < 4; ++h) most = max_u16x2(most, u[h] & 0x7FFF7FFFu);
+      for (int h = 0; h < 4; ++h) most = larger2<T>(most, u[h]);
     }
-    most = __reduce_max_sync(0xFFFFFFFFu, max(most & 0xFFFFu, most >> 16));
+    most = __reduce_max_sync(0xFFFFFFFFu, max(most & 0x7FFFu, most >> 16 & 0x7FFFu));
     const bool finite = most < kInfBits<T>;
     if (!finite) {
       most = 0;
@@ -650,6 +660,31 @@ __global__ void __launch_bounds__(kWriteThreads, 3) k_pages_write(const __grid_c
         *dst = make_uint2(y[0], y[1]);
       }
     }
+  };
+  uint4 x[J], y[J];
+  long long b = held / kPageBlock + b0;
+  int page = 0, page_y = 0;
+  if (b * kPageBlock < end) {
+    fetch(b, x);
+    page = page_at(b);
+  }
+  // two blocks a round, each one's numbers fetched while the other's are rounded
+  while (b * kPageBlock < end) {
+    const long long next = b + A.blocks;
+    const bool more = next * kPageBlock < end;
+    if (more) {
+      fetch(next, y);
+      page_y = page_at(next);
+    }
+    store(b, page, x);
+    b = next;
+    if (!more) break;
+    b = next + A.blocks;
+    if (b * kPageBlock < end) {
+      fetch(b, x);
+      page = page_at(b);
+    }
+    store(next, page_y, y);
   }
   }
 }
@@ -673,7 +708,6 @@ cudaError_t launch_write(const WriteArgs& a, long long grid, cudaStream_t st) {
 // ---------------------------------------------------------------------------
 
 bool misaligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
-bool bad_stride(int64_t s) { return s < 0 || s % 8 != 0 || s > (1LL << 40); }
 bool overlap(const void* a, long long na, const void* b, long long nb) {
   if (!a || !b || na <= 0 || nb <= 0) return false;
   const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
@@ -866,7 +900,9 @@ extern "C" rtcc_status rtcc_pages_write(const rtcc_page_config* cfg, const rtcc_
   WriteArgs a{};
   if (!page_shape(cfg, &a.s) || !t) return RTCC_E_ARG;
   if ((t->dtype != RTCC_FP16 && t->dtype != RTCC_BF16) || t->n_tokens < 0 || t->max_new < 0 || t->reserved) return RTCC_E_ARG;
-  if (bad_stride(t->k_row) || bad_stride(t->k_head) || bad_stride(t->v_row) || bad_stride(t->v_head)) return RTCC_E_ARG;
+  const int64_t strides[] = {t->k_row, t->k_head, t->v_row, t->v_head};
+  for (int64_t s : strides)
+    if (s < 0 || s % 8 || s >= (1LL << 31)) return RTCC_E_ARG;
   const long long cells = (long long)a.s.n_seqs * a.s.table_row;
   if (a.s.n_seqs > 0 && (!d_offsets || !d_held || (cells > 0 && !d_table))) return RTCC_E_ARG;
   if (t->n_tokens > 0 && (!d_k || !d_v)) return RTCC_E_ARG;
@@ -878,6 +914,8 @@ extern "C" rtcc_status rtcc_pages_write(const rtcc_page_config* cfg, const rtcc_
   for (const void* p : by4)
     if (misaligned(p, 4)) return RTCC_E_ARG;
   if (t->n_tokens == 0 || a.s.n_pages == 0 || cells == 0) return RTCC_OK;
+  const int sms = sm_count();
+  if (sms < 1) return RTCC_E_CUDA;
   a.k = d_k; a.v = d_v; a.offsets = d_offsets; a.held = d_held; a.length = d_length; a.table = d_table;
   a.k_pages = static_cast<unsigned char*>(d_k_pages); a.v_pages = static_cast<unsigned char*>(d_v_pages);
   a.scales = static_cast<signed char*>(d_scales);
@@ -887,6 +925,9 @@ extern "C" rtcc_status rtcc_pages_write(const rtcc_page_config* cfg, const rtcc_
   long long blocks = (most + 14LL) / kPageBlock + 1;       // that they touch at most, wherever they begin
   const long long each = a.s.kv_heads * 2LL;
   while (each * blocks > 0x3FFFFFFF) blocks = (blocks + 1) / 2;     // warps then loop
+  // so do they where there are more than three times as many as run at once
+  const long long rounds = each * blocks * a.s.n_seqs / (48LL * sms);
+  if (rounds > 1) blocks = (blocks + rounds - 1) / rounds;
   a.blocks = (int)blocks;
   const long long grid = (each * blocks + kWriteThreads / 32 - 1) / (kWriteThreads / 32);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
