@@ -429,6 +429,11 @@ __global__ void __launch_bounds__(kWarps * 32, 1)
   };
   auto view_group = [&](int rg) -> AttnView { return view_of(rg * tiles * qpt, tiles * qpt); };
   const AttnView view_seq = WIN && S.nq > 0 ? view_of(0, S.nq) : AttnView{0, 0};
+  // whether a tile whose reach is e and whose rows' widest view is v has step t
+  auto mine = [&](int t, int e, AttnView v) -> bool {
+    if (WIN && t * kKeys + kKeys <= v.low && t * kKeys >= v.seen) return false;
+    return t * kKeys < e;
+  };
   // whether the step has value rows to zero: rows that no token of the sequence sees
   auto patched = [&](const Walk<WIN>& k) -> bool {
     if (WIN && k.t * kKeys < view_seq.low && k.t * kKeys + kKeys > view_seq.seen) return true;
@@ -543,6 +548,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1)
     int g = 0;
     for (int rg = rg0; rg < groups && ok; rg += A.row_groups, ++item) {
       const int end = reach_all(rg), e = reach(rg, w);
+      const AttnView tile = view_of((rg * tiles + w) * qpt, qpt);
       Walk<WIN> qk(c0, end, c1, g, view_group(rg));
       qk.settle(A, S, slots, all);
       qk.seek(A, S, slots, all, streams, stream);
@@ -553,7 +559,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1)
         if (!qk.live()) return true;
         const int p = place(qk.g);
         if (!wait(C::FULL + p, phase(qk.g))) return false;
-        if (qk.t * kKeys < e) {
+        if (mine(qk.t, e, tile)) {
           tc_fence_after();
           const uint32_t s = chain * kS + (n_qk & (kS - 1));
           const uint64_t kd = dk + p * kStepUnits;
@@ -572,7 +578,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1)
       auto value = [&]() -> bool {
         const int p = place(pv.g);
         const bool zeroed = patched(pv);
-        if (pv.t * kKeys < e) {
+        if (mine(pv.t, e, tile)) {
           if (zeroed && !wait(C::VOK + p, (vok >> p) & 1)) return false;
           const uint32_t s = chain * kS + (n_pv & (kS - 1));
           if (!wait(C::PREADY + s, (n_pv / kS) & 1)) return false;
@@ -643,7 +649,11 @@ __global__ void __launch_bounds__(kWarps * 32, 1)
       Walk<WIN> k(c0, reach_all(rg), c1, g, view_group(rg));
       k.settle(A, S, slots, all);
       k.seek(A, S, slots, all, streams, stream);
-      while (k.live() && k.t * kKeys >= e) k.next_own(A, S, slots, all, streams, stream);   // other tiles' steps
+      const AttnView tile = view_of(i0, qpt);
+      auto skip = [&]() {                        // other tiles' steps
+        while (k.live() && !mine(k.t, e, tile)) k.next_own(A, S, slots, all, streams, stream);
+      };
+      skip();
       const uint32_t n0 = n;
       // Rows' maxima go up by `up`: O and the sum so far are scaled down, once the
       // product before is done with O.
@@ -686,6 +696,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1)
         if (lane == 0) mbar_arrive(&bar[C::PREADY + chain * kS + (n & (kS - 1))]);
         ++n;
         k.next_own(A, S, slots, all, streams, stream);
+        if (WIN) skip();                         // else they are all ahead of the first own one
       };
       while (k.live()) {
         const bool edge = k.partial || k.t * kKeys + kKeys > all_see ||
@@ -804,6 +815,43 @@ __global__ void __launch_bounds__(kWarps * 32, 1)
           if (!slow) continue;
         } else if (!(ok = begin())) {
           break;
+        } else if (WIN && !CAP && !DIST && begun) {
+          // an edge of windows, which are many: one pass with the maximum as it is, as above,
+          // without its order (the form below took 2 us longer a step)
+          const uint32_t ts = ts0 + (n & (kS - 1)) * kKeys;
+          const unsigned long long keep = key_mask<WIN>(A, S, slots, k.t * kKeys, hi, view);
+          const uint32_t bits[2] = {(uint32_t)keep, (uint32_t)(keep >> 32)};
+          float x[kKeys];
+          tmem_ld32_issue(ts, x);
+          tmem_ld32_issue(ts + 32, x + 32);
+          tmem_ld_wait();
+          reg_fence32(x);
+          reg_fence32(x + 32);
+          float t0 = -INFINITY, t1 = -INFINITY;
+          float2 s0 = both(0.f);
+          uint32_t pk[kKeys / 2];
+#pragma unroll
+          for (int i = 0; i < kKeys; i += 2) {
+            float2 z = fma2(make_float2(x[i], x[i + 1]), both(A.scale_log2), both(-m));
+            if (!(bits[i / 32] >> (i & 31) & 1)) z.x = -INFINITY;
+            if (!(bits[i / 32] >> ((i + 1) & 31) & 1)) z.y = -INFINITY;
+            t0 = fmaxf(t0, z.x);
+            t1 = fmaxf(t1, z.y);
+            z = make_float2(ex2(z.x), ex2(z.y));
+            s0 = add2(s0, z);
+            pk[i / 2] = Store<T>::pack2(z.x, z.y);
+          }
+          const float top = fmaxf(t0, t1);
+          if (!__any_sync(0xFFFFFFFFu, valid && top > kHard)) {
+            if (__any_sync(0xFFFFFFFFu, valid && top > kSlack<T>)) {
+              if (valid && top > kSlack<T>) late = fmaxf(late, top - kLift<T>);
+              lagging = true;
+            }
+            l += s0.x + s0.y;
+            tmem_st32(ts, pk);
+            publish();
+            continue;
+          }
         }
         const uint32_t ts = ts0 + (n & (kS - 1)) * kKeys;
         const float* py = spos + place(k.g) * 2 * kKeys;
