@@ -209,6 +209,14 @@ __device__ __forceinline__ int hidden_halves(const AttnArgs& A, const AttnSpan& 
   return A.hidden[S.kb / kKeys + t];
 }
 
+// A view in whole steps: steps [seen, low) have no key that its rows see.
+struct Steps {
+  int seen, low;
+  __device__ __forceinline__ Steps() {}
+  __device__ __forceinline__ explicit Steps(AttnView v) : seen((v.seen + kKeys - 1) / kKeys), low(v.low / kKeys) {}
+  __device__ __forceinline__ bool behind(int t) const { return t < low && t >= seen; }
+};
+
 // A walk over the steps of a chunk that have a key in a present slot, and their
 // number, from the last key a row group reaches to the chunk's first: with a
 // distance bias the nearest keys of a causal row come last, so going back the
@@ -221,21 +229,24 @@ template <bool WIN> struct Walk {
   int t, t0, c1;                                 // current step, the chunk's first
   int g;                                         // steps since the block began
   bool partial;
-  AttnView view;
+  Steps view;
   __device__ __forceinline__ Walk() {}
-  __device__ __forceinline__ Walk(int c0, int end_key, int c1_, int g_, AttnView view_)
+  __device__ __forceinline__ Walk(int c0, int end_key, int c1_, int g_, Steps view_)
       : t((end_key + kKeys - 1) / kKeys - 1), t0(c0 / kKeys), c1(c1_), g(g_), partial(false), view(view_) {
     if (end_key <= c0) t = t0 - 1;
   }
   __device__ __forceinline__ bool live() const { return t >= t0; }
   __device__ __forceinline__ void settle(const AttnArgs& A, const AttnSpan& S, unsigned long long slots, bool all) {
     partial = false;
-    if (all) return;
+    if (all) {
+      if (WIN && view.behind(t)) t = view.seen - 1;
+      return;
+    }
     for (; live(); --t) {
       bool some = false;
       if (WIN) {
-        if (t * kKeys + kKeys <= view.low && t * kKeys >= view.seen) {
-          t = (view.seen + kKeys - 1) / kKeys;   // one past the step to go on with
+        if (view.behind(t)) {
+          t = view.seen;                         // one past the step to go on with
           continue;
         }
         if (A.hidden) {
@@ -265,9 +276,13 @@ template <bool WIN> struct Walk {
   }
   __device__ __forceinline__ void next_own(const AttnArgs& A, const AttnSpan& S, unsigned long long slots, bool all,
                                            int streams, int stream) {
-    if (all) {                                   // nothing to skip
-      t -= streams;
-      g += streams;
+    if (all) {                                   // nothing to skip, or the one gap
+      if (!WIN) {
+        t -= streams;
+        g += streams;
+        return;
+      }
+      for (int i = 0; i < streams; ++i) next(A, S, slots, true);
       return;
     }
     next(A, S, slots, all);
@@ -379,11 +394,16 @@ __global__ void __launch_bounds__(kWarps * 32, 1)
     tmem_alloc(&tmem_base, 512);
     tmem_relinquish();
   }
-  __syncthreads();
+  // with pages: whether any of the chunk's keys is on none, as each step asks only then
+  bool off_page = false;
+  if (WIN && A.hidden)
+    for (int t = c0 / kKeys + tid; t * kKeys < c1; t += kWarps * 32) off_page |= hidden_halves(A, S, t) != 0;
+  if (WIN) off_page = __syncthreads_or(off_page);
+  else __syncthreads();
   tc_fence_after();
   const uint32_t tmem = tmem_base;
   const unsigned long long slots = attn_slot_mask(A, lane);
-  bool all = !WIN;                               // every slot of the chunk is present
+  bool all = !WIN || (!A.present && !off_page);  // every slot of the chunk is present, every key on a page
   if (!WIN && A.present && c1 > c0) {
     const int s0 = slot_of(A, S.kb + c0), s1 = slot_of(A, S.kb + c1 - 1);
     const unsigned long long want = ~0ull >> (63 - (s1 - s0));
@@ -427,13 +447,10 @@ __global__ void __launch_bounds__(kWarps * 32, 1)
     const AttnView a = attn_view(A, S, *first, min(i0, S.nq - 1)), b = attn_view(A, S, *first, min(i0 + n, S.nq) - 1);
     return {b.seen, a.low};
   };
-  auto view_group = [&](int rg) -> AttnView { return view_of(rg * tiles * qpt, tiles * qpt); };
+  auto view_group = [&](int rg) -> Steps { return Steps(view_of(rg * tiles * qpt, tiles * qpt)); };
   const AttnView view_seq = WIN && S.nq > 0 ? view_of(0, S.nq) : AttnView{0, 0};
   // whether a tile whose reach is e and whose rows' widest view is v has step t
-  auto mine = [&](int t, int e, AttnView v) -> bool {
-    if (WIN && t * kKeys + kKeys <= v.low && t * kKeys >= v.seen) return false;
-    return t * kKeys < e;
-  };
+  auto mine = [&](int t, int e, Steps v) -> bool { return t * kKeys < e && !(WIN && v.behind(t)); };
   // whether the step has value rows to zero: rows that no token of the sequence sees
   auto patched = [&](const Walk<WIN>& k) -> bool {
     if (WIN && k.t * kKeys < view_seq.low && k.t * kKeys + kKeys > view_seq.seen) return true;
@@ -548,7 +565,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1)
     int g = 0;
     for (int rg = rg0; rg < groups && ok; rg += A.row_groups, ++item) {
       const int end = reach_all(rg), e = reach(rg, w);
-      const AttnView tile = view_of((rg * tiles + w) * qpt, qpt);
+      const Steps tile(view_of((rg * tiles + w) * qpt, qpt));
       Walk<WIN> qk(c0, end, c1, g, view_group(rg));
       qk.settle(A, S, slots, all);
       qk.seek(A, S, slots, all, streams, stream);
@@ -571,7 +588,6 @@ __global__ void __launch_bounds__(kWarps * 32, 1)
           if (DIST && lane == 0) mbar_arrive(&bar[C::SFULL + s]);
           ++n_qk;
         }
-        qk.next_own(A, S, slots, all, streams, stream);
         return true;
       };
       // O += P V of the next step; keys and values are released when it is done
@@ -592,13 +608,20 @@ __global__ void __launch_bounds__(kWarps * 32, 1)
           mbar_arrive(&bar[C::FREE + p]);
         }
         if (zeroed) vok ^= 1u << p;
-        pv.next_own(A, S, slots, all, streams, stream);
         return true;
       };
       ok = wait(C::QFULL, item & 1);
 #pragma unroll
-      for (int i = 0; i < kS; ++i) ok = ok && score();
-      while (ok && pv.live()) ok = value() && score();
+      for (int i = 0; i < kS; ++i) {
+        ok = ok && score();
+        qk.next_own(A, S, slots, all, streams, stream);
+      }
+      // both walks go on while the softmax works, not between its end and the next products
+      while (ok && pv.live()) {
+        ok = value() && score();
+        pv.next_own(A, S, slots, all, streams, stream);
+        qk.next_own(A, S, slots, all, streams, stream);
+      }
       // the steps of the whole group, for the next group's places
       Walk<WIN> k(c0, end, c1, g, view_group(rg));
       if (rg + A.row_groups < groups)
@@ -649,7 +672,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1)
       Walk<WIN> k(c0, reach_all(rg), c1, g, view_group(rg));
       k.settle(A, S, slots, all);
       k.seek(A, S, slots, all, streams, stream);
-      const AttnView tile = view_of(i0, qpt);
+      const Steps tile(view_of(i0, qpt));
       auto skip = [&]() {                        // other tiles' steps
         while (k.live() && !mine(k.t, e, tile)) k.next_own(A, S, slots, all, streams, stream);
       };
@@ -703,7 +726,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1)
                           (WIN && k.t * kKeys < see_all.low && k.t * kKeys + kKeys > see_all.seen);
         if (begun && !edge && (!CAP || poly.limit > 0.f)) {
           // going back, no further step is at the edge unless a slot is absent
-          int run = all ? (k.t - k.t0) / streams + 1 : 1;
+          int run = all ? (k.t - (WIN && k.t * kKeys >= see_all.low ? max(k.t0, (see_all.low + kKeys - 1) / kKeys) : k.t0)) / streams + 1 : 1;
           bool slow = false;
           do {
             const uint32_t ts = ts0 + (n & (kS - 1)) * kKeys;
