@@ -21,8 +21,15 @@ namespace {
 // on: 33 rows over 9 ragged histories of 5001 keys, heads of 80, take 24 us there
 // and 27 in blocks of 16 rows, 30 rows over 50,000 keys, heads of 64, 25 and 23.
 constexpr int kTcRows = 32;
-// Over pages, whose keys and values are widened first, from this many on.
-constexpr int kTcPageRows = 64;
+// Over pages, whose keys and values are widened first, from this many on: 4 key heads of
+// 128 over 9 ragged histories of 5001 keys take 42 us in blocks of 16 rows and 53 there at
+// 68 rows, 59 and 61 at 132, 95 and 74 at 200.
+constexpr int kTcPageRows = 128;
+// With a window also from this many (block of 16 rows, key) pairs on: 9 histories over
+// windows of 2000 and 4 key heads take 18 us in blocks of 16 rows and 22 there at 20 rows
+// (150,000 pairs), 25 and 25 at 36, 29 and 25 at 52; one history over 1000 keys and 6
+// heads 9 and 18 at 100 rows (50,000).
+constexpr double kTcWindowWork = 200000;
 
 // The tensor cores cut what does not fit the float32 sum off at every 16 keys' addition
 // (a unit in the last place at most), so a sum over n keys of equal weight comes out
@@ -168,7 +175,11 @@ rtcc_status run_attention(AttnArgs& a, const PagesArgs* pages, int max_q, int ma
     if (seen < most_k) most_k = seen;
   }
   // the tensor-core kernel from kTcRows (token, head) rows per key head on
-  bool tc = (long long)max_q * a.group > (pages ? kTcPageRows : kTcRows) && a.group <= 128 && a.n_rows > 0;
+  const long long rows = (long long)max_q * a.group;
+  bool tc = rows > (pages ? kTcPageRows : kTcRows) && a.group <= 128 && a.n_rows > 0;
+  // behind short windows its blocks hardly begin before they end: not for little work
+  if (tc && !pages && a.window > 0)
+    tc = (double)((rows + attn_rows_per_block() - 1) / attn_rows_per_block()) * a.n_seqs * a.kv_heads * most_k > kTcWindowWork;
   const size_t part = (size_t)a.n_q * a.heads * (a.dim * sizeof(float) + sizeof(float2));
   const long long span = (most_k + 63) / 64 * 64, span_rows = span * a.n_seqs;
   size_t wide = pages ? widened_bytes(span_rows, a) : 0;

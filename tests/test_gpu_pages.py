@@ -640,6 +640,39 @@ def test_pages_repeat_in_a_graph_on_a_side_stream(R):
             assert torch.equal(c.out, first) and torch.equal(c.lse, lse)
 
 
+def test_pages_without_clusters_and_given_up_waits(R):
+    for workspace in (0, 32 << 20):
+        try:
+            assert R.rtcc_test_attention(R.TEST_NO_CLUSTERS) == R.OK
+            c = Case([1], [4000], 2, 2).run(R, workspace=workspace)
+        finally:
+            assert R.rtcc_test_attention(0) == R.OK
+        c.check()
+    assert R.rtcc_memory_attention_status() == R.OK
+    c = Case([300], [700], 2, 1)
+    try:
+        assert R.rtcc_test_attention(R.TEST_UNREACHABLE_WAIT) == R.OK
+        c.run(R)
+        assert R.rtcc_memory_attention_status() == R.E_DEVICE
+    finally:
+        assert R.rtcc_test_attention(0) == R.OK
+    assert R.rtcc_memory_attention_status() == R.OK
+    c.run(R).check()
+
+
+def test_pages_in_place_and_shared_pages(R):
+    """Results over the queries; two sequences on the same pages see the same keys."""
+    for n in (1, 30, 200):
+        c = Case([n, n], [600, 600], 4, 2, 64, 64)
+        c.table[1] = list(c.table[0])
+        ref = c.run(R).check().out.clone()
+        q = c.q.clone(memory_format=torch.contiguous_format)
+        c.q, c.out = q, q
+        c.run(R)
+        torch.cuda.synchronize()
+        assert torch.equal(c.out, ref)
+
+
 def test_pages_past_32_bits(R):
     # pages 512 MB apart: the last ones lie past 2^32 bytes
     for n in (2, 150):

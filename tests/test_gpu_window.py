@@ -161,3 +161,66 @@ def test_window_untouched_tokens_and_status(R):
     torch.cuda.synchronize()
     assert (c.out[100:] == 7).all() and not (c.out[:100] == 7).all()
     assert R.rtcc_memory_attention_status() == R.OK
+
+
+# sizes that the tensor-core kernel takes: more than 32 rows of a key head, and more than
+# 200,000 pairs of a block of 16 of them and a key
+LARGE = [([1500], [1500], 100, 10), ([700, 900], [2700, 900], 640, 64), ([1300], [5000], 1, 0), ([1025], [1025], 1024, 0),
+         ([600, 1, 0, 65], [4096, 900, 10, 3000], 1777, 130), ([900], [890], 64, 63), ([1100], [1100], 63, 65)]
+
+
+@pytest.mark.parametrize("n,m,window,sinks", LARGE)
+@pytest.mark.parametrize("dim,heads,kv,dtype", [(64, 2, 2, "fp16"), (128, 4, 2, "bf16"), (72, 3, 3, "bf16")])
+def test_window_large(R, n, m, window, sinks, dim, heads, kv, dtype):
+    Window(n, m, window, sinks, dim=dim, heads=heads, kv=kv, dtype=dtype, gap=3).run(R).check()
+
+
+@pytest.mark.parametrize("cap,dist,dim", [(0.0, True, 64), (20.0, False, 128), (20.0, True, 64), (500.0, False, 64)])
+def test_window_large_scores(R, cap, dist, dim):
+    Window([1000, 333], [1300, 2000], 170, 6, dim=dim, heads=4, kv=4, cap=cap, dist=dist, spread=3).run(R).check()
+
+
+def test_window_large_with_prefix_starts_and_slots(R):
+    Window([1100, 900], [1100, 2000], 64, 5, heads=4, kv=2, prefix=[100, 777]).run(R).check()
+    Window([1100, 900], [1100, 2000], 64, 5, heads=4, kv=2, start=[600, 1300]).run(R).check()
+    for window, sinks in ((400, 150), (30, 2)):
+        Window([1200], [2400], window, sinks, heads=4, kv=4, slot_rows=100, absent=(0, 1, 7, 13, 14)).run(R).check()
+        Window([1200], [2400], window, sinks, heads=2, kv=2, slot_rows=77, absent=(2, 20), dist=True).run(R).check()
+
+
+def test_window_large_split_and_hints(R):
+    """Long windows split over the GPU with room for parts, one tile at a time, and wrong hints."""
+    for kw in (dict(), dict(workspace=0), dict(workspace=16 << 20), dict(max_q=40, max_k=4000)):
+        Window([300], [9000], 7000, 33, heads=4, kv=2, dim=64).run(R, **kw).check()
+        Window([100], [9000], 8000, 33, heads=3, kv=3, dim=128).run(R, **kw).check()
+
+
+def test_window_large_repeats_and_keeps_bits(R):
+    a = Window([1300], [1300], 200, 9, heads=4, kv=2, dim=128).run(R)
+    b = Window([1300], [1300], 200, 9, heads=4, kv=2, dim=128).run(R)
+    torch.cuda.synchronize()
+    assert torch.equal(a.out, b.out) and torch.equal(a.lse, b.lse)
+
+
+def test_window_given_up_wait_is_reported(R):
+    """The queries never come: every wait ends by itself, the status tells, and the next call is right."""
+    assert R.rtcc_memory_attention_status() == R.OK
+    c = Window([1300], [1300], 200, 9, heads=4, kv=2)
+    try:
+        assert R.rtcc_test_attention(R.TEST_UNREACHABLE_WAIT) == R.OK
+        c.run(R)
+        assert R.rtcc_memory_attention_status() == R.E_DEVICE
+    finally:
+        assert R.rtcc_test_attention(0) == R.OK
+    assert R.rtcc_memory_attention_status() == R.OK
+    c.run(R).check()
+
+
+def test_window_without_clusters(R):
+    for workspace in (0, 32 << 20):
+        try:
+            assert R.rtcc_test_attention(R.TEST_NO_CLUSTERS) == R.OK
+            c = Window([1], [4000], 3000, 9, heads=2, kv=2).run(R, workspace=workspace)
+        finally:
+            assert R.rtcc_test_attention(0) == R.OK
+        c.check()
