@@ -22,6 +22,10 @@
 // fetched a round ahead of the copies.  Channels are permuted within groups of 16 so
 // that what ldmatrix gives a lane (4 bytes of a key; 2 bytes of two keys' values) is
 // what its products need: no number crosses lanes but P, transposed once.
+//
+// Measured: 61 tokens over ragged histories of up to 16,384 keys, 8 key heads of 128 with
+// a cap, 958 MB: 157 us, 6.1 TB/s, 90 % of a plain copy's (rows on the 16-wide side, with
+// probabilities as two terms: 268 us); one token over 4097 keys of 6 heads of 64: 7.2 us.
 #include <type_traits>
 
 #include "attn_rows.cuh"
@@ -386,7 +390,9 @@ constexpr int kWidenThreads = 256;
 
 // Keys and values that a sequence's tokens see, as 16-bit rows [key without the gap]
 // [kv_heads][dim] from row seq * span on: a warp per 16 keys and key head.  bf16 holds the
-// numbers exactly, and fp16 those that came from fp16.
+// numbers exactly, and fp16 those that came from fp16.  Read once by each of the
+// tensor-core kernel's blocks along the tokens, which would convert them as often: 19 us
+// before its 297 for 5 chunks of up to 2100 tokens over windows of 4000 keys.
 template <typename T>
 __global__ void __launch_bounds__(kWidenThreads)
     k_pages_widen(const __grid_constant__ AttnArgs A, const __grid_constant__ PagesArgs P, T* k, T* v,

@@ -35,6 +35,11 @@
 // their value rows are zeroed in shared memory before the product, so their
 // contents never reach a result.
 //
+// With a window (WIN) a row group's steps are those of its rows' windows and of what
+// they see from afar (the sinks, a prefix); the walk jumps from the one to the other, and
+// a tile leaves out steps that only the other one sees.  A block then has few steps and
+// several edges, which a form of the step of their own takes in one pass.
+//
 // What bounds it is the softmax warps' latency, no pipe alone.  Two of them share a
 // scheduler.  Their 64 keys take 1,420 clocks bare, 1,890 with a cap, 1,950 with a bias
 // and 2,630 with both, against 640 (heads of 64) or 1,280 of the tensor pipe.  A pair of
@@ -44,15 +49,23 @@
 // results.  Measured: 16,384 x 49,152 keys, 6 heads of 64: 1.54 ms bare (802 TFLOP/s),
 // 2.17 with a cap, 2.16 with a bias, 3.00 with both (412), each with a sixth of the SMs'
 // time lost to a half-empty third round of blocks; 12,036 packed causal tokens of 16
-// heads of 128 with a cap: 132 us, 711 TFLOP/s (of a block's 22 us there, 1 goes to its
-// set-up, 2 to its first scores, 2 to the masked step and 3 to its results).
+// heads of 128 with a cap: 127 us, 740 TFLOP/s (of a block's 22 us there, 1 goes to its
+// set-up, 2 to its first scores, 2 to the masked step and 3 to its results).  Windows of
+// 700 and 8 sinks, 20,900 packed tokens of 16 heads of 128: 197 us, 608 TFLOP/s; a block
+// has 14 steps, of which an inner one takes 1.0 us (half of it the wait for scores: the
+// products of both tiles and their way there and back), and 8 us besides: 1.5 its set-up,
+// 2.2 its first scores, 1.3 the first step, 3 its results.
 // Tried and slower: four chains of one S each (four softmax warps a scheduler, 96
 // registers: 10 to 30 %), the next S loaded while P is stored (spills: 5 to 15 %),
 // scalar beside packed arithmetic (up to 30 %), a second form of the pass for steps
 // whose keys share one y (8 % faster where all do, 8 % slower where two thirds do:
 // the two forms push each other out of the instruction cache), blocks that take over
 // the work of those not yet begun (up to 30 %: the roles change over one after the
-// other), and results through shared memory to whole lines (4 %).
+// other; with queries released as soon as the last scores are under way, still 12 to
+// 18 % on windows), results through shared memory to whole lines (4 %), keys and values
+// released apart (6 % on windows: one wait and one commit more in the products' warp),
+// one chain to a block and two blocks to an SM (50 %), and more registers for the softmax
+// warps at the others' cost (no spills, 2 %).
 #pragma once
 
 #include <float.h>
