@@ -96,7 +96,6 @@ __global__ void __launch_bounds__(kWarps * 32, NR == 1 ? 3 : 2)
   const uint32_t ring = smem_u32(smem) + w * kStages * C::kStageBytes;
   const uint32_t notes = smem_u32(smem) + C::kRing + w * kStages * 8;
   uint32_t* notes_g = reinterpret_cast<uint32_t*>(smem + C::kRing + w * kStages * 8);
-  const bool far_cap = A.cap_log2 > kAbsCap * kLog2e;
   const int* table = P.table + (long long)seq * P.s.table_row;
   const long long head_at = (long long)kvh * P.s.page_rows * A.dim;
   const long long scale_at = (long long)kvh * (P.s.page_rows / kPageBlock) * 2;
@@ -264,7 +263,7 @@ __global__ void __launch_bounds__(kWarps * 32, NR == 1 ? 3 : 2)
             for (int h = 0; h < 2; ++h) {
               float& y = s[i >> 1][n][2 * h + (i & 1)];
               float x = y * f;
-              if (A.cap_log2 > 0.f) x = A.cap_log2 * (far_cap ? tanh_rel(x) : tanh_abs(x));
+              if (A.cap_log2 > 0.f) x = A.cap_log2 * tanh_rel(x);      // few keys' lse is a score: to 2^-20 of itself
               if (edge) {
                 const int key = n * 16 + h * 8 + lane / 4, j = j0 + key;
                 if (!((bits >> key) & 1) || j >= hi[i] || (j >= view[i].seen && j < view[i].low)) x = -INFINITY;

@@ -84,7 +84,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) k_attn_rows(const __grid_const
   const unsigned long long slots = attn_slot_mask(A, lane);
   const uint32_t ring = smem_u32(smem) + w * kStages * C::kStageBytes;
   const unsigned char* ring_g = smem + w * kStages * C::kStageBytes;
-  const bool dist = A.slopes != nullptr, far_cap = A.cap_log2 > kAbsCap * kLog2e;
+  const bool dist = A.slopes != nullptr, far_cap = WIN || A.cap_log2 > kAbsCap * kLog2e;   // windows: few keys, whose lse is a score
   const T* kbase = static_cast<const T*>(A.k) + (long long)kvh * A.k_head;
   const T* vbase = static_cast<const T*>(A.v) + (long long)kvh * A.v_head;
 
