@@ -5,11 +5,12 @@
 // exponent for every 16 places of a page and key head.  e4m3 numbers are fp16 numbers, so
 // both products run on them exactly (mma.m16n8k16 fp16, float32 sums), for queries of
 // either type, and the exponents go where they cost least: e_k into the factor of the
-// scores, e_v into the probabilities, relative to the largest e_v that the warp has met
-// (E; its accumulators are in units of 2^E).  bf16 queries are scaled by a power of two
-// per row so that the largest is below 2^15; what is more than 2^39 below it is lost.
-// Probabilities are rounded to fp16's 11 bits, seven more than the values have; the
-// largest is 2^15, so that 2^-40 of it still counts.
+// scores x (in log2), e_v into the values' weights 2^(x + e_v).  These have a running
+// maximum of their own beside the scores': large values that hardly count, as of a key
+// with a low score, do not press the others' weights out of fp16's range.  bf16 queries
+// are scaled by a power of two per row so that the largest is below 2^15; what is more
+// than 2^39 below it is lost.  Weights are rounded to fp16's 11 bits, seven more than the
+// values have; the largest is 2^15, so that 2^-40 of it still counts.
 //
 // Keys and channels are the products' 16-wide side, query rows the 8-wide one,
 //   S^T = K Q^T,   O^T = V^T P^T,
@@ -61,9 +62,6 @@ __device__ __forceinline__ uint32_t tile8_off(int r, int c) {
   if (DP == 128) return (uint32_t)(r * 128 + ((c ^ (r & 7)) * 16));
   return (uint32_t)((r >> 1) * 128 + ((((r & 1) * 4 + c) ^ ((r >> 1) & 3)) * 16));
 }
-
-// 2^e, 0 below the float range.
-__device__ __forceinline__ float pow2_or_0(int e) { return e < -126 ? 0.f : pow2(e); }
 
 // Transposes an 8 x 8 matrix of 16-bit numbers, two of a row per lane.
 __device__ __forceinline__ uint32_t transpose8(uint32_t x) {
@@ -169,10 +167,10 @@ __global__ void __launch_bounds__(kWarps * 32, NR == 1 ? 3 : 2)
     for (int i = 0; i < NR; ++i)
 #pragma unroll
       for (int u = 0; u < DP / 16; ++u) o[i][u][0] = o[i][u][1] = o[i][u][2] = o[i][u][3] = 0.f;
-    float m[N], l[N];
+    float m[N], l[N];                            // of the scores
+    float mo[N];                                 // o is in units of 2^mo
 #pragma unroll
-    for (int i = 0; i < N; ++i) m[i] = -INFINITY, l[i] = 0.f;
-    int unit = kExpMin;                          // o is in units of 2^unit
+    for (int i = 0; i < N; ++i) m[i] = mo[i] = -INFINITY, l[i] = 0.f;
 
     const int n_tiles = end > c0 ? (end - c0 + KT - 1) / KT : 0;
     auto page_of = [&](int t) -> int {           // of tile t, -1: none
@@ -249,16 +247,19 @@ __global__ void __launch_bounds__(kWarps * 32, NR == 1 ? 3 : 2)
           }
         const int j0 = c0 + t * KT;
         const bool edge = bits != 0xFFFFFFFFu || j0 + KT > least || (j0 < last.low && j0 + KT > first.seen);
-        float top[N];
+        float top[N], heavy[N];                  // largest score, largest weight (log2)
 #pragma unroll
-        for (int i = 0; i < N; ++i) top[i] = -INFINITY;
+        for (int i = 0; i < N; ++i) top[i] = heavy[i] = -INFINITY;
+        float ve[KT / 16];
 #pragma unroll
         for (int n = 0; n < KT / 16; ++n) {
           const float ke = pow2(max((int)(signed char)(exps >> (n * 16)), kExpMin));
+          ve[n] = (float)(signed char)(exps >> (n * 16 + 8));
 #pragma unroll
           for (int i = 0; i < N; ++i) {
             // finite: a score of 0 stays 0 whatever the factor
             const float f = fminf(fmaxf(qs[i] * ke, -3e38f), 3e38f);
+            float t = -INFINITY;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
               float& y = s[i >> 1][n][2 * h + (i & 1)];
@@ -269,60 +270,57 @@ __global__ void __launch_bounds__(kWarps * 32, NR == 1 ? 3 : 2)
                 if (!((bits >> key) & 1) || j >= hi[i] || (j >= view[i].seen && j < view[i].low)) x = -INFINITY;
               }
               y = x;
-              top[i] = fmaxf(top[i], x);
+              t = fmaxf(t, x);
             }
+            top[i] = fmaxf(top[i], t);
+            heavy[i] = fmaxf(heavy[i], t + ve[n]);
           }
         }
-        constexpr float kLift = 15.0f;           // log2 of the largest probability, for fp16's range
+        constexpr float kLift = 15.0f;           // log2 of the largest weight, for fp16's range
         bool moved = false;
         float f[N];
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-          top[i] = fmaxf(top[i], __shfl_xor_sync(0xFFFFFFFFu, top[i], 4));
-          top[i] = fmaxf(top[i], __shfl_xor_sync(0xFFFFFFFFu, top[i], 8));
-          top[i] = fmaxf(top[i], __shfl_xor_sync(0xFFFFFFFFu, top[i], 16));
-          const float mn = fmaxf(m[i], top[i] - kLift);
-          const float base = mn == -INFINITY ? 0.f : mn;
-          f[i] = exp2f(m[i] - base);             // m = -inf: 0
+#pragma unroll
+          for (int d = 4; d < 32; d <<= 1) {
+            top[i] = fmaxf(top[i], __shfl_xor_sync(0xFFFFFFFFu, top[i], d));
+            heavy[i] = fmaxf(heavy[i], __shfl_xor_sync(0xFFFFFFFFu, heavy[i], d));
+          }
+          const float mn = fmaxf(m[i], top[i]), on = fmaxf(mo[i], heavy[i] - kLift);
+          top[i] = mn == -INFINITY ? 0.f : mn;
+          heavy[i] = on == -INFINITY ? 0.f : on;
+          l[i] *= exp2f(m[i] - top[i]);          // m = -inf: 0
+          f[i] = ex2(mo[i] - heavy[i]);
           moved = moved || f[i] != 1.0f;
           m[i] = mn;
-          l[i] *= f[i];
-          top[i] = base;
+          mo[i] = on;
         }
-        // values' exponents; a block that nobody sees has none
-        int ve[2];
-#pragma unroll
-        for (int kk = 0; kk < 2; ++kk)
-          ve[kk] = (bits >> (kk * 16)) & 0xFFFFu ? max((int)(signed char)(exps >> (kk * 16 + 8)), kExpMin) : kExpMin;
-        const int up = max(ve[0], ve[1]);
-        if (__any_sync(0xFFFFFFFFu, moved) || up > unit) {
-          const float g = pow2_or_0(min(unit - up, 0));
-          unit = max(unit, up);
+        if (__any_sync(0xFFFFFFFFu, moved)) {
 #pragma unroll
           for (int i = 0; i < NR; ++i)
 #pragma unroll
             for (int u = 0; u < DP / 16; ++u) {
-              o[i][u][0] *= f[2 * i] * g;
-              o[i][u][1] *= f[2 * i + 1] * g;
-              o[i][u][2] *= f[2 * i] * g;
-              o[i][u][3] *= f[2 * i + 1] * g;
+              o[i][u][0] *= f[2 * i];
+              o[i][u][1] *= f[2 * i + 1];
+              o[i][u][2] *= f[2 * i];
+              o[i][u][3] *= f[2 * i + 1];
             }
         }
-        uint32_t pb[NR][KT / 16][2];             // B fragments of P^T
+        uint32_t pb[NR][KT / 16][2];             // B fragments of the weights, transposed
         float sum[N];                            // a tile's sum first, as in attn_rows.cu
 #pragma unroll
         for (int i = 0; i < N; ++i) sum[i] = 0.f;
 #pragma unroll
         for (int n = 0; n < KT / 16; ++n) {
-          const float g = pow2_or_0(ve[n] - unit);
 #pragma unroll
           for (int i = 0; i < NR; ++i) {
+            const float w0 = ve[n] - heavy[2 * i], w1 = ve[n] - heavy[2 * i + 1];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-              const float p0 = exp2f(s[i][n][2 * h] - top[2 * i]), p1 = exp2f(s[i][n][2 * h + 1] - top[2 * i + 1]);
-              sum[2 * i] += p0;
-              sum[2 * i + 1] += p1;
-              pb[i][n][h] = transpose8(Store<__half>::pack2(p0 * g, p1 * g));
+              const float x0 = s[i][n][2 * h], x1 = s[i][n][2 * h + 1];
+              sum[2 * i] += exp2f(x0 - top[2 * i]);
+              sum[2 * i + 1] += exp2f(x1 - top[2 * i + 1]);
+              pb[i][n][h] = transpose8(Store<__half>::pack2(ex2(x0 + w0), ex2(x1 + w1)));
             }
           }
         }
@@ -354,24 +352,23 @@ __global__ void __launch_bounds__(kWarps * 32, NR == 1 ? 3 : 2)
       l[i] += __shfl_xor_sync(0xFFFFFFFFu, l[i], 8);
       l[i] += __shfl_xor_sync(0xFFFFFFFFu, l[i], 16);
     }
-    // the states leave with probabilities of at most 1 and without units
+    // the states leave in units of the scores' maximum
     __syncthreads();
-    float* mo = reinterpret_cast<float*>(smem);
-    constexpr float kDrop = 1.0f / 32768.0f;
-    const float back = pow2(unit);
+    float* state = reinterpret_cast<float*>(smem);
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      float* dst = mo + (w * kRows + (i >> 1) * 8 + (lane & 3) * 2 + (i & 1)) * (DP + 4);
+      const float back = mo[i] == -INFINITY ? 0.f : exp2f(mo[i] - m[i]);
+      float* dst = state + (w * kRows + (i >> 1) * 8 + (lane & 3) * 2 + (i & 1)) * (DP + 4);
 #pragma unroll
       for (int u = 0; u < DP / 16; ++u)
         *reinterpret_cast<float2*>(dst + u * 16 + (lane / 4) * 2) =
-            make_float2(o[i >> 1][u][i & 1] * kDrop * back, o[i >> 1][u][2 + (i & 1)] * kDrop * back);
+            make_float2(o[i >> 1][u][i & 1] * back, o[i >> 1][u][2 + (i & 1)] * back);
       if (lane / 4 == 0) {
-        dst[DP] = m[i] + 15.0f;
-        dst[DP + 1] = l[i] * kDrop;
+        dst[DP] = m[i];
+        dst[DP + 1] = l[i];
       }
     }
-    merge_states<T, DP, CLUSTER>(A, S, mo, r0, rows_all, kvh, chunk);
+    merge_states<T, DP, CLUSTER>(A, S, state, r0, rows_all, kvh, chunk);
     __syncthreads();
   }
 }

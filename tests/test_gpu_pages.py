@@ -597,6 +597,20 @@ def test_pages_exponents_far_apart(R):
         c.run(R).check()
 
 
+def test_pages_large_values_that_hardly_count(R):
+    """A block of values up to 2^60 whose keys have scores 96 below the others': its share is
+    2^-70 of the result, and the others keep their digits."""
+    for n in (1, 40, 200):
+        c = Case([n], [400], 2, 1, 64, 64, "bf16", causal=False)
+        c.q = torch.full_like(c.q, 4.0)
+        page, row = c.table[0][2], 16
+        c.k.view(c.pages, 1, 64, 64)[page, 0, row:row + 16] = torch.tensor(-3.0).to(torch.float8_e4m3fn).view(torch.uint8).item()
+        s = c.s.view(c.pages, 1, 4, 2)
+        s[page, 0, row // 16, 0], s[page, 0, row // 16, 1] = 0, 52
+        s[..., 0].sub_((s[..., 0] != 0).to(torch.int8))        # the others' keys are small
+        c.run(R).check()
+
+
 def test_pages_wide_queries(R):
     """bf16 queries far outside fp16's range, scores of ordinary size."""
     for n in (1, 40):
