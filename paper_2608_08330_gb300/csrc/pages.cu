@@ -931,9 +931,13 @@ extern "C" rtcc_status rtcc_pages_write(const rtcc_page_config* cfg, const rtcc_
   long long blocks = (most + 14LL) / kPageBlock + 1;       // that they touch at most, wherever they begin
   const long long each = a.s.kv_heads * 2LL;
   while (each * blocks > 0x3FFFFFFF) blocks = (blocks + 1) / 2;     // warps then loop
-  // so do they where there are more than three times as many as run at once
-  const long long rounds = each * blocks * a.s.n_seqs / (48LL * sms);
+  // so do they where there are more than three times as many as run at once, and no more
+  // than eight to a block that there is: one long sequence among many short ones
+  const long long most_blocks = t->n_tokens / kPageBlock + 2LL * a.s.n_seqs;
+  const long long live = blocks * a.s.n_seqs < most_blocks ? blocks * a.s.n_seqs : most_blocks;
+  const long long rounds = each * live / (48LL * sms);
   if (rounds > 1) blocks = (blocks + rounds - 1) / rounds;
+  if (blocks > 8 * most_blocks / a.s.n_seqs) blocks = 8 * most_blocks / a.s.n_seqs;
   a.blocks = (int)blocks;
   const long long grid = (each * blocks + kWriteThreads / 32 - 1) / (kWriteThreads / 32);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
