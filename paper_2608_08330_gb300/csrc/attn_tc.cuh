@@ -52,8 +52,8 @@
 // heads of 128 with a cap: 127 us, 740 TFLOP/s (of a block's 22 us there, 1 goes to its
 // set-up, 2 to its first scores, 2 to the masked step and 3 to its results).  Windows of
 // 700 and 8 sinks, 20,900 packed tokens of 16 heads of 128: 197 us, 608 TFLOP/s; a block
-// has 14 steps, of which an inner one takes 1.0 us (half of it the wait for scores: the
-// products of both tiles and their way there and back), and 8 us besides: 1.5 its set-up,
+// has 14 steps, of which an inner one takes 1.0 us (0.67 are both tiles' products: Q is
+// read from shared memory anew for every 64 keys), and 8 us besides: 1.5 its set-up,
 // 2.2 its first scores, 1.3 the first step, 3 its results.
 // Tried and slower: four chains of one S each (four softmax warps a scheduler, 96
 // registers: 10 to 30 %), the next S loaded while P is stored (spills: 5 to 15 %),
@@ -64,8 +64,10 @@
 // other; with queries released as soon as the last scores are under way, still 12 to
 // 18 % on windows), results through shared memory to whole lines (4 %), keys and values
 // released apart (6 % on windows: one wait and one commit more in the products' warp),
-// one chain to a block and two blocks to an SM (50 %), and more registers for the softmax
-// warps at the others' cost (no spills, 2 %).
+// one chain to a block and two blocks to an SM (50 %), more registers for the softmax
+// warps at the others' cost (no spills, 2 %), and S released as soon as it is in
+// registers, with a place of its own for P (the same time with heads of 128, 15 % more
+// with 64).
 #pragma once
 
 #include <float.h>
