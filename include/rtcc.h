@@ -794,10 +794,12 @@ typedef struct {
  * visible to the token at place p where
  *   not causal, or j <= p and (no window, or j > p - window or j < sinks),
  *   or j < d_prefix[s] (NULL = 0),
- * and its page is one.  out and lse as there; pages that no token sees may hold
- * anything.  Products are exact in the 8-bit numbers; queries of bf16 are scaled by a
- * power of two per row and lose what is below 2^-39 of the row's largest where a key
- * head has few query rows.
+ * and its page is one.  out and lse as there; places that no token sees may hold
+ * anything.  With few query rows to a key head products are exact in the 8-bit numbers;
+ * queries of bf16 are scaled by a power of two per row and lose what is below 2^-39 of
+ * the row's largest, and a value's weight (its probability times its power of two) is
+ * rounded to 11 bits, down to 2^-40 of the row's largest weight.  With many rows
+ * probabilities are rounded as there.
  * Many rows (tokens times heads to a key head) want room in the workspace: besides the
  * parts of rtcc_memory_attention the keys and values that tokens see are widened to
  * 16 bits once, n_seqs * S * kv_heads * head_dim * 4 bytes and n_seqs * S / 64 + 256 more

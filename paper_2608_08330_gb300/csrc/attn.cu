@@ -113,8 +113,10 @@ long long rows_cluster(long long units, long long steps, long long split, long l
 // about 1.2 us).  With 384 units of 768 steps, one chunk leaves the third round half
 // empty and five would fill 13 rounds, if the workspace has room for them: at 16,384
 // tokens of 6 heads of 64 a part takes 26 MB.
+// Over pages and behind windows, whose steps are shorter, the merge's own time counts too:
+// a few steps, and one for 5,000 rows.
 long long tc_chunks(long long units, long long steps, long long least_chunks, long long most, int sms, int streams,
-                    long long n_q, int heads, int dim) {
+                    long long n_q, int heads, int dim, bool merge_counts) {
   const long long first = std::max(1LL, std::min(least_chunks, most));
   long long best = first;
   double least = 0;
@@ -122,12 +124,28 @@ long long tc_chunks(long long units, long long steps, long long least_chunks, lo
     const double rounds = (double)((units * c + sms - 1) / sms);
     double cost = rounds * ((double)((steps + c - 1) / c) + 4);
     if (c * streams > 1) cost += 2 + 8e-6 * (double)(c * streams * n_q * heads) * dim / (6.8 * 1.2);
+    if (c * streams > 1 && merge_counts) cost += 4 + (double)(n_q * heads) / 5000;
     if (c == first || cost < least) {
       least = cost;
       best = c;
     }
   }
   return best;
+}
+
+// Whether the two chains of a block share a tile (see attn_tc.cuh), where the number of tiles
+// is odd: half the steps to a block, but as many blocks as tiles, and a merge.  In steps'
+// time (1 us): a block has 8 besides its steps, a merge 6 and the partial results' traffic.
+// 3 sequences of up to 926 tokens and as many keys, 12 query and 4 key heads of 128 on pages
+// (23 tiles) take 70 us with shared tiles and 44 without.
+int tc_streams(const AttnArgs& a, int max_q, long long most_k, int sms) {
+  const long long tokens = 128 / a.group, tiles = (max_q + tokens - 1) / tokens;
+  long long keys = most_k;
+  if (a.window > 0) keys = std::min(keys, (long long)a.window + a.sinks + 2 * tokens + 128);
+  const double steps = (double)(keys + 63) / 64, units = (double)a.n_seqs * a.kv_heads;
+  const double one = ceil(units * ((tiles + 1) / 2) / sms) * (steps + 8);
+  const double two = ceil(units * tiles / sms) * (steps / 2 + 8) + 6 + 16.0 * a.n_q * a.heads * a.dim / 6.8e6;
+  return two < one ? 2 : 1;
 }
 
 std::atomic<int> g_test{0};                      // bits of rtcc_test_attention
@@ -202,6 +220,7 @@ rtcc_status run_attention(AttnArgs& a, const PagesArgs* pages, int max_q, int ma
     }
     const long long room = (long long)(left / part);
     w.streams = tc ? attn_tc_streams(w.group, max_q) : 1;
+    if (w.streams > 1 && (pages || a.window > 0)) w.streams = tc_streams(a, max_q, most_k, sms);
     if (w.streams > room) w.streams = 1;
     w.unit = tc ? attn_tc_unit(w.streams) : pages ? attn_pages_unit() : attn_rows_unit(w.dim);
     const long long step = tc ? attn_tc_tokens_per_block(w.group, w.streams) : 1;
@@ -220,7 +239,8 @@ rtcc_status run_attention(AttnArgs& a, const PagesArgs* pages, int max_q, int ma
     if (most > 0x7FFFFFFF / units) most = 0x7FFFFFFF / units;
     const long long sums = tc ? w.streams : 4;     // of a block
     const long long least = (most_k + sums * kSumKeys - 1) / (sums * kSumKeys);
-    long long chunks = tc ? tc_chunks(units, steps, least, most, sms, w.streams, w.n_q, w.heads, w.dim)
+    long long chunks = tc ? tc_chunks(units, steps, least, most, sms, w.streams, w.n_q, w.heads, w.dim,
+                                      pages || w.window > 0)
                           : rows_chunks(units, w.n_seqs > 1, most_k < max_k, steps, least, most, sms,
                                         pages && (long long)max_q * w.group <= 8 ? 3 : 2, pages ? 8.0 : 10.0);
     if (tc && most_k / (chunks * sums) > kLongSum) continue;

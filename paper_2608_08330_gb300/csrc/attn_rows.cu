@@ -301,7 +301,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) k_attn_rows(const __grid_const
 // would read one after another: 5 rows of 600 took 120 us), 4 channels per lane.
 // Every warp sums its share in index order, then the shares are summed in order.
 constexpr int kJoinWarps = 4;
-template <typename T, int W>
+template <typename T, int W, int U>              // U: loads in flight
 __global__ void __launch_bounds__(kJoinWarps * 32) k_attn_join(const __grid_constant__ AttnArgs A, int blocks_per_seq) {
   __shared__ float4 sum_o[kJoinWarps][32];
   __shared__ float2 sum_ml[kJoinWarps];
@@ -325,7 +325,6 @@ __global__ void __launch_bounds__(kJoinWarps * 32) k_attn_join(const __grid_cons
     float ll = 0.f;
     const int c4 = lane * 4;
     const bool on = c4 < A.dim;
-    constexpr int U = 8;                         // loads in flight
     for (int c0 = first; c0 < used; c0 += U * W) {
       float2 ml[U];
       float4 x[U];
@@ -417,13 +416,21 @@ cudaError_t launch_attn_join(const AttnArgs& a, int max_q, bool bf16, cudaStream
   long long per = ((long long)max_q * a.heads + at_once - 1) / at_once;
   if (per < 1) per = 1;
   if (per > 4096) per = 4096;
+  // no more blocks than are resident, each with several rows: 2,700 tokens of 12 heads, two
+  // parts each, take 25 us in blocks of 4 rows
+  const long long fit = 16LL * sm_count() / a.n_seqs;
+  if (!wide && per > fit) per = fit < 1 ? 1 : fit;
   while ((long long)a.n_seqs * per > 0x7FFFFFFF && per > 1) per /= 2;
   const dim3 grid((unsigned)((long long)a.n_seqs * per)), block(kJoinWarps * 32);
-  if (wide)
-    return bf16 ? launch_pdl(k_attn_join<__nv_bfloat16, kJoinWarps>, grid, block, 0, st, a, (int)per)
-                : launch_pdl(k_attn_join<__half, kJoinWarps>, grid, block, 0, st, a, (int)per);
-  return bf16 ? launch_pdl(k_attn_join<__nv_bfloat16, 1>, grid, block, 0, st, a, (int)per)
-              : launch_pdl(k_attn_join<__half, 1>, grid, block, 0, st, a, (int)per);
+  const int parts = a.n_chunks * a.streams;
+  if (bf16) {
+    const auto kern = wide ? k_attn_join<__nv_bfloat16, kJoinWarps, 8>
+                      : parts > 2 ? k_attn_join<__nv_bfloat16, 1, 8> : k_attn_join<__nv_bfloat16, 1, 2>;
+    return launch_pdl(kern, grid, block, 0, st, a, (int)per);
+  }
+  const auto kern = wide ? k_attn_join<__half, kJoinWarps, 8>
+                    : parts > 2 ? k_attn_join<__half, 1, 8> : k_attn_join<__half, 1, 2>;
+  return launch_pdl(kern, grid, block, 0, st, a, (int)per);
 }
 
 }  // namespace rtcc
