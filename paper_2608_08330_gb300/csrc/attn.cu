@@ -30,6 +30,10 @@ constexpr int kTcPageRows = 128;
 // (150,000 pairs), 25 and 25 at 36, 29 and 25 at 52; one history over 1000 keys and 6
 // heads 9 and 18 at 100 rows (50,000).
 constexpr double kTcWindowWork = 200000;
+// Over pages from this many on: 14 histories of 689 keys, 196 rows of one head of 32 (125,000)
+// take 15 us in blocks of 16 rows and 26 there, 2 of 615 keys, 1230 rows of 3 heads of 48
+// (284,000) 20 and 26, 6 of 389 keys, 482 rows of 5 heads of 80 (361,000) 24 and 30.
+constexpr double kTcPageWork = 300000;
 
 // The tensor cores cut what does not fit the float32 sum off at every 16 keys' addition
 // (a unit in the last place at most), so a sum over n keys of equal weight comes out
@@ -195,9 +199,11 @@ rtcc_status run_attention(AttnArgs& a, const PagesArgs* pages, int max_q, int ma
   // the tensor-core kernel from kTcRows (token, head) rows per key head on
   const long long rows = (long long)max_q * a.group;
   bool tc = rows > (pages ? kTcPageRows : kTcRows) && a.group <= 128 && a.n_rows > 0;
-  // behind short windows its blocks hardly begin before they end: not for little work
-  if (tc && !pages && a.window > 0)
-    tc = (double)((rows + attn_rows_per_block() - 1) / attn_rows_per_block()) * a.n_seqs * a.kv_heads * most_k > kTcWindowWork;
+  // behind short windows its blocks hardly begin before they end, and over pages there is the
+  // widening: not for little work
+  const double work = (double)((rows + attn_rows_per_block() - 1) / attn_rows_per_block()) * a.n_seqs * a.kv_heads * most_k;
+  if (pages) tc = tc && work > kTcPageWork;
+  else if (a.window > 0) tc = tc && work > kTcWindowWork;
   const size_t part = (size_t)a.n_q * a.heads * (a.dim * sizeof(float) + sizeof(float2));
   const long long span = (most_k + 63) / 64 * 64, span_rows = span * a.n_seqs;
   size_t wide = pages ? widened_bytes(span_rows, a) : 0;

@@ -394,47 +394,56 @@ __global__ void __launch_bounds__(kWidenThreads)
     k_pages_widen(const __grid_constant__ AttnArgs A, const __grid_constant__ PagesArgs P, T* k, T* v,
                   unsigned char* hidden, int span) {
   const int lane = threadIdx.x & 31;
-  long long item = (long long)blockIdx.x * (kWidenThreads / 32) + (threadIdx.x >> 5);
-  const int head = (int)(item % A.kv_heads);
-  item /= A.kv_heads;
-  const int blocks = span / kPageBlock, j0 = (int)(item % blocks) * kPageBlock, seq = (int)(item / blocks);
-  if (seq >= A.n_seqs) return;
-  const AttnSpan S = attn_span<true>(A, seq);
-  if (S.nq == 0 || j0 >= S.nk) return;
-  auto page_at = [&](int j) -> int {
-    const int page = P.table[(long long)seq * P.s.table_row + (attn_row(S, j) >> P.s.shift)];
-    return (unsigned)page < (unsigned)P.s.n_pages ? page : -1;
-  };
-  const int page = page_at(j0);
-  if (head == 0 && lane == 0 && j0 % 64 == 0)
-    hidden[((long long)seq * span + j0) / 64] =
-        (unsigned char)((page < 0) | (j0 + 32 < S.nk && page_at(j0 + 32) < 0 ? 2 : 0));
-  if (page < 0) return;
-  const int row = attn_row(S, j0) & (P.s.page_rows - 1);
-  const long long at = page * P.s.page_bytes + ((long long)head * P.s.page_rows + row) * A.dim;
-  const signed char* e =
-      P.scales + page * P.s.scale_bytes + ((long long)head * (P.s.page_rows / kPageBlock) + row / kPageBlock) * 2;
-  const float fk = pow2(max((int)e[0], kExpMin)), fv = pow2(max((int)e[1], kExpMin));
-  const int units = A.dim / 16;                  // of a row
-  for (int i = lane; i < kPageBlock * units; i += 32) {
-    const int r = i / units, c = i % units;
-    const uint4 x[2] = {__ldcs(reinterpret_cast<const uint4*>(P.k + at) + i),
-                        __ldcs(reinterpret_cast<const uint4*>(P.v + at) + i)};
-    const long long to = (((long long)seq * span + j0 + r) * A.kv_heads + head) * A.dim + c * 16;
+  const unsigned item = blockIdx.x * (kWidenThreads / 32) + (threadIdx.x >> 5);
+  const int head = (int)(item % (unsigned)A.kv_heads), j0 = (int)(item / (unsigned)A.kv_heads) * kPageBlock;
+  if (j0 >= span) return;
+  for (int seq = blockIdx.y; seq < A.n_seqs; seq += gridDim.y) {
+    const AttnSpan S = attn_span<true>(A, seq);
+    if (S.nq == 0 || j0 >= S.nk) continue;
+    auto page_at = [&](int j) -> int {
+      const int page = P.table[(long long)seq * P.s.table_row + (attn_row(S, j) >> P.s.shift)];
+      return (unsigned)page < (unsigned)P.s.n_pages ? page : -1;
+    };
+    const int page = page_at(j0);
+    if (head == 0 && lane == 0 && j0 % 64 == 0)
+      hidden[((long long)seq * span + j0) / 64] =
+          (unsigned char)((page < 0) | (j0 + 32 < S.nk && page_at(j0 + 32) < 0 ? 2 : 0));
+    if (page < 0) continue;
+    const int row = attn_row(S, j0) & (P.s.page_rows - 1);
+    const long long at = page * P.s.page_bytes + ((long long)head * P.s.page_rows + row) * A.dim;
+    const char2 e = *reinterpret_cast<const char2*>(P.scales + page * P.s.scale_bytes +
+                                                   ((long long)head * (P.s.page_rows / kPageBlock) + row / kPageBlock) * 2);
+    const int units = A.dim / 16, all = kPageBlock * units;          // 16-byte units of a row, of the block
+    constexpr int N = 4;                         // of a lane at most
+    uint4 x[2][N];                               // all loads first
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const uint32_t u[4] = {x[h].x, x[h].y, x[h].z, x[h].w};
-      const float f = h ? fv : fk;
-      uint32_t y[8];
-#pragma unroll
-      for (int n = 0; n < 4; ++n) {
-        const float2 p = Store<__half>::unpack2(widen_e4m3x2(u[n])), q = Store<__half>::unpack2(widen_e4m3x2(u[n] >> 16));
-        y[2 * n] = Store<T>::pack2(in_range<T>(p.x * f), in_range<T>(p.y * f));
-        y[2 * n + 1] = Store<T>::pack2(in_range<T>(q.x * f), in_range<T>(q.y * f));
+    for (int n = 0; n < N; ++n) {
+      const int i = n * 32 + lane;
+      if (i < all) {
+        x[0][n] = __ldcs(reinterpret_cast<const uint4*>(P.k + at) + i);
+        x[1][n] = __ldcs(reinterpret_cast<const uint4*>(P.v + at) + i);
       }
-      uint4* dst = reinterpret_cast<uint4*>((h ? v : k) + to);
-      dst[0] = make_uint4(y[0], y[1], y[2], y[3]);
-      dst[1] = make_uint4(y[4], y[5], y[6], y[7]);
+    }
+    const float f[2] = {pow2(max((int)e.x, kExpMin)), pow2(max((int)e.y, kExpMin))};
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const int i = n * 32 + lane, r = i / units, c = i % units;
+      if (i >= all) continue;
+      const long long to = (((long long)seq * span + j0 + r) * A.kv_heads + head) * A.dim + c * 16;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const uint32_t u[4] = {x[h][n].x, x[h][n].y, x[h][n].z, x[h][n].w};
+        uint32_t y[8];
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {
+          const float2 p = Store<__half>::unpack2(widen_e4m3x2(u[m])), q = Store<__half>::unpack2(widen_e4m3x2(u[m] >> 16));
+          y[2 * m] = Store<T>::pack2(in_range<T>(p.x * f[h]), in_range<T>(p.y * f[h]));
+          y[2 * m + 1] = Store<T>::pack2(in_range<T>(q.x * f[h]), in_range<T>(q.y * f[h]));
+        }
+        uint4* dst = reinterpret_cast<uint4*>((h ? v : k) + to);
+        dst[0] = make_uint4(y[0], y[1], y[2], y[3]);
+        dst[1] = make_uint4(y[4], y[5], y[6], y[7]);
+      }
     }
   }
 }
@@ -486,15 +495,16 @@ cudaError_t launch_attn_pages(const AttnArgs& a, const PagesArgs& p, bool bf16, 
 
 cudaError_t launch_pages_widen(const AttnArgs& a, const PagesArgs& p, void* k, void* v, unsigned char* hidden, int span,
                                bool bf16, cudaStream_t st) {
-  const long long warps = (long long)a.n_seqs * (span / kPageBlock) * a.kv_heads;
-  const long long grid = (warps + kWidenThreads / 32 - 1) / (kWidenThreads / 32);
-  if (grid > 0x7FFFFFFF) return cudaErrorNotSupported;
+  const long long warps = (long long)(span / kPageBlock) * a.kv_heads;
+  if (warps > 0x7FFFFFFF) return cudaErrorNotSupported;
+  const dim3 grid((unsigned)((warps + kWidenThreads / 32 - 1) / (kWidenThreads / 32)),
+                  (unsigned)(a.n_seqs < 65535 ? a.n_seqs : 65535));
   if (bf16)
-    k_pages_widen<__nv_bfloat16><<<(unsigned)grid, kWidenThreads, 0, st>>>(a, p, static_cast<__nv_bfloat16*>(k),
-                                                                         static_cast<__nv_bfloat16*>(v), hidden, span);
+    k_pages_widen<__nv_bfloat16><<<grid, kWidenThreads, 0, st>>>(a, p, static_cast<__nv_bfloat16*>(k),
+                                                               static_cast<__nv_bfloat16*>(v), hidden, span);
   else
-    k_pages_widen<__half><<<(unsigned)grid, kWidenThreads, 0, st>>>(a, p, static_cast<__half*>(k), static_cast<__half*>(v),
-                                                                  hidden, span);
+    k_pages_widen<__half><<<grid, kWidenThreads, 0, st>>>(a, p, static_cast<__half*>(k), static_cast<__half*>(v), hidden,
+                                                        span);
   return cudaGetLastError();
 }
 

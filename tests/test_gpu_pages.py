@@ -567,6 +567,33 @@ def test_pages_missing(R, n):
         Case([n, n], [1000, 300], 2, 1, 64, pr, missing=missing, window=300, sinks=40).run(R).check()
 
 
+# sizes that the tensor-core kernel takes: more than 128 rows of a key head, and more than
+# 300,000 pairs of a block of 16 of them and a key
+@pytest.mark.parametrize("n,m", [([1500], [1500]), ([700, 900], [2700, 900]), ([1300], [5000]), ([600, 1, 0, 65], [4096, 900, 10, 3000]),
+                                 ([1025], [1020])])
+@pytest.mark.parametrize("dim,heads,kv,pr,dtype", [(64, 4, 4, 32, "fp16"), (128, 4, 2, 64, "bf16"), (80, 6, 3, 128, "bf16")])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (100, 10), (640, 64), (1, 0)])
+def test_pages_large(R, n, m, dim, heads, kv, pr, dtype, window, sinks):
+    Case(n, m, heads, kv, dim, pr, dtype, window=window, sinks=sinks, pad=16).run(R).check()
+
+
+@pytest.mark.parametrize("dim", [16, 48, 96, 112])
+def test_pages_large_heads_scores_and_starts(R, dim):
+    Case([1200, 700], [1300, 2000], 4, 4, dim, 64, "bf16", cap=20.0, spread=3.0).run(R).check()
+    Case([1200, 700], [1300, 2000], 4, 4, dim, 64, "fp16", cap=500.0, window=300, sinks=7).run(R).check()
+    Case([1200, 700], [1300, 2000], 4, 4, dim, 32, "fp16", prefix=[100, 1999], window=64, sinks=5).run(R).check()
+    Case([1200, 700], [1300, 2000], 8, 4, dim, 128, "fp16", start=[700, 1500]).run(R).check()
+    Case([1200], [1300], 8, 4, dim, 128, "fp16", causal=False).run(R).check()
+
+
+def test_pages_large_missing(R):
+    """Entries that name no page hide their keys: halves of steps, whole steps, the sequence's ends, all of it."""
+    for pr, missing in ((32, ((0, 0), (0, 3), (0, 8), (0, 9), (0, 46), (1, 5))), (64, ((0, 2), (0, 22), (1, 0))),
+                        (128, tuple((0, i) for i in range(12)))):
+        Case([1500, 600], [1500, 900], 4, 4, 64, pr, missing=missing).run(R).check()
+        Case([1500, 600], [1500, 900], 4, 4, 64, pr, missing=missing, window=300, sinks=40).run(R).check()
+
+
 @pytest.mark.parametrize("n,m,window", [(1, 60000, 0), (2, 9000, 8000), (40, 9000, 3000), (300, 9000, 0)])
 def test_pages_split(R, n, m, window):
     """With and without room for parts or widened keys: the same result."""
@@ -574,14 +601,14 @@ def test_pages_split(R, n, m, window):
         Case([n, 3], [m, 200], 2, 1, 64, 64, window=window, sinks=33 if window else 0).run(R, workspace=workspace).check()
 
 
-@pytest.mark.parametrize("n", [3, 200])
+@pytest.mark.parametrize("n", [3, 200, 1500])
 def test_pages_limits_cut(R, n):
     """Tokens from max_q on and keys from max_k on are left out."""
     for max_q, max_k in ((n - 2, 1000), (n, 500), (1, 64), (0, 1000), (n, 0)):
-        c = Case([n], [1000], 2, 1, 64, 64, causal=False).run(R, max_q=max_q, max_k=max_k)
+        c = Case([n], [1000], 8, 8, 64, 64, causal=False).run(R, max_q=max_q, max_k=max_k)
         torch.cuda.synchronize()
         assert (c.out[max_q:] == 7).all()
-        ref = Case([n], [1000], 2, 1, 64, 64, causal=False)
+        ref = Case([n], [1000], 8, 8, 64, 64, causal=False)
         ref.m = [max_k]
         ref.out, ref.lse = c.out[:max_q], c.lse[:max_q]
         ref.n = [max_q]
@@ -600,13 +627,13 @@ def test_pages_exponents_far_apart(R):
 def test_pages_large_values_that_hardly_count(R):
     """A block of values up to 2^60 whose keys have scores 96 below the others': its share is
     2^-70 of the result, and the others keep their digits."""
-    for n in (1, 40, 200):
-        c = Case([n], [400], 2, 1, 64, 64, "bf16", causal=False)
+    for n in (1, 40, 3000):
+        c = Case([n], [400], 8, 4, 64, 64, "bf16", causal=False)
         c.q = torch.full_like(c.q, 4.0)
         page, row = c.table[0][2], 16
-        c.k.view(c.pages, 1, 64, 64)[page, 0, row:row + 16] = torch.tensor(-3.0).to(torch.float8_e4m3fn).view(torch.uint8).item()
-        s = c.s.view(c.pages, 1, 4, 2)
-        s[page, 0, row // 16, 0], s[page, 0, row // 16, 1] = 0, 52
+        c.k.view(c.pages, 4, 64, 64)[page, :, row:row + 16] = torch.tensor(-3.0).to(torch.float8_e4m3fn).view(torch.uint8).item()
+        s = c.s.view(c.pages, 4, 4, 2)
+        s[page, :, row // 16, 0], s[page, :, row // 16, 1] = 0, 52
         s[..., 0].sub_((s[..., 0] != 0).to(torch.int8))        # the others' keys are small
         c.run(R).check()
 
@@ -635,8 +662,8 @@ def test_pages_non_finite_stays_in_its_rows(R):
 
 
 def test_pages_repeat_in_a_graph_on_a_side_stream(R):
-    for n, m, window in (([1, 1], [5000, 300], 0), ([40], [900], 200), ([300], [1900], 0), ([300], [1900], 500)):
-        c = Case(n, m, 2, 1, 128, window=window)
+    for n, m, window in (([1, 1], [5000, 300], 0), ([40], [900], 200), ([300], [1900], 0), ([1500], [1900], 500)):
+        c = Case(n, m, 4, 2, 128, window=window)
         s = torch.cuda.Stream()
         torch.cuda.synchronize()
         c.run(R, stream=s.cuda_stream)
@@ -663,7 +690,7 @@ def test_pages_without_clusters_and_given_up_waits(R):
             assert R.rtcc_test_attention(0) == R.OK
         c.check()
     assert R.rtcc_memory_attention_status() == R.OK
-    c = Case([300], [700], 2, 1)
+    c = Case([1500], [1500], 4, 4)
     try:
         assert R.rtcc_test_attention(R.TEST_UNREACHABLE_WAIT) == R.OK
         c.run(R)
@@ -676,8 +703,8 @@ def test_pages_without_clusters_and_given_up_waits(R):
 
 def test_pages_in_place_and_shared_pages(R):
     """Results over the queries; two sequences on the same pages see the same keys."""
-    for n in (1, 30, 200):
-        c = Case([n, n], [600, 600], 4, 2, 64, 64)
+    for n in (1, 30, 1200):
+        c = Case([n, n], [1200, 1200], 4, 4, 64, 64)
         c.table[1] = list(c.table[0])
         ref = c.run(R).check().out.clone()
         q = c.q.clone(memory_format=torch.contiguous_format)
