@@ -25,8 +25,8 @@
 // what its products need: no number crosses lanes but P, transposed once.
 //
 // Measured: 61 tokens over ragged histories of up to 16,384 keys, 8 key heads of 128 with
-// a cap, 958 MB: 157 us, 6.1 TB/s, 90 % of a plain copy's (rows on the 16-wide side, with
-// probabilities as two terms: 268 us); one token over 4097 keys of 6 heads of 64: 7.2 us.
+// a cap, 958 MB: 161 us, 6.0 TB/s, 88 % of a plain copy's (rows on the 16-wide side, with
+// probabilities as two terms: 268 us); one token over 4097 keys of 6 heads of 64: 7.5 us.
 #include <type_traits>
 
 #include "attn_rows.cuh"

@@ -27,7 +27,7 @@
 // 6 heads of 64 takes 8.2 us, most of which is the launch, a block's first copies
 // and three steps.  WIN: with a window; keys between the sinks and the window of a
 // sequence's first token are numbered away (attn_span), so that chunks are of what is
-// read.  The 61 tokens over windows of 5000 keys, 1.1 GB: 174 us, 6.3 TB/s; one token over
+// read.  The 61 tokens over windows of 5000 keys, 1.1 GB: 177 us, 6.2 TB/s; one token over
 // 1000 keys of 4 key heads of 80: 7.6 us.
 #include "attn_rows.cuh"
 #include "kernels.h"
