@@ -701,6 +701,27 @@ def test_pages_without_clusters_and_given_up_waits(R):
     c.run(R).check()
 
 
+def test_pages_untouched_tokens_and_streams(R):
+    """Tokens of no sequence stay as they were; two calls on two streams do not disturb one another."""
+    for n in (9, 1500):
+        c = Case([5, n], [600, 1500], 4, 4, 64, 64).run(R).check()
+        part = c.out[:5 + n // 2].clone()
+        off, c.out[:] = i32([0, 5, 5 + n // 2]), 7.0
+        c.s_d = i32(c.start)
+        c.args[3], c.args[4] = ptr(off), ptr(c.s_d)
+        R.check(R.rtcc_pages_attention(*c.args, 0))
+        torch.cuda.synchronize()
+        assert (c.out[5 + n // 2:] == 7).all() and torch.equal(c.out[:5 + n // 2], part)
+        a, b = Case([n], [1500], 4, 4, 128, 32), Case([3, n], [900, 1500], 4, 2, 64, 64, "bf16", window=300, sinks=5)
+        sa, sb = torch.cuda.Stream(), torch.cuda.Stream()
+        torch.cuda.synchronize()
+        for _ in range(4):
+            a.run(R, stream=sa.cuda_stream)
+            b.run(R, stream=sb.cuda_stream)
+        a.check()
+        b.check()
+
+
 def test_pages_in_place_and_shared_pages(R):
     """Results over the queries; two sequences on the same pages see the same keys."""
     for n in (1, 30, 1200):
