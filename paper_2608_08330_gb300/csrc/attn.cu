@@ -189,13 +189,7 @@ rtcc_status run_attention(AttnArgs& a, const PagesArgs* pages, int max_q, int ma
   const int test = g_test.load(std::memory_order_relaxed);
   a.stall = (test & RTCC_TEST_UNREACHABLE_WAIT) != 0;
   a.budget = a.stall ? kWaitBudgetCycles / 100 : kWaitBudgetCycles;
-  // keys of a sequence that its tokens see: with a window no more than the sinks, the
-  // tokens and a window, in whole steps
-  long long most_k = max_k;
-  if (a.window > 0 && !a.prefix) {
-    const long long seen = ((long long)a.sinks + 63) / 64 * 64 + a.window + max_q + 63LL;
-    if (seen < most_k) most_k = seen;
-  }
+  const long long most_k = attn_most_keys(a, max_q, max_k);
   // the tensor-core kernel from kTcRows (token, head) rows per key head on
   const long long rows = (long long)max_q * a.group;
   bool tc = rows > (pages ? kTcPageRows : kTcRows) && a.group <= 128 && a.n_rows > 0;

@@ -53,13 +53,15 @@ struct AttnArgs {
 // without them from there on (nk and first too), `dead` is the first number after the
 // gap and `shift` its length; attn_row gives a number's row.  Every token's window then
 // begins past `dead`, so that masks need no gap.
+//
+// Host code too, so that the numbering is checked without a GPU.
 struct AttnSpan {
   int q0, nq, kb, nk, prefix, first;
   int dead, shift;
 };
 
 template <bool WIN = false>
-__device__ __forceinline__ AttnSpan attn_span(const AttnArgs& A, int seq) {
+__host__ __device__ __forceinline__ AttnSpan attn_span(const AttnArgs& A, int seq) {
   AttnSpan s;
   const int q0 = A.q_offsets[seq], q1 = A.q_offsets[seq + 1];
   s.q0 = min(max(q0, 0), A.n_q);
@@ -76,12 +78,11 @@ __device__ __forceinline__ AttnSpan attn_span(const AttnArgs& A, int seq) {
   }
   s.prefix = A.prefix ? min(max(A.prefix[seq], 0), s.nk) : 0;
   s.first = s.nk - s.nq;
-  if (A.causal && A.q_start) {
-    s.first = min(max(A.q_start[seq], 0), s.nk);
-    if (s.nk - s.first > s.nq) s.nk = max(s.prefix, s.first + s.nq);
-  }
+  if (A.causal && A.q_start) s.first = min(max(A.q_start[seq], 0), s.nk);
+  // tokens that are left out take the keys along that only they see
+  if (WIN && !A.k_begin) s.nq = min(s.nq, A.most_q);
+  if (A.causal && s.nk - s.first > s.nq) s.nk = max(s.prefix, max(s.first + s.nq, 0));
   if (WIN) {
-    if (!A.k_begin) s.nq = min(s.nq, A.most_q);
     if (A.window > 0) {
       const int own = s.nq < s.nk - s.first ? s.first + s.nq : s.nk;
       const int seen = max(s.prefix, min(A.sinks, own));                 // keys before this are seen from afar
@@ -102,11 +103,20 @@ __device__ __forceinline__ AttnSpan attn_span(const AttnArgs& A, int seq) {
   return s;
 }
 
+// Keys of a sequence at most, numbered without the gap (attn_span's nk), where it has no more
+// than max_q tokens and max_k keys: with a window and no prefix the sinks, the tokens and a
+// window, in whole steps.  Sizes the room for keys widened from pages.
+__host__ inline long long attn_most_keys(const AttnArgs& a, int max_q, int max_k) {
+  if (a.window == 0 || a.prefix) return max_k;
+  const long long seen = ((long long)a.sinks + 63) / 64 * 64 + a.window + max_q + 63LL;
+  return seen < max_k ? seen : max_k;
+}
+
 // Memory row of key j.
-__device__ __forceinline__ int attn_row(const AttnSpan& s, int j) { return s.kb + j + (j >= s.dead ? s.shift : 0); }
+__host__ __device__ __forceinline__ int attn_row(const AttnSpan& s, int j) { return s.kb + j + (j >= s.dead ? s.shift : 0); }
 
 // Keys [0, n) of the span that token i of the sequence sees (slots aside).
-__device__ __forceinline__ int attn_visible(const AttnArgs& A, const AttnSpan& s, int first, int i) {
+__host__ __device__ __forceinline__ int attn_visible(const AttnArgs& A, const AttnSpan& s, int first, int i) {
   if (!A.causal) return s.nk;
   const int own = i < s.nk - first ? first + i + 1 : s.nk;
   return max(0, max(s.prefix, own));
@@ -116,7 +126,7 @@ __device__ __forceinline__ int attn_visible(const AttnArgs& A, const AttnSpan& s
 struct AttnView {
   int seen, low;
 };
-__device__ __forceinline__ AttnView attn_view(const AttnArgs& A, const AttnSpan& s, int first, int i) {
+__host__ __device__ __forceinline__ AttnView attn_view(const AttnArgs& A, const AttnSpan& s, int first, int i) {
   if (A.window == 0) return {0, 0};
   const int own = i < s.nk - first ? first + i + 1 : s.nk;
   return {max(s.prefix, min(A.sinks, own)), (int)max(0LL, (long long)first + i + 1 - A.window)};

@@ -615,6 +615,48 @@ def test_pages_limits_cut(R, n):
         ref.check()
 
 
+class Limited(Case):
+    """Tokens from most_q on and keys from most_k on are left out; what no token that is left sees holds NaN."""
+
+    def __init__(self, n, m, most_q, most_k, **kw):
+        self.most_q, self.most_k = most_q, most_k
+        super().__init__(n, m, **kw)
+
+    def visible(self, s):
+        see = super().visible(s)
+        see[self.most_q:] = False
+        see[:, self.most_k:] = False
+        return see
+
+    def run(self, R, **kw):
+        return super().run(R, max_q=self.most_q, max_k=self.most_k, **kw)
+
+    def check(self):
+        torch.cuda.synchronize()
+        at = 0
+        for n in self.n:
+            out, lse = self.out[at + min(n, self.most_q):at + n], self.lse[at + min(n, self.most_q):at + n]
+            assert bool((out == 7).all()) and bool((lse == 7).all())
+            out.zero_()
+            lse.fill_(-math.inf)
+            at += n
+        return super().check()
+
+
+@pytest.mark.parametrize("n,m,most_q", [([9, 4], [300, 900], 3), ([200, 30], [700, 900], 60), ([3000, 20, 900], [4000, 700, 900], 1000),
+                                         ([2500], [2500], 1400), ([1700, 1600], [300, 1500], 1500)])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (100, 10), (640, 64), (1, 0)])
+@pytest.mark.parametrize("given", [False, True])
+def test_pages_left_out_tokens_and_their_keys(R, n, m, most_q, window, sinks, given):
+    """Causal: keys that only left-out tokens would see are not read, and may hold anything, those
+    in the last step of what is read too."""
+    start = [max(0, b - a) for a, b in zip(n, m)] if given else None
+    Limited(n, m, most_q, max(m), heads=4, kv=4, dim=64, pr=64, window=window, sinks=sinks, start=start).run(R).check()
+    if not given:
+        Limited(n, m, most_q, max(m), heads=4, kv=2, dim=80, pr=32, dtype="bf16", window=window, sinks=sinks,
+                prefix=[x // 3 for x in m]).run(R).check()
+
+
 def test_pages_exponents_far_apart(R):
     """Blocks from 2^-100 to 2^100: none overflows, none of the large ones is lost."""
     for n in (1, 40):
