@@ -5,12 +5,14 @@
 // exponent for every 16 places of a page and key head.  e4m3 numbers are fp16 numbers, so
 // both products run on them exactly (mma.m16n8k16 fp16, float32 sums), for queries of
 // either type, and the exponents go where they cost least: e_k into the factor of the
-// scores x (in log2), e_v into the values' weights 2^(x + e_v).  These have a running
-// maximum of their own beside the scores': large values that hardly count, as of a key
-// with a low score, do not press the others' weights out of fp16's range.  bf16 queries
+// scores x (in log2), e_v into the values' weights 2^(x - m + e_v), m the scores' running
+// maximum.  The weights have a running maximum of their own, as a difference from m:
+// large values that hardly count, as of a key with a low score, do not press the others'
+// weights out of fp16's range, and large scores, whose float32 steps are whole numbers
+// from 2^24 on, do not round the exponents away.  bf16 queries
 // are scaled by a power of two per row so that the largest is below 2^15; what is more
 // than 2^39 below it is lost.  Weights are rounded to fp16's 11 bits, seven more than the
-// values have; the largest is 2^15, so that 2^-40 of it still counts.
+// values have; the largest is 2^15 to 2^16, so that 2^-40 of it still counts.
 //
 // Keys and channels are the products' 16-wide side, query rows the 8-wide one,
 //   S^T = K Q^T,   O^T = V^T P^T,
@@ -69,6 +71,10 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t x) {
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
   return y;
 }
+
+// The whole power of two that a row's results are in units of, above 2^m, where h is its
+// largest weight (log2): weights of at most 2^(16 - 1/256), below fp16's largest number.
+__device__ __forceinline__ float weight_unit(float h) { return h == -INFINITY ? 0.f : ceilf(h + 0x1p-8f) - 16.0f; }
 
 // NR: groups of 8 rows of a block.
 template <typename T, int DP, int NR, bool CLUSTER>
@@ -168,9 +174,9 @@ __global__ void __launch_bounds__(kWarps * 32, NR == 1 ? 3 : 2)
 #pragma unroll
       for (int u = 0; u < DP / 16; ++u) o[i][u][0] = o[i][u][1] = o[i][u][2] = o[i][u][3] = 0.f;
     float m[N], l[N];                            // of the scores
-    float mo[N];                                 // o is in units of 2^mo
+    float wt[N];                                 // largest weight (log2, from m): o is in units of 2^(m + weight_unit)
 #pragma unroll
-    for (int i = 0; i < N; ++i) m[i] = mo[i] = -INFINITY, l[i] = 0.f;
+    for (int i = 0; i < N; ++i) m[i] = wt[i] = -INFINITY, l[i] = 0.f;
 
     const int n_tiles = end > c0 ? (end - c0 + KT - 1) / KT : 0;
     auto page_of = [&](int t) -> int {           // of tile t, -1: none
@@ -247,9 +253,7 @@ __global__ void __launch_bounds__(kWarps * 32, NR == 1 ? 3 : 2)
           }
         const int j0 = c0 + t * KT;
         const bool edge = bits != 0xFFFFFFFFu || j0 + KT > least || (j0 < last.low && j0 + KT > first.seen);
-        float top[N], heavy[N];                  // largest score, largest weight (log2)
-#pragma unroll
-        for (int i = 0; i < N; ++i) top[i] = heavy[i] = -INFINITY;
+        float top[N][KT / 16];                   // largest score of each exponent's keys
         float ve[KT / 16];
 #pragma unroll
         for (int n = 0; n < KT / 16; ++n) {
@@ -272,28 +276,31 @@ __global__ void __launch_bounds__(kWarps * 32, NR == 1 ? 3 : 2)
               y = x;
               t = fmaxf(t, x);
             }
-            top[i] = fmaxf(top[i], t);
-            heavy[i] = fmaxf(heavy[i], t + ve[n]);
+            top[i][n] = t;
           }
         }
-        constexpr float kLift = 15.0f;           // log2 of the largest weight, for fp16's range
         bool moved = false;
-        float f[N];
+        float base[N], unit[N], f[N];
 #pragma unroll
         for (int i = 0; i < N; ++i) {
+          float mn = m[i];
 #pragma unroll
-          for (int d = 4; d < 32; d <<= 1) {
-            top[i] = fmaxf(top[i], __shfl_xor_sync(0xFFFFFFFFu, top[i], d));
-            heavy[i] = fmaxf(heavy[i], __shfl_xor_sync(0xFFFFFFFFu, heavy[i], d));
+          for (int n = 0; n < KT / 16; ++n) {
+#pragma unroll
+            for (int d = 4; d < 32; d <<= 1) top[i][n] = fmaxf(top[i][n], __shfl_xor_sync(0xFFFFFFFFu, top[i][n], d));
+            mn = fmaxf(mn, top[i][n]);
           }
-          const float mn = fmaxf(m[i], top[i]), on = fmaxf(mo[i], heavy[i] - kLift);
-          top[i] = mn == -INFINITY ? 0.f : mn;
-          heavy[i] = on == -INFINITY ? 0.f : on;
-          l[i] *= exp2f(m[i] - top[i]);          // m = -inf: 0
-          f[i] = ex2(mo[i] - heavy[i]);
+          base[i] = mn == -INFINITY ? 0.f : mn;
+          const float fall = m[i] - base[i];     // m = -inf: -inf
+          float h = wt[i] + fall;
+#pragma unroll
+          for (int n = 0; n < KT / 16; ++n) h = fmaxf(h, (top[i][n] - base[i]) + ve[n]);
+          unit[i] = weight_unit(h);
+          l[i] *= exp2f(fall);
+          f[i] = ex2(fall + (weight_unit(wt[i]) - unit[i]));
           moved = moved || f[i] != 1.0f;
           m[i] = mn;
-          mo[i] = on;
+          wt[i] = h;
         }
         if (__any_sync(0xFFFFFFFFu, moved)) {
 #pragma unroll
@@ -314,12 +321,12 @@ __global__ void __launch_bounds__(kWarps * 32, NR == 1 ? 3 : 2)
         for (int n = 0; n < KT / 16; ++n) {
 #pragma unroll
           for (int i = 0; i < NR; ++i) {
-            const float w0 = ve[n] - heavy[2 * i], w1 = ve[n] - heavy[2 * i + 1];
+            const float w0 = ve[n] - unit[2 * i], w1 = ve[n] - unit[2 * i + 1];      // whole numbers
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-              const float x0 = s[i][n][2 * h], x1 = s[i][n][2 * h + 1];
-              sum[2 * i] += exp2f(x0 - top[2 * i]);
-              sum[2 * i + 1] += exp2f(x1 - top[2 * i + 1]);
+              const float x0 = s[i][n][2 * h] - base[2 * i], x1 = s[i][n][2 * h + 1] - base[2 * i + 1];
+              sum[2 * i] += exp2f(x0);
+              sum[2 * i + 1] += exp2f(x1);
               pb[i][n][h] = transpose8(Store<__half>::pack2(ex2(x0 + w0), ex2(x1 + w1)));
             }
           }
@@ -357,7 +364,7 @@ __global__ void __launch_bounds__(kWarps * 32, NR == 1 ? 3 : 2)
     float* state = reinterpret_cast<float*>(smem);
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const float back = mo[i] == -INFINITY ? 0.f : exp2f(mo[i] - m[i]);
+      const float back = wt[i] == -INFINITY ? 0.f : exp2f(weight_unit(wt[i]));
       float* dst = state + (w * kRows + (i >> 1) * 8 + (lane & 3) * 2 + (i & 1)) * (DP + 4);
 #pragma unroll
       for (int u = 0; u < DP / 16; ++u)

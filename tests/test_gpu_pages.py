@@ -680,6 +680,59 @@ def test_pages_large_values_that_hardly_count(R):
         c.run(R).check()
 
 
+def one_number(c, which, page, row, x):
+    """All channels and heads of place `row` of a page: the e4m3 number x."""
+    t = (c.k, c.v)[which][:, :c.kv * c.pr * c.dim].view(c.pages, c.kv, c.pr, c.dim)
+    t[page, :, row] = torch.tensor(float(x)).to(torch.float8_e4m3fn).view(torch.uint8).item()
+
+
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+@pytest.mark.parametrize("size", [1.3e7, 2e8, -2e8, 1e9, -1e9, 1e12, -1e30])
+def test_pages_large_scores(R, dtype, size):
+    """Scores beyond 2^24, where float32 has no fractions left: a token's only key, or the one
+    whose score is a sixteenth of all scores above the next, is the result, whatever the sizes
+    of the values.  One rounding of the result and one of the weight: 2 u |v|."""
+    u = ROUND[dtype]
+    for n, kv, window in ((1, 1, 0), (1, 1, 1), (40, 1, 0), (40, 1, 1), (1500, 4, 0), (1500, 4, 1)):
+        c = Case([n], [1500], 4 * kv if n == 1 else kv, kv, 64, 64, dtype, causal=window > 0, window=window)
+        c.s.view(c.pages, kv, 4, 2)[..., 0] = -3
+        keys = torch.tensor([1.0 + i / 16 for i in range(4)] * 375)[torch.randperm(1500, generator=torch.Generator().manual_seed(1))]
+        best = 777
+        keys[best] = 2.0 if size > 0 else 0.8125
+        for j in range(1500):
+            one_number(c, 0, c.table[0][j // 64], j % 64, keys[j])
+        c.q = torch.full_like(c.q, 1024.0)
+        c.scale = size / (64 * 1024.0 * (0.25 if size > 0 else 0.8125 / 8))         # the winner's score is `size`
+        c.run(R)
+        torch.cuda.synchronize()
+        for h in range(c.heads):
+            v = c.values(0, 1, h // (c.heads // kv))
+            want = v[1500 - n:] if window else v[best].expand(n, 64)
+            assert bool(((c.out[:, h].double() - want).abs() <= 2 * u * want.abs() + TINY[dtype]).all()), (n, window)
+            k = c.values(0, 0, h // (c.heads // kv))[:, 0]
+            top = size * (k[1500 - n:] / k[best] if window else torch.ones_like(k[:n]))
+            assert bool(((c.lse[:, h].double() - top).abs() <= 2.0 ** -20 * top.abs()).all()), (n, window)
+
+
+@pytest.mark.parametrize("size", [1.3e7, -1e9])
+def test_pages_large_scores_alike(R, size):
+    """Few rows, all scores the same large number: the values' mean, though their exponents differ."""
+    for n in (1, 40):
+        c = Case([n], [700], 2, 1, 64, 64, causal=False)
+        c.s.view(c.pages, 1, 4, 2)[..., 0] = -3
+        c.s.view(c.pages, 1, 4, 2)[:, 0, :, 1] = torch.randint(-9, 3, (c.pages, 4), generator=gen(2), device="cuda").to(torch.int8)
+        for j in range(700):
+            one_number(c, 0, c.table[0][j // 64], j % 64, 1.0)
+        c.q = torch.full_like(c.q, 1024.0)
+        c.scale = size / (64 * 1024.0 / 8)
+        c.run(R)
+        torch.cuda.synchronize()
+        v = c.values(0, 1, 0)
+        want, A = v.mean(0), v.abs().mean(0)
+        # one rounding of the result, one of the weights, float32 sums
+        assert bool(((c.out.double() - want).abs() <= (2 * 2.0 ** -11 + 2.0 ** -20) * A + TINY["fp16"]).all())
+
+
 def test_pages_wide_queries(R):
     """bf16 queries far outside fp16's range, scores of ordinary size."""
     for n in (1, 40):
