@@ -790,8 +790,9 @@ typedef struct {
 /*
  * rtcc_memory_attention over the pages: sequence s has the tokens
  * [d_q_offsets[s], d_q_offsets[s + 1]) and the keys at places [0, d_length[s]), its
- * first token is at place d_start[s] (NULL: its tokens are the last places).  Key j is
- * visible to the token at place p where
+ * first token is at place d_start[s], at least 0 (NULL: its tokens are the last of the
+ * d_length[s] places, whatever max_q and max_k leave out).  A place may be past the last
+ * key.  Key j is visible to the token at place p where
  *   not causal, or j <= p and (no window, or j > p - window or j < sinks),
  *   or j < d_prefix[s] (NULL = 0),
  * and its page is one.  out and lse as there; places that no token sees may hold

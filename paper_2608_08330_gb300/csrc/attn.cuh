@@ -45,7 +45,7 @@ struct AttnArgs {
 
 // One sequence: its tokens [q0, q0 + nq) and memory rows [kb, kb + nk), the first
 // token's place among the keys (a causal token i sees keys up to first + i; negative
-// where there are more tokens than keys).  Offsets come from device memory, so they
+// where there are more tokens than keys, nk or more behind the last of them).  Offsets come from device memory, so they
 // are cut to the arrays' extents; keys after the last token's are left out.
 //
 // With a window, keys behind the first token's, past the sinks and the prefix, are seen
@@ -69,16 +69,20 @@ __host__ __device__ __forceinline__ AttnSpan attn_span(const AttnArgs& A, int se
   s.dead = 0x7FFFFFFF;
   s.shift = 0;
   if (WIN && !A.k_begin) {                       // pages: places from 0 on
+    const int held = max(A.k_end[seq], 0);
     s.kb = 0;
-    s.nk = min(max(A.k_end[seq], 0), A.most_k);
+    s.nk = min(held, A.most_k);
+    s.first = held - s.nq;                       // of all that it holds, whatever is left out
   } else {
     const int kb = A.k_begin[seq], ke = A.k_end[seq];
     s.kb = min(max(kb, 0), A.n_rows);
     s.nk = min(max(ke, s.kb), A.n_rows) - s.kb;
+    s.first = s.nk - s.nq;
   }
   s.prefix = A.prefix ? min(max(A.prefix[seq], 0), s.nk) : 0;
-  s.first = s.nk - s.nq;
-  if (A.causal && A.q_start) s.first = min(max(A.q_start[seq], 0), s.nk);
+  if (A.causal && A.q_start) s.first = max(A.q_start[seq], 0);
+  // a place may be past the last key; past it by a window or more no key is in the window
+  s.first = (int)min((long long)s.first, (long long)s.nk + A.window);
   // tokens that are left out take the keys along that only they see
   if (WIN && !A.k_begin) s.nq = min(s.nq, A.most_q);
   if (A.causal && s.nk - s.first > s.nq) s.nk = max(s.prefix, max(s.first + s.nq, 0));
@@ -86,7 +90,7 @@ __host__ __device__ __forceinline__ AttnSpan attn_span(const AttnArgs& A, int se
     if (A.window > 0) {
       const int own = s.nq < s.nk - s.first ? s.first + s.nq : s.nk;
       const int seen = max(s.prefix, min(A.sinks, own));                 // keys before this are seen from afar
-      const int low = (int)max(0LL, (long long)s.first + 1 - A.window);
+      const int low = (int)min(max(0LL, (long long)s.first + 1 - A.window), (long long)s.nk);
       const int dead = (seen + 63) & ~63;
       if ((low & ~63) > dead) {
         s.dead = dead;

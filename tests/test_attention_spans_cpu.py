@@ -118,3 +118,33 @@ def test_pages_many_left_out_tokens_stay_within_the_room(span):
     """100,000 tokens of which 2,000 are taken, windows of 100: the keys of 2,000."""
     q0, nq, nk, room, rows, sees = span([0, 100000], None, [100000], 0, 1, 100, 0, most_q=2000, most_k=100000)
     assert nq == 2000 and nk <= room == 100 + 2000 + 63
+
+
+@pytest.mark.parametrize("pages", [False, True])
+def test_places_are_what_they_are_given_as(span, pages):
+    """A token is at the place that its start says, behind the span's end too, and, without
+    starts, counts from the sequence's own length, not from what max_k leaves of it."""
+    rng = random.Random(2 + pages)
+    behind = cut = 0
+    for _ in range(4000):
+        n, m = rng.choice([1, 2, 40, rng.randint(0, 400)]), sizes(rng, 1500)
+        window = rng.choice([0, 1, 64, rng.randint(1, 300), rng.randint(1, 3000), 2 ** 31 - 1])
+        sinks = rng.choice([0, 1, 64, rng.randint(0, 200), 2 ** 31 - 1])
+        prefix = rng.choice([None, None, 0, rng.randint(0, m), m + 7])
+        start = rng.choice([None, rng.randint(0, m), m, m + rng.randint(0, 500), 2 ** 31 - 1])
+        most_k = rng.choice([m, m + 9, rng.randint(0, m), 64]) if pages else m
+        kw = dict(prefix=None if prefix is None else [prefix], start=None if start is None else [start], most_q=n)
+        if pages:
+            _, nq, nk, room, rows, sees = span([0, n], None, [m], 0, 1, window, sinks, most_k=most_k, **kw)
+        else:
+            _, nq, nk, room, rows, sees = span([0, n], [5], [5 + m], 0, 1, window, sinks, n_rows=5 + m, most_k=max(m, 1), **kw)
+        assert nq == n and nk <= max(0, min(m, room))
+        have = min(m, most_k)
+        first = m - n if start is None else start
+        for i in range(n):
+            want = [j for j in definition(m, first + i, True, window, sinks, prefix or 0) if j < have]
+            got = rows_seen(nk, rows, sees[i], window) - (0 if pages else 5)
+            assert got.tolist() == want, (n, m, window, sinks, prefix, start, most_k, i)
+        behind += window > 0 and n > 0 and first > have
+        cut += have < m
+    assert behind > 300 and (cut > 300 or not pages)

@@ -657,6 +657,25 @@ def test_pages_left_out_tokens_and_their_keys(R, n, m, most_q, window, sinks, gi
                 prefix=[x // 3 for x in m]).run(R).check()
 
 
+@pytest.mark.parametrize("n,m,most_k", [([1], [1000], 500), ([3, 40], [1000, 300], 400), ([200, 90], [700, 1500], 600),
+                                         ([1500, 30], [3000, 900], 2000), ([1300], [1300], 1000)])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (100, 10), (640, 64)])
+@pytest.mark.parametrize("given", [False, True])
+def test_pages_left_out_keys_move_no_token(R, n, m, most_k, window, sinks, given):
+    """Keys from max_k on are left out; the tokens stay where they were."""
+    start = [b - a for a, b in zip(n, m)] if given else None
+    Limited(n, m, max(n), most_k, heads=4, kv=4, dim=64, pr=64, window=window, sinks=sinks, start=start).run(R).check()
+    Limited(n, m, max(n), most_k, heads=4, kv=2, dim=128, pr=32, dtype="bf16", window=window, sinks=sinks, start=start,
+            prefix=[x // 4 for x in m]).run(R).check()
+
+
+@pytest.mark.parametrize("n,m", [(1, 1000), (8, 1000), (200, 777), (1300, 1500)])
+def test_pages_starts_behind_the_keys(R, n, m):
+    for window, sinks in ((0, 0), (50, 7), (640, 64), (3000, 0)):
+        for start in ([m, m + 30], [m + 100, m - n], [2 ** 31 - 1, m + window]):
+            Case([n, n], [m, m], 4, 4, 64, 64, window=window, sinks=sinks, start=start).run(R).check()
+
+
 def test_pages_exponents_far_apart(R):
     """Blocks from 2^-100 to 2^100: none overflows, none of the large ones is lost."""
     for n in (1, 40):

@@ -224,3 +224,13 @@ def test_window_without_clusters(R):
         finally:
             assert R.rtcc_test_attention(0) == R.OK
         c.check()
+
+
+@pytest.mark.parametrize("n,m", [(1, 1000), (8, 1000), (200, 777), (1300, 1500)])
+@pytest.mark.parametrize("dim,heads,kv,dtype", [(64, 4, 4, "fp16"), (128, 4, 2, "bf16")])
+def test_window_starts_behind_the_span(R, n, m, dim, heads, kv, dtype):
+    """Tokens at places past the last key: their windows reach back over fewer keys, or none."""
+    for window, sinks in ((50, 0), (50, 7), (640, 64), (3000, 0)):
+        for start in ([m, m + 30, m + 1], [m + 100, m - n, m + 700], [2 ** 31 - 1, m + window, m + window - 1]):
+            Window([n, n, 2], [m, m, m], window, sinks, start=start, dim=dim, heads=heads, kv=kv, dtype=dtype).run(R).check()
+    Window([n, n], [m, m], 50, 3, start=[m + 500, 2 ** 31 - 1], prefix=[0, 300], dim=dim, heads=heads, kv=kv, dtype=dtype).run(R).check()
