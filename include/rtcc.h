@@ -565,7 +565,7 @@ typedef struct {
  * more parts than fill the GPU, or than keep sums within 65,536 keys, are not
  * made, and without room for two (NULL, or too small) spans are not split.  A
  * float32 sum over n equally weighted keys may come out smaller by n 2^-28 of
- * itself, so long spans want a workspace (and max_k): room for max_k / 65,536 + 2
+ * itself, by 3 n 2^-28 at worst, so long spans want a workspace (and max_k): room for max_k / 65,536 + 2
  * parts keeps sums that short.  Calls with more than 128 query heads to a key head,
  * with a stride of 0 (several heads or rows at one place), or without room and with
  * a max_k above 2^20 (so do not overstate it) take the kernel for few query rows

@@ -35,10 +35,11 @@ constexpr double kTcWindowWork = 200000;
 // (284,000) 20 and 26, 6 of 389 keys, 482 rows of 5 heads of 80 (361,000) 24 and 30.
 constexpr double kTcPageWork = 300000;
 
-// The tensor cores cut what does not fit the float32 sum off at every 16 keys' addition
-// (a unit in the last place at most), so a sum over n keys of equal weight comes out
-// smaller by up to (n / 32) 2^-23: 2^-12 at 65,536 keys, half of fp16's rounding; measured
-// 0.1 % at 2^18 keys, 0.6 % at 2^20.  Parts of a span are no longer than this where the
+// The tensor cores cut what does not fit the float32 sum off whenever they add the products
+// of four keys (a unit in the last place at most), so a sum over n keys of equal weight and
+// values of one sign comes out smaller by up to 3 n 2^-28: measured at 65,536, 2^18 and 10^6
+// keys 0.03 %, 0.16 % and 0.6 % with random values, 0.05 %, 0.26 % and 1.04 % with the worst
+// (fp16's rounding is 0.05 %).  Parts of a span are no longer than this where the
 // workspace has room: kSumKeys per sum, a block of the few-rows kernel has a sum in each
 // of its four warps.  A call of the tensor-core kernel without room, whose parts would be
 // longer than kLongSum, goes to the few-rows kernel instead: slower, but a cluster of its
@@ -145,7 +146,7 @@ long long tc_chunks(long long units, long long steps, long long least_chunks, lo
 int tc_streams(const AttnArgs& a, int max_q, long long most_k, int sms) {
   const long long tokens = 128 / a.group, tiles = (max_q + tokens - 1) / tokens;
   long long keys = most_k;
-  if (a.window > 0) keys = std::min(keys, (long long)a.window + a.sinks + 2 * tokens + 128);
+  if (a.window > 0 && !a.prefix) keys = std::min(keys, (long long)a.window + a.sinks + 2 * tokens + 128);
   const double steps = (double)(keys + 63) / 64, units = (double)a.n_seqs * a.kv_heads;
   const double one = ceil(units * ((tiles + 1) / 2) / sms) * (steps + 8);
   const double two = ceil(units * tiles / sms) * (steps / 2 + 8) + 6 + 16.0 * a.n_q * a.heads * a.dim / 6.8e6;
@@ -233,17 +234,19 @@ rtcc_status run_attention(AttnArgs& a, const PagesArgs* pages, int max_q, int ma
     w.row_groups = (int)groups;
     const long long steps = (most_k + w.unit - 1LL) / w.unit;
     long long most = tc ? (steps + 3) / 4 : steps;
-    // tokens that see mostly other keys than one another's leave nothing to split
-    if (tc && w.window > 0 && max_q > w.window) most = 1;
-    if (most > room / w.streams) most = room / w.streams;
-    if (most > 0x7FFFFFFF / units) most = 0x7FFFFFFF / units;
     const long long sums = tc ? w.streams : 4;     // of a block
     const long long least = (most_k + sums * kSumKeys - 1) / (sums * kSumKeys);
+    // keys of a token: tokens that see mostly other keys than one another's leave nothing to
+    // split but long sums, over a prefix, sinks or a window of their own
+    const long long sees = w.window > 0 && !w.prefix ? std::min(most_k, (long long)w.sinks + w.window) : most_k;
+    if (tc && w.window > 0 && max_q > w.window) most = std::min(most, sees > sums * kSumKeys ? least : 1);
+    if (most > room / w.streams) most = room / w.streams;
+    if (most > 0x7FFFFFFF / units) most = 0x7FFFFFFF / units;
     long long chunks = tc ? tc_chunks(units, steps, least, most, sms, w.streams, w.n_q, w.heads, w.dim,
                                       pages || w.window > 0)
                           : rows_chunks(units, w.n_seqs > 1, most_k < max_k, steps, least, most, sms,
                                         pages && (long long)max_q * w.group <= 8 ? 3 : 2, pages ? 8.0 : 10.0);
-    if (tc && most_k / (chunks * sums) > kLongSum) continue;
+    if (tc && std::min(sees, most_k / chunks) / sums > kLongSum) continue;
     const long long joined = tc || !clusters ? 1 : rows_cluster(units, steps, chunks, least, sms, w.dim);
     w.cluster = joined > 1;
     if (w.cluster) chunks = joined;

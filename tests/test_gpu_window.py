@@ -234,3 +234,47 @@ def test_window_starts_behind_the_span(R, n, m, dim, heads, kv, dtype):
         for start in ([m, m + 30, m + 1], [m + 100, m - n, m + 700], [2 ** 31 - 1, m + window, m + window - 1]):
             Window([n, n, 2], [m, m, m], window, sinks, start=start, dim=dim, heads=heads, kv=kv, dtype=dtype).run(R).check()
     Window([n, n], [m, m], 50, 3, start=[m + 500, 2 ** 31 - 1], prefix=[0, 300], dim=dim, heads=heads, kv=kv, dtype=dtype).run(R).check()
+
+
+@pytest.mark.parametrize("pages", [False, True])
+@pytest.mark.parametrize("n,window,seen", [(200, 64, 700001), (200, 150, 1000000), (70, 64, 700001)])
+@pytest.mark.parametrize("by", ["prefix", "sinks"])
+def test_window_behind_a_long_shared_part(R, pages, n, window, seen, by):
+    """More tokens than a window is long, all of which see the same long part: sums over no
+    more than 65,536 keys of equal weight there too.  The tensor cores add four keys' products to
+    a sum at a time and cut it by a unit in the last place at most.  A sum that ends in
+    [2^k, 2^(k + 1)) at S = t 2^k over N keys was in that octave for (1 - 1/t) N keys, N (1 - 1/t) / 4
+    units of 2^(k - 23), and below for N / t, which cost N / (6 t) 2^(k - 24): together, over S,
+    N 2^-24 (1/2 - 1/(3 t)) / t, largest at t = 4/3: 3/16 N 2^-24 = 3 N 2^-28, 3 2^-12 for 65,536 keys.  The
+    result's rounding is 2^-11.  The shared keys weigh
+    1365/1024 of the windows' (11 bits, so rounding them costs nothing) and all values are 15/8,
+    so that 16 products add up to a number with fraction bits for the sum to lose."""
+    m, heads, kv, dim = seen + 500, 2, 1, 64
+    weight, value = 1365 / 1024, 1.875
+    q = torch.zeros(n, heads, dim, device="cuda").half()
+    q[..., 0] = 1
+    out, lse = torch.zeros_like(q), torch.zeros(n, heads, device="cuda")
+    off, end, ws = i32([0, n]), i32([m]), torch.full((192 << 20,), 0xFF, dtype=torch.uint8, device="cuda")
+    prefix, sinks = (i32([seen]), 0) if by == "prefix" else (None, seen)
+    pre, scale = None if prefix is None else prefix.data_ptr(), math.log(weight)
+    per = -(-m // 128)
+    k, v = torch.zeros(per * 128, kv, dim, device="cuda"), torch.full((per * 128, kv, dim), value, device="cuda")
+    k[:seen, :, 0] = 1
+    if pages:
+        k, v = (t.view(per, 128, kv, dim).transpose(1, 2).contiguous().to(torch.float8_e4m3fn).view(torch.uint8) for t in (k, v))
+        e, table = torch.zeros(per, kv, 8, 2, device="cuda", dtype=torch.int8), i32(list(range(per)))
+        R.check(R.rtcc_pages_attention(
+            R.page_config(kv, dim, 128, per, 1, per),
+            R.page_attn_config(heads, R.FP16, n, q.stride()[:2], out.stride()[:2], n, m, window=window, sinks=sinks, scale=scale),
+            q.data_ptr(), off.data_ptr(), None, end.data_ptr(), pre, table.data_ptr(), k.data_ptr(), v.data_ptr(), e.data_ptr(),
+            out.data_ptr(), lse.data_ptr(), ws.data_ptr(), ws.numel()))
+    else:
+        k, v, begin = k.half(), v.half(), i32([0])
+        cfg = R.attn_config(heads, kv, dim, R.FP16, n, m, q.stride()[:2], k.stride()[:2], v.stride()[:2], out.stride()[:2], 1, n, m,
+                            causal=True, scale=scale)
+        R.check(R.rtcc_memory_window_attention(cfg, window, sinks, q.data_ptr(), k.data_ptr(), v.data_ptr(), off.data_ptr(),
+                                               begin.data_ptr(), end.data_ptr(), pre, None, None, None, None, out.data_ptr(),
+                                               lse.data_ptr(), ws.data_ptr(), ws.numel()))
+    torch.cuda.synchronize()
+    assert float((out.double() / value - 1).abs().max()) <= 2.0 ** -11 + 3 * 2.0 ** -12 + 2.0 ** -20
+    assert float((lse.double() - math.log(seen * weight + window)).abs().max()) <= 2.0 ** -20 * 15
