@@ -271,7 +271,7 @@ rtcc_status run_attention(AttnArgs& a, const PagesArgs* pages, int max_q, int ma
       continue;
     }
     if (e != cudaSuccess) return RTCC_E_CUDA;
-    if (!w.cluster && chunks * w.streams > 1 && launch_attn_join(w, max_q, bf16, st) != cudaSuccess) return RTCC_E_CUDA;
+    if (!w.cluster && chunks * w.streams > 1 && launch_attn_join(w, bf16, st) != cudaSuccess) return RTCC_E_CUDA;
     return RTCC_OK;
   }
 }

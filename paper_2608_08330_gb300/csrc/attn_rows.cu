@@ -296,26 +296,55 @@ __global__ void __launch_bounds__(kWarps * 32, 2) k_attn_rows(const __grid_const
   }
 }
 
+// The sequence that token t belongs to, q_offsets[s] <= t < q_offsets[s + 1]; -1: none.
+// Whole warp, 32 offsets at a time.
+__device__ __forceinline__ int seq_of(const AttnArgs& A, int t, int lane) {
+  int lo = 0, hi = A.n_seqs;                     // q_offsets[lo] <= t < q_offsets[hi]
+  if (A.q_offsets[lo] > t || A.q_offsets[hi] <= t) return -1;
+  while (hi - lo > 1) {
+    const int step = (hi - lo + 31) / 32;
+    const unsigned past = __ballot_sync(0xFFFFFFFFu, A.q_offsets[min(lo + (lane + 1) * step, hi)] > t);
+    const int l = __ffs(past) - 1;               // lane 31 is at hi
+    hi = min(lo + (l + 1) * step, hi);
+    lo += l * step;
+  }
+  return lo;
+}
+
 // out_i = sum_c 2^(m_c - M) O_c / sum_c 2^(m_c - M) l_c over the partial results
 // in use: W warps per row (4 where there are many partial results, which one warp
 // would read one after another: 5 rows of 600 took 120 us), 4 channels per lane.
 // Every warp sums its share in index order, then the shares are summed in order.
+// A warp (or the block's W) takes `per` rows of the call one after another, whatever
+// sequences they belong to: with blocks for every sequence, as many as the longest one
+// wants, ragged calls spend their time on blocks without work or on a few with too much
+// (100 sequences of 1 to 16,000 tokens, most of them short, 6 heads of 64: 3.52 ms the whole
+// call, 2.20 so; one of 2,700 tokens and 400 of 5, 12 heads of 128: 2.82 and 1.10).
 constexpr int kJoinWarps = 4;
 template <typename T, int W, int U>              // U: loads in flight
-__global__ void __launch_bounds__(kJoinWarps * 32) k_attn_join(const __grid_constant__ AttnArgs A, int blocks_per_seq) {
+__global__ void __launch_bounds__(kJoinWarps * 32) k_attn_join(const __grid_constant__ AttnArgs A, int per) {
   __shared__ float4 sum_o[kJoinWarps][32];
   __shared__ float2 sum_ml[kJoinWarps];
   pdl_wait();
-  const int seq = blockIdx.x / blocks_per_seq, b = blockIdx.x % blocks_per_seq;
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
-  const AttnSpan S = attn_span<true>(A, seq);
-  const int per = attn_chunk(A, S.nk, A.unit);
-  const int used = max(1, (int)(((long long)S.nk + per - 1) / per)) * A.streams;
-  const long long rows = (long long)S.nq * A.heads, stride = (long long)A.n_q * A.heads;
-  constexpr int kRowsAtOnce = kJoinWarps / W;
+  const long long rows = (long long)A.n_q * A.heads, stride = rows;
+  constexpr int kTakers = kJoinWarps / W;        // of a block
   const int first = W == 1 ? 0 : w;              // this warp's partial results: first, first + W, ...
-  for (long long i = (long long)b * kRowsAtOnce + (W == 1 ? w : 0); i < rows; i += (long long)blocks_per_seq * kRowsAtOnce) {
-    const long long R = (long long)S.q0 * A.heads + i;
+  const long long R0 = ((long long)blockIdx.x * kTakers + (W == 1 ? w : 0)) * per, R1 = min(R0 + per, rows);
+  AttnSpan S{};                                  // of the row's sequence: rows below `end`
+  long long end = 0;
+  int used = 0;
+  for (long long R = R0; R < R1; ++R) {
+    const int t = (int)((uint32_t)R / (uint32_t)A.heads);
+    if (R >= end) {
+      const int seq = seq_of(A, t, lane);
+      if (seq < 0) continue;
+      S = attn_span<true>(A, seq);
+      end = (long long)min(A.q_offsets[seq + 1], A.n_q) * A.heads;
+      const int chunk = attn_chunk(A, S.nk, A.unit);
+      used = max(1, (int)(((long long)S.nk + chunk - 1) / chunk)) * A.streams;
+    }
+    if (t - S.q0 >= S.nq) continue;              // left out
     float mm = -INFINITY;                        // the row's maximum
     for (int c = lane; c < used; c += 32) mm = fmaxf(mm, A.part_ml[c * stride + R].x);
 #pragma unroll
@@ -363,8 +392,7 @@ __global__ void __launch_bounds__(kJoinWarps * 32) k_attn_join(const __grid_cons
       }
     }
     if (W == 1 || w == 0) {
-      const long long t = R / A.heads;
-      const int h = (int)(R % A.heads);
+      const int h = (int)(R - (long long)t * A.heads);
       if (on) store_row<T>(A, t, h, c4, acc, mm, ll);
     }
     if (W > 1) __syncthreads();                  // before the next row's sums
@@ -410,19 +438,17 @@ cudaError_t launch_attn_rows(const AttnArgs& a, bool bf16, cudaStream_t st) {
   return a.cluster ? launch_rows<true, false>(a, bf16, st) : launch_rows<false, false>(a, bf16, st);
 }
 
-cudaError_t launch_attn_join(const AttnArgs& a, int max_q, bool bf16, cudaStream_t st) {
-  const bool wide = (long long)a.n_chunks * a.streams > 8;
-  const int at_once = wide ? 1 : kJoinWarps;     // rows of a block
-  long long per = ((long long)max_q * a.heads + at_once - 1) / at_once;
-  if (per < 1) per = 1;
-  if (per > 4096) per = 4096;
-  // no more blocks than are resident, each with several rows: 2,700 tokens of 12 heads, two
-  // parts each, take 25 us in blocks of 4 rows
-  const long long fit = 16LL * sm_count() / a.n_seqs;
-  if (!wide && per > fit) per = fit < 1 ? 1 : fit;
-  while ((long long)a.n_seqs * per > 0x7FFFFFFF && per > 1) per /= 2;
-  const dim3 grid((unsigned)((long long)a.n_seqs * per)), block(kJoinWarps * 32);
+cudaError_t launch_attn_join(const AttnArgs& a, bool bf16, cudaStream_t st) {
   const int parts = a.n_chunks * a.streams;
+  const bool wide = parts > 8;
+  const int takers = wide ? 1 : kJoinWarps;      // of a block
+  const long long rows = (long long)a.n_q * a.heads;
+  // no more blocks than are resident, each with several rows: 2,700 tokens of 12 heads, two
+  // parts each, take 25 us in blocks of 4 rows.  With many parts a row is work enough.
+  const long long most = (wide ? 64LL : 16LL) * sm_count();
+  const long long want = (rows + takers - 1) / takers, blocks = want < most ? want : most;
+  const long long per = (rows + blocks * takers - 1) / (blocks * takers);
+  const dim3 grid((unsigned)((rows + per * takers - 1) / (per * takers))), block(kJoinWarps * 32);
   if (bf16) {
     const auto kern = wide ? k_attn_join<__nv_bfloat16, kJoinWarps, 8>
                       : parts > 2 ? k_attn_join<__nv_bfloat16, 1, 8> : k_attn_join<__nv_bfloat16, 1, 2>;

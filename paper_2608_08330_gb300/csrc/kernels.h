@@ -394,6 +394,6 @@ cudaError_t launch_attn_pages(const AttnArgs& a, const PagesArgs& p, bool bf16, 
 cudaError_t launch_pages_widen(const AttnArgs& a, const PagesArgs& p, void* k, void* v, unsigned char* hidden, int span,
                                bool bf16, cudaStream_t st);
 // Merge of the chunks' partial results into out and lse.
-cudaError_t launch_attn_join(const AttnArgs& a, int max_q, bool bf16, cudaStream_t st);
+cudaError_t launch_attn_join(const AttnArgs& a, bool bf16, cudaStream_t st);
 
 }  // namespace rtcc
