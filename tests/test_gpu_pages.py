@@ -775,6 +775,114 @@ def test_pages_non_finite_stays_in_its_rows(R):
         assert torch.equal(c.out[same], ref.out[same]) and torch.equal(c.lse[same], ref.lse[same])
 
 
+@pytest.mark.parametrize("window,sinks,cap", [(0, 0, 0.0), (300, 9, 0.0), (300, 9, 20.0), (1, 0, 0.0)])
+def test_pages_large_non_finite_stays_in_its_rows(R, window, sinks, cap):
+    """The kernel for many rows: queries with NaN or infinities make their own rows NaN, no other."""
+    c = Case([1500, 40], [1500, 900], 4, 4, window=window, sinks=sinks, cap=cap)
+    q = c.q.clone()
+    bad = [(0, 0), (130, 1), (700, 3), (1499, 2), (1510, 0)]
+    for i, (t, h) in enumerate(bad):
+        c.q[t, h, 3 + i] = float("nan" if i % 2 == 0 else "inf")
+        if i % 2:
+            c.q[t, h, 9] = float("nan")
+    c.run(R)
+    torch.cuda.synchronize()
+    ref = Case([1500, 40], [1500, 900], 4, 4, window=window, sinks=sinks, cap=cap).run(R).check()
+    for t, h in bad:
+        assert torch.isnan(c.out[t, h]).all() and torch.isnan(c.lse[t, h])
+        c.out[t, h], c.lse[t, h] = ref.out[t, h], ref.lse[t, h]
+    c.q.copy_(q)
+    c.check()
+
+
+class Narrow(Case):
+    """Keys and values as fp16 has them: cut to its largest, rounded to multiples of its smallest."""
+
+    def values(self, s, which, h):
+        return super().values(s, which, h).clamp(-65504, 65504).half().double()
+
+
+@pytest.mark.parametrize("up", [True, False])
+def test_pages_fp16_queries_over_what_fp16_cannot_hold(R, up):
+    """Pools of bf16 tokens and fp16 queries: few rows take the numbers as they are, many rows as
+    fp16 has them."""
+    for n, kv, kind in ((1, 1, Case), (40, 1, Case), (1500, 4, Narrow)):
+        c = kind([n], [1500], kv, kv, 64, 64, causal=False)
+        g = gen(4)
+        if up:                                               # keys up to 448 * 2^13, queries to match
+            c.s.view(c.pages, kv, 4, 2)[..., 0] = torch.randint(6, 14, (c.pages, kv, 4), generator=g, device="cuda").to(torch.int8)
+            c.scale *= 2.0 ** -14
+        else:                                                # keys around 2^-26, values around 2^-20
+            e = torch.randint(-36, -30, (c.pages, kv, 4), generator=g, device="cuda").to(torch.int8)
+            c.s.view(c.pages, kv, 4, 2)[..., 0], c.s.view(c.pages, kv, 4, 2)[..., 1] = e, e + 8
+            c.scale *= 2.0 ** 24
+        x, w = (torch.abs(Case.values(c, 0, which, 0)) for which in (0, 1))
+        assert bool((x > 65504).any()) if up else bool((x < 2.0 ** -25).any()) and bool((w < 2.0 ** -14).any())
+        c.run(R).check()
+
+
+def test_pages_more_sequences_than_a_grid_is_high(R):
+    """70,000 sequences, the first 69,997 of them empty."""
+    c = Case([150, 3, 40], [64, 60, 33], 2, 1, 16, 32).run(R).check()
+    more = 69997
+    off, length = i32([0] * more + [0, 150, 153, 193]), i32([0] * more + c.m)
+    table = torch.cat([full((more, c.per), -1), i32(c.table)])
+    cfg = R.page_config(1, 16, 32, c.pages, more + 3, c.per, page_bytes=c.k.stride(0), scale_bytes=c.s.stride(0))
+    ws = torch.full((400 << 20,), 0xFF, dtype=torch.uint8, device="cuda")
+    for size in (ws.numel(), 0):
+        c.out.fill_(7)
+        c.lse.fill_(7)
+        R.check(R.rtcc_pages_attention(cfg, c.args[1], ptr(c.q), ptr(off), None, ptr(length), None, ptr(table), ptr(c.k), ptr(c.v),
+                                       ptr(c.s), ptr(c.out), ptr(c.lse), ws.data_ptr() if size else None, size))
+        c.check()
+
+
+def test_write_more_sequences_than_a_grid_is_high(R):
+    """70,000 sequences of one or two tokens in one call, and in two."""
+    n, g = 70000, gen(11)
+    new = torch.arange(n, device="cuda") % 2 + 1
+    off = torch.cat([torch.zeros(1, device="cuda", dtype=torch.int64), new.cumsum(0)]).int()
+    tokens = int(off[-1])
+    k, v = (torch.randn(tokens, 1, 16, generator=g, device="cuda").half() for _ in range(2))
+    held, table = full(n, 0), torch.randperm(n, generator=g, device="cuda").int()
+    pools = []
+    for cuts in ((0, n), (0, n // 2, n)):
+        kp, vp = (torch.zeros(n, 1, 32, 16, dtype=torch.uint8, device="cuda") for _ in range(2))
+        sc = torch.zeros(n, 1, 2, 2, dtype=torch.int8, device="cuda")
+        for a, b in zip(cuts, cuts[1:]):
+            cfg, o = R.page_config(1, 16, 32, n, b - a, 1), off[a:b + 1].contiguous()
+            t = table[a:b].contiguous()
+            R.check(R.rtcc_pages_write(cfg, R.write_config(R.FP16, tokens, 2, (16, 16), (16, 16)), ptr(k), ptr(v), ptr(o), ptr(held),
+                                       None, ptr(t), ptr(kp), ptr(vp), ptr(sc)))
+        torch.cuda.synchronize()
+        pools.append((kp, vp, sc))
+    assert all(torch.equal(a, b) for a, b in zip(*pools))
+    e = pools[0][2][table.long(), 0, 0, 0].double()
+    first = pools[0][0][table.long(), 0, 0].view(torch.float8_e4m3fn).double() * torch.exp2(e)[:, None]
+    x = k[off[:-1].long(), 0].double()
+    assert bool(((first - x).abs() <= x.abs() / 16 + torch.exp2(e - 10)[:, None]).all())
+
+
+@pytest.mark.parametrize("window", [0, 200])
+def test_pages_workspace_of_just_the_widened_size(R, window):
+    """The room that the header states, and a byte less; what lies behind it stays."""
+    n, m, kv, dim = [1500, 700], [2000, 1900], 4, 64
+    c = Case(n, m, 4, kv, dim, 64, window=window, sinks=10 if window else 0)
+    S = max(m) if not window else 10 + window + max(n) + 192
+    S = min(-(-S // 64) * 64, -(-max(m) // 64) * 64)
+    room = 2 * S * kv * dim * 4 + 2 * S // 64 + 256
+    ws = torch.full((room + 4096,), 0xA5, dtype=torch.uint8, device="cuda")
+    c.run(R, workspace=0)
+    for size in (room, room - 257 - 2 * S // 64):
+        c.out.fill_(7)
+        ws.fill_(0xA5)
+        c.args[-2], c.args[-1] = ws.data_ptr(), size
+        R.check(R.rtcc_pages_attention(*c.args, 0))
+        c.check()
+        assert bool((ws[size:] == 0xA5).all())
+        assert size < room or bool((ws[:size // 2] != 0xA5).any())       # with less, parts of few rows may lie there
+
+
 def test_pages_repeat_in_a_graph_on_a_side_stream(R):
     for n, m, window in (([1, 1], [5000, 300], 0), ([40], [900], 200), ([300], [1900], 0), ([1500], [1900], 500)):
         c = Case(n, m, 4, 2, 128, window=window)

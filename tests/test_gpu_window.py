@@ -278,3 +278,21 @@ def test_window_behind_a_long_shared_part(R, pages, n, window, seen, by):
     torch.cuda.synchronize()
     assert float((out.double() / value - 1).abs().max()) <= 2.0 ** -11 + 3 * 2.0 ** -12 + 2.0 ** -20
     assert float((lse.double() - math.log(seen * weight + window)).abs().max()) <= 2.0 ** -20 * 15
+
+
+@pytest.mark.parametrize("window,sinks,cap,dist", [(200, 9, 0.0, False), (200, 9, 20.0, False), (200, 9, 0.0, True), (1, 0, 0.0, False)])
+def test_window_non_finite_queries_stay_in_their_rows(R, window, sinks, cap, dist):
+    for n, m in ((1500, 1500), (300, 9000), (6, 700)):
+        make = lambda: Window([n], [m], window, sinks, heads=4, kv=4, dim=64, cap=cap, dist=dist)  # noqa: E731
+        c, ref = make(), make().run(R).check()
+        q, bad = c.q.clone(), [(0, 0), (n // 2, 1), (n - 1, 3), (n // 3, 2)]
+        for i, (t, h) in enumerate(bad):
+            c.q[t, h, 5 * i] = float("nan")
+            c.q[t, h, 7] = float("inf")
+        c.run(R)
+        torch.cuda.synchronize()
+        for t, h in bad:
+            assert torch.isnan(c.out[t, h]).all() and torch.isnan(c.lse[t, h])
+            c.out[t, h], c.lse[t, h] = ref.out[t, h], ref.lse[t, h]
+        c.q.copy_(q)
+        c.check()
