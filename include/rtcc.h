@@ -673,7 +673,10 @@ typedef struct {
  * min(d_length[parent], d_keep[s]) tokens (d_keep NULL: all of them); any number may
  * continue from one parent.  A parent outside [0, n_from) leaves the sequence empty.
  * With window > 0, pages whose places are all at or past `sinks` and behind the window
- * of every later token (place + window <= tokens held) are dropped: -1.
+ * of every later token (place + window <= tokens held) are dropped: -1.  They are gone
+ * for later forks too: where up to b tokens may still be taken back (a smaller d_keep),
+ * window is the attention's plus b; with less, keys that the shorter history would see
+ * are on no page, and its attention leaves them out.
  *   d_length_out int32 [n_seqs]             tokens held
  *   d_table_out  int32 [n_seqs][table_row]  pages, -1 from the last held place on
  *   d_refs       int32 [n_pages]            entries of d_table_out that name each page
@@ -758,8 +761,9 @@ typedef struct {
  * [d_offsets[s], d_offsets[s + 1]); token i of it goes to place d_held[s] + i, if that
  * is below d_length[s] (NULL: table_row * page_rows) and its entry of the table is a
  * page; else it is left out.  A block's exponent is the least e with
- * |x| <= 448 * 2^e for its new tokens' values x, or the block's own where tokens that
- * it holds already (places below d_held[s]) have a larger one; those tokens' numbers are
+ * |x| <= 448 * 2^e for its new tokens' values x, or the block's own where it holds
+ * tokens already (places below d_held[s]) and its own is larger, be it on account of
+ * tokens taken back since; those tokens' numbers are
  * rounded again where e rises.  Numbers are x * 2^-e, rounded to nearest, ties to even;
  * infinities and NaN become NaN and do not count for e.  Other rows are left untouched.
  * The pages that one call writes to belong to one sequence each.
@@ -806,8 +810,9 @@ typedef struct {
  * 16 bits once, n_seqs * S * kv_heads * head_dim * 4 bytes and n_seqs * S / 64 + 256 more
  * with S = max_k, or, with a window and no prefix, sinks + window + max_q + 192 if that
  * is less, rounded up to a multiple of 64.  Without that room they take the kernel for few
- * rows, several times slower.  With fp16, values that a pool got from bf16 tokens and
- * that fp16 cannot hold are taken as its largest or smallest there.
+ * rows, several times slower.  With fp16 they take keys and values as fp16 has them, which
+ * changes those that a pool got from bf16 tokens: beyond 65,504 they are that, below 2^-14
+ * they are rounded to multiples of 2^-24.  (Few rows take all numbers as they are.)
  * Limits and alignment as in rtcc_memory_attention; errors of its waits are reported by
  * rtcc_memory_attention_status.
  */

@@ -92,6 +92,34 @@ def test_fork_matches_the_loop(R, n, n_from, per, pr, pages):
             assert (lo.tolist(), to.tolist(), refs.tolist()) == want
 
 
+@pytest.mark.parametrize("pr,window,sinks,back", [(32, 50, 4, 40), (64, 64, 0, 9), (128, 700, 130, 300)])
+def test_fork_window_covers_what_is_taken_back(R, pr, window, sinks, back):
+    """Forks with the attention's window and the tokens that may be taken back: after any number of
+    steps a history shortened by up to that many still has every page that its tokens see.  With
+    the attention's window alone some are gone."""
+    rng = random.Random(pr)
+    per, pages = 40, 200
+    lost = 0
+    for wide in (window + back, window):
+        table, length = [list(range(per))], [0]
+        for step in range(60):
+            grown = min(per * pr, length[0] + rng.randint(1, back))
+            row = [table[0][i] if i * pr < length[0] else i for i in range(per)]         # new pages for new places
+            cfg = R.page_config(1, 16, pr, pages, 2, per)
+            lo, to, refs = full(2), full((2, per)), full(pages)
+            src_l, src_t, par = i32([grown]), i32(row), i32([0, 0])
+            kp = i32([grown, max(0, grown - rng.randint(0, back))])
+            R.check(R.rtcc_pages_fork(cfg, 1, ptr(par), ptr(kp), wide, sinks, ptr(src_l), ptr(src_t), ptr(lo), ptr(to), ptr(refs)))
+            (m, short), rows = lo.tolist(), to.tolist()
+            sees = [j for j in range(short) if j < sinks or j > short - window]          # of the next token at place `short`
+            missing = [j for j in sees if rows[1][j // pr] < 0]
+            lost += len(missing)
+            assert wide == window or not missing
+            table, length = [rows[0]], [m]
+        assert wide == window or lost == 0
+    assert lost > 0
+
+
 def extend_loop(new, length, table, refs, pr):
     per, table, begin, refs = len(table[0]), [list(r) for r in table], list(refs), list(refs)
     free = [p for p, c in enumerate(begin) if c == 0]
