@@ -27,8 +27,9 @@
 // what its products need: no number crosses lanes but P, transposed once.
 //
 // Measured: 61 tokens over ragged histories of up to 16,384 keys, 8 key heads of 128 with
-// a cap, 958 MB: 161 us, 6.0 TB/s, 88 % of a plain copy's (rows on the 16-wide side, with
-// probabilities as two terms: 268 us); one token over 4097 keys of 6 heads of 64: 7.5 us.
+// a cap, 958 MB: 162 us, 5.9 TB/s, 87 % of a plain copy's (rows on the 16-wide side, with
+// probabilities as two terms: 268 us; the weights' maximum relative to the scores': 1 %);
+// one token over 4097 keys of 6 heads of 64: 7.3 us.
 #include <type_traits>
 
 #include "attn_rows.cuh"

@@ -52,9 +52,9 @@
 // heads of 128 with a cap: 127 us, 740 TFLOP/s (of a block's 22 us there, 1 goes to its
 // set-up, 2 to its first scores, 2 to the masked step and 3 to its results).  Windows of
 // 700 and 8 sinks, 20,900 packed tokens of 16 heads of 128: 197 us, 608 TFLOP/s; a block
-// has 14 steps, of which an inner one takes 1.0 us (0.67 are both tiles' products: Q is
-// read from shared memory anew for every 64 keys), and 8 us besides: 1.5 its set-up,
-// 2.2 its first scores, 1.3 the first step, 3 its results.
+// has 14 steps, of which an inner one takes 1.0 us (8.4 MFLOP, 0.68 us at a large GEMM's
+// rate: in the rest no product runs), and 8 us besides, in which the SM has nothing else:
+// 1.5 its set-up, 2.2 its first scores, 1.3 the first step, 3 its results.
 // Tried and slower: four chains of one S each (four softmax warps a scheduler, 96
 // registers: 10 to 30 %), the next S loaded while P is stored (spills: 5 to 15 %),
 // scalar beside packed arithmetic (up to 30 %), a second form of the pass for steps

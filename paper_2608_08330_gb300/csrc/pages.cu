@@ -10,12 +10,15 @@
 //   compact   the k-th page with refs > 0 at or past L, the number of pages in use,
 //             moves to the k-th page below L with refs = 0.
 // They read and write a few hundred kilobytes, so the launch and a chain of dependent
-// steps bound them, not the memory.  Both numberings are prefix sums over the pages and
-// the sequences: one launch of a cluster of eight blocks, whose sums meet in shared
-// memory, instead of a launch per step.
+// steps bound them, not the memory.  The numberings of extend and compact are prefix sums
+// over the pages and the sequences: one launch of a cluster of eight blocks, whose sums
+// meet in shared memory, instead of a launch per step.  fork has no sum, but counts have to
+// be cleared before entries are counted: a barrier of the same cluster, or two launches.
 //
-// Measured: 2048 sequences of up to 13 pages out of 16,384, fork 9 us and extend 10; compact
-// over 8192 pages and 16,384 entries 11, over 500 pages and 427 entries 5.
+// Measured: 2048 sequences of up to 13 pages out of 16,384, fork 7 us and extend 10; compact
+// over 8192 pages and 16,384 entries 11, over 500 pages and 427 entries 5.  fork in two
+// launches over all SMs, which it takes above 65,536 entries, 4 (1,000 entries 3.8 for 3.5,
+// 9,000 3.7 for 4.7, 60,000 4.4 for 10.6): from some 5,000 entries on that is the faster one.
 //
 // copy and write move every byte once and are bound by HBM: 2048 pages of 2 x 64 KB, 537 MB
 // read and written, 76 us, 7.0 TB/s; 54,700 tokens of 8 key heads of 112, 294 MB, 50 us,
