@@ -676,7 +676,8 @@ typedef struct {
  * of every later token (place + window <= tokens held) are dropped: -1.  They are gone
  * for later forks too: where up to b tokens may still be taken back (a smaller d_keep),
  * window is the attention's plus b; with less, keys that the shorter history would see
- * are on no page, and its attention leaves them out.
+ * are on no page, and its attention leaves them out (all but those of a last, partly
+ * filled page, which rtcc_pages_extend replaces by one without them).
  *   d_length_out int32 [n_seqs]             tokens held
  *   d_table_out  int32 [n_seqs][table_row]  pages, -1 from the last held place on
  *   d_refs       int32 [n_pages]            entries of d_table_out that name each page
@@ -696,7 +697,8 @@ size_t rtcc_pages_workspace(const rtcc_page_config* cfg);
  * Pages for the d_new[s] tokens that follow the d_length[s] held ones (at most up to
  * place table_row * page_rows).  Wanted are, sequence by sequence in order of places, a
  * page of its own for the last held place's page if that page has room left and others
- * have it too when the call begins (or if there is none), and a page for every page_rows
+ * have it too when the call begins (or if there is none: the sequence's places on it then
+ * hold what the page happened to hold), and a page for every page_rows
  * places after it; earlier contents of those entries are ignored.  The k-th wanted page
  * is the k-th lowest-numbered page without references.  Where there are none left,
  * entries are -1, the shared page stays, and the sequence's tokens end before.
